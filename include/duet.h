@@ -275,6 +275,73 @@ int duet_qkv_split(duet_ctx* ctx, const duet_shape* shape, const void* qkv, void
                    int64_t num_phys_pages, const int32_t* page_table, int32_t max_pages_per_req,
                    const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- token-level operators of a served model.  No passage of the paper: what a serving step needs beside
+ * the operators above.  Work is enqueued on `stream`; under capture a call goes into the graph with its batch. ---- */
+
+/* Rotary position embedding of a head's first rot_dim dimensions: pair i, (a, b), turns by t = p f_i to
+ * (a cos t - b sin t, a sin t + b cos t), p the token's position on the pair's axis. */
+typedef struct {
+  int32_t rot_dim;          /* a multiple of 16 in [16, head_dim]; dimensions past it are copied */
+  int32_t adjacent;         /* pair i is dimensions (i, i + rot_dim / 2) if 0, (2 i, 2 i + 1) if 1 */
+  int32_t axes;             /* position axes, 1 .. 4 (3: time, height and width of images and video) */
+  const double* inv_freq;   /* host, [rot_dim / 2]: f_i in radians per position, within [-64, 64] */
+  const uint8_t* pair_axis; /* host, [rot_dim / 2]: the axis of each pair, below axes; NULL: axis 0 */
+} duet_rope;
+
+/* Workspace of duet_qkv_rope_split: an error word and the table of the requests.  Host only. */
+int duet_rope_workspace_bytes(const duet_batch* batch, size_t* bytes);
+/* duet_qkv_split with the rotation on the way: the query and key columns of qkv [T, (h_q + 2 h_kv) d] are
+ * turned by their token's position before they go to q and k_cache; values are copied.  shape.dtype bf16
+ * or fp32 (qkv, q and both caches).  positions [axes, T] int32 (device), row a for axis a in seq_meta order, any
+ * values; NULL: every axis takes the token's place in its request's cache, cached_len + its index.  Angles are formed
+ * in 64 bits, the rotation in fp32 with one rounding.  qkv, q, the caches and the workspace lie on 16 bytes; q
+ * may not be qkv.  Requests must not share the pages that they write.  At most 2^22 tokens.  Page ids outside the pool are not
+ * written and set the error word (duet_check_device_error). */
+int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope* rope, const void* qkv,
+                        const int32_t* positions, void* q, void* k_cache, void* v_cache, int64_t num_phys_pages,
+                        const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters of one projection d_in -> d_out (bf16 device arrays, on 16 bytes). */
+typedef struct {
+  const void* a;       /* [num_adapters, rank, d_in] */
+  const void* b;       /* [num_adapters, d_out, rank] */
+  const float* scale;  /* [num_adapters] (device), or NULL: 1 */
+  int32_t num_adapters;
+  int32_t rank;        /* a multiple of 8 in [8, 128]; smaller ones are padded with zeros */
+  int32_t d_in, d_out; /* multiples of 8, at most 2^20 */
+} duet_lora;
+
+/* Workspace of duet_lora_add (a and b may be NULL).  Host only. */
+int duet_lora_workspace_bytes(const duet_lora* lora, const duet_batch* batch, size_t* bytes);
+/* out[t] = base[t] + scale_a B_a (A_a x[t]) for the tokens t of every request with adapter a =
+ * adapter_ids[r] (host, [num_reqs]), out[t] = base[t] where it is -1: x [T, d_in] the projection's input, base
+ * [T, d_out] its output, rows in seq_meta order, ldx, ld_base and ld_out elements apart (multiples of 8).
+ * bf16, fp32 sums, one rounding.  out may be base; otherwise it overlaps no input.  base and out may be some of the columns
+ * of a wider projection.  The workspace lies on 16 bytes.  At most 2^22 tokens. */
+int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t ldx, const void* base, int64_t ld_base,
+                  void* out, int64_t ld_out, const duet_batch* batch, const int32_t* adapter_ids, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* What the rows' requests ask for: device arrays [rows], each may be NULL (off). */
+typedef struct {
+  const float* temperature; /* T; NULL: 1.  Not above 0 (or NaN): the largest logit's token */
+  const int32_t* top_k;     /* keep the first k ranks; not above 0: all */
+  const float* top_p;       /* of those, keep rank r if the mass before it is less than top_p times theirs (the
+                               first rank always); 1 and more, NaN: all */
+  const float* min_p;       /* keep tokens of at least min_p times the largest weight; not above 0, NaN: all */
+} duet_sampling;
+
+/* One token for each row of logits [rows, vocab] (dtype bf16 or fp32, rows row_stride elements apart; vocab at
+ * most 2^18, rows at most 2^20).  Tokens are ranked by falling logit, ties by the lower index, with weights
+ * exp((logit - max) / T); top-k, then top-p, then min-p each keep a run of ranks from the first; ids[row] (int32) is the
+ * first rank whose cumulative kept weight exceeds u[row] times all of it, probs[row] (may be NULL) its weight's
+ * share of it.  u is a given random number in [0, 1); others are taken as 0 or the largest below 1.  NaN and -inf are
+ * tokens that a mask took out; a row of nothing else gives -1 with probability 0.  +inf outweighs all finite
+ * logits.  params NULL: all off.  The result does not depend on other rows nor on the stream. */
+int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* stream);
+
 /* ---- GPU context ----------------------------------------------------------------------------- */
 
 /* Infrastructure (no passage of its own): the device state every call below uses.

@@ -21,7 +21,7 @@ from ._native import (AGG, BF16, CONCURRENT, CU_STEP, F32, KIND_DECODE, KIND_PRE
 from .workloads import AttnShape
 
 __all__ = ["AGG", "SPLIT", "CONCURRENT", "CuSplit", "Context", "Model", "DuetError", "attn_mixed_batch", "predict_iter_latency",
-           "choose_cu_split", "default_context", "AttnShape", "STATUS_SLO_INFEASIBLE", "STATUS_UNCALIBRATED"]
+           "choose_cu_split", "default_context", "AttnShape", "Rope", "Lora", "STATUS_SLO_INFEASIBLE", "STATUS_UNCALIBRATED"]
 
 
 @dataclass(frozen=True)
@@ -363,6 +363,50 @@ def shape_of(q, k_cache, num_layers: int = 1) -> AttnShape:
     return AttnShape(int(q.shape[1]), int(k_cache.shape[1]), int(q.shape[2]), dt, int(k_cache.shape[2]), num_layers)
 
 
+class Rope:
+    """The position rotation of duet_qkv_rope_split (duet_rope): inv_freq, a frequency in radians per position for
+    each rotated pair (so 2 len(inv_freq) dimensions of a head turn); adjacent: pairs are neighbouring dimensions, else
+    the two halves; pair_axis, the position axis of each pair (None: axis 0), of `axes` (1 .. 4)."""
+
+    def __init__(self, inv_freq, *, adjacent: bool = False, pair_axis=None, axes: int = 1):
+        f = [float(x) for x in inv_freq]
+        self.axes = int(axes)
+        self._freq = (ctypes.c_double * max(len(f), 1))(*f)
+        self._axis = None
+        if pair_axis is not None:
+            ids = [int(x) for x in pair_axis]
+            if len(ids) != len(f) or any(not 0 <= a < self.axes for a in ids):
+                raise ValueError(f"pair_axis must name an axis in [0, {self.axes}) for each of the {len(f)} pairs")
+            self._axis = (ctypes.c_uint8 * max(len(ids), 1))(*ids)
+        self.c = N.Rope(2 * len(f), 1 if adjacent else 0, self.axes, self._freq, self._axis)
+
+    @staticmethod
+    def base(theta: float, rot_dim: int, **kw) -> "Rope":
+        """Frequencies theta^(-2 i / rot_dim)."""
+        return Rope([theta ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)], **kw)
+
+
+class Lora:
+    """Adapters of one projection (duet_lora): contiguous bf16 device tensors a [N, rank, d_in] and b [N, d_out, rank],
+    scale [N] float32 (None: 1)."""
+
+    def __init__(self, a, b, scale=None):
+        import torch
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+            raise ValueError("a must be [N, rank, d_in] and b [N, d_out, rank]")
+        for t, name in ((a, "a"), (b, "b")):
+            if t.dtype != torch.bfloat16 or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous bf16 device tensor")
+        if scale is not None and (scale.dtype != torch.float32 or not scale.is_cuda or not scale.is_contiguous() or
+                                  tuple(scale.shape) != (a.shape[0],)):
+            raise ValueError(f"scale must be a contiguous float32 device tensor [{a.shape[0]}]")
+        if b.device != a.device or (scale is not None and scale.device != a.device):
+            raise ValueError("a, b and scale must lie on one device")
+        self.a, self.b, self.scale = a, b, scale
+        self.c = N.Lora(a.data_ptr(), b.data_ptr(), scale.data_ptr() if scale is not None else None, int(a.shape[0]),
+                        int(a.shape[1]), int(a.shape[2]), int(b.shape[1]))
+
+
 def _stream_of(t, stream) -> ctypes.c_void_p:
     """The caller's stream, or torch's current one on the tensor's device."""
     if stream is None:
@@ -562,6 +606,123 @@ class Context:
             N.check(N.lib().duet_check_device_error(self.handle, ws.data_ptr(), st),
                     "duet_check_device_error")
         return q
+
+    def _empty(self, shape, dtype, stream):
+        """Memory for one call that runs on `stream` (None: the current one): the allocator hands it to no later
+        work before the call's, and under capture it belongs to the graph."""
+        import torch
+        dev = f"cuda:{self.device}"
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=dev)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)):
+            return torch.empty(shape, dtype=dtype, device=dev)
+
+    def _check_on(self, t, name, dtype, shape):
+        """A contiguous tensor of this context's device."""
+        if t.device.type != "cuda" or t.device.index != self.device or t.dtype != dtype or tuple(t.shape) != shape or \
+                not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{self.device}")
+
+    def qkv_rope_split(self, qkv, k_cache, v_cache, page_table, seq_meta, shape: AttnShape, rope: Rope, *, positions=None,
+                       q=None, workspace=None, stream=None, check_errors: bool = False):
+        """duet_qkv_rope_split: the rotated query rows out of qkv [T, (h_q + 2 h_kv) d], rotated keys and values into the
+        cache.  positions: int32 [axes, T] ([T] for one axis); None: the tokens' places in the cache."""
+        import torch
+        b = _BatchC(seq_meta)
+        T = b.num_tokens()
+        dt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
+        hq, hkv, d, ps = shape.num_q_heads, shape.num_kv_heads, shape.head_dim, shape.page_size
+        pages = int(k_cache.shape[0])
+        self._check_on(qkv, "qkv", dt, (T, (hq + 2 * hkv) * d))
+        self._check_on(k_cache, "k_cache", dt, (pages, hkv, ps, d))
+        self._check_on(v_cache, "v_cache", dt, (pages, hkv, d, ps))
+        if page_table.dim() != 2 or page_table.shape[0] < len(b.rows):
+            raise ValueError("page_table must be [R, max_pages] with a row per request")
+        self._check_on(page_table, "page_table", torch.int32, tuple(page_table.shape))
+        if positions is not None:
+            self._check_on(positions, "positions", torch.int32,
+                           (T,) if rope.axes == 1 and positions.dim() == 1 else (rope.axes, T))
+        if q is None:
+            q = self._empty((T, hq, d), dt, stream)
+        else:
+            self._check_on(q, "q", dt, (T, hq, d))
+        if workspace is None:
+            n = ctypes.c_size_t()
+            N.check(N.lib().duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+            workspace = self._empty(n.value, torch.uint8, stream)
+        if T == 0:
+            return q
+        st = _stream_of(qkv, stream)
+        N.check(N.lib().duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
+                                            positions.data_ptr() if positions is not None else None, q.data_ptr(),
+                                            k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(),
+                                            int(page_table.shape[1]), ctypes.byref(b.c), workspace.data_ptr(),
+                                            workspace.numel(), st), "duet_qkv_rope_split")
+        if check_errors:
+            N.check(N.lib().duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
+        return q
+
+    def lora_add(self, x, base, lora: Lora, seq_meta, adapter_ids, *, out=None, workspace=None, stream=None):
+        """duet_lora_add: base [T, d_out] plus each request's adapter applied to x [T, d_in] (bf16, rows may be strided).
+        adapter_ids: one int per request, -1 for none.  out may be base."""
+        import torch
+        b = _BatchC(seq_meta)
+        T = b.num_tokens()
+        ids = np.ascontiguousarray(adapter_ids, dtype=np.int32)
+        if ids.shape != (len(b.rows),):
+            raise ValueError(f"adapter_ids must hold {len(b.rows)} values, one per request")
+        if out is None:
+            out = self._empty((T, lora.c.d_out), torch.bfloat16, stream)
+        for t, name, width in ((x, "x", lora.c.d_in), (base, "base", lora.c.d_out), (out, "out", lora.c.d_out)):
+            if t.device.type != "cuda" or t.device.index != self.device or t.dtype != torch.bfloat16 or \
+                    tuple(t.shape) != (T, width) or t.stride(1) != 1:
+                raise ValueError(f"{name} must be a bf16 tensor [{T}, {width}] on cuda:{self.device} with contiguous rows")
+        if lora.a.device.index != self.device:
+            raise ValueError(f"the adapters must lie on cuda:{self.device}")
+        if workspace is None:
+            n = ctypes.c_size_t()
+            N.check(N.lib().duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
+                    "duet_lora_workspace_bytes")
+            workspace = self._empty(n.value, torch.uint8, stream)
+        if T == 0:
+            return out
+        ld = lambda t: int(t.shape[1]) if T == 1 else int(t.stride(0))  # noqa: E731
+        N.check(N.lib().duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld(x), base.data_ptr(), ld(base),
+                                      out.data_ptr(), ld(out), ctypes.byref(b.c), ids.ctypes.data, workspace.data_ptr(),
+                                      workspace.numel(), _stream_of(x, stream)), "duet_lora_add")
+        return out
+
+    def sample(self, logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None, stream=None):
+        """duet_sample: (ids int32 [rows], probs float32 [rows]), one token for each row of logits [rows, vocab] (bf16 or
+        float32, rows may be strided) from the given random numbers u [rows] float32 in [0, 1).  temperature, top_p,
+        min_p: float32 [rows]; top_k: int32 [rows]; None: off."""
+        import torch
+        if logits.device.type != "cuda" or logits.device.index != self.device or logits.dim() != 2 or \
+                logits.dtype not in (torch.bfloat16, torch.float32) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError(f"logits must be a bf16 or float32 tensor [rows, vocab] on cuda:{self.device} with contiguous rows")
+        rows, vocab = int(logits.shape[0]), int(logits.shape[1])
+        self._check_on(u, "u", torch.float32, (rows,))
+        params = N.Sampling()
+        for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                            ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+            if t is not None:
+                self._check_on(t, name, dt, (rows,))
+                setattr(params, name, t.data_ptr())
+        if out is None:
+            out = self._empty(rows, torch.int32, stream)
+        else:
+            self._check_on(out, "out", torch.int32, (rows,))
+        if probs is None:
+            probs = self._empty(rows, torch.float32, stream)
+        else:
+            self._check_on(probs, "probs", torch.float32, (rows,))
+        if rows == 0:
+            return out, probs
+        stride = vocab if rows == 1 else int(logits.stride(0))
+        N.check(N.lib().duet_sample(self.handle, logits.data_ptr(), BF16 if logits.dtype == torch.bfloat16 else F32, rows,
+                                    vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
+                                    _stream_of(logits, stream)), "duet_sample")
+        return out, probs
 
     def attn_iteration(self, qs, k_caches, v_caches, page_table, seq_meta, cu_split: CuSplit = CuSplit.agg(), *,
                        outs=None, workspace=None, stream=None, check_errors: bool = False):

@@ -45,6 +45,20 @@ class BlockWeights(ctypes.Structure):
                 ("w_gate_up", c_void_p), ("w_down", c_void_p)]
 
 
+class Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", c_int32), ("adjacent", c_int32), ("axes", c_int32), ("inv_freq", ctypes.POINTER(c_double)),
+                ("pair_axis", ctypes.POINTER(ctypes.c_uint8))]
+
+
+class Lora(ctypes.Structure):
+    _fields_ = [("a", c_void_p), ("b", c_void_p), ("scale", c_void_p), ("num_adapters", c_int32), ("rank", c_int32),
+                ("d_in", c_int32), ("d_out", c_int32)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", c_void_p), ("top_k", c_void_p), ("top_p", c_void_p), ("min_p", c_void_p)]
+
+
 class KernelTimes(ctypes.Structure):
     _fields_ = [("decode_partial_us", c_double), ("decode_reduce_us", c_double), ("prefill_us", c_double),
                 ("decode_total_us", c_double), ("iteration_us", c_double),
@@ -97,6 +111,14 @@ _SIGS = {
     "duet_swiglu": (c_int32, [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p]),
     "duet_qkv_split": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32,
                                  P(Batch), c_void_p, c_size_t, c_void_p]),
+    "duet_rope_workspace_bytes": (c_int32, [P(Batch), P(c_size_t)]),
+    "duet_qkv_rope_split": (c_int32, [c_void_p, P(Shape), P(Rope), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64,
+                                      c_void_p, c_int32, P(Batch), c_void_p, c_size_t, c_void_p]),
+    "duet_lora_workspace_bytes": (c_int32, [P(Lora), P(Batch), P(c_size_t)]),
+    "duet_lora_add": (c_int32, [c_void_p, P(Lora), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, P(Batch),
+                                c_void_p, c_void_p, c_size_t, c_void_p]),
+    "duet_sample": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int64, P(Sampling), c_void_p, c_void_p,
+                              c_void_p, c_void_p]),
     "duet_attn_mixed_batch": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32,
                                         P(Batch), CuSplit, c_void_p, c_size_t, c_void_p, c_void_p]),
     "duet_attn_mixed_batch_noalloc": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p,

@@ -216,6 +216,49 @@ struct QkvSplitArgs {
   int32_t row0, rows;      // the launch's rows
 };
 
+// The QKV split with the position rotation on the way (rope_split.hip), bf16 or fp32.
+struct RopeSplitArgs {
+  const void* qkv;         // [T, (h_q + 2 h_kv) d]
+  void* q;                 // [T, h_q, d]
+  void* k_cache;           // [P, h_kv, 16, d]
+  void* v_cache;           // [P, h_kv, d, 16]
+  const int4* meta;        // [R] (kind, q_start, q_len, cached_len)
+  const int32_t* page_table;
+  const int32_t* positions;  // [axes, T], or null: the tokens' places in the cache
+  long long num_phys_pages;
+  int32_t* err;
+  int32_t num_reqs, max_pages, h_q, h_kv, head_dim, dtype, tokens;
+  int32_t rot_dim, adjacent;
+  double turns[64];        // turns per position of each pair (frequency / 2 pi)
+  uint8_t pair_axis[64];
+};
+hipError_t launch_rope_split(const RopeSplitArgs& a, hipStream_t s);
+
+// out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).
+struct LoraArgs {
+  const __bf16 *x, *base, *a, *b;  // x [T, d_in], base [T, d_out], a [N, rank, d_in], b [N, d_out, rank]
+  __bf16* out;                     // [T, d_out]
+  const float* scale;              // [N], or null: 1
+  float* h;                        // [T, rank]
+  const int4* reqs;                // [R] (adapter or -1, first row, rows, 0)
+  long long ldx, ldb, ldo;
+  int32_t num_reqs, tokens, rank, d_in, d_out;
+};
+hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
+
+// One token from each row of logits (sample.hip); the parameters' arrays may be null.
+struct SampleArgs {
+  const void* logits;  // [rows, vocab]
+  long long row_stride;
+  const float *temperature, *top_p, *min_p, *u;
+  const int32_t* top_k;
+  int32_t* ids;
+  float* probs;  // may be null
+  int32_t dtype, rows, vocab;
+};
+constexpr int kMaxVocab = 1 << 18;
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 // Projections of few rows (gemm_skinny.hip) instead of the library's, for a partition of `rows` rows on
 // `cus` CUs and layers of model width d, QKV width d_qkv and MLP width m: where one part of the widest product in
 // fp32 fits in `bytes` (at 64 rows more than 131072 columns do not), and where they are faster.  A layer

@@ -1250,6 +1250,80 @@ int check_block_exec(const duet_shape* s, const duet_block_shape* blk) {
   return DUET_OK;
 }
 
+// The caller's current device is put back when a call returns.
+struct DeviceGuard {
+  int before = -1;
+  hipError_t status;
+  explicit DeviceGuard(int device) {
+    status = hipGetDevice(&before);
+    if (status == hipSuccess && before != device) status = hipSetDevice(device);
+    else before = -1;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// Tokens of the calls below: rows times the widest row stays far from 2^63 bytes and a row per workgroup
+// fits a grid.
+constexpr int kMaxOpTokens = 1 << 22;
+constexpr int kMaxSampleRows = 1 << 20;
+
+int batch_tokens(const duet_batch* b, int32_t* tokens) {
+  int64_t t = 0;
+  for (int r = 0; r < b->num_reqs; ++r) t += b->reqs[r].q_len;
+  if (t > kMaxOpTokens) return fail(DUET_EUNSUPPORTED, "%lld tokens, at most %d", (long long)t, kMaxOpTokens);
+  *tokens = (int32_t)t;
+  return DUET_OK;
+}
+
+// A workspace that holds an error word and a table of the requests only.
+size_t request_table_bytes(const duet_batch* b) { return kAlign + align_up((size_t)b->num_reqs * sizeof(int4)); }
+
+template <typename F>
+int upload_requests(duet_ctx* ctx, const duet_batch* b, char* ws, hipStream_t st, F row) {
+  try {
+    Plan p;
+    p.meta.reserve(b->num_reqs);
+    for (int r = 0; r < b->num_reqs; ++r) p.meta.push_back(row(b->reqs[r], r));
+    p.off_meta = p.off_pitems = p.off_dreq = p.off_ditems = p.off_punits = p.off_pcount = p.off_append = kAlign;
+    p.upload_bytes = request_table_bytes(b);
+    return stage_upload(ctx, p, ws, st);
+  } catch (const std::bad_alloc&) {
+    return fail(DUET_ENOMEM, "host allocation failed");
+  }
+}
+
+int check_rope(const duet_shape* s, const duet_rope* r) {
+  if (!r || !r->inv_freq) return fail(DUET_EINVAL, "rope or its frequencies are NULL");
+  if (r->rot_dim < 16 || r->rot_dim > s->head_dim || r->rot_dim % 16)
+    return fail(DUET_EINVAL, "rot_dim %d must be a multiple of 16 in [16, head_dim]", r->rot_dim);
+  if (r->adjacent != 0 && r->adjacent != 1) return fail(DUET_EINVAL, "adjacent must be 0 or 1");
+  if (r->axes < 1 || r->axes > 4) return fail(DUET_EINVAL, "axes %d not in [1, 4]", r->axes);
+  for (int i = 0; i < r->rot_dim / 2; ++i) {
+    if (!(std::fabs(r->inv_freq[i]) <= 64.0)) return fail(DUET_EINVAL, "frequency %d is not within [-64, 64]", i);
+    if (r->pair_axis && r->pair_axis[i] >= r->axes)
+      return fail(DUET_EINVAL, "pair %d: axis %d not in [0, %d)", i, r->pair_axis[i], r->axes);
+  }
+  return DUET_OK;
+}
+
+int check_lora(const duet_lora* l) {
+  if (!l) return fail(DUET_EINVAL, "lora is NULL");
+  if (l->num_adapters < 1 || l->num_adapters > (1 << 20))
+    return fail(DUET_EINVAL, "num_adapters %d not in [1, %d]", l->num_adapters, 1 << 20);
+  if (l->rank < 8 || l->rank > 128 || l->rank % 8)
+    return fail(DUET_EUNSUPPORTED, "rank %d must be a multiple of 8 in [8, 128]", l->rank);
+  for (int d : {l->d_in, l->d_out})
+    if (d < 8 || d > (1 << 20) || d % 8) return fail(DUET_EINVAL, "d_in %d / d_out %d: multiples of 8", l->d_in, l->d_out);
+  return DUET_OK;
+}
+
+// The request table, then h [tokens, rank].
+size_t lora_layout(const duet_lora* l, const duet_batch* b, int32_t tokens) {
+  return request_table_bytes(b) + align_up((size_t)tokens * l->rank * sizeof(float));
+}
+
 // Rows [row0, row0 + rows) of the requests of one kind, or rows = -1 when they are not one
 // contiguous range (rows = 0: none of that kind).
 void kind_rows(const duet_batch* b, int kind, int* row0, int* rows) {
@@ -1733,6 +1807,171 @@ int duet_qkv_split(duet_ctx* ctx, const duet_shape* shape, const void* qkv, void
   a.row0 = 0;
   a.rows = (int)T;
   HIP_TRY(launch_qkv_split(a, st));
+  return DUET_OK;
+}
+
+int duet_rope_workspace_bytes(const duet_batch* batch, size_t* bytes) {
+  clear_error();
+  const int rc = check_batch(nullptr, batch, false);
+  if (rc) return rc;
+  if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
+  *bytes = request_table_bytes(batch);
+  return DUET_OK;
+}
+
+int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope* rope, const void* qkv,
+                        const int32_t* positions, void* q, void* k_cache, void* v_cache, int64_t num_phys_pages,
+                        const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  clear_error();
+  if (!shape) return fail(DUET_EINVAL, "shape is NULL");
+  int rc = check_rope(shape, rope);
+  if (rc) return rc;
+  const void* q_l[1] = {qkv};
+  const void* k_l[1] = {k_cache};
+  const void* v_l[1] = {v_cache};
+  const void* o_l[1] = {q};
+  rc = check_call(ctx, shape, 1, q_l, k_l, v_l, num_phys_pages, page_table, max_pages_per_req, batch,
+                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace, o_l, 0);
+  if (rc) return rc;
+  for (const void* p : {qkv, static_cast<const void*>(q), static_cast<const void*>(k_cache),
+                        static_cast<const void*>(v_cache)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "qkv, q and the caches must lie on 16 bytes");
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
+  if (workspace_bytes < request_table_bytes(batch))
+    return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, request_table_bytes(batch));
+  RopeSplitArgs a{};
+  if ((rc = batch_tokens(batch, &a.tokens))) return rc;
+  a.qkv = qkv;
+  a.q = q;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.page_table = page_table;
+  a.positions = positions;
+  a.num_phys_pages = num_phys_pages;
+  a.num_reqs = batch->num_reqs;
+  a.max_pages = max_pages_per_req;
+  a.h_q = shape->num_q_heads;
+  a.h_kv = shape->num_kv_heads;
+  a.head_dim = shape->head_dim;
+  a.dtype = shape->dtype;
+  a.rot_dim = rope->rot_dim;
+  a.adjacent = rope->adjacent;
+  for (int i = 0; i < rope->rot_dim / 2; ++i) {
+    a.turns[i] = rope->inv_freq[i] / 6.283185307179586476925;
+    a.pair_axis[i] = rope->pair_axis ? rope->pair_axis[i] : 0;
+  }
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  if ((rc = upload_requests(ctx, batch, ws, st, [](const duet_seq_meta& m, int) {
+         return make_int4(m.kind, m.q_start, m.q_len, m.cached_len);
+       })))
+    return rc;
+  a.meta = reinterpret_cast<const int4*>(ws + kAlign);
+  a.err = reinterpret_cast<int32_t*>(ws);
+  HIP_TRY(launch_rope_split(a, st));
+  return DUET_OK;
+}
+
+int duet_lora_workspace_bytes(const duet_lora* lora, const duet_batch* batch, size_t* bytes) {
+  clear_error();
+  int rc = check_lora(lora);
+  if (rc || (rc = check_batch(nullptr, batch, false))) return rc;
+  if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
+  int32_t tokens = 0;
+  if ((rc = batch_tokens(batch, &tokens))) return rc;
+  *bytes = lora_layout(lora, batch, tokens);
+  return DUET_OK;
+}
+
+int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t ldx, const void* base, int64_t ld_base,
+                  void* out, int64_t ld_out, const duet_batch* batch, const int32_t* adapter_ids, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+  clear_error();
+  if (!ctx) return fail(DUET_EINVAL, "ctx is NULL");
+  int rc = check_lora(lora);
+  if (rc || (rc = check_batch(nullptr, batch, true))) return rc;
+  if ((rc = check_device_ptr(lora->a, "a")) || (rc = check_device_ptr(lora->b, "b")) ||
+      (rc = check_device_ptr(x, "x")) || (rc = check_device_ptr(base, "base")) || (rc = check_device_ptr(out, "out")) ||
+      (rc = check_device_ptr(workspace, "workspace")))
+    return rc;
+  if (batch->num_reqs > 0 && !adapter_ids) return fail(DUET_EINVAL, "adapter_ids is NULL");
+  for (int r = 0; r < batch->num_reqs; ++r)
+    if (adapter_ids[r] < -1 || adapter_ids[r] >= lora->num_adapters)
+      return fail(DUET_EINVAL, "request %d: adapter %d not in [-1, %d)", r, adapter_ids[r], lora->num_adapters);
+  if (ldx < lora->d_in || ld_base < lora->d_out || ld_out < lora->d_out || ldx % 8 || ld_base % 8 || ld_out % 8)
+    return fail(DUET_EINVAL, "row strides %lld, %lld, %lld: multiples of 8, at least the rows' lengths", (long long)ldx,
+                (long long)ld_base, (long long)ld_out);
+  for (const void* p : {lora->a, lora->b, x, base, static_cast<const void*>(out)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "a, b, x, base and out must lie on 16 bytes");
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
+  if (out == x || out == lora->a || out == lora->b) return fail(DUET_EINVAL, "out aliases an input");
+  if (out == base && ld_out != ld_base) return fail(DUET_EINVAL, "out is base with another row stride");
+  LoraArgs a{};
+  if ((rc = batch_tokens(batch, &a.tokens))) return rc;
+  const size_t need = lora_layout(lora, batch, a.tokens);
+  if (workspace_bytes < need) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
+  a.x = static_cast<const __bf16*>(x);
+  a.base = static_cast<const __bf16*>(base);
+  a.a = static_cast<const __bf16*>(lora->a);
+  a.b = static_cast<const __bf16*>(lora->b);
+  a.out = static_cast<__bf16*>(out);
+  a.scale = lora->scale;
+  a.ldx = ldx;
+  a.ldb = ld_base;
+  a.ldo = ld_out;
+  a.num_reqs = batch->num_reqs;
+  a.rank = lora->rank;
+  a.d_in = lora->d_in;
+  a.d_out = lora->d_out;
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  if ((rc = upload_requests(ctx, batch, ws, st, [&](const duet_seq_meta& m, int r) {
+         return make_int4(adapter_ids[r], m.q_start, m.q_len, 0);
+       })))
+    return rc;
+  a.reqs = reinterpret_cast<const int4*>(ws + kAlign);
+  a.h = reinterpret_cast<float*>(ws + request_table_bytes(batch));
+  HIP_TRY(launch_lora(a, st));
+  return DUET_OK;
+}
+
+int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* stream) {
+  clear_error();
+  if (!ctx) return fail(DUET_EINVAL, "ctx is NULL");
+  int rc;
+  if ((rc = check_device_ptr(logits, "logits")) || (rc = check_device_ptr(u, "u")) || (rc = check_device_ptr(ids, "ids")))
+    return rc;
+  if (dtype != DUET_BF16 && dtype != DUET_F32) return fail(DUET_EUNSUPPORTED, "dtype must be bf16 or f32");
+  if (rows < 0 || rows > kMaxSampleRows) return fail(DUET_EINVAL, "rows %d not in [0, %d]", rows, kMaxSampleRows);
+  if (vocab < 1) return fail(DUET_EINVAL, "vocab %d < 1", vocab);
+  if (vocab > kMaxVocab) return fail(DUET_EUNSUPPORTED, "vocab %d: at most %d", vocab, kMaxVocab);
+  if (row_stride < vocab) return fail(DUET_EINVAL, "row_stride %lld < vocab %d", (long long)row_stride, vocab);
+  SampleArgs a{};
+  a.logits = logits;
+  a.row_stride = row_stride;
+  if (params) {
+    a.temperature = params->temperature;
+    a.top_k = params->top_k;
+    a.top_p = params->top_p;
+    a.min_p = params->min_p;
+  }
+  a.u = u;
+  a.ids = ids;
+  a.probs = probs;
+  a.dtype = dtype;
+  a.rows = rows;
+  a.vocab = vocab;
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  HIP_TRY(launch_sample(a, static_cast<hipStream_t>(stream)));
   return DUET_OK;
 }
 
