@@ -234,16 +234,24 @@ struct RopeSplitArgs {
 };
 hipError_t launch_rope_split(const RopeSplitArgs& a, hipStream_t s);
 
-// out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).
+// out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).  The rows are listed by adapter and taken in
+// tiles: rows[first] .. rows[first + count - 1] have this adapter (-1: none).
+constexpr int kLoraTileRows = 64;
+struct LoraTile {
+  int32_t adapter, first, count, pad;
+};
 struct LoraArgs {
   const __bf16 *x, *base, *a, *b;  // x [T, d_in], base [T, d_out], a [N, rank, d_in], b [N, d_out, rank]
   __bf16* out;                     // [T, d_out]
   const float* scale;              // [N], or null: 1
-  float* h;                        // [T, rank]
-  const int4* reqs;                // [R] (adapter or -1, first row, rows, 0)
+  float* h;                        // [parts, T, rank], rows in the order of the list
+  const LoraTile* tiles;
+  const int32_t* rows;             // [T]
   long long ldx, ldb, ldo;
-  int32_t num_reqs, tokens, rank, d_in, d_out;
+  int32_t n_tiles, parts, tokens, rank, d_in, d_out;
 };
+// Parts of the input's columns, each a workgroup a tile, that fill the chip when there are few rows.
+int lora_parts(int tokens, int d_in);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
 
 // One token from each row of logits (sample.hip); the parameters' arrays may be null.

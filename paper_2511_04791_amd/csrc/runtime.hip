@@ -604,37 +604,42 @@ void write_lists(const Plan& p, char* h) {
   }
 }
 
-int stage_upload(duet_ctx* ctx, const Plan& p, char* ws, hipStream_t st, bool may_allocate = true) {
+// Sends `bytes` to the workspace, the first `zero` of them as zeros, the others as write(h) puts them at h.
+template <typename F>
+int stage_bytes(duet_ctx* ctx, size_t zero, size_t bytes, F write, char* ws, hipStream_t st, bool may_allocate = true) {
   StagingSlot& slot = ctx->slots[ctx->next_slot];
-  if (!may_allocate && slot.cap < p.upload_bytes)
-    return fail(DUET_EWORKSPACE, "work lists of %zu bytes exceed the %zu bytes of preallocated staging", p.upload_bytes,
-                slot.cap);
+  if (!may_allocate && slot.cap < bytes)
+    return fail(DUET_EWORKSPACE, "work lists of %zu bytes exceed the %zu bytes of preallocated staging", bytes, slot.cap);
   hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
   HIP_TRY(hipStreamIsCapturing(st, &capturing));
   if (capturing != hipStreamCaptureStatusNone) {
     // No staging buffer: replays would find another call's lists in it.
-    std::vector<char> lists(p.upload_bytes);
-    write_lists(p, lists.data());
-    HIP_TRY(launch_upload_by_value(lists.data(), ws, p.upload_bytes, st));
+    std::vector<char> lists(bytes);
+    write(lists.data());
+    HIP_TRY(launch_upload_by_value(lists.data(), ws, bytes, st));
     return DUET_OK;
   }
   ctx->next_slot = (ctx->next_slot + 1) % kStagingSlots;
   int rc = wait_slot(&slot);
   if (rc) return rc;
-  if (slot.cap < p.upload_bytes && (rc = alloc_slot(&slot, std::max<size_t>(p.upload_bytes * 2, 1 << 16)))) return rc;
+  if (slot.cap < bytes && (rc = alloc_slot(&slot, std::max<size_t>(bytes * 2, 1 << 16)))) return rc;
   char* h = slot.data();
-  write_lists(p, h);
+  write(h);
   if (reinterpret_cast<uintptr_t>(ws) % 16 == 0) {
-    slot.blocks = upload_blocks(p.upload_bytes);
-    HIP_TRY(launch_upload(h, ws, p.off_meta, p.upload_bytes, slot.flags(), ++slot.seq, st));
+    slot.blocks = upload_blocks(bytes);
+    HIP_TRY(launch_upload(h, ws, zero, bytes, slot.flags(), ++slot.seq, st));
     slot.reader = StagingSlot::kKernel;
     return DUET_OK;
   }
-  std::memset(h, 0, p.off_meta);  // the error word and the decode work counters
-  HIP_TRY(hipMemcpyAsync(ws, h, p.upload_bytes, hipMemcpyHostToDevice, st));
+  std::memset(h, 0, zero);  // the error word and the decode work counters
+  HIP_TRY(hipMemcpyAsync(ws, h, bytes, hipMemcpyHostToDevice, st));
   HIP_TRY(hipEventRecord(slot.done, st));
   slot.reader = StagingSlot::kCopy;
   return DUET_OK;
+}
+
+int stage_upload(duet_ctx* ctx, const Plan& p, char* ws, hipStream_t st, bool may_allocate = true) {
+  return stage_bytes(ctx, p.off_meta, p.upload_bytes, [&](char* h) { write_lists(p, h); }, ws, st, may_allocate);
 }
 
 int check_device_ptr(const void* p, const char* name) {
@@ -1280,15 +1285,18 @@ int batch_tokens(const duet_batch* b, int32_t* tokens) {
 // A workspace that holds an error word and a table of the requests only.
 size_t request_table_bytes(const duet_batch* b) { return kAlign + align_up((size_t)b->num_reqs * sizeof(int4)); }
 
-template <typename F>
-int upload_requests(duet_ctx* ctx, const duet_batch* b, char* ws, hipStream_t st, F row) {
+// Parts of a workspace whose first kAlign bytes the upload clears, in rising order.
+struct UploadPart {
+  const void* data;
+  size_t bytes, at;
+};
+int upload_parts(duet_ctx* ctx, const UploadPart* parts, int n, char* ws, hipStream_t st) {
   try {
-    Plan p;
-    p.meta.reserve(b->num_reqs);
-    for (int r = 0; r < b->num_reqs; ++r) p.meta.push_back(row(b->reqs[r], r));
-    p.off_meta = p.off_pitems = p.off_dreq = p.off_ditems = p.off_punits = p.off_pcount = p.off_append = kAlign;
-    p.upload_bytes = request_table_bytes(b);
-    return stage_upload(ctx, p, ws, st);
+    const size_t bytes = align_up(parts[n - 1].at + parts[n - 1].bytes);
+    return stage_bytes(ctx, kAlign, bytes, [&](char* h) {
+      for (int i = 0; i < n; ++i)
+        if (parts[i].bytes) std::memcpy(h + parts[i].at, parts[i].data, parts[i].bytes);
+    }, ws, st);
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
   }
@@ -1319,9 +1327,43 @@ int check_lora(const duet_lora* l) {
   return DUET_OK;
 }
 
-// The request table, then h [tokens, rank].
-size_t lora_layout(const duet_lora* l, const duet_batch* b, int32_t tokens) {
-  return request_table_bytes(b) + align_up((size_t)tokens * l->rank * sizeof(float));
+// Workspace of duet_lora_add: a head that the upload clears, the tiles, the rows by adapter, h.  There are at most as
+// many tiles that are not full as adapters and requests (and one of rows without an adapter).
+struct LoraLayout {
+  size_t tiles, rows, h, total;
+};
+LoraLayout lora_layout(const duet_lora* l, const duet_batch* b, int32_t tokens) {
+  const size_t most = (size_t)tokens / kLoraTileRows + std::min(l->num_adapters + 1, b->num_reqs);
+  LoraLayout L;
+  L.tiles = kAlign;
+  L.rows = L.tiles + align_up(most * sizeof(LoraTile));
+  L.h = L.rows + align_up((size_t)tokens * sizeof(int32_t));
+  L.total = L.h + align_up((size_t)lora_parts(tokens, l->d_in) * tokens * l->rank * sizeof(float));
+  return L;
+}
+
+// The batch's rows by adapter (in order within each), and their tiles; rows without one only if `with_none`.
+int lora_lists(const duet_lora* l, const duet_batch* b, const int32_t* ids, bool with_none, std::vector<LoraTile>* tiles,
+               std::vector<int32_t>* rows) {
+  try {
+    std::vector<int> order;
+    for (int r = 0; r < b->num_reqs; ++r)
+      if (ids[r] >= 0 || with_none) order.push_back(r);
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return ids[x] < ids[y]; });
+    for (size_t i = 0; i < order.size();) {
+      const int id = ids[order[i]];
+      int first = (int)rows->size();
+      for (; i < order.size() && ids[order[i]] == id; ++i) {
+        const duet_seq_meta& m = b->reqs[order[i]];
+        for (int t = 0; t < m.q_len; ++t) rows->push_back(m.q_start + t);
+      }
+      for (; first < (int)rows->size(); first += kLoraTileRows)
+        tiles->push_back(LoraTile{id, first, std::min(kLoraTileRows, (int)rows->size() - first), 0});
+    }
+    return DUET_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(DUET_ENOMEM, "host allocation failed");
+  }
 }
 
 // Rows [row0, row0 + rows) of the requests of one kind, or rows = -1 when they are not one
@@ -1866,10 +1908,9 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   HIP_TRY(device.status);
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  if ((rc = upload_requests(ctx, batch, ws, st, [](const duet_seq_meta& m, int) {
-         return make_int4(m.kind, m.q_start, m.q_len, m.cached_len);
-       })))
-    return rc;
+  static_assert(sizeof(duet_seq_meta) == sizeof(int4), "the kernels read the requests as they are");
+  const UploadPart table{batch->reqs, batch->num_reqs * sizeof(int4), kAlign};
+  if ((rc = upload_parts(ctx, &table, 1, ws, st))) return rc;
   a.meta = reinterpret_cast<const int4*>(ws + kAlign);
   a.err = reinterpret_cast<int32_t*>(ws);
   HIP_TRY(launch_rope_split(a, st));
@@ -1883,7 +1924,7 @@ int duet_lora_workspace_bytes(const duet_lora* lora, const duet_batch* batch, si
   if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
   int32_t tokens = 0;
   if ((rc = batch_tokens(batch, &tokens))) return rc;
-  *bytes = lora_layout(lora, batch, tokens);
+  *bytes = lora_layout(lora, batch, tokens).total;
   return DUET_OK;
 }
 
@@ -1912,8 +1953,11 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   if (out == base && ld_out != ld_base) return fail(DUET_EINVAL, "out is base with another row stride");
   LoraArgs a{};
   if ((rc = batch_tokens(batch, &a.tokens))) return rc;
-  const size_t need = lora_layout(lora, batch, a.tokens);
-  if (workspace_bytes < need) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
+  const LoraLayout L = lora_layout(lora, batch, a.tokens);
+  if (workspace_bytes < L.total) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, L.total);
+  std::vector<LoraTile> tiles;
+  std::vector<int32_t> rows;
+  if ((rc = lora_lists(lora, batch, adapter_ids, out != base, &tiles, &rows))) return rc;
   a.x = static_cast<const __bf16*>(x);
   a.base = static_cast<const __bf16*>(base);
   a.a = static_cast<const __bf16*>(lora->a);
@@ -1923,7 +1967,6 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   a.ldx = ldx;
   a.ldb = ld_base;
   a.ldo = ld_out;
-  a.num_reqs = batch->num_reqs;
   a.rank = lora->rank;
   a.d_in = lora->d_in;
   a.d_out = lora->d_out;
@@ -1932,12 +1975,15 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   HIP_TRY(device.status);
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  if ((rc = upload_requests(ctx, batch, ws, st, [&](const duet_seq_meta& m, int r) {
-         return make_int4(adapter_ids[r], m.q_start, m.q_len, 0);
-       })))
-    return rc;
-  a.reqs = reinterpret_cast<const int4*>(ws + kAlign);
-  a.h = reinterpret_cast<float*>(ws + request_table_bytes(batch));
+  if (tiles.empty()) return DUET_OK;
+  const UploadPart parts[2] = {{tiles.data(), tiles.size() * sizeof(LoraTile), L.tiles},
+                               {rows.data(), rows.size() * sizeof(int32_t), L.rows}};
+  if ((rc = upload_parts(ctx, parts, 2, ws, st))) return rc;
+  a.tiles = reinterpret_cast<const LoraTile*>(ws + L.tiles);
+  a.rows = reinterpret_cast<const int32_t*>(ws + L.rows);
+  a.n_tiles = (int)tiles.size();
+  a.parts = lora_parts(a.tokens, lora->d_in);
+  a.h = reinterpret_cast<float*>(ws + L.h);
   HIP_TRY(launch_lora(a, st));
   return DUET_OK;
 }
