@@ -244,13 +244,16 @@ struct LoraArgs {
   const __bf16 *x, *base, *a, *b;  // x [T, d_in], base [T, d_out], a [N, rank, d_in], b [N, d_out, rank]
   __bf16* out;                     // [T, d_out]
   const float* scale;              // [N], or null: 1
-  float* h;                        // [parts, T, rank], rows in the order of the list
+  float* part;                     // [parts, T, rank], rows in the order of the list
+  __bf16* h;                       // [T, 2 rank]: h and the rounding it leaves out
+  int32_t* done;                   // [tiles] parts finished; zero before the call
   const LoraTile* tiles;
   const int32_t* rows;             // [T]
   long long ldx, ldb, ldo;
   int32_t n_tiles, parts, tokens, rank, d_in, d_out;
 };
 // Parts of the input's columns, each a workgroup a tile, that fill the chip when there are few rows.
+constexpr int kLoraMaxParts = 16;
 int lora_parts(int tokens, int d_in);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
 

@@ -1,6 +1,6 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   out[t] = base[t] + scale_a B_a (A_a x[t]),  a the adapter of token t's request.
-// Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h with one rounding to bf16.
+// Two kernels: h = scale_a A_a x into the workspace, then out = base + B_a h with one rounding to bf16.
 // Both are bound by memory: x, base and out pass once, the adapters are a few MB.
 //
 // Rows of one adapter, wherever in the batch they stand, are taken in tiles of up to kTileRows, so its weights are
@@ -17,24 +17,42 @@ namespace duet {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRowTiles = kLoraTileRows / 16;
-constexpr int kUnit = 64;  // input columns of a wave's step: 128 bytes of each row
 
 __device__ __forceinline__ bf16x8 load8(const __bf16* p) { return *reinterpret_cast<const bf16x8*>(p); }
 __device__ __forceinline__ bf16x8 zero8() { return __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
 
-// h of a tile over the columns of one part: four waves take its 64-column units in turn, each all of the tile's
-// rows and ranks, and are summed through LDS in a fixed order.  NT: 16-rank tiles.
+// Four values that another workgroup, on whatever XCD, reads or wrote within the launch: device-scope accesses go
+// past the XCD's L2, without the write-back and invalidation of all of it that a device-scope fence costs.
+__device__ __forceinline__ void store_shared(float* p, f32x4 v) {
+  const ulonglong2 u = __builtin_bit_cast(ulonglong2, v);
+  unsigned long long* q = reinterpret_cast<unsigned long long*>(p);
+  __hip_atomic_store(q, u.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(q + 1, u.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4 load_shared(const float* p) {
+  const unsigned long long* q = reinterpret_cast<const unsigned long long*>(p);
+  return __builtin_bit_cast(f32x4, make_ulonglong2(__hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                                   __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
+}
+
+// h of a tile over the columns of one part: four waves take its units of kUnit columns in turn, each all of the
+// tile's rows and ranks, and are summed through LDS in a fixed order.  NT: 16-rank tiles.  A unit's loads are issued
+// ahead of the products of the one before it.  The part that finishes last adds all of them in their order and
+// writes h for the second kernel: scaled, as two bf16 (its value and what that leaves out, 16 bits together).
 template <int NT>
 __global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
+  constexpr int kHalves = NT == 8 ? 1 : 2, kUnit = 32 * kHalves;
   __shared__ f32x4 sums[2][kRowTiles * NT][64];
+  __shared__ int last;
   const LoraTile tile = s.tiles[blockIdx.x];
   if (tile.adapter < 0) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int units = (s.d_in + kUnit - 1) / kUnit;
-  const int u1 = (int)((long long)units * (blockIdx.y + 1) / s.parts);
+  const int u0 = (int)((long long)units * blockIdx.y / s.parts), u1 = (int)((long long)units * (blockIdx.y + 1) / s.parts);
   const int row_tiles = (tile.count + 15) / 16;
   const __bf16* x[kRowTiles];
 #pragma unroll
@@ -42,23 +60,35 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
   const __bf16* w[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) w[n] = s.a + ((size_t)tile.adapter * s.rank + min(16 * n + m, s.rank - 1)) * s.d_in + 8 * g;
-  f32x4 acc[kRowTiles][NT] = {};
-  for (int u = (int)((long long)units * blockIdx.y / s.parts) + wave; u < u1; u += 4) {
+  struct Unit {
+    bf16x8 w[kHalves][NT], x[kHalves][kRowTiles];
+  };
+  auto load = [&](int u, Unit* f) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < kHalves; ++half) {
       const int k = u * kUnit + 32 * half;
-      const bool in = k + 8 * g < s.d_in;  // d_in is a multiple of 8
-      bf16x8 wv[NT], xv[kRowTiles];
+      const bool in = u < u1 && k + 8 * g < s.d_in;  // d_in is a multiple of 8
 #pragma unroll
-      for (int n = 0; n < NT; ++n) wv[n] = in ? load8(w[n] + k) : zero8();
+      for (int n = 0; n < NT; ++n) f->w[half][n] = in ? load8(w[n] + k) : zero8();
 #pragma unroll
-      for (int t = 0; t < kRowTiles; ++t) xv[t] = in && t < row_tiles ? load8(x[t] + k) : zero8();
+      for (int t = 0; t < kRowTiles; ++t) f->x[half][t] = in && t < row_tiles ? load8(x[t] + k) : zero8();
+    }
+  };
+  f32x4 acc[kRowTiles][NT] = {};
+  Unit now, next;
+  load(u0 + wave, &now);
+  for (int u = u0 + wave; u < u1; u += 4) {
+    load(u + 4, &next);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int half = 0; half < kHalves; ++half)
 #pragma unroll
       for (int t = 0; t < kRowTiles; ++t)
         if (t < row_tiles)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], xv[t], acc[t][n], 0, 0, 0);
-    }
+          for (int n = 0; n < NT; ++n)
+            acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.w[half][n], now.x[half][t], acc[t][n], 0, 0, 0);
+    now = next;
   }
   auto put = [&](int b) {
 #pragma unroll
@@ -80,47 +110,68 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
   __syncthreads();
   if (wave == 1) put(0);
   __syncthreads();
-  if (wave) return;
-  add(0);
-  float* h = s.h + ((size_t)blockIdx.y * s.tokens + tile.first) * s.rank;
+  if (wave == 0) {
+    add(0);
+    float* part = s.part + ((size_t)blockIdx.y * s.tokens + tile.first) * s.rank;
 #pragma unroll
-  for (int t = 0; t < kRowTiles; ++t)
+    for (int t = 0; t < kRowTiles; ++t)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank)
-        *reinterpret_cast<f32x4*>(h + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g) = acc[t][n];
-}
-
-// out of a tile, 64 columns a wave at a time.  h is summed over its parts, scaled and held in LDS as two bf16 (its
-// value and what that leaves out: 16 bits together), side by side along the product's axis: [h_hi | h_lo] times
-// [B | B].  The 16 columns of an MFMA are taken in fours out of 32, so that two MFMAs give a lane eight neighbours.
-__global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
-  extern __shared__ __align__(16) __bf16 hs[];  // [kLoraTileRows][stride]
-  const LoraTile tile = s.tiles[blockIdx.x];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const int chunks = s.rank / 8, steps = (2 * chunks + 3) / 4, stride = steps * 32 + 8;
-  const int row_tiles = (tile.count + 15) / 16;
-  if (tile.adapter >= 0) {
-    const float scale = s.scale ? s.scale[tile.adapter] : 1.f;
-    for (int i = threadIdx.x; i < row_tiles * 16 * steps * 32; i += 256) {
-      const int row = i / (steps * 32), c = i % (steps * 32);
-      if (c < s.rank) {
-        float h = 0.f;
-        if (row < tile.count)
-          for (int p = 0; p < s.parts; ++p) h += s.h[((size_t)p * s.tokens + tile.first + row) * s.rank + c];
-        h *= scale;
-        const __bf16 hi = static_cast<__bf16>(h);
-        hs[row * stride + c] = hi;
-        hs[row * stride + s.rank + c] = static_cast<__bf16>(__builtin_isfinite(h) ? h - static_cast<float>(hi) : 0.f);
-      } else if (c >= 2 * s.rank) {
-        hs[row * stride + c] = static_cast<__bf16>(0.f);
-      }
-    }
+      for (int n = 0; n < NT; ++n)
+        if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank)
+          store_shared(part + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g, acc[t][n]);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores have completed
+    if (lane == 0) last = atomicAdd(s.done + blockIdx.x, 1) == s.parts - 1;
   }
   __syncthreads();
-  long long row[kRowTiles];
+  if (!last) return;
+  const float scale = s.scale ? s.scale[tile.adapter] : 1.f;
+  const size_t step = (size_t)s.tokens * s.rank, at = (size_t)tile.first * s.rank;
+  for (int i = threadIdx.x; i < tile.count * s.rank / 4; i += 256) {
+    f32x4 v[kLoraMaxParts];
 #pragma unroll
-  for (int t = 0; t < kRowTiles; ++t) row[t] = s.rows[tile.first + min(16 * t + m, tile.count - 1)];
+    for (int p = 0; p < kLoraMaxParts; ++p) v[p] = load_shared(s.part + min(p, s.parts - 1) * step + at + 4 * i);
+    f32x4 h = v[0];
+#pragma unroll
+    for (int p = 1; p < kLoraMaxParts; ++p)
+      if (p < s.parts) h += v[p];
+    h *= scale;
+    bf16x4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      hi[e] = static_cast<__bf16>(h[e]);
+      lo[e] = static_cast<__bf16>(__builtin_isfinite(h[e]) ? h[e] - static_cast<float>(hi[e]) : 0.f);
+    }
+    __bf16* to = s.h + (size_t)(tile.first + 4 * i / s.rank) * 2 * s.rank + 4 * i % s.rank;
+    *reinterpret_cast<bf16x4*>(to) = hi;
+    *reinterpret_cast<bf16x4*>(to + s.rank) = lo;
+  }
+}
+
+// out of a tile, 64 columns a wave at a time: [h_hi | h_lo] times [B | B], STEPS MFMAs of 32 along that axis.  The 16
+// columns of an MFMA are taken in fours out of 32, so that two MFMAs give a lane eight neighbours.
+template <int STEPS>
+__global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
+  constexpr bool kKeep = STEPS <= 4;  // the tile's h stays in registers
+  const LoraTile tile = s.tiles[blockIdx.x];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int chunks = s.rank / 8, row_tiles = (tile.count + 15) / 16;
+  const bool some = tile.adapter >= 0;
+  long long row[kRowTiles];
+  const __bf16* h[kRowTiles];
+#pragma unroll
+  for (int t = 0; t < kRowTiles; ++t) {
+    const int i = tile.first + min(16 * t + m, tile.count - 1);
+    row[t] = s.rows[i];
+    h[t] = s.h + (size_t)i * 2 * s.rank;
+  }
+  auto h_of = [&](int t, int st) { return 4 * st + g < 2 * chunks ? load8(h[t] + 8 * (4 * st + g)) : zero8(); };
+  bf16x8 kept[kKeep ? STEPS : 1][kRowTiles];
+  if (kKeep && some)
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+      for (int t = 0; t < kRowTiles; ++t)
+        if (kKeep) kept[kKeep ? st : 0][t] = h_of(t, st);
   const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
   for (int c0 = (blockIdx.y * 4 + wave) * 64; c0 < s.d_out; c0 += gridDim.y * 256) {
     bf16x8 base[kRowTiles][2];
@@ -132,8 +183,9 @@ __global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
         if (16 * t + m < tile.count && c < s.d_out) base[t][p] = load8(s.base + row[t] * s.ldb + c);
       }
     f32x4 acc[kRowTiles][4] = {};
-    if (tile.adapter >= 0) {
-      for (int st = 0; st < steps; ++st) {
+    if (some) {
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
         const int q = 4 * st + g;
         bf16x8 wv[4];
 #pragma unroll
@@ -144,7 +196,7 @@ __global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
 #pragma unroll
         for (int t = 0; t < kRowTiles; ++t)
           if (t < row_tiles) {
-            const bf16x8 hv = load8(hs + (16 * t + m) * stride + 8 * q);
+            const bf16x8 hv = kKeep ? kept[kKeep ? st : 0][t] : h_of(t, st);
 #pragma unroll
             for (int n = 0; n < 4; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], hv, acc[t][n], 0, 0, 0);
           }
@@ -157,7 +209,7 @@ __global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
         const int c = c0 + 32 * p + 8 * g;
         if (16 * t + m >= tile.count || c >= s.d_out) continue;
         bf16x8 o = base[t][p];
-        if (tile.adapter >= 0)
+        if (some)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             o[e] = static_cast<__bf16>(static_cast<float>(base[t][p][e]) + acc[t][2 * p + e / 4][e % 4]);
@@ -169,8 +221,8 @@ __global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
 }  // namespace
 
 int lora_parts(int tokens, int d_in) {
-  const int tiles = (tokens + kLoraTileRows - 1) / kLoraTileRows, units = (d_in + kUnit - 1) / kUnit;
-  return std::max(1, std::min({16, 512 / std::max(tiles, 1), (units + 3) / 4}));
+  const int tiles = (tokens + kLoraTileRows - 1) / kLoraTileRows, units = (d_in + 63) / 64;
+  return std::max(1, std::min({kLoraMaxParts, 512 / std::max(tiles, 1), (units + 3) / 4}));
 }
 
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s) {
@@ -182,10 +234,12 @@ hipError_t launch_lora(const LoraArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL(lora_down<8>, down, block, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int steps = (a.rank / 4 + 3) / 4;
   const int blocks = (a.d_out + 255) / 256;
   const dim3 up(a.n_tiles, std::max(1, std::min(blocks, 2048 / a.n_tiles)));
-  hipLaunchKernelGGL(lora_up, up, block, kLoraTileRows * (steps * 32 + 8) * sizeof(__bf16), s, a);
+  if (a.rank <= 16) hipLaunchKernelGGL(lora_up<1>, up, block, 0, s, a);
+  else if (a.rank <= 32) hipLaunchKernelGGL(lora_up<2>, up, block, 0, s, a);
+  else if (a.rank <= 64) hipLaunchKernelGGL(lora_up<4>, up, block, 0, s, a);
+  else hipLaunchKernelGGL(lora_up<8>, up, block, 0, s, a);
   return hipGetLastError();
 }
 
