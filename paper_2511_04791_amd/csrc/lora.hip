@@ -39,70 +39,82 @@ __device__ __forceinline__ f32x4 load_shared(const float* p) {
                                                    __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
 }
 
-// h of a tile over the columns of one part: four waves take its units of kUnit columns in turn, each all of the
-// tile's rows and ranks, and are summed through LDS in a fixed order.  NT: 16-rank tiles.  A unit's loads are issued
-// ahead of the products of the one before it.  The part that finishes last adds all of them in their order and
-// writes h for the second kernel: scaled, as two bf16 (its value and what that leaves out, 16 bits together).
-template <int NT>
-__global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
+// Partial sums of h of a tile's 16 RT rows over the columns of one part: four waves take its units of kUnit columns in
+// turn, each all of the rows and ranks (NT 16-rank tiles), and are summed through LDS in a fixed order.  A unit's
+// loads are issued ahead of the products of the one before it.
+template <int NT, int RT>
+__device__ __forceinline__ void down_part(const LoraArgs& s, const LoraTile& tile, f32x4 (*sums)[kRowTiles * NT][64]) {
   constexpr int kHalves = NT == 8 ? 1 : 2, kUnit = 32 * kHalves;
-  __shared__ f32x4 sums[2][kRowTiles * NT][64];
-  __shared__ int last;
-  const LoraTile tile = s.tiles[blockIdx.x];
-  if (tile.adapter < 0) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int units = (s.d_in + kUnit - 1) / kUnit;
-  const int u0 = (int)((long long)units * blockIdx.y / s.parts), u1 = (int)((long long)units * (blockIdx.y + 1) / s.parts);
-  const int row_tiles = (tile.count + 15) / 16;
-  const __bf16* x[kRowTiles];
+  const int u0 = (int)((long long)units * blockIdx.y / s.parts) + wave;
+  const int u1 = (int)((long long)units * (blockIdx.y + 1) / s.parts);
+  const __bf16 *x[RT], *w[NT];
 #pragma unroll
-  for (int t = 0; t < kRowTiles; ++t) x[t] = s.x + s.rows[tile.first + min(16 * t + m, tile.count - 1)] * s.ldx + 8 * g;
-  const __bf16* w[NT];
+  for (int t = 0; t < RT; ++t) x[t] = s.x + s.rows[tile.first + min(16 * t + m, tile.count - 1)] * s.ldx + 8 * g;
 #pragma unroll
   for (int n = 0; n < NT; ++n) w[n] = s.a + ((size_t)tile.adapter * s.rank + min(16 * n + m, s.rank - 1)) * s.d_in + 8 * g;
   struct Unit {
-    bf16x8 w[kHalves][NT], x[kHalves][kRowTiles];
+    bf16x8 w[kHalves][NT], x[kHalves][RT];
   };
-  auto load = [&](int u, Unit* f) {
+  f32x4 acc[RT][NT] = {};
+  auto load = [&](int u, Unit& f) {
 #pragma unroll
     for (int half = 0; half < kHalves; ++half) {
-      const int k = u * kUnit + 32 * half;
-      const bool in = u < u1 && k + 8 * g < s.d_in;  // d_in is a multiple of 8
 #pragma unroll
-      for (int n = 0; n < NT; ++n) f->w[half][n] = in ? load8(w[n] + k) : zero8();
+      for (int n = 0; n < NT; ++n) f.w[half][n] = load8(w[n] + u * kUnit + 32 * half);
 #pragma unroll
-      for (int t = 0; t < kRowTiles; ++t) f->x[half][t] = in && t < row_tiles ? load8(x[t] + k) : zero8();
+      for (int t = 0; t < RT; ++t) f.x[half][t] = load8(x[t] + u * kUnit + 32 * half);
     }
-  };
-  f32x4 acc[kRowTiles][NT] = {};
-  Unit now, next;
-  load(u0 + wave, &now);
-  for (int u = u0 + wave; u < u1; u += 4) {
-    load(u + 4, &next);
     __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](const Unit& f) {
 #pragma unroll
     for (int half = 0; half < kHalves; ++half)
 #pragma unroll
-      for (int t = 0; t < kRowTiles; ++t)
-        if (t < row_tiles)
+      for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.w[half][n], now.x[half][t], acc[t][n], 0, 0, 0);
-    now = next;
+        for (int n = 0; n < NT; ++n)
+          acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[half][n], f.x[half][t], acc[t][n], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int whole = min(u1, s.d_in / kUnit);  // the last unit may be cut off, at a multiple of 8 columns
+  if (u0 < whole) {
+    const int n = (whole - u0 + 3) / 4;
+    Unit even, odd;
+    load(u0, even);
+    for (int i = 0; i + 2 <= n; i += 2) {
+      load(u0 + 4 * (i + 1), odd);
+      multiply(even);
+      load(u0 + 4 * min(i + 2, n - 1), even);
+      multiply(odd);
+    }
+    if (n & 1) multiply(even);
+  }
+  if (whole < u1 && (whole - u0) % 4 == 0) {
+    Unit cut;
+#pragma unroll
+    for (int half = 0; half < kHalves; ++half) {
+      const int k = whole * kUnit + 32 * half;
+      const bool in = k + 8 * g < s.d_in;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) cut.w[half][n] = in ? load8(w[n] + k) : zero8();
+#pragma unroll
+      for (int t = 0; t < RT; ++t) cut.x[half][t] = in ? load8(x[t] + k) : zero8();
+    }
+    multiply(cut);
   }
   auto put = [&](int b) {
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (t < row_tiles) sums[b][t * NT + n][lane] = acc[t][n];
+      for (int n = 0; n < NT; ++n) sums[b][t * NT + n][lane] = acc[t][n];
   };
   auto add = [&](int b) {
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (t < row_tiles) acc[t][n] += sums[b][t * NT + n][lane];
+      for (int n = 0; n < NT; ++n) acc[t][n] += sums[b][t * NT + n][lane];
   };
   if (wave >= 2) put(wave - 2);
   __syncthreads();
@@ -110,17 +122,31 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
   __syncthreads();
   if (wave == 1) put(0);
   __syncthreads();
-  if (wave == 0) {
-    add(0);
-    float* part = s.part + ((size_t)blockIdx.y * s.tokens + tile.first) * s.rank;
+  if (wave) return;
+  add(0);
+  float* part = s.part + ((size_t)blockIdx.y * s.tokens + tile.first) * s.rank;
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t)
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank)
-          store_shared(part + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g, acc[t][n]);
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores have completed
-    if (lane == 0) last = atomicAdd(s.done + blockIdx.x, 1) == s.parts - 1;
+    for (int n = 0; n < NT; ++n)
+      if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank)
+        store_shared(part + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g, acc[t][n]);
+}
+
+// The part of a tile that finishes last adds all of them in their order and writes h for the second kernel: scaled, as
+// two bf16 (its value and what that leaves out, 16 bits together).
+template <int NT>
+__global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
+  __shared__ f32x4 sums[2][kRowTiles * NT][64];
+  __shared__ int last;
+  const LoraTile tile = s.tiles[blockIdx.x];
+  if (tile.adapter < 0) return;
+  if (tile.count > 32) down_part<NT, 4>(s, tile, sums);
+  else if (tile.count > 16) down_part<NT, 2>(s, tile, sums);
+  else down_part<NT, 1>(s, tile, sums);
+  if (threadIdx.x < 64) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's stores have completed
+    if (threadIdx.x == 0) last = atomicAdd(s.done + blockIdx.x, 1) == s.parts - 1;
   }
   __syncthreads();
   if (!last) return;
@@ -147,82 +173,105 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s) {
   }
 }
 
-// out of a tile, 64 columns a wave at a time: [h_hi | h_lo] times [B | B], STEPS MFMAs of 32 along that axis.  The 16
-// columns of an MFMA are taken in fours out of 32, so that two MFMAs give a lane eight neighbours.
-template <int STEPS>
-__global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
-  constexpr bool kKeep = STEPS <= 4;  // the tile's h stays in registers
-  const LoraTile tile = s.tiles[blockIdx.x];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const int chunks = s.rank / 8, row_tiles = (tile.count + 15) / 16;
+// out of 16 RT rows of a tile from row0 on, 64 columns at a time, every col_step-th from col0 on.  Ranks up to 16 (STEPS 0)
+// take h's two halves and B twice along one MFMA, [h_hi | h_lo] times [B | B]; others STEPS times 32 ranks, B for both
+// halves.  The 16 columns of an MFMA are taken in fours out of 32, so that two MFMAs give a lane eight neighbours.  The next
+// columns' base is read ahead of the products.
+template <int STEPS, int RT>
+__device__ __forceinline__ void up_rows(const LoraArgs& s, const LoraTile& tile, int row0, int col0, int col_step) {
+  constexpr int kSteps = STEPS ? STEPS : 1, kParts = STEPS ? 2 : 1;
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0;
-  long long row[kRowTiles];
-  const __bf16* h[kRowTiles];
+  if (col0 >= s.d_out) return;
+  const __bf16 *h[RT], *base[RT];
+  __bf16* out[RT];
 #pragma unroll
-  for (int t = 0; t < kRowTiles; ++t) {
-    const int i = tile.first + min(16 * t + m, tile.count - 1);
-    row[t] = s.rows[i];
+  for (int t = 0; t < RT; ++t) {
+    const int i = tile.first + min(row0 + 16 * t + m, tile.count - 1);
+    const long long row = s.rows[i];
     h[t] = s.h + (size_t)i * 2 * s.rank;
+    base[t] = s.base + row * s.ldb;
+    out[t] = s.out + row * s.ldo;
   }
-  auto h_of = [&](int t, int st) { return 4 * st + g < 2 * chunks ? load8(h[t] + 8 * (4 * st + g)) : zero8(); };
-  bf16x8 kept[kKeep ? STEPS : 1][kRowTiles];
-  if (kKeep && some)
+  auto read = [&](int c0, bf16x8 (*v)[2]) {  // past the last column: the last eight again
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int t = 0; t < kRowTiles; ++t)
-        if (kKeep) kept[kKeep ? st : 0][t] = h_of(t, st);
+      for (int p = 0; p < 2; ++p) v[t][p] = load8(base[t] + min(c0 + 32 * p + 8 * g, s.d_out - 8));
+  };
+  bf16x8 now[RT][2], next[RT][2];
+  read(col0, now);
+  bf16x8 hv[kSteps][kParts][RT];
+  if (some) {
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+      for (int p = 0; p < kParts; ++p)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const int q = 4 * st + g;
+          hv[st][p][t] = q < (STEPS ? chunks : 2 * chunks) ? load8(h[t] + p * s.rank + 8 * q) : zero8();
+        }
+  }
   const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
-  for (int c0 = (blockIdx.y * 4 + wave) * 64; c0 < s.d_out; c0 += gridDim.y * 256) {
-    bf16x8 base[kRowTiles][2];
-#pragma unroll
-    for (int t = 0; t < kRowTiles; ++t)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int c = c0 + 32 * p + 8 * g;
-        if (16 * t + m < tile.count && c < s.d_out) base[t][p] = load8(s.base + row[t] * s.ldb + c);
-      }
-    f32x4 acc[kRowTiles][4] = {};
+  for (int c0 = col0; c0 < s.d_out; c0 += col_step) {
+    f32x4 acc[RT][4] = {};
     if (some) {
+      bf16x8 wv[kSteps][4];
 #pragma unroll
-      for (int st = 0; st < STEPS; ++st) {
-        const int q = 4 * st + g;
-        bf16x8 wv[4];
+      for (int st = 0; st < kSteps; ++st)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const int c = c0 + 32 * (n / 2) + 8 * (m / 4) + 4 * (n % 2) + m % 4;
-          wv[n] = q < 2 * chunks && c < s.d_out ? load8(w + (size_t)c * s.rank + 8 * (q < chunks ? q : q - chunks)) : zero8();
+          const int q = 4 * st + g, c = min(c0 + 32 * (n / 2) + 8 * (m / 4) + 4 * (n % 2) + m % 4, s.d_out - 1);
+          const __bf16* wc = w + (size_t)c * s.rank;
+          if (STEPS) wv[st][n] = q < chunks ? load8(wc + 8 * q) : zero8();
+          else wv[st][n] = q < 2 * chunks ? load8(wc + 8 * (q < chunks ? q : q - chunks)) : zero8();
         }
+      read(c0 + col_step, next);
 #pragma unroll
-        for (int t = 0; t < kRowTiles; ++t)
-          if (t < row_tiles) {
-            const bf16x8 hv = kKeep ? kept[kKeep ? st : 0][t] : h_of(t, st);
+      for (int st = 0; st < kSteps; ++st)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], hv, acc[t][n], 0, 0, 0);
-          }
-      }
+        for (int p = 0; p < kParts; ++p)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+              acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], hv[st][p][t], acc[t][n], 0, 0, 0);
+    } else {
+      read(c0 + col_step, next);
     }
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const int c = c0 + 32 * p + 8 * g;
-        if (16 * t + m >= tile.count || c >= s.d_out) continue;
-        bf16x8 o = base[t][p];
+        bf16x8 o = now[t][p];
         if (some)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            o[e] = static_cast<__bf16>(static_cast<float>(base[t][p][e]) + acc[t][2 * p + e / 4][e % 4]);
-        *reinterpret_cast<bf16x8*>(s.out + row[t] * s.ldo + c) = o;
+            o[e] = static_cast<__bf16>(static_cast<float>(o[e]) + acc[t][2 * p + e / 4][e % 4]);
+        const int c = c0 + 32 * p + 8 * g;
+        if (row0 + 16 * t + m < tile.count && c < s.d_out) *reinterpret_cast<bf16x8*>(out[t] + c) = o;
+        now[t][p] = next[t][p];
       }
   }
+}
+
+// A wave takes 32 rows of a tile: two waves the rows of one that holds more, so two 64-column blocks at a time for the
+// workgroup, else four.
+template <int STEPS>
+__global__ __launch_bounds__(256) void lora_up(LoraArgs s) {
+  const LoraTile tile = s.tiles[blockIdx.x];
+  const int wave = threadIdx.x >> 6;
+  if (tile.count > 32) up_rows<STEPS, 2>(s, tile, 32 * (wave & 1), (blockIdx.y * 2 + (wave >> 1)) * 64, gridDim.y * 128);
+  else if (tile.count > 16) up_rows<STEPS, 2>(s, tile, 0, (blockIdx.y * 4 + wave) * 64, gridDim.y * 256);
+  else up_rows<STEPS, 1>(s, tile, 0, (blockIdx.y * 4 + wave) * 64, gridDim.y * 256);
 }
 
 }  // namespace
 
 int lora_parts(int tokens, int d_in) {
-  const int tiles = (tokens + kLoraTileRows - 1) / kLoraTileRows, units = (d_in + 63) / 64;
-  return std::max(1, std::min({kLoraMaxParts, 512 / std::max(tiles, 1), (units + 3) / 4}));
+  const int tiles = std::max(1, (tokens + kLoraTileRows - 1) / kLoraTileRows), units = (d_in + 63) / 64;
+  return std::max(1, std::min({kLoraMaxParts, (160 + tiles - 1) / tiles, (units + 3) / 4}));
 }
 
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s) {
@@ -234,12 +283,12 @@ hipError_t launch_lora(const LoraArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL(lora_down<8>, down, block, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int blocks = (a.d_out + 255) / 256;
+  const int blocks = (a.d_out + 127) / 128;
   const dim3 up(a.n_tiles, std::max(1, std::min(blocks, 2048 / a.n_tiles)));
-  if (a.rank <= 16) hipLaunchKernelGGL(lora_up<1>, up, block, 0, s, a);
-  else if (a.rank <= 32) hipLaunchKernelGGL(lora_up<2>, up, block, 0, s, a);
-  else if (a.rank <= 64) hipLaunchKernelGGL(lora_up<4>, up, block, 0, s, a);
-  else hipLaunchKernelGGL(lora_up<8>, up, block, 0, s, a);
+  if (a.rank <= 16) hipLaunchKernelGGL(lora_up<0>, up, block, 0, s, a);
+  else if (a.rank <= 32) hipLaunchKernelGGL(lora_up<1>, up, block, 0, s, a);
+  else if (a.rank <= 64) hipLaunchKernelGGL(lora_up<2>, up, block, 0, s, a);
+  else hipLaunchKernelGGL(lora_up<4>, up, block, 0, s, a);
   return hipGetLastError();
 }
 
