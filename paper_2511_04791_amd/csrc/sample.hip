@@ -6,13 +6,16 @@
 // whose kept cumulative mass exceeds u times the kept mass S.
 //
 // So every step looks for a place in the ranking, and a row need not be sorted: a histogram over
-// d = (max - x) / T gives the mass before each of its bins, and the bin that holds the place is narrowed by
-// the bits of its logits, down to one value, whose tokens weigh the same.  The mass of tokens with d >= kSpan
-// (e^-48 each, at most 4e-16 of the largest's over a row) is less than a unit in the last place of S in 64 bits.
+// d = (max - x) / T gives the mass before each of its bins, and only the tokens of the few bins that can hold
+// the places looked for are listed, sorted and summed.  The mass of tokens with d >= kSpan (e^-48 each, at most
+// 4e-16 of the largest's over a row) is less than a unit in the last place of S in 64 bits.
 //
 // Sums do not depend on the order of atomics: a token adds an integer to its bin, 2^45 + (1 - v) 2^33, with
 // v = e^-(d - d_bin) in (1 - 2^-6.4, 1] its weight relative to the bin's first.  The count stands in bits 45 on,
 // the sum of up to 2^18 terms under 2^(26.6 + 18) below.  Each term rounds by 2^-34 of the token's weight.
+//
+// One workgroup a row.  It reads the row twice (its maximum, the histogram), a third time where the places lie past
+// the largest few hundred tokens, which the second pass lists as it goes.
 #include <hip/hip_runtime.h>
 
 #include "kernels.h"
@@ -21,14 +24,18 @@
 namespace duet {
 namespace {
 
+typedef unsigned long long u64;
+
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBins = 4096, kSubBins = 2048;
+constexpr int kBins = 4096, kSubBins = 2048, kBinsPerThread = kBins / kThreads;
 constexpr double kSpan = 48.0, kBinsPerUnit = kBins / kSpan, kBinWidth = kSpan / kBins;
 constexpr int kCountShift = 45;
 constexpr double kFraction = 8589934592.0;  // 2^33
+constexpr int kList = 2048;                 // tokens listed and sorted; more are narrowed down by their bits
+constexpr int kListPerThread = kList / kThreads;
 
-__device__ __forceinline__ float logit(const __bf16* x) { return static_cast<float>(*x); }
-__device__ __forceinline__ float logit(const float* x) { return *x; }
+__device__ __forceinline__ float as_float(const __bf16& x) { return static_cast<float>(x); }
+__device__ __forceinline__ float as_float(const float& x) { return x; }
 
 // Larger logits have larger keys; both zeros the same one, NaN and -inf (masked tokens) key 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -43,31 +50,87 @@ struct Place {
   double mass;
 };
 
+// A run of listed tokens of one bin, summed; `first`: it begins with the bin's first.
+struct Run {
+  uint32_t first, n;
+  u64 fraction;
+};
+
 struct Shared {
-  unsigned long long hist[kBins];
-  double mass[kWaves];
-  uint32_t count[kWaves];
-  uint32_t key;
-  int found;
+  union {
+    u64 hist[kBins];
+    double mass[kBins];  // mass before each bin, once the histogram is summed
+  };
+  uint32_t before[kBins];  // tokens before each bin
+  u64 list[kList];         // (~key, index): in rank order when sorted
+  union {
+    Run runs[kWaves];
+    struct {
+      double wave_mass[kWaves];
+      uint32_t wave_count[kWaves];
+    };
+  };
   Place place;
+  Place lows[8], highs[8];
+  int found[8];
+  double value;
+  float wave_max[kWaves], wave_low[kWaves];
+  uint32_t key, listed, wanted;
+  int at, pos, last_pos;
 };
 
 struct Row {
   double max, inv_t;
-  __device__ double gap(uint32_t key) const {
-    const double x = of_key(key);
-    return x == max ? 0.0 : (max - x) * inv_t;  // infinite past an infinite max
+  __device__ __forceinline__ double gap(float x) const {
+    return x == max ? 0.0 : (max - x) * inv_t;  // infinite or NaN past an infinite max
   }
-  __device__ int bin(double d) const { return min((int)(d * kBinsPerUnit), kBins - 1); }
 };
+__device__ __forceinline__ int bin_of(double d) { return min((int)(d * kBinsPerUnit), kBins - 1); }
+// (1 - v) 2^33 to the nearest, by the series of 1 - e^-y: y < kBinWidth leaves out y^5 / 120 < 2^-39.
+__device__ __forceinline__ uint32_t fraction_of(double d, int bin) {
+  const double y = fma(-kBinWidth, (double)bin, d);
+  const double s = y * (kFraction - y * (kFraction / 2 - y * (kFraction / 6 - y * (kFraction / 24))));
+  return (uint32_t)(s + 0.5);
+}
+__device__ __forceinline__ u64 token_bits(double d, int bin) { return (1ull << kCountShift) + fraction_of(d, bin); }
+__device__ __forceinline__ uint32_t count_of(u64 h) { return (uint32_t)(h >> kCountShift); }
+__device__ __forceinline__ double scale_of(int bin) { return exp(-bin * kBinWidth); }
+__device__ __forceinline__ double mass_of(uint32_t n, u64 fraction, double scale) {
+  return (n - (double)fraction / kFraction) * scale;
+}
+__device__ __forceinline__ double mass_of(u64 h, double scale) {
+  return mass_of(count_of(h), h & ((1ull << kCountShift) - 1), scale);
+}
 
-__device__ __forceinline__ unsigned long long token_bits(double d, int bin) {
-  return (1ull << kCountShift) + (unsigned long long)((1.0 - exp(bin * kBinWidth - d)) * kFraction + 0.5);
+// f(logit, index) for every token of the row, 16 bytes at a time past the first boundary.
+template <typename T, typename F>
+__device__ __forceinline__ void each(const T* x, int n, F f) {
+  constexpr int V = 16 / sizeof(T), U = 8;
+  const int tid = threadIdx.x;
+  const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
+  const int body = (n - head) / V, rest = n - head - body * V;
+  const uint4* p = reinterpret_cast<const uint4*>(x + head);
+  auto eight = [&](uint4 v, int i) {
+    const T* t = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f(as_float(t[e]), head + i * V + e);
+  };
+  int i = tid;
+  for (; i + (U - 1) * kThreads < body; i += U * kThreads) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = p[i + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < U; ++u) eight(v[u], i + u * kThreads);
+  }
+  for (; i < body; i += kThreads) eight(p[i], i);
+  if (tid < head + rest) {
+    const int k = tid < head ? tid : n - rest + tid - head;
+    f(as_float(x[k]), k);
+  }
 }
-__device__ __forceinline__ uint32_t count_of(unsigned long long h) { return (uint32_t)(h >> kCountShift); }
-__device__ __forceinline__ double mass_of(unsigned long long h, int bin) {
-  return (count_of(h) - (double)(h & ((1ull << kCountShift) - 1)) / kFraction) * exp(-bin * kBinWidth);
-}
+
+// ---- narrowing by bits: any number of tokens in a bin ------------------------------------------------
 
 // The first of the n bins (rank order) with reached(place after it); its place before it.  The last bin holding
 // a token where none reaches.  fixed_bin >= 0: all are parts of that bin of the first histogram.
@@ -79,7 +142,7 @@ __device__ int find_bin(Shared& s, int n, int fixed_bin, Place at, F reached, Pl
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
     c += count_of(s.hist[b]);
-    m += mass_of(s.hist[b], fixed_bin >= 0 ? fixed_bin : b);
+    m += mass_of(s.hist[b], scale_of(fixed_bin >= 0 ? fixed_bin : b));
   }
   uint32_t ci = c;
   double mi = m;
@@ -88,35 +151,35 @@ __device__ int find_bin(Shared& s, int n, int fixed_bin, Place at, F reached, Pl
     const double mu = __shfl_up(mi, off);
     if (lane >= off) ci += cu, mi += mu;
   }
-  if (lane == 63) s.count[wave] = ci, s.mass[wave] = mi;
-  if (tid == 0) s.found = 1 << 30;
+  if (lane == 63) s.wave_count[wave] = ci, s.wave_mass[wave] = mi;
+  if (tid == 0) s.at = 1 << 30;
   __syncthreads();
   Place p = at;
-  for (int w = 0; w < wave; ++w) p.n += s.count[w], p.mass += s.mass[w];
+  for (int w = 0; w < wave; ++w) p.n += s.wave_count[w], p.mass += s.wave_mass[w];
   p.n += ci - c;
   p.mass += mi - m;
   Place mine = p, last_place = p;
   int first = -1, last = -1;
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
-    const unsigned long long h = s.hist[b];
+    const u64 h = s.hist[b];
     if (!h) continue;
     last = b, last_place = p;
     p.n += count_of(h);
-    p.mass += mass_of(h, fixed_bin >= 0 ? fixed_bin : b);
+    p.mass += mass_of(h, scale_of(fixed_bin >= 0 ? fixed_bin : b));
     if (first < 0 && reached(p)) first = b, mine = last_place;
   }
-  if (first >= 0) atomicMin(&s.found, first);
+  if (first >= 0) atomicMin(&s.at, first);
   __syncthreads();
-  if (s.found == 1 << 30) {
+  if (s.at == 1 << 30) {
     __syncthreads();
-    if (tid == 0) s.found = -1;
+    if (tid == 0) s.at = -1;
     __syncthreads();
-    if (last >= 0) atomicMax(&s.found, last);
+    if (last >= 0) atomicMax(&s.at, last);
     __syncthreads();
     first = last, mine = last_place;
   }
-  const int found = s.found;
+  const int found = s.at;
   if (first == found) s.place = mine;
   __syncthreads();
   *before = s.place;
@@ -134,13 +197,12 @@ struct Found {
 template <typename T, typename F>
 __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reached) {
   const int tid = threadIdx.x;
-  auto each = [&](auto f) {
-    for (int i = tid; i < vocab; i += kThreads) {
-      const uint32_t k = key_of(logit(x + i));
-      if (!k) continue;
-      const double d = row.gap(k);
-      if (d < kSpan) f(k, d);
-    }
+  auto inside = [&](auto f) {
+    each(x, vocab, [&](float v, int) {
+      if (!(v > -INFINITY)) return;
+      const double d = row.gap(v);
+      if (d < kSpan) f(key_of(v), d);
+    });
   };
   auto clear = [&](int n) {
     __syncthreads();
@@ -148,31 +210,23 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
     __syncthreads();
   };
   clear(kBins);
-  each([&](uint32_t, double d) { atomicAdd(&s.hist[row.bin(d)], token_bits(d, row.bin(d))); });
+  inside([&](uint32_t, double d) { atomicAdd(&s.hist[bin_of(d)], token_bits(d, bin_of(d))); });
   __syncthreads();
   Place before{0, 0.0};
   const int bin = find_bin(s, kBins, -1, before, reached, &before);
-  // The bin's keys: from the largest down to one past the smallest.
-  if (tid == 0) s.key = 0, s.found = -1;
+  // The bin's largest and smallest key.
+  if (tid == 0) s.key = 0, s.wanted = 0xffffffffu;
   __syncthreads();
-  each([&](uint32_t k, double d) {
-    if (row.bin(d) == bin) atomicMax(&s.key, k);
+  inside([&](uint32_t k, double d) {
+    if (bin_of(d) == bin) atomicMax(&s.key, k), atomicMin(&s.wanted, k);
   });
   __syncthreads();
-  uint32_t hi = s.key;
-  __syncthreads();
-  if (tid == 0) s.key = 0xffffffffu;
-  __syncthreads();
-  each([&](uint32_t k, double d) {
-    if (row.bin(d) == bin) atomicMin(&s.key, k);
-  });
-  __syncthreads();
-  uint32_t lo = s.key;
+  uint32_t hi = s.key, lo = s.wanted;
   while (true) {
     int shift = 0;
     while (((hi - lo) >> shift) >= kSubBins) ++shift;
     clear(kSubBins);
-    each([&](uint32_t k, double d) {
+    inside([&](uint32_t k, double d) {
       if (k <= hi && k >= lo) atomicAdd(&s.hist[(hi - k) >> shift], token_bits(d, bin));
     });
     __syncthreads();
@@ -181,7 +235,7 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
     hi -= (uint32_t)sub << shift;
     lo = hi - min(hi - lo, (1u << shift) - 1);
     if (shift == 0) {
-      const double w = exp(-row.gap(hi));
+      const double w = exp(-row.gap(of_key(hi)));
       // ties before or at the place: the fewest with which it is reached
       uint32_t a = 1, b = n;
       while (a < b) {
@@ -200,85 +254,422 @@ __device__ int index_of(Shared& s, const T* x, int vocab, uint32_t key, uint32_t
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int per = ((vocab + kWaves - 1) / kWaves + 63) / 64 * 64;  // a wave's tokens
   const int lo = wave * per, hi = min(vocab, lo + per);
+  auto is = [&](int i) { return i + lane < hi && key_of(as_float(x[min(i + lane, vocab - 1)])) == key; };
   uint32_t c = 0;
-  for (int i = lo; i < hi; i += 64) c += __popcll(__ballot(i + lane < hi && key_of(logit(x + min(i + lane, vocab - 1))) == key));
+  for (int i = lo; i < hi; i += 64) c += __popcll(__ballot(is(i)));
   __syncthreads();
-  if (lane == 0) s.count[wave] = c;
+  if (lane == 0) s.wave_count[wave] = c;
   __syncthreads();
   uint32_t before = 0;
-  for (int w = 0; w < wave; ++w) before += s.count[w];
+  for (int w = 0; w < wave; ++w) before += s.wave_count[w];
   if (before < n && n <= before + c) {
     for (int i = lo; i < hi; i += 64) {
-      const bool is = i + lane < hi && key_of(logit(x + min(i + lane, vocab - 1))) == key;
-      const unsigned long long all = __ballot(is);
-      if (is && before + __popcll(all & ((1ull << lane) - 1)) + 1 == n) s.found = i + lane;
+      const bool one = is(i);
+      const u64 all = __ballot(one);
+      if (one && before + __popcll(all & ((1ull << lane) - 1)) + 1 == n) s.at = i + lane;
       before += __popcll(all);
     }
   }
   __syncthreads();
-  return s.found;
+  return s.at;
+}
+
+struct Settings {
+  uint32_t top_k;  // 0: off
+  double top_p;    // 1: off
+  double min_p;    // 0: off, at most 1
+  double u;
+};
+struct Pick {
+  int index;
+  float prob;
+};
+
+template <typename T>
+__device__ Pick narrow(Shared& s, const T* x, int vocab, const Row& row, const Settings& c) {
+  const uint32_t k = c.top_k ? c.top_k : 0xffffffffu;
+  Place kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= k; }).end;
+  if (c.top_p < 1) {
+    const double need = c.top_p * kept.mass;
+    const uint32_t n = kept.n;
+    kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n || p.mass >= need; }).end;
+  }
+  if (c.min_p > 0) {
+    __syncthreads();
+    if (threadIdx.x == 0) s.wanted = 0;
+    __syncthreads();
+    uint32_t own = 0;
+    each(x, vocab, [&](float v, int) { own += v > -INFINITY && exp(-row.gap(v)) >= c.min_p; });
+    atomicAdd(&s.wanted, own);
+    __syncthreads();
+    const uint32_t n = s.wanted;
+    __syncthreads();
+    if (n < kept.n) kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n; }).end;
+  }
+  const double target = c.u * kept.mass;
+  const uint32_t n = kept.n;
+  const Found f = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n || p.mass > target; });
+  const int i = index_of(s, x, vocab, f.key, f.ties);
+  return Pick{i, (float)(exp(-row.gap(of_key(f.key))) / kept.mass)};
+}
+
+// ---- the histogram and a short list -------------------------------------------------------------------
+
+// s.list[0 .. n) into rising order; n <= kList.
+__device__ void sort_list(Shared& s, int n) {
+  const int tid = threadIdx.x;
+  int size = 64;
+  while (size < n) size <<= 1;
+  u64 v[kListPerThread];
+#pragma unroll
+  for (int j = 0; j < kListPerThread; ++j) v[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
+  const bool busy = tid < size;  // waves past the list only meet the barriers
+  for (int k = 2; k <= size; k <<= 1) {
+    for (int step = k >> 1; step > 0; step >>= 1) {
+      if (step >= kThreads) {  // the thread's own two
+        const bool up = (tid & k) == 0;
+        if ((v[0] > v[kListPerThread - 1]) == up) {
+          const u64 t = v[0];
+          v[0] = v[kListPerThread - 1];
+          v[kListPerThread - 1] = t;
+        }
+        continue;
+      }
+      u64 other[kListPerThread];
+      if (step >= 64) {
+        __syncthreads();
+        if (busy)
+#pragma unroll
+          for (int j = 0; j < kListPerThread; ++j) s.list[tid + j * kThreads] = v[j];
+        __syncthreads();
+        if (busy)
+#pragma unroll
+          for (int j = 0; j < kListPerThread; ++j) other[j] = s.list[(tid ^ step) + j * kThreads];
+      } else if (busy) {
+#pragma unroll
+        for (int j = 0; j < kListPerThread; ++j) other[j] = __shfl_xor(v[j], step);
+      }
+      if (!busy) continue;
+#pragma unroll
+      for (int j = 0; j < kListPerThread; ++j) {
+        const bool up = ((tid + j * kThreads) & k) == 0, low = (tid & step) == 0;
+        if ((v[j] > other[j]) == (up == low)) v[j] = other[j];
+      }
+    }
+  }
+  __syncthreads();
+  if (busy)
+#pragma unroll
+    for (int j = 0; j < kListPerThread; ++j) s.list[tid + j * kThreads] = v[j];
+  __syncthreads();
+}
+
+// The bins that a row's places may lie in: those of top-k's end, top-p's, min-p's and the token's.
+struct Wanted {
+  int lo[4], hi[4];  // empty where hi < lo
+  int last;
+  Place min_p;       // before min-p's bin
+  Place all;         // the whole row
+  __device__ __forceinline__ bool has(int b) const {
+    bool in = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) in |= b >= lo[i] && b <= hi[i];
+    return in;
+  }
+};
+
+// Sums the histogram: its place before every bin stays in s.mass and s.before.
+__device__ Wanted decide(Shared& s, const Settings& c) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  uint32_t n[kBinsPerThread], cn = 0;
+  double m[kBinsPerThread], cm = 0;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) {
+    const int b = tid * kBinsPerThread + i;
+    const u64 h = s.hist[b];
+    n[i] = count_of(h);
+    m[i] = n[i] ? mass_of(h, scale_of(b)) : 0.0;
+    cn += n[i];
+    cm += m[i];
+  }
+  uint32_t in = cn;
+  double im = cm;
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t un = __shfl_up(in, off);
+    const double um = __shfl_up(im, off);
+    if (lane >= off) in += un, im += um;
+  }
+  if (lane == 63) s.wave_count[wave] = in, s.wave_mass[wave] = im;
+  if (tid < 8) s.found[tid] = kBins;
+  if (tid == 0) s.at = -1, s.wanted = 0;
+  __syncthreads();
+  Place p{0, 0.0}, all{0, 0.0};
+  for (int w = 0; w < kWaves; ++w) {
+    if (w == wave) p = all;
+    all.n += s.wave_count[w];
+    all.mass += s.wave_mass[w];
+  }
+  p.n += in - cn;
+  p.mass += im - cm;
+  Place low[kBinsPerThread + 1];
+  low[0] = p;
+  int last = -1;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) {
+    const int b = tid * kBinsPerThread + i;
+    s.mass[b] = low[i].mass;
+    s.before[b] = low[i].n;
+    low[i + 1] = Place{low[i].n + n[i], low[i].mass + m[i]};
+    if (n[i]) last = b;
+  }
+  if (last >= 0) atomicMax(&s.at, last);
+  __syncthreads();
+  last = s.at;
+  // The first bin holding a token with reached(place after it), else the last; slot q's use is up to the caller.
+  auto first = [&](int q, auto reached) {
+    int b = kBins;
+#pragma unroll
+    for (int i = kBinsPerThread - 1; i >= 0; --i)
+      if (n[i] && reached(low[i + 1])) b = tid * kBinsPerThread + i;
+    if (b < kBins) atomicMin(&s.found[q], b);
+    __syncthreads();
+    return min(s.found[q], last);
+  };
+  // The place before a bin and after it.
+  auto around = [&](int q, int b, Place* lo, Place* hi) {
+#pragma unroll
+    for (int i = 0; i < kBinsPerThread; ++i)
+      if (b == tid * kBinsPerThread + i) s.lows[q] = low[i], s.highs[q] = low[i + 1];
+    __syncthreads();
+    *lo = s.lows[q];
+    *hi = s.highs[q];
+  };
+  Wanted w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w.lo[i] = 0, w.hi[i] = -1;
+  w.all = all;
+  w.min_p = Place{0, 0.0};
+  Place zlo = all, zhi = all;
+  int kb = last, plo = last, phi = last, mb = last;
+  const bool k = c.top_k && c.top_k < all.n;
+  if (k) {
+    kb = first(0, [&](const Place& q) { return q.n >= c.top_k; });
+    around(0, kb, &zlo, &zhi);
+  }
+  if (c.top_p < 1) {
+    const double least = c.top_p * zlo.mass, most = c.top_p * zhi.mass;
+    plo = min(kb, first(1, [&](const Place& q) { return q.mass >= least; }));
+    phi = min(kb, first(2, [&](const Place& q) { return q.mass >= most; }));
+  }
+  if (c.min_p > 0) {
+    mb = bin_of(fmin(2e-16 - log(c.min_p), kSpan));  // weights that round to min-p count
+    Place after;
+    around(1, mb, &w.min_p, &after);
+  }
+  const int elo = min(min(kb, plo), mb), ehi = min(min(kb, phi), mb);
+  Place slo, shi, unused;
+  around(2, elo, &slo, &unused);
+  around(3, ehi, &unused, &shi);
+  const double tlo = c.u * slo.mass, thi = c.u * shi.mass;
+  w.lo[3] = min(ehi, first(3, [&](const Place& q) { return q.mass > tlo; }));
+  w.hi[3] = min(ehi, first(4, [&](const Place& q) { return q.mass > thi; }));
+  if (k && (c.top_p < 1 || kb <= ehi)) w.lo[0] = w.hi[0] = kb;
+  if (c.top_p < 1 && plo <= ehi) w.lo[1] = plo, w.hi[1] = min(phi, ehi);
+  if (c.min_p > 0 && mb <= ehi) w.lo[2] = w.hi[2] = mb;
+  w.last = max(max(w.hi[0], w.hi[1]), max(w.hi[2], w.hi[3]));
+  uint32_t wanted = 0;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i)
+    if (w.has(tid * kBinsPerThread + i)) wanted += n[i];
+  if (wanted) atomicAdd(&s.wanted, wanted);
+  __syncthreads();
+  return w;
+}
+
+// The token from the sorted list of n tokens, which holds all of the wanted bins.
+__device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, const Wanted& w) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  constexpr int P = kListPerThread;
+  double d[P], scale[P];
+  int bin[P];
+  uint32_t fraction[P];
+  Run run[P];
+  auto bin_at = [&](int i) { return bin_of(row.gap(of_key(~(uint32_t)(s.list[i] >> 32)))); };
+  auto join = [](const Run& a, const Run& b) { return b.first ? b : Run{a.first, a.n + b.n, a.fraction + b.fraction}; };
+  Run sum{0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    const int i = tid * P + j;
+    const int k = min(i, n - 1);
+    d[j] = row.gap(of_key(~(uint32_t)(s.list[k] >> 32)));
+    bin[j] = bin_of(d[j]);
+    fraction[j] = fraction_of(d[j], bin[j]);
+    const Run one{i == 0 || i >= n || bin_at(k - 1) != bin[j], 1, fraction[j]};
+    sum = j ? join(sum, one) : one;
+    run[j] = sum;
+    scale[j] = scale_of(bin[j]);
+  }
+  for (int off = 1; off < 64; off <<= 1) {
+    const Run up{__shfl_up(sum.first, off), __shfl_up(sum.n, off), __shfl_up(sum.fraction, off)};
+    if (lane >= off) sum = join(up, sum);
+  }
+  if (lane == 63) s.runs[wave] = sum;
+  Run left{__shfl_up(sum.first, 1), __shfl_up(sum.n, 1), __shfl_up(sum.fraction, 1)};
+  if (lane == 0) left = Run{0, 0, 0};
+  if (tid == 0) s.pos = 1 << 30, s.last_pos = -1, s.at = -1, s.found[0] = 0, s.value = w.all.mass;
+  __syncthreads();
+  Run before{0, 0, 0};
+  for (int v = 0; v < wave; ++v) before = join(before, s.runs[v]);
+  left = lane ? join(before, left) : before;
+  Place low[P], high[P];
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    const Run r = join(left, run[j]);
+    const Place b{s.before[bin[j]], s.mass[bin[j]]};
+    low[j] = Place{b.n + r.n - 1, b.mass + mass_of(r.n - 1, r.fraction - fraction[j], scale[j])};
+    high[j] = Place{b.n + r.n, b.mass + mass_of(r.n, r.fraction, scale[j])};
+  }
+  auto listed = [&](int j) { return tid * P + j < n && bin[j] <= w.last; };
+  const bool k = c.top_k && c.top_k < w.all.n;
+  if (k)
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+      if (listed(j) && high[j].n == c.top_k) s.value = high[j].mass;
+#pragma unroll
+  for (int j = P - 1; j >= 0; --j)
+    if (listed(j)) {
+      atomicMax(&s.last_pos, tid * P + j);
+      break;
+    }
+  __syncthreads();
+  Place kept{k ? c.top_k : w.all.n, s.value};
+  // The first listed rank at or past a place, the last one where none is.
+  auto first = [&](auto reached) {
+#pragma unroll
+    for (int j = P - 1; j >= 0; --j)
+      if (listed(j) && reached(high[j])) atomicMin(&s.pos, tid * P + j);
+    __syncthreads();
+    const int at = s.pos == 1 << 30 ? s.last_pos : s.pos;
+    if (at / P == tid) s.place = high[at % P];
+    __syncthreads();
+    if (tid == 0) s.pos = 1 << 30;
+    return at;
+  };
+  if (c.top_p < 1 && w.lo[1] <= w.hi[1]) {
+    const double need = c.top_p * kept.mass;
+    first([&](const Place& p) { return p.mass >= need; });
+    if (s.place.n < kept.n) kept = s.place;
+    __syncthreads();
+  }
+  if (c.min_p > 0 && w.lo[2] <= w.hi[2]) {
+    int own = -1;
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+      if (listed(j) && bin[j] == w.lo[2] && exp(-d[j]) >= c.min_p) own = tid * P + j;
+    if (own >= 0) atomicMax(&s.at, own);
+    __syncthreads();
+    if (s.at >= 0 && s.at / P == tid) s.place = high[s.at % P];
+    if (s.at < 0 && tid == 0) s.place = w.min_p;
+    __syncthreads();
+    if (s.place.n < kept.n) kept = s.place;
+    __syncthreads();
+  }
+  const double target = c.u * kept.mass;
+  const int at = first([&](const Place& p) { return p.mass > target; });
+  if (at / P == tid) s.value = exp(-d[at % P]);
+  __syncthreads();
+  return Pick{(int)(uint32_t)s.list[at], (float)(s.value / kept.mass)};
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   __shared__ Shared s;
-  const int r = blockIdx.x, tid = threadIdx.x;
+  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const T* x = static_cast<const T*>(a.logits) + (size_t)r * a.row_stride;
-  if (tid == 0) s.key = 0;
-  __syncthreads();
-  uint32_t most = 0;
-  for (int i = tid; i < a.vocab; i += kThreads) most = max(most, key_of(logit(x + i)));
-  atomicMax(&s.key, most);
-  __syncthreads();
-  most = s.key;
-  __syncthreads();
   const float t = a.temperature ? a.temperature[r] : 1.f;
-  if (!most || !(t > 0.f)) {  // nothing left, or the largest
-    const int i = most ? index_of(s, x, a.vocab, most, 1) : -1;
+  const int top_k = a.top_k ? a.top_k[r] : 0;
+  const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
+  const bool greedy = !(t > 0.f) || top_k == 1 || top_p <= 0.f;  // the first rank alone
+  float most = -INFINITY;
+  int index = 0;
+  if (greedy) {
+    each(x, a.vocab, [&](float v, int i) {
+      if (v > most || (v == most && i < index)) most = v, index = i;
+    });
+  } else {
+    each(x, a.vocab, [&](float v, int) { most = fmaxf(most, v); });
+  }
+  // The smallest of the maxima of groups of eight threads: some hundred tokens lie above it, 128 at least if the groups
+  // have a token each.
+  float group = most;
+  for (int off = 1; off < 8; off <<= 1) group = fmaxf(group, __shfl_xor(group, off));
+  float low = group, high = group;
+  for (int off = 8; off < 64; off <<= 1) {
+    high = fmaxf(high, __shfl_xor(high, off));
+    low = fminf(low, __shfl_xor(low, off));
+  }
+  if (lane == 0) s.wave_max[wave] = high, s.wave_low[wave] = low;
+  if (tid == 0) s.at = 0x7fffffff, s.listed = 0;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) high = fmaxf(high, s.wave_max[w]), low = fminf(low, s.wave_low[w]);
+  if (high == -INFINITY || greedy) {
+    if (greedy && most == high && high > -INFINITY) atomicMin(&s.at, index);
+    __syncthreads();
     if (tid == 0) {
-      a.ids[r] = i;
-      if (a.probs) a.probs[r] = most ? 1.f : 0.f;
+      a.ids[r] = high == -INFINITY ? -1 : s.at;
+      if (a.probs) a.probs[r] = high == -INFINITY ? 0.f : 1.f;
     }
     return;
   }
-  const Row row{of_key(most), 1.0 / t};
-  const int top_k = a.top_k ? a.top_k[r] : 0;
-  const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
-  // The last kept rank.
-  const uint32_t all = 0xffffffffu;
-  uint32_t most_n = top_k > 0 ? top_k : all;
-  auto kept = find(s, x, a.vocab, row, [&](const Place& p) { return p.n >= most_n; });
-  if (top_p < 1.f) {
-    const double need = fmax(0.0, (double)top_p) * kept.end.mass;
-    const uint32_t n = kept.end.n;
-    kept = find(s, x, a.vocab, row, [&](const Place& p) { return p.n >= n || p.mass >= need; });
-  }
-  if (min_p > 0.f) {
-    // Count the tokens of at least that weight.
-    __syncthreads();
-    if (tid == 0) s.key = 0;
-    __syncthreads();
-    uint32_t c = 0;
-    const double least = fmin(1.0, (double)min_p);
-    for (int i = tid; i < a.vocab; i += kThreads) {
-      const uint32_t k = key_of(logit(x + i));
-      c += k && exp(-row.gap(k)) >= least;
+  const Row row{high, 1.0 / t};
+  const float u = a.u[r];
+  const Settings c{(uint32_t)max(top_k, 0), top_p < 1.f ? top_p : 1.0, min_p > 0.f ? fmin(1.0, (double)min_p) : 0.0,
+                   u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.0};
+  auto put = [&](float v, int i) {
+    const uint32_t at = atomicAdd(&s.listed, 1u);
+    if (at < kList) s.list[at] = (u64)(~key_of(v)) << 32 | (uint32_t)i;
+  };
+  each(x, a.vocab, [&](float v, int i) {
+    if (!(v > -INFINITY)) return;
+    const double d = row.gap(v);
+    if (!(d < kSpan)) return;
+    const int b = bin_of(d);
+    atomicAdd(&s.hist[b], token_bits(d, b));
+    if (v >= low) put(v, i);
+  });
+  __syncthreads();
+  const Wanted w = decide(s, c);
+  // The list holds every bin before the one that `low` lies in.
+  const double low_gap = row.gap(low);
+  const int whole = low_gap < kSpan ? bin_of(low_gap) : kBins;
+  uint32_t n = s.listed;
+  if (n > kList || w.last >= whole) {
+    if (s.wanted > kList) {
+      const Pick p = narrow(s, x, a.vocab, row, c);
+      if (tid == 0) {
+        a.ids[r] = p.index;
+        if (a.probs) a.probs[r] = p.prob;
+      }
+      return;
     }
-    atomicAdd(&s.key, c);
     __syncthreads();
-    const uint32_t n = min(s.key, kept.end.n);
+    if (tid == 0) s.listed = 0;
     __syncthreads();
-    if (n < kept.end.n) kept = find(s, x, a.vocab, row, [&](const Place& p) { return p.n >= n; });
+    each(x, a.vocab, [&](float v, int i) {
+      if (!(v > -INFINITY)) return;
+      const double d = row.gap(v);
+      if (d < kSpan && w.has(bin_of(d))) put(v, i);
+    });
+    __syncthreads();
+    n = s.listed;
   }
-  float u = a.u[r];
-  u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-  const double target = u * kept.end.mass;
-  const uint32_t n = kept.end.n;
-  const auto pick = find(s, x, a.vocab, row, [&](const Place& p) { return p.n >= n || p.mass > target; });
-  const int i = index_of(s, x, a.vocab, pick.key, pick.ties);
+  sort_list(s, n);
+  const Pick p = finish(s, n, row, c, w);
   if (tid == 0) {
-    a.ids[r] = i;
-    if (a.probs) a.probs[r] = (float)(exp(-row.gap(pick.key)) / kept.end.mass);
+    a.ids[r] = p.index;
+    if (a.probs) a.probs[r] = p.prob;
   }
 }
 
