@@ -59,10 +59,10 @@ struct Run {
 struct Shared {
   union {
     u64 hist[kBins];
-    double mass[kBins];  // mass before each bin, once the histogram is summed
+    double mass[kBins + 1];  // mass before each bin, once the histogram is summed
   };
-  uint32_t before[kBins];  // tokens before each bin
-  u64 list[kList];         // (~key, index): in rank order when sorted
+  uint32_t before[kBins + 1];  // tokens before each bin
+  u64 list[kList];             // (~key, index): in rank order when sorted
   union {
     Run runs[kWaves];
     struct {
@@ -71,8 +71,7 @@ struct Shared {
     };
   };
   Place place;
-  Place lows[8], highs[8];
-  int found[8];
+  int found[5];
   double value;
   float wave_max[kWaves], wave_low[kWaves];
   uint32_t key, listed, wanted;
@@ -80,21 +79,21 @@ struct Shared {
 };
 
 struct Row {
-  double max, inv_t;
-  __device__ __forceinline__ double gap(float x) const {
-    return x == max ? 0.0 : (max - x) * inv_t;  // infinite or NaN past an infinite max
-  }
+  double max, scale;  // of a gap to bins
+  // (max - x) / T in bins; not below kBins for masked tokens, NaN among them.
+  __device__ __forceinline__ double bins(float x) const { return (max - x) * scale; }
+  __device__ __forceinline__ double bins_of_key(uint32_t k) const { return bins(of_key(k)); }
 };
-__device__ __forceinline__ int bin_of(double d) { return min((int)(d * kBinsPerUnit), kBins - 1); }
+__device__ __forceinline__ double weight_of(double bins) { return exp(-bins * kBinWidth); }
 // (1 - v) 2^33 to the nearest, by the series of 1 - e^-y: y < kBinWidth leaves out y^5 / 120 < 2^-39.
-__device__ __forceinline__ uint32_t fraction_of(double d, int bin) {
-  const double y = fma(-kBinWidth, (double)bin, d);
-  const double s = y * (kFraction - y * (kFraction / 2 - y * (kFraction / 6 - y * (kFraction / 24))));
-  return (uint32_t)(s + 0.5);
+__device__ __forceinline__ uint32_t fraction_of(double bins) {
+  constexpr double w = kBinWidth, c1 = kFraction * w, c2 = c1 * w / 2, c3 = c2 * w / 3, c4 = c3 * w / 4;
+  const double y = bins - (double)(int)bins;
+  return (uint32_t)fma(y, fma(y, fma(y, fma(y, -c4, c3), -c2), c1), 0.5);
 }
-__device__ __forceinline__ u64 token_bits(double d, int bin) { return (1ull << kCountShift) + fraction_of(d, bin); }
+__device__ __forceinline__ u64 token_bits(double bins) { return (1ull << kCountShift) + fraction_of(bins); }
 __device__ __forceinline__ uint32_t count_of(u64 h) { return (uint32_t)(h >> kCountShift); }
-__device__ __forceinline__ double scale_of(int bin) { return exp(-bin * kBinWidth); }
+__device__ __forceinline__ double scale_of(int bin) { return weight_of(bin); }
 __device__ __forceinline__ double mass_of(uint32_t n, u64 fraction, double scale) {
   return (n - (double)fraction / kFraction) * scale;
 }
@@ -102,33 +101,63 @@ __device__ __forceinline__ double mass_of(u64 h, double scale) {
   return mass_of(count_of(h), h & ((1ull << kCountShift) - 1), scale);
 }
 
-// f(logit, index) for every token of the row, 16 bytes at a time past the first boundary.
-template <typename T, typename F>
-__device__ __forceinline__ void each(const T* x, int n, F f) {
-  constexpr int V = 16 / sizeof(T), U = 8;
-  const int tid = threadIdx.x;
-  const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
-  const int body = (n - head) / V, rest = n - head - body * V;
-  const uint4* p = reinterpret_cast<const uint4*>(x + head);
-  auto eight = [&](uint4 v, int i) {
-    const T* t = reinterpret_cast<const T*>(&v);
+// A row's logits.  If its largest is infinite, the infinities count as 0 and the rest as masked.
+template <typename T>
+struct Logits {
+  const T* x;
+  int n;
+  bool infinite;
+
+  __device__ __forceinline__ float plain(float v) const { return infinite ? (v == INFINITY ? 0.f : -INFINITY) : v; }
+  __device__ __forceinline__ float at(int i) const { return plain(as_float(x[i])); }
+
+  // f(four logits, index of the first): vectors of four past the first boundary, U of them in flight; the tokens before
+  // and after those one by one, with three masked ones.
+  template <int U, typename F>
+  __device__ __forceinline__ void fours(F f) const {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    const int tid = threadIdx.x;
+    const int off = (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) & 3);
+    const int head = min(n, (4 - off) & 3), body = (n - head) / 4, rest = n - head - 4 * body;
+    const Four* p = reinterpret_cast<const Four*>(x + head);
+    auto four = [&](const Four& v, int i) {
+      float y[4];
 #pragma unroll
-    for (int e = 0; e < V; ++e) f(as_float(t[e]), head + i * V + e);
-  };
-  int i = tid;
-  for (; i + (U - 1) * kThreads < body; i += U * kThreads) {
-    uint4 v[U];
+      for (int e = 0; e < 4; ++e) y[e] = as_float(v[e]);
+      if (infinite)
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = p[i + u * kThreads];
+        for (int e = 0; e < 4; ++e) y[e] = plain(y[e]);
+      f(y, head + 4 * i);
+    };
+    int i = tid;
+    for (; i + (U - 1) * kThreads < body; i += U * kThreads) {
+      Four v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) eight(v[u], i + u * kThreads);
+      for (int u = 0; u < U; ++u) v[u] = p[i + u * kThreads];
+#pragma unroll
+      for (int u = 0; u < U; ++u) four(v[u], i + u * kThreads);
+    }
+    for (; i < body + head + rest; i += kThreads) {
+      Four v = {};
+      int at = 4 * i + head;
+      if (i < body) {
+        v = p[i];
+        four(v, i);
+      } else {
+        at = i - body < head ? i - body : n - rest + i - body - head;
+        const float y[4] = {this->at(at), -INFINITY, -INFINITY, -INFINITY};
+        f(y, at);
+      }
+    }
   }
-  for (; i < body; i += kThreads) eight(p[i], i);
-  if (tid < head + rest) {
-    const int k = tid < head ? tid : n - rest + tid - head;
-    f(as_float(x[k]), k);
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    fours<2>([&](const float* v, int i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(v[e], i + e);
+    });
   }
-}
+};
 
 // ---- narrowing by bits: any number of tokens in a bin ------------------------------------------------
 
@@ -195,13 +224,12 @@ struct Found {
 
 // reached(place): whether the place is at or past the one looked for.
 template <typename T, typename F>
-__device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reached) {
+__device__ Found find(Shared& s, const Logits<T>& x, const Row& row, F reached) {
   const int tid = threadIdx.x;
   auto inside = [&](auto f) {
-    each(x, vocab, [&](float v, int) {
-      if (!(v > -INFINITY)) return;
-      const double d = row.gap(v);
-      if (d < kSpan) f(key_of(v), d);
+    x.each([&](float v, int) {
+      const double d = row.bins(v);
+      if (d < kBins) f(key_of(v), d);
     });
   };
   auto clear = [&](int n) {
@@ -210,7 +238,7 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
     __syncthreads();
   };
   clear(kBins);
-  inside([&](uint32_t, double d) { atomicAdd(&s.hist[bin_of(d)], token_bits(d, bin_of(d))); });
+  inside([&](uint32_t, double d) { atomicAdd(&s.hist[(int)d], token_bits(d)); });
   __syncthreads();
   Place before{0, 0.0};
   const int bin = find_bin(s, kBins, -1, before, reached, &before);
@@ -218,7 +246,7 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
   if (tid == 0) s.key = 0, s.wanted = 0xffffffffu;
   __syncthreads();
   inside([&](uint32_t k, double d) {
-    if (bin_of(d) == bin) atomicMax(&s.key, k), atomicMin(&s.wanted, k);
+    if ((int)d == bin) atomicMax(&s.key, k), atomicMin(&s.wanted, k);
   });
   __syncthreads();
   uint32_t hi = s.key, lo = s.wanted;
@@ -227,7 +255,7 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
     while (((hi - lo) >> shift) >= kSubBins) ++shift;
     clear(kSubBins);
     inside([&](uint32_t k, double d) {
-      if (k <= hi && k >= lo) atomicAdd(&s.hist[(hi - k) >> shift], token_bits(d, bin));
+      if (k <= hi && k >= lo) atomicAdd(&s.hist[(hi - k) >> shift], token_bits(d));
     });
     __syncthreads();
     const int sub = find_bin(s, kSubBins, bin, before, reached, &before);
@@ -235,7 +263,7 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
     hi -= (uint32_t)sub << shift;
     lo = hi - min(hi - lo, (1u << shift) - 1);
     if (shift == 0) {
-      const double w = exp(-row.gap(of_key(hi)));
+      const double w = weight_of(row.bins_of_key(hi));
       // ties before or at the place: the fewest with which it is reached
       uint32_t a = 1, b = n;
       while (a < b) {
@@ -250,11 +278,11 @@ __device__ Found find(Shared& s, const T* x, int vocab, const Row& row, F reache
 
 // Index of the n-th token (from 1) with this key.
 template <typename T>
-__device__ int index_of(Shared& s, const T* x, int vocab, uint32_t key, uint32_t n) {
+__device__ int index_of(Shared& s, const Logits<T>& x, uint32_t key, uint32_t n) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int per = ((vocab + kWaves - 1) / kWaves + 63) / 64 * 64;  // a wave's tokens
-  const int lo = wave * per, hi = min(vocab, lo + per);
-  auto is = [&](int i) { return i + lane < hi && key_of(as_float(x[min(i + lane, vocab - 1)])) == key; };
+  const int per = ((x.n + kWaves - 1) / kWaves + 63) / 64 * 64;  // a wave's tokens
+  const int lo = wave * per, hi = min(x.n, lo + per);
+  auto is = [&](int i) { return i + lane < hi && key_of(x.at(min(i + lane, x.n - 1))) == key; };
   uint32_t c = 0;
   for (int i = lo; i < hi; i += 64) c += __popcll(__ballot(is(i)));
   __syncthreads();
@@ -286,81 +314,78 @@ struct Pick {
 };
 
 template <typename T>
-__device__ Pick narrow(Shared& s, const T* x, int vocab, const Row& row, const Settings& c) {
+__device__ __attribute__((noinline)) Pick narrow(Shared& s, const Logits<T>& x, const Row& row, const Settings& c) {
   const uint32_t k = c.top_k ? c.top_k : 0xffffffffu;
-  Place kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= k; }).end;
+  Place kept = find(s, x, row, [&](const Place& p) { return p.n >= k; }).end;
   if (c.top_p < 1) {
     const double need = c.top_p * kept.mass;
     const uint32_t n = kept.n;
-    kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n || p.mass >= need; }).end;
+    kept = find(s, x, row, [&](const Place& p) { return p.n >= n || p.mass >= need; }).end;
   }
   if (c.min_p > 0) {
     __syncthreads();
     if (threadIdx.x == 0) s.wanted = 0;
     __syncthreads();
     uint32_t own = 0;
-    each(x, vocab, [&](float v, int) { own += v > -INFINITY && exp(-row.gap(v)) >= c.min_p; });
+    x.each([&](float v, int) { own += weight_of(row.bins(v)) >= c.min_p; });
     atomicAdd(&s.wanted, own);
     __syncthreads();
     const uint32_t n = s.wanted;
     __syncthreads();
-    if (n < kept.n) kept = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n; }).end;
+    if (n < kept.n) kept = find(s, x, row, [&](const Place& p) { return p.n >= n; }).end;
   }
   const double target = c.u * kept.mass;
   const uint32_t n = kept.n;
-  const Found f = find(s, x, vocab, row, [&](const Place& p) { return p.n >= n || p.mass > target; });
-  const int i = index_of(s, x, vocab, f.key, f.ties);
-  return Pick{i, (float)(exp(-row.gap(of_key(f.key))) / kept.mass)};
+  const Found f = find(s, x, row, [&](const Place& p) { return p.n >= n || p.mass > target; });
+  const int i = index_of(s, x, f.key, f.ties);
+  return Pick{i, (float)(weight_of(row.bins_of_key(f.key)) / kept.mass)};
 }
 
 // ---- the histogram and a short list -------------------------------------------------------------------
 
-// s.list[0 .. n) into rising order; n <= kList.
+// s.list[0 .. n) into rising order; n <= kList, no two alike.  Each wave sorts runs of 64 in registers; a token's place is
+// then its place in its own run and, by bisection, in the others.
 __device__ void sort_list(Shared& s, int n) {
-  const int tid = threadIdx.x;
-  int size = 64;
-  while (size < n) size <<= 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, runs = (n + 63) / 64;
+  for (int r = wave; r < runs; r += kWaves) {
+    u64 v = 64 * r + lane < n ? s.list[64 * r + lane] : ~0ull;
+    for (int k = 2; k <= 64; k <<= 1)
+      for (int step = k >> 1; step > 0; step >>= 1) {
+        const u64 other = __shfl_xor(v, step);
+        if ((v > other) == (((lane & k) == 0) == ((lane & step) == 0))) v = other;
+      }
+    s.list[64 * r + lane] = v;
+  }
+  __syncthreads();
+  if (runs == 1) return;
   u64 v[kListPerThread];
+  int rank[kListPerThread];
 #pragma unroll
-  for (int j = 0; j < kListPerThread; ++j) v[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
-  const bool busy = tid < size;  // waves past the list only meet the barriers
-  for (int k = 2; k <= size; k <<= 1) {
-    for (int step = k >> 1; step > 0; step >>= 1) {
-      if (step >= kThreads) {  // the thread's own two
-        const bool up = (tid & k) == 0;
-        if ((v[0] > v[kListPerThread - 1]) == up) {
-          const u64 t = v[0];
-          v[0] = v[kListPerThread - 1];
-          v[kListPerThread - 1] = t;
-        }
-        continue;
-      }
-      u64 other[kListPerThread];
-      if (step >= 64) {
-        __syncthreads();
-        if (busy)
+  for (int j = 0; j < kListPerThread; ++j) {
+    const int own = wave + j * kWaves;
+    if (own >= runs) continue;
+    v[j] = s.list[64 * own + lane];
+    rank[j] = lane;
+    for (int r = 0; r < runs; r += 4) {
+      int at[4];
 #pragma unroll
-          for (int j = 0; j < kListPerThread; ++j) s.list[tid + j * kThreads] = v[j];
-        __syncthreads();
-        if (busy)
+      for (int q = 0; q < 4; ++q) at[q] = 0;
 #pragma unroll
-          for (int j = 0; j < kListPerThread; ++j) other[j] = s.list[(tid ^ step) + j * kThreads];
-      } else if (busy) {
+      for (int step = 32; step > 0; step >>= 1)
 #pragma unroll
-        for (int j = 0; j < kListPerThread; ++j) other[j] = __shfl_xor(v[j], step);
-      }
-      if (!busy) continue;
+        for (int q = 0; q < 4; ++q)
+          if (s.list[64 * min(r + q, runs - 1) + at[q] + step - 1] < v[j]) at[q] += step;
 #pragma unroll
-      for (int j = 0; j < kListPerThread; ++j) {
-        const bool up = ((tid + j * kThreads) & k) == 0, low = (tid & step) == 0;
-        if ((v[j] > other[j]) == (up == low)) v[j] = other[j];
+      for (int q = 0; q < 4; ++q) {
+        at[q] += s.list[64 * min(r + q, runs - 1) + at[q]] < v[j];
+        if (r + q < runs && r + q != own) rank[j] += at[q];
       }
     }
   }
   __syncthreads();
-  if (busy)
 #pragma unroll
-    for (int j = 0; j < kListPerThread; ++j) s.list[tid + j * kThreads] = v[j];
+  for (int j = 0; j < kListPerThread; ++j)
+    if (64 * (wave + j * kWaves) + lane < n) s.list[rank[j]] = v[j];
   __syncthreads();
 }
 
@@ -368,8 +393,7 @@ __device__ void sort_list(Shared& s, int n) {
 struct Wanted {
   int lo[4], hi[4];  // empty where hi < lo
   int last;
-  Place min_p;       // before min-p's bin
-  Place all;         // the whole row
+  Place all;  // the whole row
   __device__ __forceinline__ bool has(int b) const {
     bool in = false;
 #pragma unroll
@@ -378,17 +402,18 @@ struct Wanted {
   }
 };
 
-// Sums the histogram: its place before every bin stays in s.mass and s.before.
+// Sums the histogram: its place before every bin stays in s.mass and s.before, that of the whole row past the last.
 __device__ Wanted decide(Shared& s, const Settings& c) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   uint32_t n[kBinsPerThread], cn = 0;
   double m[kBinsPerThread], cm = 0;
+  double scale = scale_of(tid * kBinsPerThread);
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) {
-    const int b = tid * kBinsPerThread + i;
-    const u64 h = s.hist[b];
+    const u64 h = s.hist[tid * kBinsPerThread + i];
     n[i] = count_of(h);
-    m[i] = n[i] ? mass_of(h, scale_of(b)) : 0.0;
+    m[i] = mass_of(h, scale);
+    scale *= 0.9883496471138451;  // e^-kBinWidth
     cn += n[i];
     cm += m[i];
   }
@@ -400,79 +425,62 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
     if (lane >= off) in += un, im += um;
   }
   if (lane == 63) s.wave_count[wave] = in, s.wave_mass[wave] = im;
-  if (tid < 8) s.found[tid] = kBins;
+  if (tid < 5) s.found[tid] = kBins;
   if (tid == 0) s.at = -1, s.wanted = 0;
   __syncthreads();
-  Place p{0, 0.0}, all{0, 0.0};
+  Place low{0, 0.0}, all{0, 0.0};
   for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) p = all;
+    if (w == wave) low = all;
     all.n += s.wave_count[w];
     all.mass += s.wave_mass[w];
   }
-  p.n += in - cn;
-  p.mass += im - cm;
-  Place low[kBinsPerThread + 1];
-  low[0] = p;
+  low.n += in - cn;
+  low.mass += im - cm;
+  Place high[kBinsPerThread];
   int last = -1;
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) {
     const int b = tid * kBinsPerThread + i;
-    s.mass[b] = low[i].mass;
-    s.before[b] = low[i].n;
-    low[i + 1] = Place{low[i].n + n[i], low[i].mass + m[i]};
+    s.mass[b] = low.mass;
+    s.before[b] = low.n;
+    low = high[i] = Place{low.n + n[i], low.mass + m[i]};
     if (n[i]) last = b;
   }
+  if (tid == 0) s.mass[kBins] = all.mass, s.before[kBins] = all.n;
   if (last >= 0) atomicMax(&s.at, last);
-  __syncthreads();
-  last = s.at;
-  // The first bin holding a token with reached(place after it), else the last; slot q's use is up to the caller.
-  auto first = [&](int q, auto reached) {
+  // The first bin holding a token with reached(place after it) goes to slot q; the last bin if there is none.
+  auto look = [&](int q, auto reached) {
     int b = kBins;
 #pragma unroll
     for (int i = kBinsPerThread - 1; i >= 0; --i)
-      if (n[i] && reached(low[i + 1])) b = tid * kBinsPerThread + i;
+      if (n[i] && reached(high[i])) b = tid * kBinsPerThread + i;
     if (b < kBins) atomicMin(&s.found[q], b);
-    __syncthreads();
-    return min(s.found[q], last);
   };
-  // The place before a bin and after it.
-  auto around = [&](int q, int b, Place* lo, Place* hi) {
-#pragma unroll
-    for (int i = 0; i < kBinsPerThread; ++i)
-      if (b == tid * kBinsPerThread + i) s.lows[q] = low[i], s.highs[q] = low[i + 1];
-    __syncthreads();
-    *lo = s.lows[q];
-    *hi = s.highs[q];
-  };
+  const bool k = c.top_k && c.top_k < all.n;
+  if (k) look(0, [&](const Place& q) { return q.n >= c.top_k; });
+  __syncthreads();
+  last = s.at;
   Wanted w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w.lo[i] = 0, w.hi[i] = -1;
   w.all = all;
-  w.min_p = Place{0, 0.0};
-  Place zlo = all, zhi = all;
-  int kb = last, plo = last, phi = last, mb = last;
-  const bool k = c.top_k && c.top_k < all.n;
-  if (k) {
-    kb = first(0, [&](const Place& q) { return q.n >= c.top_k; });
-    around(0, kb, &zlo, &zhi);
-  }
+  const int kb = k ? min(s.found[0], last) : last;
+  int plo = last, phi = last, mb = last;
   if (c.top_p < 1) {
-    const double least = c.top_p * zlo.mass, most = c.top_p * zhi.mass;
-    plo = min(kb, first(1, [&](const Place& q) { return q.mass >= least; }));
-    phi = min(kb, first(2, [&](const Place& q) { return q.mass >= most; }));
+    const double least = c.top_p * (k ? s.mass[kb] : all.mass), most = c.top_p * (k ? s.mass[kb + 1] : all.mass);
+    look(1, [&](const Place& q) { return q.mass >= least; });
+    look(2, [&](const Place& q) { return q.mass >= most; });
+    __syncthreads();
+    plo = min(kb, s.found[1]), phi = min(kb, s.found[2]);
   }
-  if (c.min_p > 0) {
-    mb = bin_of(fmin(2e-16 - log(c.min_p), kSpan));  // weights that round to min-p count
-    Place after;
-    around(1, mb, &w.min_p, &after);
-  }
+  if (c.min_p > 0) mb = min((int)((2e-16 - log(c.min_p)) * kBinsPerUnit), kBins - 1);  // weights that round to min-p count
   const int elo = min(min(kb, plo), mb), ehi = min(min(kb, phi), mb);
-  Place slo, shi, unused;
-  around(2, elo, &slo, &unused);
-  around(3, ehi, &unused, &shi);
-  const double tlo = c.u * slo.mass, thi = c.u * shi.mass;
-  w.lo[3] = min(ehi, first(3, [&](const Place& q) { return q.mass > tlo; }));
-  w.hi[3] = min(ehi, first(4, [&](const Place& q) { return q.mass > thi; }));
+  const double tlo = c.u * s.mass[elo], thi = c.u * s.mass[ehi + 1];
+  look(3, [&](const Place& q) { return q.mass > tlo; });
+  look(4, [&](const Place& q) { return q.mass > thi; });
+  __syncthreads();
+  w.lo[3] = min(ehi, min(last, s.found[3]));
+  w.hi[3] = min(ehi, min(last, s.found[4]));
   if (k && (c.top_p < 1 || kb <= ehi)) w.lo[0] = w.hi[0] = kb;
   if (c.top_p < 1 && plo <= ehi) w.lo[1] = plo, w.hi[1] = min(phi, ehi);
   if (c.min_p > 0 && mb <= ehi) w.lo[2] = w.hi[2] = mb;
@@ -490,21 +498,21 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
 __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, const Wanted& w) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   constexpr int P = kListPerThread;
-  double d[P], scale[P];
+  double d[P], scale[P];  // d: in bins
   int bin[P];
   uint32_t fraction[P];
   Run run[P];
-  auto bin_at = [&](int i) { return bin_of(row.gap(of_key(~(uint32_t)(s.list[i] >> 32)))); };
+  auto bins_at = [&](int i) { return row.bins_of_key(~(uint32_t)(s.list[i] >> 32)); };
   auto join = [](const Run& a, const Run& b) { return b.first ? b : Run{a.first, a.n + b.n, a.fraction + b.fraction}; };
   Run sum{0, 0, 0};
 #pragma unroll
   for (int j = 0; j < P; ++j) {
     const int i = tid * P + j;
     const int k = min(i, n - 1);
-    d[j] = row.gap(of_key(~(uint32_t)(s.list[k] >> 32)));
-    bin[j] = bin_of(d[j]);
-    fraction[j] = fraction_of(d[j], bin[j]);
-    const Run one{i == 0 || i >= n || bin_at(k - 1) != bin[j], 1, fraction[j]};
+    d[j] = bins_at(k);
+    bin[j] = (int)d[j];
+    fraction[j] = fraction_of(d[j]);
+    const Run one{i == 0 || i >= n || (int)bins_at(k - 1) != bin[j], 1, fraction[j]};
     sum = j ? join(sum, one) : one;
     run[j] = sum;
     scale[j] = scale_of(bin[j]);
@@ -516,7 +524,7 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
   if (lane == 63) s.runs[wave] = sum;
   Run left{__shfl_up(sum.first, 1), __shfl_up(sum.n, 1), __shfl_up(sum.fraction, 1)};
   if (lane == 0) left = Run{0, 0, 0};
-  if (tid == 0) s.pos = 1 << 30, s.last_pos = -1, s.at = -1, s.found[0] = 0, s.value = w.all.mass;
+  if (tid == 0) s.pos = 1 << 30, s.last_pos = -1, s.at = -1, s.value = w.all.mass;
   __syncthreads();
   Run before{0, 0, 0};
   for (int v = 0; v < wave; ++v) before = join(before, s.runs[v]);
@@ -565,18 +573,18 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
     int own = -1;
 #pragma unroll
     for (int j = 0; j < P; ++j)
-      if (listed(j) && bin[j] == w.lo[2] && exp(-d[j]) >= c.min_p) own = tid * P + j;
+      if (listed(j) && bin[j] == w.lo[2] && weight_of(d[j]) >= c.min_p) own = tid * P + j;
     if (own >= 0) atomicMax(&s.at, own);
     __syncthreads();
     if (s.at >= 0 && s.at / P == tid) s.place = high[s.at % P];
-    if (s.at < 0 && tid == 0) s.place = w.min_p;
+    if (s.at < 0 && tid == 0) s.place = Place{s.before[w.lo[2]], s.mass[w.lo[2]]};
     __syncthreads();
     if (s.place.n < kept.n) kept = s.place;
     __syncthreads();
   }
   const double target = c.u * kept.mass;
   const int at = first([&](const Place& p) { return p.mass > target; });
-  if (at / P == tid) s.value = exp(-d[at % P]);
+  if (at / P == tid) s.value = weight_of(d[at % P]);
   __syncthreads();
   return Pick{(int)(uint32_t)s.list[at], (float)(s.value / kept.mass)};
 }
@@ -585,7 +593,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   __shared__ Shared s;
   const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const T* x = static_cast<const T*>(a.logits) + (size_t)r * a.row_stride;
+  Logits<T> x{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride, a.vocab, false};
   const float t = a.temperature ? a.temperature[r] : 1.f;
   const int top_k = a.top_k ? a.top_k[r] : 0;
   const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
@@ -593,11 +601,11 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   float most = -INFINITY;
   int index = 0;
   if (greedy) {
-    each(x, a.vocab, [&](float v, int i) {
+    x.each([&](float v, int i) {
       if (v > most || (v == most && i < index)) most = v, index = i;
     });
   } else {
-    each(x, a.vocab, [&](float v, int) { most = fmaxf(most, v); });
+    x.template fours<8>([&](const float* v, int) { most = fmaxf(most, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))); });
   }
   // The smallest of the maxima of groups of eight threads: some hundred tokens lie above it, 128 at least if the groups
   // have a token each.
@@ -623,7 +631,10 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
     }
     return;
   }
-  const Row row{high, 1.0 / t};
+  x.infinite = high == INFINITY;
+  if (x.infinite) high = 0.f, low = x.plain(low);
+  const double inv_t = 1.0 / t;
+  const Row row{high, inv_t * kBinsPerUnit};
   const float u = a.u[r];
   const Settings c{(uint32_t)max(top_k, 0), top_p < 1.f ? top_p : 1.0, min_p > 0.f ? fmin(1.0, (double)min_p) : 0.0,
                    u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.0};
@@ -631,23 +642,28 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
     const uint32_t at = atomicAdd(&s.listed, 1u);
     if (at < kList) s.list[at] = (u64)(~key_of(v)) << 32 | (uint32_t)i;
   };
-  each(x, a.vocab, [&](float v, int i) {
-    if (!(v > -INFINITY)) return;
-    const double d = row.gap(v);
-    if (!(d < kSpan)) return;
-    const int b = bin_of(d);
-    atomicAdd(&s.hist[b], token_bits(d, b));
-    if (v >= low) put(v, i);
+  x.template fours<4>([&](const float* v, int i) {
+    double d[4];
+    u64 bits[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = row.bins(v[e]), bits[e] = token_bits(d[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d[e] < kBins) atomicAdd(&s.hist[(int)d[e]], bits[e]);
+    if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= low)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v[e] >= low && d[e] < kBins) put(v[e], i + e);
   });
   __syncthreads();
   const Wanted w = decide(s, c);
   // The list holds every bin before the one that `low` lies in.
-  const double low_gap = row.gap(low);
-  const int whole = low_gap < kSpan ? bin_of(low_gap) : kBins;
+  const double low_bins = row.bins(low);
+  const int whole = low_bins < kBins ? (int)low_bins : kBins;
   uint32_t n = s.listed;
   if (n > kList || w.last >= whole) {
     if (s.wanted > kList) {
-      const Pick p = narrow(s, x, a.vocab, row, c);
+      const Pick p = narrow(s, x, row, c);
       if (tid == 0) {
         a.ids[r] = p.index;
         if (a.probs) a.probs[r] = p.prob;
@@ -657,10 +673,29 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
     __syncthreads();
     if (tid == 0) s.listed = 0;
     __syncthreads();
-    each(x, a.vocab, [&](float v, int i) {
-      if (!(v > -INFINITY)) return;
-      const double d = row.gap(v);
-      if (d < kSpan && w.has(bin_of(d))) put(v, i);
+    // Logits that can lie in the wanted bins: within a float's rounding of each run of bins, in 32 bits.
+    float mid[4], half[4];
+    const double width = kBinWidth * t;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const double top = row.max - w.lo[q] * width, bottom = row.max - (w.hi[q] + 1) * width;
+      mid[q] = (float)(0.5 * (top + bottom));
+      half[q] = w.hi[q] < w.lo[q] ? -1.f : (float)(0.5 * (top - bottom) + 2e-7 * (fabs(top) + fabs(bottom)) + 1e-44);
+    }
+    const bool all = !(width < 1e30) || !(fabs(row.max) < 1e30);  // where that could overflow, every token is looked at
+    x.template fours<4>([&](const float* v, int i) {
+      bool any = all;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (half[q] >= 0.f)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) any |= fabsf(v[e] - mid[q]) <= half[q];
+      if (any)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double d = row.bins(v[e]);
+          if (d < kBins && w.has((int)d)) put(v[e], i + e);
+        }
     });
     __syncthreads();
     n = s.listed;
