@@ -673,29 +673,36 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
     __syncthreads();
     if (tid == 0) s.listed = 0;
     __syncthreads();
-    // Logits that can lie in the wanted bins: within a float's rounding of each run of bins, in 32 bits.
-    float mid[4], half[4];
-    const double width = kBinWidth * t;
+    // The bins fall with the logits, so the wanted runs of bins are runs of logits: lane 2 q (and 2 q + 1) of each wave finds
+    // by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
+    uint32_t below = 0, at = 0x7f800000u | 0x80000000u;  // keys of masked tokens, and past every finite logit's
+    {
+      int edge = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const double top = row.max - w.lo[q] * width, bottom = row.max - (w.hi[q] + 1) * width;
-      mid[q] = (float)(0.5 * (top + bottom));
-      half[q] = w.hi[q] < w.lo[q] ? -1.f : (float)(0.5 * (top - bottom) + 2e-7 * (fabs(top) + fabs(bottom)) + 1e-44);
+      for (int q = 0; q < 4; ++q) {
+        if (lane == 2 * q) edge = w.hi[q] < w.lo[q] ? -1 : w.hi[q] + 1;
+        if (lane == 2 * q + 1) edge = w.hi[q] < w.lo[q] ? -1 : w.lo[q];
+      }
+      while (at - below > 1) {
+        const uint32_t mid = below + (at - below) / 2;
+        if (row.bins_of_key(mid) < edge) at = mid;
+        else below = mid;
+      }
     }
-    const bool all = !(width < 1e30) || !(fabs(row.max) < 1e30);  // where that could overflow, every token is looked at
+    float from[4], past[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) from[q] = of_key(__shfl(at, 2 * q)), past[q] = of_key(__shfl(at, 2 * q + 1));
     x.template fours<4>([&](const float* v, int i) {
-      bool any = all;
+      bool in[4] = {};
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (half[q] >= 0.f)
+        if (w.hi[q] >= w.lo[q])
 #pragma unroll
-          for (int e = 0; e < 4; ++e) any |= fabsf(v[e] - mid[q]) <= half[q];
-      if (any)
+          for (int e = 0; e < 4; ++e) in[e] |= v[e] >= from[q] && v[e] < past[q];
+      if (in[0] | in[1] | in[2] | in[3])
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const double d = row.bins(v[e]);
-          if (d < kBins && w.has((int)d)) put(v[e], i + e);
-        }
+        for (int e = 0; e < 4; ++e)
+          if (in[e]) put(v[e], i + e);
     });
     __syncthreads();
     n = s.listed;
