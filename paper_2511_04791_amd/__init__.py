@@ -90,6 +90,10 @@ class _BatchC:
     def num_tokens(self) -> int:
         return sum(self.rows[:, 2].tolist()) if len(self.rows) else 0
 
+    def end_row(self) -> int:
+        """One past the last request's rows: the tokens of a batch whose rows are packed, as the library checks."""
+        return int(self.rows[-1][1]) + int(self.rows[-1][2]) if len(self.rows) else 0
+
     def num_decodes(self) -> int:
         return self.rows[:, 0].tolist().count(KIND_DECODE) if len(self.rows) else 0
 
@@ -433,6 +437,7 @@ class Context:
         else:
             N.check(N.lib().duet_init_with_model(device, model_path.encode(), ctypes.byref(h)), "duet_init_with_model")
         self.handle = h
+        self._dev = torch.device("cuda", device)
         self.model = Model(N.lib().duet_ctx_model(h), owner=self)
         self._ws = None
 
@@ -611,34 +616,39 @@ class Context:
         """Memory for one call that runs on `stream` (None: the current one): the allocator hands it to no later
         work before the call's, and under capture it belongs to the graph."""
         import torch
-        dev = f"cuda:{self.device}"
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=dev)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)):
-            return torch.empty(shape, dtype=dtype, device=dev)
+            return torch.empty(shape, dtype=dtype, device=self._dev)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self._dev) if stream else
+                               torch.cuda.default_stream(self._dev)):
+            return torch.empty(shape, dtype=dtype, device=self._dev)
 
     def _check_on(self, t, name, dtype, shape):
         """A contiguous tensor of this context's device."""
-        if t.device.type != "cuda" or t.device.index != self.device or t.dtype != dtype or tuple(t.shape) != shape or \
-                not t.is_contiguous():
+        if not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == self.device and t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{self.device}")
+
+    def _current(self, stream) -> int:
+        """The caller's stream, or torch's current one on this context's device."""
+        import torch
+        return torch.cuda.current_stream(self._dev).cuda_stream if stream is None else stream
 
     def qkv_rope_split(self, qkv, k_cache, v_cache, page_table, seq_meta, shape: AttnShape, rope: Rope, *, positions=None,
                        q=None, workspace=None, stream=None, check_errors: bool = False):
         """duet_qkv_rope_split: the rotated query rows out of qkv [T, (h_q + 2 h_kv) d], rotated keys and values into the
         cache.  positions: int32 [axes, T] ([T] for one axis); None: the tokens' places in the cache."""
         import torch
-        b = _BatchC(seq_meta)
-        T = b.num_tokens()
+        lib, b = N.lib(), _BatchC(seq_meta)
+        T = b.end_row()
         dt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
         hq, hkv, d, ps = shape.num_q_heads, shape.num_kv_heads, shape.head_dim, shape.page_size
         pages = int(k_cache.shape[0])
         self._check_on(qkv, "qkv", dt, (T, (hq + 2 * hkv) * d))
         self._check_on(k_cache, "k_cache", dt, (pages, hkv, ps, d))
         self._check_on(v_cache, "v_cache", dt, (pages, hkv, d, ps))
-        if page_table.dim() != 2 or page_table.shape[0] < len(b.rows):
+        table = page_table.shape
+        if len(table) != 2 or table[0] < len(b.rows):
             raise ValueError("page_table must be [R, max_pages] with a row per request")
-        self._check_on(page_table, "page_table", torch.int32, tuple(page_table.shape))
+        self._check_on(page_table, "page_table", torch.int32, table)
         if positions is not None:
             self._check_on(positions, "positions", torch.int32,
                            (T,) if rope.axes == 1 and positions.dim() == 1 else (rope.axes, T))
@@ -648,48 +658,47 @@ class Context:
             self._check_on(q, "q", dt, (T, hq, d))
         if workspace is None:
             n = ctypes.c_size_t()
-            N.check(N.lib().duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+            N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
             workspace = self._empty(n.value, torch.uint8, stream)
         if T == 0:
             return q
-        st = _stream_of(qkv, stream)
-        N.check(N.lib().duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
-                                            positions.data_ptr() if positions is not None else None, q.data_ptr(),
-                                            k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(),
-                                            int(page_table.shape[1]), ctypes.byref(b.c), workspace.data_ptr(),
-                                            workspace.numel(), st), "duet_qkv_rope_split")
+        st = self._current(stream)
+        N.check(lib.duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
+                                        positions.data_ptr() if positions is not None else None, q.data_ptr(),
+                                        k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(), table[1],
+                                        ctypes.byref(b.c), workspace.data_ptr(), workspace.numel(), st), "duet_qkv_rope_split")
         if check_errors:
-            N.check(N.lib().duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
+            N.check(lib.duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
         return q
 
     def lora_add(self, x, base, lora: Lora, seq_meta, adapter_ids, *, out=None, workspace=None, stream=None):
         """duet_lora_add: base [T, d_out] plus each request's adapter applied to x [T, d_in] (bf16, rows may be strided).
         adapter_ids: one int per request, -1 for none.  out may be base."""
         import torch
-        b = _BatchC(seq_meta)
-        T = b.num_tokens()
+        lib, b = N.lib(), _BatchC(seq_meta)
+        T = b.end_row()
         ids = np.ascontiguousarray(adapter_ids, dtype=np.int32)
         if ids.shape != (len(b.rows),):
             raise ValueError(f"adapter_ids must hold {len(b.rows)} values, one per request")
         if out is None:
             out = self._empty((T, lora.c.d_out), torch.bfloat16, stream)
+        dt, ld = torch.bfloat16, []
         for t, name, width in ((x, "x", lora.c.d_in), (base, "base", lora.c.d_out), (out, "out", lora.c.d_out)):
-            if t.device.type != "cuda" or t.device.index != self.device or t.dtype != torch.bfloat16 or \
-                    tuple(t.shape) != (T, width) or t.stride(1) != 1:
+            if not (t.dtype is dt and t.shape == (T, width) and t.is_cuda and t.get_device() == self.device and t.stride(1) == 1):
                 raise ValueError(f"{name} must be a bf16 tensor [{T}, {width}] on cuda:{self.device} with contiguous rows")
-        if lora.a.device.index != self.device:
+            ld.append(t.stride(0) if T > 1 else width)
+        if lora.a.get_device() != self.device:
             raise ValueError(f"the adapters must lie on cuda:{self.device}")
         if workspace is None:
             n = ctypes.c_size_t()
-            N.check(N.lib().duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
+            N.check(lib.duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
                     "duet_lora_workspace_bytes")
             workspace = self._empty(n.value, torch.uint8, stream)
         if T == 0:
             return out
-        ld = lambda t: int(t.shape[1]) if T == 1 else int(t.stride(0))  # noqa: E731
-        N.check(N.lib().duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld(x), base.data_ptr(), ld(base),
-                                      out.data_ptr(), ld(out), ctypes.byref(b.c), ids.ctypes.data, workspace.data_ptr(),
-                                      workspace.numel(), _stream_of(x, stream)), "duet_lora_add")
+        N.check(lib.duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld[0], base.data_ptr(), ld[1],
+                                  out.data_ptr(), ld[2], ctypes.byref(b.c), ids.ctypes.data, workspace.data_ptr(),
+                                  workspace.numel(), self._current(stream)), "duet_lora_add")
         return out
 
     def sample(self, logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None, stream=None):
@@ -697,10 +706,10 @@ class Context:
         float32, rows may be strided) from the given random numbers u [rows] float32 in [0, 1).  temperature, top_p,
         min_p: float32 [rows]; top_k: int32 [rows]; None: off."""
         import torch
-        if logits.device.type != "cuda" or logits.device.index != self.device or logits.dim() != 2 or \
-                logits.dtype not in (torch.bfloat16, torch.float32) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        if not (logits.is_cuda and logits.get_device() == self.device and logits.dim() == 2 and
+                logits.dtype in (torch.bfloat16, torch.float32) and (logits.stride(1) == 1 or logits.shape[1] == 1)):
             raise ValueError(f"logits must be a bf16 or float32 tensor [rows, vocab] on cuda:{self.device} with contiguous rows")
-        rows, vocab = int(logits.shape[0]), int(logits.shape[1])
+        rows, vocab = logits.shape
         self._check_on(u, "u", torch.float32, (rows,))
         params = N.Sampling()
         for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
@@ -718,10 +727,10 @@ class Context:
             self._check_on(probs, "probs", torch.float32, (rows,))
         if rows == 0:
             return out, probs
-        stride = vocab if rows == 1 else int(logits.stride(0))
+        stride = vocab if rows == 1 else logits.stride(0)
         N.check(N.lib().duet_sample(self.handle, logits.data_ptr(), BF16 if logits.dtype == torch.bfloat16 else F32, rows,
                                     vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
-                                    _stream_of(logits, stream)), "duet_sample")
+                                    self._current(stream)), "duet_sample")
         return out, probs
 
     def attn_iteration(self, qs, k_caches, v_caches, page_table, seq_meta, cu_split: CuSplit = CuSplit.agg(), *,
