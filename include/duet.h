@@ -332,15 +332,19 @@ typedef struct {
   const float* min_p;       /* keep tokens of at least min_p times the largest weight; not above 0, NaN: all */
 } duet_sampling;
 
+/* Workspace of duet_sample: 0 where one workgroup takes a whole row.  Host only. */
+int duet_sample_workspace_bytes(int32_t rows, int32_t vocab, size_t* bytes);
 /* One token for each row of logits [rows, vocab] (dtype bf16 or fp32, rows row_stride elements apart; vocab at
  * most 2^18, rows at most 2^20).  Tokens are ranked by falling logit, ties by the lower index, with weights
  * exp((logit - max) / T); top-k, then top-p, then min-p each keep a run of ranks from the first; ids[row] (int32) is the
  * first rank whose cumulative kept weight exceeds u[row] times all of it, probs[row] (may be NULL) its weight's
  * share of it.  u is a given random number in [0, 1); others are taken as 0 or the largest below 1.  NaN and -inf are
  * tokens that a mask took out; a row of nothing else gives -1 with probability 0.  +inf outweighs all finite
- * logits.  params NULL: all off.  The result does not depend on other rows nor on the stream. */
+ * logits.  params NULL: all off.  The workspace lies on 16 bytes (NULL where none is needed).  The result does not depend
+ * on other rows nor on the stream. */
 int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
-                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* stream);
+                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* workspace,
+                size_t workspace_bytes, void* stream);
 
 /* ---- GPU context ----------------------------------------------------------------------------- */
 

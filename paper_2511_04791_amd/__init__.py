@@ -701,7 +701,8 @@ class Context:
                                   workspace.numel(), self._current(stream)), "duet_lora_add")
         return out
 
-    def sample(self, logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None, stream=None):
+    def sample(self, logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None,
+               workspace=None, stream=None):
         """duet_sample: (ids int32 [rows], probs float32 [rows]), one token for each row of logits [rows, vocab] (bf16 or
         float32, rows may be strided) from the given random numbers u [rows] float32 in [0, 1).  temperature, top_p,
         min_p: float32 [rows]; top_k: int32 [rows]; None: off."""
@@ -727,10 +728,14 @@ class Context:
             self._check_on(probs, "probs", torch.float32, (rows,))
         if rows == 0:
             return out, probs
-        stride = vocab if rows == 1 else logits.stride(0)
-        N.check(N.lib().duet_sample(self.handle, logits.data_ptr(), BF16 if logits.dtype == torch.bfloat16 else F32, rows,
-                                    vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
-                                    self._current(stream)), "duet_sample")
+        stride, lib = vocab if rows == 1 else logits.stride(0), N.lib()
+        if workspace is None:
+            n = ctypes.c_size_t()
+            N.check(lib.duet_sample_workspace_bytes(rows, vocab, ctypes.byref(n)), "duet_sample_workspace_bytes")
+            workspace = self._empty(n.value, torch.uint8, stream)
+        N.check(lib.duet_sample(self.handle, logits.data_ptr(), BF16 if logits.dtype == torch.bfloat16 else F32, rows,
+                                vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
+                                workspace.data_ptr(), workspace.numel(), self._current(stream)), "duet_sample")
         return out, probs
 
     def attn_iteration(self, qs, k_caches, v_caches, page_table, seq_meta, cu_split: CuSplit = CuSplit.agg(), *,

@@ -117,8 +117,9 @@ _SIGS = {
     "duet_lora_workspace_bytes": (c_int32, [P(Lora), P(Batch), P(c_size_t)]),
     "duet_lora_add": (c_int32, [c_void_p, P(Lora), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, P(Batch),
                                 c_void_p, c_void_p, c_size_t, c_void_p]),
+    "duet_sample_workspace_bytes": (c_int32, [c_int32, c_int32, P(c_size_t)]),
     "duet_sample": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int64, P(Sampling), c_void_p, c_void_p,
-                              c_void_p, c_void_p]),
+                              c_void_p, c_void_p, c_size_t, c_void_p]),
     "duet_attn_mixed_batch": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32,
                                         P(Batch), CuSplit, c_void_p, c_size_t, c_void_p, c_void_p]),
     "duet_attn_mixed_batch_noalloc": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p,

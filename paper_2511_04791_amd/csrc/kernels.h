@@ -271,7 +271,8 @@ struct SampleArgs {
   int32_t dtype, rows, vocab;
 };
 constexpr int kMaxVocab = 1 << 18;
-hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+size_t sample_workspace(int rows, int vocab);  // bytes, on 16; may be 0
+hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s);
 
 // Projections of few rows (gemm_skinny.hip) instead of the library's, for a partition of `rows` rows on
 // `cus` CUs and layers of model width d, QKV width d_qkv and MLP width m: where one part of the widest product in

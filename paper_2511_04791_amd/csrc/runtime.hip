@@ -1992,17 +1992,38 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   return DUET_OK;
 }
 
+namespace {
+int check_sample(int32_t rows, int32_t vocab) {
+  if (rows < 0 || rows > kMaxSampleRows) return fail(DUET_EINVAL, "rows %d not in [0, %d]", rows, kMaxSampleRows);
+  if (vocab < 1) return fail(DUET_EINVAL, "vocab %d < 1", vocab);
+  if (vocab > kMaxVocab) return fail(DUET_EUNSUPPORTED, "vocab %d: at most %d", vocab, kMaxVocab);
+  return DUET_OK;
+}
+}  // namespace
+
+int duet_sample_workspace_bytes(int32_t rows, int32_t vocab, size_t* bytes) {
+  clear_error();
+  const int rc = check_sample(rows, vocab);
+  if (rc) return rc;
+  if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
+  *bytes = sample_workspace(rows, vocab);
+  return DUET_OK;
+}
+
 int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
-                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* stream) {
+                const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* workspace,
+                size_t workspace_bytes, void* stream) {
   clear_error();
   if (!ctx) return fail(DUET_EINVAL, "ctx is NULL");
   int rc;
   if ((rc = check_device_ptr(logits, "logits")) || (rc = check_device_ptr(u, "u")) || (rc = check_device_ptr(ids, "ids")))
     return rc;
   if (dtype != DUET_BF16 && dtype != DUET_F32) return fail(DUET_EUNSUPPORTED, "dtype must be bf16 or f32");
-  if (rows < 0 || rows > kMaxSampleRows) return fail(DUET_EINVAL, "rows %d not in [0, %d]", rows, kMaxSampleRows);
-  if (vocab < 1) return fail(DUET_EINVAL, "vocab %d < 1", vocab);
-  if (vocab > kMaxVocab) return fail(DUET_EUNSUPPORTED, "vocab %d: at most %d", vocab, kMaxVocab);
+  if ((rc = check_sample(rows, vocab))) return rc;
+  const size_t need = sample_workspace(rows, vocab);
+  if (need && !workspace) return fail(DUET_EINVAL, "workspace is NULL");
+  if (workspace_bytes < need) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
+  if (need && reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
   if (row_stride < vocab) return fail(DUET_EINVAL, "row_stride %lld < vocab %d", (long long)row_stride, vocab);
   SampleArgs a{};
   a.logits = logits;
@@ -2021,7 +2042,7 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
   a.vocab = vocab;
   DeviceGuard device(ctx->device);
   HIP_TRY(device.status);
-  HIP_TRY(launch_sample(a, static_cast<hipStream_t>(stream)));
+  HIP_TRY(launch_sample(a, workspace, static_cast<hipStream_t>(stream)));
   return DUET_OK;
 }
 

@@ -14,9 +14,11 @@
 // v = e^-(d - d_bin) in (1 - 2^-6.4, 1] its weight relative to the bin's first.  The count stands in bits 45 on,
 // the sum of up to 2^18 terms under 2^(26.6 + 18) below.  Each term rounds by 2^-34 of the token's weight.
 //
-// One workgroup a row.  It reads the row twice (its maximum, the histogram), a third time where the places lie past
-// the largest few hundred tokens, which the second pass lists as it goes.
+// A row is read twice (its maximum, the histogram), a third time where the places lie past the largest few hundred tokens,
+// which the second pass lists as it goes; by one workgroup, or in slices by several where there are few rows.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kernels.h"
 #include "wave_ops.h"
@@ -85,11 +87,12 @@ struct Row {
   __device__ __forceinline__ double bins_of_key(uint32_t k) const { return bins(of_key(k)); }
 };
 __device__ __forceinline__ double weight_of(double bins) { return exp(-bins * kBinWidth); }
-// (1 - v) 2^33 to the nearest, by the series of 1 - e^-y: y < kBinWidth leaves out y^5 / 120 < 2^-39.
+// (1 - v) 2^33 to the nearest: the series of 1 - e^-y, y = x kBinWidth, x in [0, 1), up to y^3, and y^4 by the cubic nearest
+// to it there; within 2^-37.
 __device__ __forceinline__ uint32_t fraction_of(double bins) {
-  constexpr double w = kBinWidth, c1 = kFraction * w, c2 = c1 * w / 2, c3 = c2 * w / 3, c4 = c3 * w / 4;
-  const double y = bins - (double)(int)bins;
-  return (uint32_t)fma(y, fma(y, fma(y, fma(y, -c4, c3), -c2), c1), 0.5);
+  constexpr double w = kBinWidth, f = kFraction, q = f * w * w * w * w / 24;
+  const double x = __builtin_amdgcn_fract(bins);
+  return (uint32_t)fma(x, fma(x, fma(x, f * w * w * w / 6 - 2 * q, -f * w * w / 2 + 1.25 * q), f * w - 0.25 * q), 0.5 + q / 128);
 }
 __device__ __forceinline__ u64 token_bits(double bins) { return (1ull << kCountShift) + fraction_of(bins); }
 __device__ __forceinline__ uint32_t count_of(u64 h) { return (uint32_t)(h >> kCountShift); }
@@ -129,25 +132,24 @@ struct Logits {
         for (int e = 0; e < 4; ++e) y[e] = plain(y[e]);
       f(y, head + 4 * i);
     };
-    int i = tid;
-    for (; i + (U - 1) * kThreads < body; i += U * kThreads) {
+    // Each vector's registers are loaded again as soon as it is used.
+    if (body > 0) {
       Four v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = p[i + u * kThreads];
+      for (int u = 0; u < U; ++u) v[u] = p[min(tid + u * kThreads, body - 1)];
+      for (int i = tid; i < body; i += U * kThreads) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) four(v[u], i + u * kThreads);
-    }
-    for (; i < body + head + rest; i += kThreads) {
-      Four v = {};
-      int at = 4 * i + head;
-      if (i < body) {
-        v = p[i];
-        four(v, i);
-      } else {
-        at = i - body < head ? i - body : n - rest + i - body - head;
-        const float y[4] = {this->at(at), -INFINITY, -INFINITY, -INFINITY};
-        f(y, at);
+        for (int u = 0; u < U; ++u) {
+          const int k = i + u * kThreads;
+          if (k < body) four(v[u], k);
+          v[u] = p[min(k + U * kThreads, body - 1)];
+        }
       }
+    }
+    if (tid < head + rest) {
+      const int k = tid < head ? tid : n - rest + tid - head;
+      const float y[4] = {at(k), -INFINITY, -INFINITY, -INFINITY};
+      f(y, k);
     }
   }
   template <typename F>
@@ -158,6 +160,33 @@ struct Logits {
     });
   }
 };
+
+// A value of the lane one (two, four, eight) before in its row of 16, of the last lane of the row before, of the last of the
+// first two rows, for an inclusive scan over the wave; zero where there is none.  Vector instructions: no LDS round trip.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t before_in_wave(uint32_t x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 before_in_wave(u64 x) {
+  return (u64)before_in_wave<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | before_in_wave<CTRL, ROWS>((uint32_t)x);
+}
+template <typename F>
+__device__ __forceinline__ void scan_steps(F step) {
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+}
+__device__ __forceinline__ void scan_place(uint32_t* n, double* m) {
+  scan_steps([&](auto ctrl, auto rows) {
+    constexpr int c = decltype(ctrl)::value, r = decltype(rows)::value;
+    *n += before_in_wave<c, r>(*n);
+    *m += __longlong_as_double(before_in_wave<c, r>((u64)__double_as_longlong(*m)));
+  });
+}
 
 // ---- narrowing by bits: any number of tokens in a bin ------------------------------------------------
 
@@ -175,11 +204,7 @@ __device__ int find_bin(Shared& s, int n, int fixed_bin, Place at, F reached, Pl
   }
   uint32_t ci = c;
   double mi = m;
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t cu = __shfl_up(ci, off);
-    const double mu = __shfl_up(mi, off);
-    if (lane >= off) ci += cu, mi += mu;
-  }
+  scan_place(&ci, &mi);
   if (lane == 63) s.wave_count[wave] = ci, s.wave_mass[wave] = mi;
   if (tid == 0) s.at = 1 << 30;
   __syncthreads();
@@ -389,6 +414,11 @@ __device__ void sort_list(Shared& s, int n) {
   __syncthreads();
 }
 
+__device__ __forceinline__ void put(Shared& s, float v, int i) {
+  const uint32_t at = atomicAdd(&s.listed, 1u);
+  if (at < kList) s.list[at] = (u64)(~key_of(v)) << 32 | (uint32_t)i;
+}
+
 // The bins that a row's places may lie in: those of top-k's end, top-p's, min-p's and the token's.
 struct Wanted {
   int lo[4], hi[4];  // empty where hi < lo
@@ -419,11 +449,7 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
   }
   uint32_t in = cn;
   double im = cm;
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t un = __shfl_up(in, off);
-    const double um = __shfl_up(im, off);
-    if (lane >= off) in += un, im += um;
-  }
+  scan_place(&in, &im);
   if (lane == 63) s.wave_count[wave] = in, s.wave_mass[wave] = im;
   if (tid < 5) s.found[tid] = kBins;
   if (tid == 0) s.at = -1, s.wanted = 0;
@@ -447,14 +473,15 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
     if (n[i]) last = b;
   }
   if (tid == 0) s.mass[kBins] = all.mass, s.before[kBins] = all.n;
-  if (last >= 0) atomicMax(&s.at, last);
+  if (last >= 0 && !(__ballot(last >= 0) >> lane >> 1)) atomicMax(&s.at, last);
   // The first bin holding a token with reached(place after it) goes to slot q; the last bin if there is none.
   auto look = [&](int q, auto reached) {
     int b = kBins;
 #pragma unroll
     for (int i = kBinsPerThread - 1; i >= 0; --i)
       if (n[i] && reached(high[i])) b = tid * kBinsPerThread + i;
-    if (b < kBins) atomicMin(&s.found[q], b);
+    const u64 some = __ballot(b < kBins);  // bins rise with the lanes: the first lane has the wave's least
+    if (b < kBins && !(some & ((1ull << lane) - 1))) atomicMin(&s.found[q], b);
   };
   const bool k = c.top_k && c.top_k < all.n;
   if (k) look(0, [&](const Place& q) { return q.n >= c.top_k; });
@@ -517,13 +544,12 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
     run[j] = sum;
     scale[j] = scale_of(bin[j]);
   }
-  for (int off = 1; off < 64; off <<= 1) {
-    const Run up{__shfl_up(sum.first, off), __shfl_up(sum.n, off), __shfl_up(sum.fraction, off)};
-    if (lane >= off) sum = join(up, sum);
-  }
+  scan_steps([&](auto ctrl, auto rows) {
+    constexpr int c = decltype(ctrl)::value, r = decltype(rows)::value;
+    sum = join(Run{before_in_wave<c, r>(sum.first), before_in_wave<c, r>(sum.n), before_in_wave<c, r>(sum.fraction)}, sum);
+  });
   if (lane == 63) s.runs[wave] = sum;
-  Run left{__shfl_up(sum.first, 1), __shfl_up(sum.n, 1), __shfl_up(sum.fraction, 1)};
-  if (lane == 0) left = Run{0, 0, 0};
+  Run left{before_in_wave<0x138, 0xf>(sum.first), before_in_wave<0x138, 0xf>(sum.n), before_in_wave<0x138, 0xf>(sum.fraction)};
   if (tid == 0) s.pos = 1 << 30, s.last_pos = -1, s.at = -1, s.value = w.all.mass;
   __syncthreads();
   Run before{0, 0, 0};
@@ -543,19 +569,21 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
 #pragma unroll
     for (int j = 0; j < P; ++j)
       if (listed(j) && high[j].n == c.top_k) s.value = high[j].mass;
+  int last = -1;
 #pragma unroll
-  for (int j = P - 1; j >= 0; --j)
-    if (listed(j)) {
-      atomicMax(&s.last_pos, tid * P + j);
-      break;
-    }
+  for (int j = 0; j < P; ++j)
+    if (listed(j)) last = tid * P + j;
+  if (last >= 0 && !(__ballot(last >= 0) >> lane >> 1)) atomicMax(&s.last_pos, last);
   __syncthreads();
   Place kept{k ? c.top_k : w.all.n, s.value};
   // The first listed rank at or past a place, the last one where none is.
   auto first = [&](auto reached) {
+    int i = 1 << 30;
 #pragma unroll
     for (int j = P - 1; j >= 0; --j)
-      if (listed(j) && reached(high[j])) atomicMin(&s.pos, tid * P + j);
+      if (listed(j) && reached(high[j])) i = tid * P + j;
+    const u64 some = __ballot(i < 1 << 30);
+    if (i < 1 << 30 && !(some & ((1ull << lane) - 1))) atomicMin(&s.pos, i);
     __syncthreads();
     const int at = s.pos == 1 << 30 ? s.last_pos : s.pos;
     if (at / P == tid) s.place = high[at % P];
@@ -589,15 +617,29 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
   return Pick{(int)(uint32_t)s.list[at], (float)(s.value / kept.mass)};
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
-  __shared__ Shared s;
-  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  Logits<T> x{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride, a.vocab, false};
+// ---- one row: the pieces that one workgroup, or several, run --------------------------------------------
+
+// What a row's request asks for; the first rank alone needs no more than the maximum.
+__device__ __forceinline__ Settings settings_of(const SampleArgs& a, int r, double* inv_t, bool* greedy) {
   const float t = a.temperature ? a.temperature[r] : 1.f;
   const int top_k = a.top_k ? a.top_k[r] : 0;
-  const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
-  const bool greedy = !(t > 0.f) || top_k == 1 || top_p <= 0.f;  // the first rank alone
+  const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
+  *inv_t = 1.0 / t;
+  *greedy = !(t > 0.f) || top_k == 1 || top_p <= 0.f;
+  return Settings{(uint32_t)max(top_k, 0), top_p < 1.f ? top_p : 1.0, min_p > 0.f ? fmin(1.0, (double)min_p) : 0.0,
+                  u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.0};
+}
+
+// A slice's largest logit (and, for the first rank alone, its lowest index), and the smallest of the maxima of groups of
+// `lanes` threads: some hundred tokens of a row lie above the smallest of 128 such, 128 at least if the groups have a token
+// each.
+struct Part {
+  float max, low;
+  int index, pad;
+};
+template <typename T>
+__device__ Part largest(Shared& s, const Logits<T>& x, int lanes, bool greedy) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   float most = -INFINITY;
   int index = 0;
   if (greedy) {
@@ -607,41 +649,33 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   } else {
     x.template fours<8>([&](const float* v, int) { most = fmaxf(most, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))); });
   }
-  // The smallest of the maxima of groups of eight threads: some hundred tokens lie above it, 128 at least if the groups
-  // have a token each.
-  float group = most;
-  for (int off = 1; off < 8; off <<= 1) group = fmaxf(group, __shfl_xor(group, off));
-  float low = group, high = group;
-  for (int off = 8; off < 64; off <<= 1) {
+  float low = most, high = most;
+  for (int off = 1; off < 64; off <<= 1) {
     high = fmaxf(high, __shfl_xor(high, off));
-    low = fminf(low, __shfl_xor(low, off));
+    const float other = __shfl_xor(low, off);
+    low = off < lanes ? fmaxf(low, other) : fminf(low, other);
   }
   if (lane == 0) s.wave_max[wave] = high, s.wave_low[wave] = low;
-  if (tid == 0) s.at = 0x7fffffff, s.listed = 0;
-#pragma unroll
-  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
+  if (tid == 0) s.at = 0x7fffffff;
   __syncthreads();
   for (int w = 0; w < kWaves; ++w) high = fmaxf(high, s.wave_max[w]), low = fminf(low, s.wave_low[w]);
-  if (high == -INFINITY || greedy) {
-    if (greedy && most == high && high > -INFINITY) atomicMin(&s.at, index);
+  if (greedy) {
+    if (most == high && high > -INFINITY) atomicMin(&s.at, index);
     __syncthreads();
-    if (tid == 0) {
-      a.ids[r] = high == -INFINITY ? -1 : s.at;
-      if (a.probs) a.probs[r] = high == -INFINITY ? 0.f : 1.f;
-    }
-    return;
+    index = s.at;
   }
-  x.infinite = high == INFINITY;
-  if (x.infinite) high = 0.f, low = x.plain(low);
-  const double inv_t = 1.0 / t;
-  const Row row{high, inv_t * kBinsPerUnit};
-  const float u = a.u[r];
-  const Settings c{(uint32_t)max(top_k, 0), top_p < 1.f ? top_p : 1.0, min_p > 0.f ? fmin(1.0, (double)min_p) : 0.0,
-                   u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.0};
-  auto put = [&](float v, int i) {
-    const uint32_t at = atomicAdd(&s.listed, 1u);
-    if (at < kList) s.list[at] = (u64)(~key_of(v)) << 32 | (uint32_t)i;
-  };
+  return Part{high, low, index, 0};
+}
+
+__device__ __forceinline__ void answer(const SampleArgs& a, int r, int index, float prob) {
+  if (threadIdx.x) return;
+  a.ids[r] = index;
+  if (a.probs) a.probs[r] = prob;
+}
+
+// The slice's tokens into s.hist, those not below `low` into s.list (s.listed counts them all).
+template <typename T>
+__device__ void count(Shared& s, const Logits<T>& x, int first, const Row& row, float low) {
   x.template fours<4>([&](const float* v, int i) {
     double d[4];
     u64 bits[4];
@@ -653,75 +687,305 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
     if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= low)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (v[e] >= low && d[e] < kBins) put(v[e], i + e);
+        if (v[e] >= low && d[e] < kBins) put(s, v[e], first + i + e);
   });
+}
+
+// The wanted bins fall with the logits, so their runs are runs of logits, [from, past).  Lane 2 q (and 2 q + 1) of each wave
+// finds by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
+struct Edges {
+  float from[4], past[4];
+};
+__device__ Edges edges_of(const Row& row, const Wanted& w) {
+  const int lane = threadIdx.x & 63;
+  uint32_t below = 0, at = 0xff800000u;  // the keys of masked tokens, and past every finite logit's
+  int edge = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (lane == 2 * q) edge = w.hi[q] < w.lo[q] ? -1 : w.hi[q] + 1;
+    if (lane == 2 * q + 1) edge = w.hi[q] < w.lo[q] ? -1 : w.lo[q];
+  }
+  // The key of the edge's place on the scale, if rounding left it near enough; else all of them.
+  const uint32_t near = key_of((float)(row.max - edge / row.scale));
+  if (near > 0x00800010u && near < 0xff7ffff0u && row.bins_of_key(near + 2) < edge && !(row.bins_of_key(near - 2) < edge))
+    below = near - 2, at = near + 2;
+  while (at - below > 1) {
+    const uint32_t mid = below + (at - below) / 2;
+    if (row.bins_of_key(mid) < edge) at = mid;
+    else below = mid;
+  }
+  Edges e;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    e.from[q] = of_key(__shfl(at, 2 * q));
+    e.past[q] = w.hi[q] < w.lo[q] ? e.from[q] : of_key(__shfl(at, 2 * q + 1));
+  }
+  return e;
+}
+
+// The slice's tokens within the edges into s.list.
+template <typename T>
+__device__ void gather(Shared& s, const Logits<T>& x, int first, const Edges& edges) {
+  x.template fours<4>([&](const float* v, int i) {
+    bool in[4] = {};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (edges.from[q] < edges.past[q])
+#pragma unroll
+        for (int e = 0; e < 4; ++e) in[e] |= v[e] >= edges.from[q] && v[e] < edges.past[q];
+    if (in[0] | in[1] | in[2] | in[3])
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (in[e]) put(s, v[e], first + i + e);
+  });
+}
+
+// Whether the list of the tokens not below `low` holds every wanted bin (it does the bins before the one that `low` lies
+// in).  If so, leaves those bins' tokens in it.
+__device__ bool list_serves(Shared& s, const Row& row, const Wanted& w, float low) {
+  const double b = row.bins(low);
+  const uint32_t n = s.listed;
+  if (n > kList || w.last >= (b < kBins ? (int)b : kBins)) return false;
+  u64 v[kListPerThread];
+#pragma unroll
+  for (int j = 0; j < kListPerThread; ++j) v[j] = threadIdx.x + j * kThreads < n ? s.list[threadIdx.x + j * kThreads] : ~0ull;
+  __syncthreads();
+  if (threadIdx.x == 0) s.listed = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kListPerThread; ++j)
+    if (v[j] != ~0ull && w.has((int)row.bins_of_key(~(uint32_t)(v[j] >> 32)))) s.list[atomicAdd(&s.listed, 1u)] = v[j];
+  __syncthreads();
+  return true;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
+  __shared__ Shared s;
+  const int r = blockIdx.x, tid = threadIdx.x;
+  Logits<T> x{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride, a.vocab, false};
+  double inv_t;
+  bool greedy;
+  const Settings c = settings_of(a, r, &inv_t, &greedy);
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
+  if (tid == 0) s.listed = 0;
+  Part p = largest(s, x, 8, greedy);
+  if (p.max == -INFINITY) return answer(a, r, -1, 0.f);
+  if (greedy) return answer(a, r, p.index, 1.f);
+  x.infinite = p.max == INFINITY;
+  const float low = x.plain(p.low);
+  const Row row{x.plain(p.max), inv_t * kBinsPerUnit};
+  count(s, x, 0, row, low);
   __syncthreads();
   const Wanted w = decide(s, c);
-  // The list holds every bin before the one that `low` lies in.
-  const double low_bins = row.bins(low);
-  const int whole = low_bins < kBins ? (int)low_bins : kBins;
-  uint32_t n = s.listed;
-  if (n > kList || w.last >= whole) {
+  if (!list_serves(s, row, w, low)) {
     if (s.wanted > kList) {
-      const Pick p = narrow(s, x, row, c);
-      if (tid == 0) {
-        a.ids[r] = p.index;
-        if (a.probs) a.probs[r] = p.prob;
-      }
-      return;
+      const Pick pick = narrow(s, x, row, c);
+      return answer(a, r, pick.index, pick.prob);
     }
+    const Edges edges = edges_of(row, w);
     __syncthreads();
     if (tid == 0) s.listed = 0;
     __syncthreads();
-    // The bins fall with the logits, so the wanted runs of bins are runs of logits: lane 2 q (and 2 q + 1) of each wave finds
-    // by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
-    uint32_t below = 0, at = 0x7f800000u | 0x80000000u;  // keys of masked tokens, and past every finite logit's
-    {
-      int edge = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (lane == 2 * q) edge = w.hi[q] < w.lo[q] ? -1 : w.hi[q] + 1;
-        if (lane == 2 * q + 1) edge = w.hi[q] < w.lo[q] ? -1 : w.lo[q];
-      }
-      while (at - below > 1) {
-        const uint32_t mid = below + (at - below) / 2;
-        if (row.bins_of_key(mid) < edge) at = mid;
-        else below = mid;
-      }
-    }
-    float from[4], past[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) from[q] = of_key(__shfl(at, 2 * q)), past[q] = of_key(__shfl(at, 2 * q + 1));
-    x.template fours<4>([&](const float* v, int i) {
-      bool in[4] = {};
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (w.hi[q] >= w.lo[q])
-#pragma unroll
-          for (int e = 0; e < 4; ++e) in[e] |= v[e] >= from[q] && v[e] < past[q];
-      if (in[0] | in[1] | in[2] | in[3])
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (in[e]) put(v[e], i + e);
-    });
+    gather(s, x, 0, edges);
     __syncthreads();
-    n = s.listed;
   }
+  const int n = s.listed;
   sort_list(s, n);
-  const Pick p = finish(s, n, row, c, w);
-  if (tid == 0) {
-    a.ids[r] = p.index;
-    if (a.probs) a.probs[r] = p.prob;
+  const Pick pick = finish(s, n, row, c, w);
+  answer(a, r, pick.index, pick.prob);
+}
+
+// ---- several workgroups a row, for few rows -------------------------------------------------------------
+//
+// Each takes a slice: sample_max leaves the slices' maxima, sample_count adds up their histograms and lists, sample_list
+// lists the tokens of the wanted bins if that list does not serve.  The last of a row's workgroups to finish a step goes
+// on with the row alone.  What they share goes past the XCDs' L2 caches by device-scope accesses.
+
+constexpr int kMaxSlices = 16;
+struct Split {
+  u64 hist[kBins];
+  u64 list[kList];
+  Part part[kMaxSlices];
+  Edges edges;
+  uint32_t listed, counted, gathered, open;  // tokens listed, slices done with each step, whether sample_list is needed
+};
+
+template <typename V>
+__device__ __forceinline__ V load_shared(const V* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename V>
+__device__ __forceinline__ void store_shared(V* p, V v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename T>
+__device__ __forceinline__ Logits<T> slice_of(const SampleArgs& a, int r, int* first) {
+  const int per = (a.vocab + gridDim.x - 1) / gridDim.x;
+  *first = min((int)blockIdx.x * per, a.vocab);
+  return Logits<T>{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride + *first, min(per, a.vocab - *first), false};
+}
+
+// Adds the workgroup's list to the row's; true for the workgroup that counts itself last, with the row's list in s.list.
+__device__ bool join_lists(Shared& s, Split* row, uint32_t* arrived) {
+  const int tid = threadIdx.x;
+  const uint32_t n = s.listed;
+  if (tid == 0) s.wanted = n ? __hip_atomic_fetch_add(&row->listed, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  __syncthreads();
+  const uint32_t base = s.wanted;
+  for (uint32_t i = tid; i < min(n, (uint32_t)kList); i += kThreads)
+    if (base + i < kList) store_shared(&row->list[base + i], s.list[i]);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores and additions have completed
+  __syncthreads();
+  if (tid == 0)
+    s.at = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  __syncthreads();
+  if (!s.at) return false;
+  if (tid == 0) s.listed = load_shared(&row->listed);
+  __syncthreads();
+  for (uint32_t i = tid; i < min(s.listed, (uint32_t)kList); i += kThreads) s.list[i] = load_shared(&row->list[i]);
+  __syncthreads();
+  return true;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_max(SampleArgs a, Split* split) {
+  __shared__ Shared s;
+  const int r = blockIdx.y, tid = threadIdx.x;
+  Split* row = split + r;
+  for (int i = blockIdx.x * kThreads + tid; i < kBins; i += gridDim.x * kThreads) row->hist[i] = 0;
+  if (blockIdx.x == 0 && tid == 0) row->listed = row->counted = row->gathered = row->open = 0;
+  double inv_t;
+  bool greedy;
+  (void)settings_of(a, r, &inv_t, &greedy);
+  int first;
+  const Logits<T> x = slice_of<T>(a, r, &first);
+  Part p = largest(s, x, 8 * gridDim.x, greedy);
+  p.index += first;
+  if (tid == 0) row->part[blockIdx.x] = p;
+}
+
+// The row's part from its slices'; the infinities of a row whose largest is infinite count as 0 from here on.
+template <typename T>
+__device__ Part join_parts(const Split* row, Logits<T>* x) {
+  Part p{-INFINITY, INFINITY, 0x7fffffff, 0};
+  for (int i = 0; i < (int)gridDim.x; ++i) {
+    const Part q = row->part[i];
+    if (q.max > p.max || (q.max == p.max && q.index < p.index)) p.max = q.max, p.index = q.index;
+    p.low = fminf(p.low, q.low);
   }
+  x->infinite = p.max == INFINITY;
+  return p;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_count(SampleArgs a, Split* split) {
+  __shared__ Shared s;
+  const int r = blockIdx.y, tid = threadIdx.x;
+  Split* row = split + r;
+  double inv_t;
+  bool greedy;
+  const Settings c = settings_of(a, r, &inv_t, &greedy);
+  int first;
+  Logits<T> x = slice_of<T>(a, r, &first);
+  const Part p = join_parts(row, &x);
+  if (p.max == -INFINITY || greedy) {
+    if (blockIdx.x == 0) answer(a, r, p.max == -INFINITY ? -1 : p.index, p.max == -INFINITY ? 0.f : 1.f);
+    return;
+  }
+  const float low = x.plain(p.low);
+  const Row scale{x.plain(p.max), inv_t * kBinsPerUnit};
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
+  if (tid == 0) s.listed = 0;
+  __syncthreads();
+  count(s, x, first, scale, low);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) {
+    const u64 h = s.hist[tid + i * kThreads];
+    if (h) (void)__hip_atomic_fetch_add(&row->hist[tid + i * kThreads], h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (!join_lists(s, row, &row->counted)) return;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = load_shared(&row->hist[tid + i * kThreads]);
+  __syncthreads();
+  const Wanted w = decide(s, c);
+  x = Logits<T>{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride, a.vocab, x.infinite};
+  if (list_serves(s, scale, w, low)) {
+    const int n = s.listed;
+    sort_list(s, n);
+    const Pick pick = finish(s, n, scale, c, w);
+    return answer(a, r, pick.index, pick.prob);
+  }
+  if (s.wanted > kList) {
+    const Pick pick = narrow(s, x, scale, c);
+    return answer(a, r, pick.index, pick.prob);
+  }
+  const Edges edges = edges_of(scale, w);
+  if (tid == 0) row->edges = edges, row->listed = 0, row->open = 1;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* split) {
+  __shared__ Shared s;
+  const int r = blockIdx.y, tid = threadIdx.x;
+  Split* row = split + r;
+  if (!row->open) return;
+  double inv_t;
+  bool greedy;
+  const Settings c = settings_of(a, r, &inv_t, &greedy);
+  int first;
+  Logits<T> x = slice_of<T>(a, r, &first);
+  const Part p = join_parts(row, &x);
+  const Row scale{x.plain(p.max), inv_t * kBinsPerUnit};
+  if (tid == 0) s.listed = 0;
+  __syncthreads();
+  gather(s, x, first, row->edges);
+  __syncthreads();
+  if (!join_lists(s, row, &row->gathered)) return;
+#pragma unroll
+  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = row->hist[tid + i * kThreads];
+  __syncthreads();
+  const Wanted w = decide(s, c);
+  const int n = s.listed;
+  sort_list(s, n);
+  const Pick pick = finish(s, n, scale, c, w);
+  answer(a, r, pick.index, pick.prob);
 }
 
 }  // namespace
 
-hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
-  if (a.rows <= 0) return hipSuccess;
-  if (a.dtype == DUET_BF16) hipLaunchKernelGGL(sample_row<__bf16>, dim3(a.rows), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL(sample_row<float>, dim3(a.rows), dim3(kThreads), 0, s, a);
+int sample_slices(int rows, int vocab) {
+  int n = 1;
+  while (2 * n <= kMaxSlices && 2 * n * rows <= 256 && vocab >= 2 * n * 8192) n *= 2;
+  return n;
+}
+
+size_t sample_workspace(int rows, int vocab) { return sample_slices(rows, vocab) > 1 ? rows * sizeof(Split) : 0; }
+
+namespace {
+template <typename T>
+hipError_t launch(const SampleArgs& a, void* workspace, hipStream_t s) {
+  const int slices = sample_slices(a.rows, a.vocab);
+  if (slices == 1) {
+    hipLaunchKernelGGL(sample_row<T>, dim3(a.rows), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+  }
+  Split* split = static_cast<Split*>(workspace);
+  const dim3 grid(slices, a.rows);
+  hipLaunchKernelGGL(sample_max<T>, grid, dim3(kThreads), 0, s, a, split);
+  hipLaunchKernelGGL(sample_count<T>, grid, dim3(kThreads), 0, s, a, split);
+  hipLaunchKernelGGL(sample_list<T>, grid, dim3(kThreads), 0, s, a, split);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  return a.dtype == DUET_BF16 ? launch<__bf16>(a, workspace, s) : launch<float>(a, workspace, s);
 }
 
 }  // namespace duet

@@ -60,6 +60,17 @@ def test_workspace_sizes(native):
     assert native.duet_lora_workspace_bytes(B(lora), B(big), B(m)) == -2
 
 
+def test_sample_workspace(native):
+    n = ctypes.c_size_t()
+    for rows, vocab in ((0, 100), (1, 1000), (1000, 1 << 18)):
+        assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == 0
+    for rows, vocab in ((1, 128256), (64, 128256)):
+        assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == 0 and n.value >= rows * 4096 * 8
+    for rows, vocab, code in ((-1, 10, -1), (1, 0, -1), (1, (1 << 18) + 1, -2), ((1 << 20) + 1, 10, -1)):
+        assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == code
+    assert native.duet_sample_workspace_bytes(1, 10, None) == -1
+
+
 @pytest.mark.parametrize("kw,code", [(dict(rank=4), -2), (dict(rank=136), -2), (dict(rank=20), -2), (dict(num_adapters=0), -1),
                                      (dict(d_in=12), -1), (dict(d_out=0), -1), (dict(d_out=(1 << 20) + 8), -1)])
 def test_lora_descriptions(native, kw, code):
@@ -78,7 +89,7 @@ def test_lora_needs_a_context(native):
 
 
 def test_sample_needs_a_context(native):
-    assert native.duet_sample(None, 16, 0, 1, 10, 10, None, 16, 16, None, None) == -1
+    assert native.duet_sample(None, 16, 0, 1, 10, 10, None, 16, 16, None, None, 0, None) == -1
     assert b"ctx" in native.duet_last_error()
 
 
@@ -134,11 +145,13 @@ class TestWithContext:
             assert native.duet_last_error()
 
     def test_sample(self, native, ctx):
-        def call(logits=16, dtype=0, rows=1, vocab=10, stride=10, u=16, ids=16):
-            return native.duet_sample(ctx.handle, logits, dtype, rows, vocab, stride, None, u, ids, None, None)
+        def call(logits=16, dtype=0, rows=1, vocab=10, stride=10, u=16, ids=16, ws=None, nbytes=0):
+            return native.duet_sample(ctx.handle, logits, dtype, rows, vocab, stride, None, u, ids, None, ws, nbytes, None)
+        big = dict(vocab=100000, stride=100000)
         for kw, code in ((dict(logits=None), -1), (dict(u=None), -1), (dict(ids=None), -1), (dict(dtype=2), -2), (dict(rows=-1), -1),
                          (dict(rows=(1 << 20) + 1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 18) + 1, stride=1 << 19), -2),
-                         (dict(stride=9), -1)):
+                         (dict(stride=9), -1), (dict(big), -1), (dict(big, ws=16, nbytes=4096), -3),
+                         (dict(big, ws=24, nbytes=1 << 20), -1)):
             assert call(**kw) == code, kw
             assert native.duet_last_error()
         assert call(rows=0) == 0
