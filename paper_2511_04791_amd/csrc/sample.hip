@@ -114,41 +114,40 @@ struct Logits {
   __device__ __forceinline__ float plain(float v) const { return infinite ? (v == INFINITY ? 0.f : -INFINITY) : v; }
   __device__ __forceinline__ float at(int i) const { return plain(as_float(x[i])); }
 
-  // f(four logits, index of the first): vectors of four past the first boundary, U of them in flight; the tokens before
-  // and after those one by one, with three masked ones.
+  // f(four logits, index of the first): a wave takes 64 vectors of four past the first boundary at a time, U such in flight;
+  // the up to 261 tokens before and after those come one a lane, with three masked ones.  Whole waves call f.
   template <int U, typename F>
   __device__ __forceinline__ void fours(F f) const {
     typedef T Four __attribute__((ext_vector_type(4)));
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
     const int off = (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) & 3);
-    const int head = min(n, (4 - off) & 3), body = (n - head) / 4, rest = n - head - 4 * body;
+    const int head = min(n, (4 - off) & 3), units = (n - head) / 256, rest = n - 256 * units;
     const Four* p = reinterpret_cast<const Four*>(x + head);
-    auto four = [&](const Four& v, int i) {
-      float y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = as_float(v[e]);
-      if (infinite)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = plain(y[e]);
-      f(y, head + 4 * i);
-    };
-    // Each vector's registers are loaded again as soon as it is used.
-    if (body > 0) {
+    if (wave < units) {
+      // Each vector's registers are loaded again as soon as it is used.
       Four v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = p[min(tid + u * kThreads, body - 1)];
-      for (int i = tid; i < body; i += U * kThreads) {
+      for (int u = 0; u < U; ++u) v[u] = p[64 * min(wave + u * kWaves, units - 1) + lane];
+      for (int i = wave; i < units; i += U * kWaves) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int k = i + u * kThreads;
-          if (k < body) four(v[u], k);
-          v[u] = p[min(k + U * kThreads, body - 1)];
+          const int k = i + u * kWaves;
+          if (k < units) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = as_float(v[u][e]);
+            if (infinite)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = plain(y[e]);
+            f(y, head + 4 * (64 * k + lane));
+          }
+          v[u] = p[64 * min(k + U * kWaves, units - 1) + lane];
         }
       }
     }
-    if (tid < head + rest) {
-      const int k = tid < head ? tid : n - rest + tid - head;
-      const float y[4] = {at(k), -INFINITY, -INFINITY, -INFINITY};
+    if (64 * wave < rest) {
+      const int k = tid < head ? tid : 256 * units + tid;
+      const float y[4] = {tid < rest ? at(k) : -INFINITY, -INFINITY, -INFINITY, -INFINITY};
       f(y, k);
     }
   }
@@ -368,55 +367,53 @@ __device__ __attribute__((noinline)) Pick narrow(Shared& s, const Logits<T>& x, 
 
 // ---- the histogram and a short list -------------------------------------------------------------------
 
-// s.list[0 .. n) into rising order; n <= kList, no two alike.  Each wave sorts runs of 64 in registers; a token's place is
-// then its place in its own run and, by bisection, in the others.
+// s.list[0 .. n) into rising order; n <= kList, no two alike.  Each wave sorts runs of 64 in registers; runs are then joined
+// two by two, a token's place being its place in its own and, by bisection, in the other.
 __device__ void sort_list(Shared& s, int n) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, runs = (n + 63) / 64;
-  for (int r = wave; r < runs; r += kWaves) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int r = tid >> 6; 64 * r < n; r += kWaves) {
     u64 v = 64 * r + lane < n ? s.list[64 * r + lane] : ~0ull;
     for (int k = 2; k <= 64; k <<= 1)
       for (int step = k >> 1; step > 0; step >>= 1) {
         const u64 other = __shfl_xor(v, step);
         if ((v > other) == (((lane & k) == 0) == ((lane & step) == 0))) v = other;
       }
-    s.list[64 * r + lane] = v;
+    if (64 * r + lane < n) s.list[64 * r + lane] = v;
   }
   __syncthreads();
-  if (runs == 1) return;
-  u64 v[kListPerThread];
-  int rank[kListPerThread];
+  for (int len = 64; len < n; len *= 2) {
+    u64 v[kListPerThread];
+    int to[kListPerThread];
 #pragma unroll
-  for (int j = 0; j < kListPerThread; ++j) {
-    const int own = wave + j * kWaves;
-    if (own >= runs) continue;
-    v[j] = s.list[64 * own + lane];
-    rank[j] = lane;
-    for (int r = 0; r < runs; r += 4) {
-      int at[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) at[q] = 0;
-#pragma unroll
-      for (int step = 32; step > 0; step >>= 1)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (s.list[64 * min(r + q, runs - 1) + at[q] + step - 1] < v[j]) at[q] += step;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        at[q] += s.list[64 * min(r + q, runs - 1) + at[q]] < v[j];
-        if (r + q < runs && r + q != own) rank[j] += at[q];
-      }
+    for (int j = 0; j < kListPerThread; ++j) {
+      const int i = tid + j * kThreads;
+      if (i >= n) continue;
+      v[j] = s.list[i];
+      const int other = (i / len ^ 1) * len;
+      int at = 0;
+      for (int step = len; step > 0; step >>= 1)
+        if (at + step <= len && other + at + step <= n && s.list[other + at + step - 1] < v[j]) at += step;
+      to[j] = (i & ~(2 * len - 1)) + (i & (len - 1)) + at;
     }
-  }
-  __syncthreads();
+    __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kListPerThread; ++j)
-    if (64 * (wave + j * kWaves) + lane < n) s.list[rank[j]] = v[j];
-  __syncthreads();
+    for (int j = 0; j < kListPerThread; ++j)
+      if (tid + j * kThreads < n) s.list[to[j]] = v[j];
+    __syncthreads();
+  }
 }
 
-__device__ __forceinline__ void put(Shared& s, float v, int i) {
-  const uint32_t at = atomicAdd(&s.listed, 1u);
-  if (at < kList) s.list[at] = (u64)(~key_of(v)) << 32 | (uint32_t)i;
+__device__ __forceinline__ u64 entry(float v, int i) { return (u64)(~key_of(v)) << 32 | (uint32_t)i; }
+
+// Those of a wave's tokens that are `in` to the list's end.
+__device__ __forceinline__ void put(Shared& s, bool in, float v, int i) {
+  const u64 all = __ballot(in);
+  if (!all) return;
+  const int lane = threadIdx.x & 63, leader = __ffsll((long long)all) - 1;
+  uint32_t at = 0;
+  if (lane == leader) at = atomicAdd(&s.listed, (uint32_t)__popcll(all));
+  at = __builtin_amdgcn_readlane(at, leader) + __popcll(all & ((1ull << lane) - 1));
+  if (in && at < kList) s.list[at] = entry(v, i);
 }
 
 // The bins that a row's places may lie in: those of top-k's end, top-p's, min-p's and the token's.
@@ -529,39 +526,43 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
   int bin[P];
   uint32_t fraction[P];
   Run run[P];
+  const bool busy = wave * 64 * P < n;  // waves past the list only meet the barriers
   auto bins_at = [&](int i) { return row.bins_of_key(~(uint32_t)(s.list[i] >> 32)); };
   auto join = [](const Run& a, const Run& b) { return b.first ? b : Run{a.first, a.n + b.n, a.fraction + b.fraction}; };
-  Run sum{0, 0, 0};
+  Run sum{0, 0, 0}, left{0, 0, 0};
+  if (busy) {
 #pragma unroll
-  for (int j = 0; j < P; ++j) {
-    const int i = tid * P + j;
-    const int k = min(i, n - 1);
-    d[j] = bins_at(k);
-    bin[j] = (int)d[j];
-    fraction[j] = fraction_of(d[j]);
-    const Run one{i == 0 || i >= n || (int)bins_at(k - 1) != bin[j], 1, fraction[j]};
-    sum = j ? join(sum, one) : one;
-    run[j] = sum;
-    scale[j] = scale_of(bin[j]);
+    for (int j = 0; j < P; ++j) {
+      const int i = tid * P + j;
+      const int k = min(i, n - 1);
+      d[j] = bins_at(k);
+      bin[j] = (int)d[j];
+      fraction[j] = fraction_of(d[j]);
+      const Run one{i == 0 || i >= n || (int)bins_at(k - 1) != bin[j], 1, fraction[j]};
+      sum = j ? join(sum, one) : one;
+      run[j] = sum;
+      scale[j] = scale_of(bin[j]);
+    }
+    scan_steps([&](auto ctrl, auto rows) {
+      constexpr int c = decltype(ctrl)::value, r = decltype(rows)::value;
+      sum = join(Run{before_in_wave<c, r>(sum.first), before_in_wave<c, r>(sum.n), before_in_wave<c, r>(sum.fraction)}, sum);
+    });
+    if (lane == 63) s.runs[wave] = sum;
+    left = Run{before_in_wave<0x138, 0xf>(sum.first), before_in_wave<0x138, 0xf>(sum.n), before_in_wave<0x138, 0xf>(sum.fraction)};
   }
-  scan_steps([&](auto ctrl, auto rows) {
-    constexpr int c = decltype(ctrl)::value, r = decltype(rows)::value;
-    sum = join(Run{before_in_wave<c, r>(sum.first), before_in_wave<c, r>(sum.n), before_in_wave<c, r>(sum.fraction)}, sum);
-  });
-  if (lane == 63) s.runs[wave] = sum;
-  Run left{before_in_wave<0x138, 0xf>(sum.first), before_in_wave<0x138, 0xf>(sum.n), before_in_wave<0x138, 0xf>(sum.fraction)};
   if (tid == 0) s.pos = 1 << 30, s.last_pos = -1, s.at = -1, s.value = w.all.mass;
   __syncthreads();
-  Run before{0, 0, 0};
-  for (int v = 0; v < wave; ++v) before = join(before, s.runs[v]);
-  left = lane ? join(before, left) : before;
-  Place low[P], high[P];
+  Place high[P];
+  if (busy) {
+    Run before{0, 0, 0};
+    for (int v = 0; v < wave; ++v) before = join(before, s.runs[v]);
+    left = lane ? join(before, left) : before;
 #pragma unroll
-  for (int j = 0; j < P; ++j) {
-    const Run r = join(left, run[j]);
-    const Place b{s.before[bin[j]], s.mass[bin[j]]};
-    low[j] = Place{b.n + r.n - 1, b.mass + mass_of(r.n - 1, r.fraction - fraction[j], scale[j])};
-    high[j] = Place{b.n + r.n, b.mass + mass_of(r.n, r.fraction, scale[j])};
+    for (int j = 0; j < P; ++j) {
+      const Run r = join(left, run[j]);
+      const Place b{s.before[bin[j]], s.mass[bin[j]]};
+        high[j] = Place{b.n + r.n, b.mass + mass_of(r.n, r.fraction, scale[j])};
+    }
   }
   auto listed = [&](int j) { return tid * P + j < n && bin[j] <= w.last; };
   const bool k = c.top_k && c.top_k < w.all.n;
@@ -630,15 +631,15 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int r, doub
                   u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.0};
 }
 
-// A slice's largest logit (and, for the first rank alone, its lowest index), and the smallest of the maxima of groups of
-// `lanes` threads: some hundred tokens of a row lie above the smallest of 128 such, 128 at least if the groups have a token
-// each.
+// A slice's largest logit (and, for the first rank alone, its lowest index), and the smallest of the maxima of groups of 32
+// threads, or of `waves` waves: some 130 tokens of a row lie above the smallest of 32 such, 32 at least if the groups have a
+// token each.
 struct Part {
   float max, low;
   int index, pad;
 };
 template <typename T>
-__device__ Part largest(Shared& s, const Logits<T>& x, int lanes, bool greedy) {
+__device__ Part largest(Shared& s, const Logits<T>& x, int waves, bool greedy) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   float most = -INFINITY;
   int index = 0;
@@ -653,12 +654,19 @@ __device__ Part largest(Shared& s, const Logits<T>& x, int lanes, bool greedy) {
   for (int off = 1; off < 64; off <<= 1) {
     high = fmaxf(high, __shfl_xor(high, off));
     const float other = __shfl_xor(low, off);
-    low = off < lanes ? fmaxf(low, other) : fminf(low, other);
+    low = off < 32 || waves ? fmaxf(low, other) : fminf(low, other);
   }
   if (lane == 0) s.wave_max[wave] = high, s.wave_low[wave] = low;
   if (tid == 0) s.at = 0x7fffffff;
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) high = fmaxf(high, s.wave_max[w]), low = fminf(low, s.wave_low[w]);
+  float group = -INFINITY;
+  for (int w = 0; w < kWaves; ++w) {
+    high = fmaxf(high, s.wave_max[w]);
+    if (waves < 2) low = fminf(low, s.wave_low[w]);
+    else if (w % waves == 0) group = s.wave_max[w];
+    else group = fmaxf(group, s.wave_max[w]);
+    if (waves >= 2 && w % waves == waves - 1) low = w == waves - 1 ? group : fminf(low, group);
+  }
   if (greedy) {
     if (most == high && high > -INFINITY) atomicMin(&s.at, index);
     __syncthreads();
@@ -673,9 +681,14 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int r, int index, fl
   if (a.probs) a.probs[r] = prob;
 }
 
-// The slice's tokens into s.hist, those not below `low` into s.list (s.listed counts them all).
+// The slice's tokens into s.hist; those not below `low` into the wave's part of s.list, as far as there is room.  Returns how
+// many those are.
+constexpr int kWaveList = kList / kWaves;
 template <typename T>
-__device__ void count(Shared& s, const Logits<T>& x, int first, const Row& row, float low) {
+__device__ int count(Shared& s, const Logits<T>& x, int first, const Row& row, float low) {
+  const int lane = threadIdx.x & 63;
+  u64* list = s.list + (threadIdx.x >> 6) * kWaveList;
+  int n = 0;
   x.template fours<4>([&](const float* v, int i) {
     double d[4];
     u64 bits[4];
@@ -684,17 +697,24 @@ __device__ void count(Shared& s, const Logits<T>& x, int first, const Row& row, 
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (d[e] < kBins) atomicAdd(&s.hist[(int)d[e]], bits[e]);
-    if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= low)
+    if (__ballot(v[0] >= low || v[1] >= low || v[2] >= low || v[3] >= low))
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v[e] >= low && d[e] < kBins) put(s, v[e], first + i + e);
+      for (int e = 0; e < 4; ++e) {
+        const bool in = v[e] >= low && d[e] < kBins;
+        const u64 all = __ballot(in);
+        const int at = n + __popcll(all & ((1ull << lane) - 1));
+        if (in && at < kWaveList) list[at] = entry(v[e], first + i + e);
+        n += __popcll(all);
+      }
   });
+  return n;
 }
 
-// The wanted bins fall with the logits, so their runs are runs of logits, [from, past).  Lane 2 q (and 2 q + 1) of each wave
+// The wanted bins fall with the logits, so their `n` runs are runs of logits, from .. to.  Lane 2 q (and 2 q + 1) of each wave
 // finds by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
 struct Edges {
-  float from[4], past[4];
+  float from[4], to[4];
+  int n, pad;
 };
 __device__ Edges edges_of(const Row& row, const Wanted& w) {
   const int lane = threadIdx.x & 63;
@@ -715,48 +735,64 @@ __device__ Edges edges_of(const Row& row, const Wanted& w) {
     else below = mid;
   }
   Edges e;
+  e.n = e.pad = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) e.from[q] = e.to[q] = INFINITY;  // holds no finite logit
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    e.from[q] = of_key(__shfl(at, 2 * q));
-    e.past[q] = w.hi[q] < w.lo[q] ? e.from[q] : of_key(__shfl(at, 2 * q + 1));
+    const uint32_t from = __shfl(at, 2 * q), to = __shfl(at, 2 * q + 1) - 1;
+    if (w.hi[q] < w.lo[q] || to < from) continue;  // min-p's bin may have room for no logit
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i == e.n) e.from[i] = of_key(from), e.to[i] = of_key(to);
+    ++e.n;
   }
   return e;
 }
 
-// The slice's tokens within the edges into s.list.
-template <typename T>
-__device__ void gather(Shared& s, const Logits<T>& x, int first, const Edges& edges) {
+// The slice's tokens within the N runs into s.list.
+template <int N, typename T>
+__device__ __forceinline__ void gather_runs(Shared& s, const Logits<T>& x, int first, const Edges& edges) {
   x.template fours<4>([&](const float* v, int i) {
-    bool in[4] = {};
+    auto in = [&](int e) {  // the median of a logit and a run's ends is the logit
+      bool any = false;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (edges.from[q] < edges.past[q])
+      for (int q = 0; q < N; ++q) any |= __builtin_amdgcn_fmed3f(v[e], edges.from[q], edges.to[q]) == v[e];
+      return any;
+    };
+    if (__ballot(in(0) || in(1) || in(2) || in(3)))
 #pragma unroll
-        for (int e = 0; e < 4; ++e) in[e] |= v[e] >= edges.from[q] && v[e] < edges.past[q];
-    if (in[0] | in[1] | in[2] | in[3])
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (in[e]) put(s, v[e], first + i + e);
+      for (int e = 0; e < 4; ++e) put(s, in(e), v[e], first + i + e);
   });
 }
+template <typename T>
+__device__ void gather(Shared& s, const Logits<T>& x, int first, const Edges& edges) {
+  if (edges.n == 1) gather_runs<1>(s, x, first, edges);
+  else if (edges.n == 2) gather_runs<2>(s, x, first, edges);
+  else gather_runs<4>(s, x, first, edges);
+}
 
-// Whether the list of the tokens not below `low` holds every wanted bin (it does the bins before the one that `low` lies
-// in).  If so, leaves those bins' tokens in it.
-__device__ bool list_serves(Shared& s, const Row& row, const Wanted& w, float low) {
+// Whether a list of the tokens not below `low` holds every wanted bin: it does the bins before the one that `low` lies in.
+__device__ __forceinline__ bool list_serves(const Row& row, const Wanted& w, float low) {
   const double b = row.bins(low);
-  const uint32_t n = s.listed;
-  if (n > kList || w.last >= (b < kBins ? (int)b : kBins)) return false;
-  u64 v[kListPerThread];
+  return w.last < (b < kBins ? (int)b : kBins);
+}
+
+// Of the waves' parts of the list, `n` in this wave's, the tokens of the wanted bins, as one list.
+__device__ void keep_wanted(Shared& s, int n, const Row& row, const Wanted& w) {
+  const int lane = threadIdx.x & 63;
+  u64 v[kWaveList / 64];
 #pragma unroll
-  for (int j = 0; j < kListPerThread; ++j) v[j] = threadIdx.x + j * kThreads < n ? s.list[threadIdx.x + j * kThreads] : ~0ull;
-  __syncthreads();
+  for (int j = 0; j < kWaveList / 64; ++j)
+    v[j] = lane + 64 * j < n ? s.list[(threadIdx.x >> 6) * kWaveList + lane + 64 * j] : ~0ull;
   if (threadIdx.x == 0) s.listed = 0;
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kListPerThread; ++j)
-    if (v[j] != ~0ull && w.has((int)row.bins_of_key(~(uint32_t)(v[j] >> 32)))) s.list[atomicAdd(&s.listed, 1u)] = v[j];
+  for (int j = 0; j < kWaveList / 64; ++j) {
+    const float x = of_key(~(uint32_t)(v[j] >> 32));
+    put(s, v[j] != ~0ull && w.has((int)row.bins(x)), x, (int)(uint32_t)v[j]);
+  }
   __syncthreads();
-  return true;
 }
 
 template <typename T>
@@ -769,23 +805,22 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   const Settings c = settings_of(a, r, &inv_t, &greedy);
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
-  if (tid == 0) s.listed = 0;
-  Part p = largest(s, x, 8, greedy);
+  Part p = largest(s, x, 0, greedy);
   if (p.max == -INFINITY) return answer(a, r, -1, 0.f);
   if (greedy) return answer(a, r, p.index, 1.f);
   x.infinite = p.max == INFINITY;
   const float low = x.plain(p.low);
   const Row row{x.plain(p.max), inv_t * kBinsPerUnit};
-  count(s, x, 0, row, low);
-  __syncthreads();
+  const int listed = count(s, x, 0, row, low);
+  const bool whole = __syncthreads_and(listed <= kWaveList);
   const Wanted w = decide(s, c);
-  if (!list_serves(s, row, w, low)) {
-    if (s.wanted > kList) {
-      const Pick pick = narrow(s, x, row, c);
-      return answer(a, r, pick.index, pick.prob);
-    }
+  if (whole && list_serves(row, w, low)) {
+    keep_wanted(s, listed, row, w);
+  } else if (s.wanted > kList) {
+    const Pick pick = narrow(s, x, row, c);
+    return answer(a, r, pick.index, pick.prob);
+  } else {
     const Edges edges = edges_of(row, w);
-    __syncthreads();
     if (tid == 0) s.listed = 0;
     __syncthreads();
     gather(s, x, 0, edges);
@@ -828,15 +863,20 @@ __device__ __forceinline__ Logits<T> slice_of(const SampleArgs& a, int r, int* f
   return Logits<T>{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride + *first, min(per, a.vocab - *first), false};
 }
 
-// Adds the workgroup's list to the row's; true for the workgroup that counts itself last, with the row's list in s.list.
-__device__ bool join_lists(Shared& s, Split* row, uint32_t* arrived) {
+// Adds a wave's list of n tokens to the row's; more than `room` do not fit, and are counted all the same.
+__device__ void send_list(Split* row, const u64* list, int n, int room) {
+  const int lane = threadIdx.x & 63;
+  if (n == 0) return;
+  uint32_t at = 0;
+  if (lane == 0) at = __hip_atomic_fetch_add(&row->listed, (uint32_t)(n > room ? kList + 1 : n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  at = __builtin_amdgcn_readfirstlane(at);
+  for (int i = lane; i < min(n, room); i += 64)
+    if (at + i < kList) store_shared(&row->list[at + i], list[i]);
+}
+
+// Whether the workgroup is the last of the row's to arrive; then the row's list is in s.list, unless it is too long.
+__device__ bool last_of_row(Shared& s, Split* row, uint32_t* arrived) {
   const int tid = threadIdx.x;
-  const uint32_t n = s.listed;
-  if (tid == 0) s.wanted = n ? __hip_atomic_fetch_add(&row->listed, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
-  __syncthreads();
-  const uint32_t base = s.wanted;
-  for (uint32_t i = tid; i < min(n, (uint32_t)kList); i += kThreads)
-    if (base + i < kList) store_shared(&row->list[base + i], s.list[i]);
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores and additions have completed
   __syncthreads();
   if (tid == 0)
@@ -862,7 +902,7 @@ __global__ __launch_bounds__(kThreads) void sample_max(SampleArgs a, Split* spli
   (void)settings_of(a, r, &inv_t, &greedy);
   int first;
   const Logits<T> x = slice_of<T>(a, r, &first);
-  Part p = largest(s, x, 8 * gridDim.x, greedy);
+  Part p = largest(s, x, gridDim.x / 2, greedy);
   p.index += first;
   if (tid == 0) row->part[blockIdx.x] = p;
 }
@@ -899,22 +939,22 @@ __global__ __launch_bounds__(kThreads) void sample_count(SampleArgs a, Split* sp
   const Row scale{x.plain(p.max), inv_t * kBinsPerUnit};
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = 0;
-  if (tid == 0) s.listed = 0;
   __syncthreads();
-  count(s, x, first, scale, low);
+  const int listed = count(s, x, first, scale, low);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) {
     const u64 h = s.hist[tid + i * kThreads];
     if (h) (void)__hip_atomic_fetch_add(&row->hist[tid + i * kThreads], h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  if (!join_lists(s, row, &row->counted)) return;
+  send_list(row, s.list + (tid >> 6) * kWaveList, listed, kWaveList);
+  if (!last_of_row(s, row, &row->counted)) return;
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = load_shared(&row->hist[tid + i * kThreads]);
   __syncthreads();
   const Wanted w = decide(s, c);
   x = Logits<T>{static_cast<const T*>(a.logits) + (size_t)r * a.row_stride, a.vocab, x.infinite};
-  if (list_serves(s, scale, w, low)) {
+  if (s.listed <= kList && list_serves(scale, w, low)) {
     const int n = s.listed;
     sort_list(s, n);
     const Pick pick = finish(s, n, scale, c, w);
@@ -945,7 +985,9 @@ __global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* spl
   __syncthreads();
   gather(s, x, first, row->edges);
   __syncthreads();
-  if (!join_lists(s, row, &row->gathered)) return;
+  const int each = (s.listed + kWaves - 1) / kWaves, from = (tid >> 6) * each;
+  send_list(row, s.list + from, max(0, min(each, (int)s.listed - from)), kList);
+  if (!last_of_row(s, row, &row->gathered)) return;
 #pragma unroll
   for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = row->hist[tid + i * kThreads];
   __syncthreads();
