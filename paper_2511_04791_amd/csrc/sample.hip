@@ -518,8 +518,9 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
   return w;
 }
 
-// The token from the sorted list of n tokens, which holds all of the wanted bins.
-__device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, const Wanted& w) {
+// The token from the sorted list of n tokens, which holds all of the wanted bins; before_bin(b): the place before a bin.
+template <typename F>
+__device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, const Wanted& w, F before_bin) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   constexpr int P = kListPerThread;
   double d[P], scale[P];  // d: in bins
@@ -560,8 +561,8 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const Run r = join(left, run[j]);
-      const Place b{s.before[bin[j]], s.mass[bin[j]]};
-        high[j] = Place{b.n + r.n, b.mass + mass_of(r.n, r.fraction, scale[j])};
+      const Place b = before_bin(bin[j]);
+      high[j] = Place{b.n + r.n, b.mass + mass_of(r.n, r.fraction, scale[j])};
     }
   }
   auto listed = [&](int j) { return tid * P + j < n && bin[j] <= w.last; };
@@ -606,7 +607,7 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
     if (own >= 0) atomicMax(&s.at, own);
     __syncthreads();
     if (s.at >= 0 && s.at / P == tid) s.place = high[s.at % P];
-    if (s.at < 0 && tid == 0) s.place = Place{s.before[w.lo[2]], s.mass[w.lo[2]]};
+    if (s.at < 0 && tid == 0) s.place = before_bin(w.lo[2]);
     __syncthreads();
     if (s.place.n < kept.n) kept = s.place;
     __syncthreads();
@@ -632,7 +633,7 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int r, doub
 }
 
 // A slice's largest logit (and, for the first rank alone, its lowest index), and the smallest of the maxima of groups of 32
-// threads, or of `waves` waves: some 130 tokens of a row lie above the smallest of 32 such, 32 at least if the groups have a
+// threads, or of `waves` waves (a power of two): some 130 tokens of a row lie above the smallest of 32 such, 32 at least if the groups have a
 // token each.
 struct Part {
   float max, low;
@@ -659,13 +660,13 @@ __device__ Part largest(Shared& s, const Logits<T>& x, int waves, bool greedy) {
   if (lane == 0) s.wave_max[wave] = high, s.wave_low[wave] = low;
   if (tid == 0) s.at = 0x7fffffff;
   __syncthreads();
-  float group = -INFINITY;
-  for (int w = 0; w < kWaves; ++w) {
-    high = fmaxf(high, s.wave_max[w]);
-    if (waves < 2) low = fminf(low, s.wave_low[w]);
-    else if (w % waves == 0) group = s.wave_max[w];
-    else group = fmaxf(group, s.wave_max[w]);
-    if (waves >= 2 && w % waves == waves - 1) low = w == waves - 1 ? group : fminf(low, group);
+  // Each lane a wave's: their maximum, and the least of the groups' (the lanes past the sixteenth repeat them).
+  high = s.wave_max[lane & (kWaves - 1)], low = s.wave_low[lane & (kWaves - 1)];
+#pragma unroll
+  for (int off = 1; off < kWaves; off <<= 1) {
+    high = fmaxf(high, __shfl_xor(high, off));
+    const float other = __shfl_xor(low, off);
+    low = off < waves ? fmaxf(low, other) : fminf(low, other);
   }
   if (greedy) {
     if (most == high && high > -INFINITY) atomicMin(&s.at, index);
@@ -828,7 +829,7 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   }
   const int n = s.listed;
   sort_list(s, n);
-  const Pick pick = finish(s, n, row, c, w);
+  const Pick pick = finish(s, n, row, c, w, [&](int b) { return Place{s.before[b], s.mass[b]}; });
   answer(a, r, pick.index, pick.prob);
 }
 
@@ -842,8 +843,11 @@ constexpr int kMaxSlices = 16;
 struct Split {
   u64 hist[kBins];
   u64 list[kList];
+  double mass[kBins];      // the place before each bin, left for sample_list
+  uint32_t before[kBins];
   Part part[kMaxSlices];
   Edges edges;
+  Wanted wanted;
   uint32_t listed, counted, gathered, open;  // tokens listed, slices done with each step, whether sample_list is needed
 };
 
@@ -957,7 +961,7 @@ __global__ __launch_bounds__(kThreads) void sample_count(SampleArgs a, Split* sp
   if (s.listed <= kList && list_serves(scale, w, low)) {
     const int n = s.listed;
     sort_list(s, n);
-    const Pick pick = finish(s, n, scale, c, w);
+    const Pick pick = finish(s, n, scale, c, w, [&](int b) { return Place{s.before[b], s.mass[b]}; });
     return answer(a, r, pick.index, pick.prob);
   }
   if (s.wanted > kList) {
@@ -965,7 +969,8 @@ __global__ __launch_bounds__(kThreads) void sample_count(SampleArgs a, Split* sp
     return answer(a, r, pick.index, pick.prob);
   }
   const Edges edges = edges_of(scale, w);
-  if (tid == 0) row->edges = edges, row->listed = 0, row->open = 1;
+  for (int i = tid; i < kBins; i += kThreads) row->mass[i] = s.mass[i], row->before[i] = s.before[i];
+  if (tid == 0) row->edges = edges, row->wanted = w, row->listed = 0, row->open = 1;
 }
 
 template <typename T>
@@ -988,13 +993,10 @@ __global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* spl
   const int each = (s.listed + kWaves - 1) / kWaves, from = (tid >> 6) * each;
   send_list(row, s.list + from, max(0, min(each, (int)s.listed - from)), kList);
   if (!last_of_row(s, row, &row->gathered)) return;
-#pragma unroll
-  for (int i = 0; i < kBinsPerThread; ++i) s.hist[tid + i * kThreads] = row->hist[tid + i * kThreads];
-  __syncthreads();
-  const Wanted w = decide(s, c);
   const int n = s.listed;
   sort_list(s, n);
-  const Pick pick = finish(s, n, scale, c, w);
+  const Wanted w = row->wanted;
+  const Pick pick = finish(s, n, scale, c, w, [&](int b) { return Place{row->before[b], row->mass[b]}; });
   answer(a, r, pick.index, pick.prob);
 }
 
