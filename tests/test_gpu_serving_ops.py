@@ -268,17 +268,16 @@ def test_sample_the_largest_vocabulary(ctx):
     _check_sample(ctx, x, torch.tensor([0.3, 0.99999]), top_k=torch.tensor([100000, 0], dtype=torch.int32))
 
 
-@pytest.mark.parametrize("rows", [1, 2, 3, 17])
-@pytest.mark.parametrize("vocab", [16383, 16384, 70001, 131072, 1 << 18])
+@pytest.mark.parametrize("rows", [1, 3, 40])
+@pytest.mark.parametrize("vocab", [65535, 65536, 70001])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sample_few_rows(ctx, rows, vocab, dtype):
-    """Two to sixteen workgroups a row."""
+    """One workgroup a row, and several."""
     x = (_randn(7150 + vocab, rows, vocab, dtype=torch.float32) * torch.linspace(0.4, 4, rows)[:, None])
     x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
-    for seed in range(3):
-        u = torch.rand(rows, generator=torch.Generator().manual_seed(7151 + seed))
-        _check_sample(ctx, x, u, **_mixed_params(7155 + seed, rows))
-        _check_sample(ctx, x, u, top_p=torch.full((rows,), 0.9))
+    u = torch.rand(rows, generator=torch.Generator().manual_seed(7151))
+    _check_sample(ctx, x, u, **_mixed_params(7155, rows))
+    _check_sample(ctx, x, u, top_p=torch.full((rows,), 0.9))
     _check_sample(ctx, x, u)
     _check_sample(ctx, x, u, temperature=torch.zeros(rows))
 
@@ -305,7 +304,7 @@ ROWS = {
 
 @pytest.mark.parametrize("name", list(ROWS))
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("vocab", [400, 9001, 40001])
+@pytest.mark.parametrize("vocab", [400, 9001, 70001])
 def test_sample_rows(ctx, name, dtype, vocab):
     """One row under many settings; the largest vocabulary goes to several workgroups a row."""
     rows = 40
@@ -415,7 +414,7 @@ def test_graphs_of_the_operators(ctx):
         meta, ids, x, base, la, lb, scale = _lora_case(seed + 10, 256, 136, 16, 3, reqs)
         s = dict(meta=meta, ids=ids, qkv=qkv.cuda(), kc=kc.cuda(), vc=vc.cuda(), x=x.cuda(), base=base.cuda(),
                  table=torch.as_tensor(b.page_table, device="cuda"), lora=duet.Lora(la.cuda(), lb.cuda(), scale.cuda()),
-                 logits=_randn(seed + 20, len(reqs), 20000, scale=2.0, dtype=torch.float32).cuda(),
+                 logits=_randn(seed + 20, len(reqs), 70000, scale=2.0, dtype=torch.float32).cuda(),
                  u=torch.rand(len(reqs), device="cuda"), top_p=torch.full((len(reqs),), 0.9, device="cuda"))
         return s
 

@@ -62,9 +62,9 @@ def test_workspace_sizes(native):
 
 def test_sample_workspace(native):
     n = ctypes.c_size_t()
-    for rows, vocab in ((0, 100), (1, 1000), (1000, 1 << 18)):
+    for rows, vocab in ((0, 100), (1, 1000), (1, 65535), (65, 1 << 18)):
         assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == 0
-    for rows, vocab in ((1, 128256), (64, 128256)):
+    for rows, vocab in ((1, 65536), (64, 128256)):
         assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == 0 and n.value >= rows * 4096 * 8
     for rows, vocab, code in ((-1, 10, -1), (1, 0, -1), (1, (1 << 18) + 1, -2), ((1 << 20) + 1, 10, -1)):
         assert native.duet_sample_workspace_bytes(rows, vocab, B(n)) == code
