@@ -222,7 +222,7 @@ struct RopeSplitArgs {
   void* q;                 // [T, h_q, d]
   void* k_cache;           // [P, h_kv, 16, d]
   void* v_cache;           // [P, h_kv, d, 16]
-  const int4* meta;        // [R] (kind, q_start, q_len, cached_len)
+  const int4* meta;        // [R] (kind, q_start, q_len, cached_len), uploaded; not used for up to kRopeTable requests
   const int32_t* page_table;
   const int32_t* positions;  // [axes, T], or null: the tokens' places in the cache
   long long num_phys_pages;
@@ -232,7 +232,8 @@ struct RopeSplitArgs {
   double turns[64];        // turns per position of each pair (frequency / 2 pi)
   uint8_t pair_axis[64];
 };
-hipError_t launch_rope_split(const RopeSplitArgs& a, hipStream_t s);
+constexpr int kRopeTable = 256;
+hipError_t launch_rope_split(const RopeSplitArgs& a, const int4* requests, hipStream_t s);  // requests: the batch, on the host
 
 // out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).  The rows are listed by adapter and taken in
 // tiles: rows[first] .. rows[first + count - 1] have this adapter (-1: none).
@@ -259,6 +260,9 @@ struct LoraArgs {
 constexpr int kLoraMaxParts = 8;
 int lora_parts(int tokens, int d_in);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
+// The same for few rows: a.tiles, a.rows, a.h and a.done are not used.
+constexpr int kLoraPassedTiles = 64, kLoraPassedRows = 256;
+hipError_t launch_lora_passed(const LoraArgs& a, const LoraTile* tiles, const int32_t* rows, int n_rows, hipStream_t s);
 
 // One token from each row of logits (sample.hip); the parameters' arrays may be null.
 struct SampleArgs {

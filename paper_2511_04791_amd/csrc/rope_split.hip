@@ -15,7 +15,13 @@
 //
 // Request r (rows q_start .. q_start + q_len - 1) has the page groups from q_start / 16 + 2 r on: more than it needs,
 // whatever its first slot, and groups past its last page end at once.
+//
+// Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
+// much on the host: one decode row 15.8 us a call with it, 10.3 without).  The upload clears the error word; without it one more
+// workgroup reads the page ids of the whole batch and stores the word.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kernels.h"
 #include "wave_ops.h"
@@ -36,7 +42,31 @@ __device__ __forceinline__ float2 cos_sin_of(double rev) {
   return make_float2(q == 1 || q == 2 ? -x : x, q >= 2 ? -y : y);
 }
 
-__device__ __forceinline__ int first_group(const RopeSplitArgs& s, int r) { return (s.meta[r].y >> 4) + 2 * r; }
+// The requests as the kernel reads them: first row, rows, cached tokens.
+struct Request {
+  int row, rows, cached;
+};
+struct Uploaded {
+  const int4* meta;
+  __device__ __forceinline__ int row(int r) const { return meta[r].y; }
+  __device__ __forceinline__ Request operator[](int r) const { return Request{meta[r].y, meta[r].z, meta[r].w}; }
+};
+struct Passed {
+  int2 at[kRopeTable + 1];  // (first row, cached tokens); the rows' end after the last
+  __device__ __forceinline__ int row(int r) const { return at[r].x; }
+  __device__ __forceinline__ Request operator[](int r) const { return Request{at[r].x, at[r + 1].x - at[r].x, at[r].y}; }
+};
+__device__ __forceinline__ int first_group(int row, int r) { return (row >> 4) + 2 * r; }
+
+// The group's page of its request: where its rows start and how many they are (0 or less: past the last page).
+struct Group {
+  int row, pos, rows, page;
+};
+__device__ __forceinline__ Group group_of(const Request& q, int r, int group) {
+  const int page = (q.cached >> 4) + group - first_group(q.row, r);
+  const int pos = max(q.cached, 16 * page);
+  return Group{q.row + pos - q.cached, pos, min(q.cached + q.rows, 16 * page + 16) - pos, page};
+}
 
 template <typename T>
 struct Chunk {
@@ -46,20 +76,48 @@ struct Chunk {
 
 constexpr int kMaxPairs = 64;
 
-template <typename T>
-__global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s) {
+// Whether any page id of the batch lies outside the pool, into the error word; one workgroup.
+__device__ void check_pages(const RopeSplitArgs& s, const Passed& requests, int2* at) {
+  for (int i = threadIdx.x; i <= s.num_reqs; i += 256) at[i] = requests.at[i];
+  __syncthreads();
+  bool bad = false;
+  const int groups = s.tokens / 16 + 2 * s.num_reqs;
+  for (int g = threadIdx.x; g < groups; g += 256) {
+    int r = 0, end = s.num_reqs;
+    while (end - r > 1) {
+      const int mid = (r + end) / 2;
+      if (first_group(at[mid].x, mid) <= g) r = mid;
+      else end = mid;
+    }
+    const Group group = group_of(Request{at[r].x, at[r + 1].x - at[r].x, at[r].y}, r, g);
+    if (group.rows > 0) bad |= !page_ok(s.page_table[(size_t)r * s.max_pages + group.page], s.num_phys_pages);
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *s.err = bad;
+}
+
+template <typename T, typename Table>
+__global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s, Table requests) {
   constexpr int N = Chunk<T>::N;
+  constexpr bool kPassed = std::is_same<Table, Passed>::value;
   __shared__ float2 turn[16][kMaxPairs];
-  const int group = blockIdx.x, d = s.head_dim, pairs = s.rot_dim / 2, tid = threadIdx.x;
-  const int r = uniform(find_request(s.num_reqs, [&](int x) { return first_group(s, x) <= group; }));
-  const int4 m = s.meta[r];
-  const int page = (m.w >> 4) + group - first_group(s, r);
-  const int pos = max(m.w, 16 * page), n = min(m.w + m.z, 16 * page + 16) - pos;
+  const int d = s.head_dim, pairs = s.rot_dim / 2, tid = threadIdx.x;
+  int group = blockIdx.x;
+  if constexpr (kPassed) {
+    static_assert(sizeof(requests.at) <= sizeof(turn), "the check keeps the requests where the sines go");
+    if (group == 0) {
+      if (blockIdx.y == 0) check_pages(s, requests, reinterpret_cast<int2*>(turn));
+      return;
+    }
+    --group;
+  }
+  const int r = uniform(find_request(s.num_reqs, [&](int x) { return first_group(requests.row(x), x) <= group; }));
+  const Group at = group_of(requests[r], r, group);
+  const int n = at.rows, pos = at.pos, row = at.row, slot = pos & 15;
   if (n <= 0) return;
-  const int row = m.y + pos - m.w, slot = pos & 15;
-  const int id = s.page_table[(size_t)r * s.max_pages + (pos >> 4)];
+  const int id = s.page_table[(size_t)r * s.max_pages + at.page];
   const bool ok = page_ok(id, s.num_phys_pages);
-  if (!ok && blockIdx.y == 0 && tid == 0) atomicOr(s.err, 1);
+  if (!kPassed && !ok && blockIdx.y == 0 && tid == 0) atomicOr(s.err, 1);
   for (int i = tid; i < n * pairs; i += 256) {
     const int t = i / pairs, pair = i - t * pairs;
     const int p = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
@@ -163,15 +221,26 @@ __global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s) {
 
 }  // namespace
 
-hipError_t launch_rope_split(const RopeSplitArgs& a, hipStream_t s) {
-  if (a.tokens <= 0) return hipSuccess;
-  const int n = a.dtype == DUET_BF16 ? 8 : 4, d = a.head_dim;
+namespace {
+template <typename T>
+hipError_t launch(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
+  const int n = 16 / sizeof(T), d = a.head_dim;
   const int units = (a.h_q + a.h_kv) * d / (2 * n) + a.h_kv * d / n;
-  const int groups = a.tokens / 16 + 2 * a.num_reqs;
-  const dim3 grid(groups, (units + 255) / 256);
-  if (a.dtype == DUET_BF16) hipLaunchKernelGGL(rope_split<__bf16>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(rope_split<float>, grid, dim3(256), 0, s, a);
+  const int groups = a.tokens / 16 + 2 * a.num_reqs, columns = (units + 255) / 256;
+  if (a.num_reqs <= kRopeTable) {
+    Passed p;
+    for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);
+    p.at[a.num_reqs] = make_int2(a.tokens, 0);
+    hipLaunchKernelGGL((rope_split<T, Passed>), dim3(groups + 1, columns), dim3(256), 0, s, a, p);
+  } else {
+    hipLaunchKernelGGL((rope_split<T, Uploaded>), dim3(groups, columns), dim3(256), 0, s, a, Uploaded{a.meta});
+  }
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_rope_split(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
+  return a.dtype == DUET_BF16 ? launch<__bf16>(a, requests, s) : launch<float>(a, requests, s);
 }
 
 }  // namespace duet

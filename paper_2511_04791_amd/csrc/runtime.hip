@@ -1912,10 +1912,10 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   char* ws = static_cast<char*>(workspace);
   static_assert(sizeof(duet_seq_meta) == sizeof(int4), "the kernels read the requests as they are");
   const UploadPart table{batch->reqs, batch->num_reqs * sizeof(int4), kAlign};
-  if ((rc = upload_parts(ctx, kAlign, &table, 1, ws, st))) return rc;
+  if (batch->num_reqs > kRopeTable && (rc = upload_parts(ctx, kAlign, &table, 1, ws, st))) return rc;
   a.meta = reinterpret_cast<const int4*>(ws + kAlign);
   a.err = reinterpret_cast<int32_t*>(ws);
-  HIP_TRY(launch_rope_split(a, st));
+  HIP_TRY(launch_rope_split(a, reinterpret_cast<const int4*>(batch->reqs), st));
   return DUET_OK;
 }
 
@@ -1978,16 +1978,20 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   if (tiles.empty()) return DUET_OK;
+  a.n_tiles = (int)tiles.size();
+  a.parts = lora_parts(a.tokens, lora->d_in);
+  a.part = reinterpret_cast<float*>(ws + L.part);
+  if (tiles.size() <= kLoraPassedTiles && rows.size() <= kLoraPassedRows) {
+    HIP_TRY(launch_lora_passed(a, tiles.data(), rows.data(), (int)rows.size(), st));
+    return DUET_OK;
+  }
   const UploadPart parts[2] = {{tiles.data(), tiles.size() * sizeof(LoraTile), L.tiles},
                                {rows.data(), rows.size() * sizeof(int32_t), L.rows}};
   if ((rc = upload_parts(ctx, L.tiles, parts, 2, ws, st))) return rc;
   a.done = reinterpret_cast<int32_t*>(ws + kAlign);
   a.tiles = reinterpret_cast<const LoraTile*>(ws + L.tiles);
   a.rows = reinterpret_cast<const int32_t*>(ws + L.rows);
-  a.n_tiles = (int)tiles.size();
-  a.parts = lora_parts(a.tokens, lora->d_in);
   a.h = reinterpret_cast<__bf16*>(ws + L.h);
-  a.part = reinterpret_cast<float*>(ws + L.part);
   HIP_TRY(launch_lora(a, st));
   return DUET_OK;
 }
