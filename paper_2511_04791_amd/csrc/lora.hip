@@ -66,70 +66,101 @@ __device__ __forceinline__ void split(float h, __bf16* hi, __bf16* lo) {
 }
 
 // Partial sums of h of a tile's 16 RT rows over the columns of one part: four waves take its units of kUnit columns in
-// turn, each all of the rows and ranks (NT 16-rank tiles), and are summed through LDS in a fixed order.  A unit's
-// loads are issued ahead of the products of the one before it.
+// turn, each all of the rows and ranks (NT 16-rank tiles), and are summed through LDS in a fixed order.
+//
+// An MFMA operand wants a row a lane, and a load of that shape costs the address unit 82 cycles (neighbouring lanes lie in
+// different rows); a load whose neighbours lie in one row costs 19.  So a unit's rows are loaded 64 or 128 bytes by
+// neighbours, put into the wave's part of LDS and read from there in the operands' shape, a row's 16-byte chunks in an order
+// by which the 16 lanes of a read meet all banks.  us of 6400 rows of 14336 columns, rank 64: 67 without this.
+template <int NT>
+struct Down {
+  static constexpr int kHalves = NT == 8 ? 1 : 2, kUnit = 32 * kHalves;
+  static constexpr int kChunks = 4 * kHalves, kLoadRows = 64 / kChunks;  // of a unit's row, of one load
+  static constexpr int kLoads = (kLoraTileRows + 16 * NT) / kLoadRows;   // of a unit, at most
+  static constexpr int kLds = 4 * kLoads > 2 * kRowTiles * NT ? 4 * kLoads : 2 * kRowTiles * NT;  // KB
+};
 template <int NT, int RT, typename Lists>
-__device__ __forceinline__ void down_part(const LoraArgs& s, const Lists& lists, const LoraTile& tile, f32x4 (*sums)[kRowTiles * NT][64]) {
-  constexpr int kHalves = NT == 8 ? 1 : 2, kUnit = 32 * kHalves;
+__device__ __forceinline__ void down_part(const LoraArgs& s, const Lists& lists, const LoraTile& tile, uint4* lds) {
+  using D = Down<NT>;
+  constexpr int kHalves = D::kHalves, kUnit = D::kUnit, C = D::kChunks, R = D::kLoadRows;
+  constexpr int kXLoads = 16 * RT / R, kWLoads = 16 * NT / R;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int units = (s.d_in + kUnit - 1) / kUnit;
   const int u0 = (int)((long long)units * blockIdx.y / s.parts) + wave;
   const int u1 = (int)((long long)units * (blockIdx.y + 1) / s.parts);
-  const __bf16 *x[RT], *w[NT];
+  uint4* const own = lds + wave * D::kLoads * 64;
+  // The chunk c of row i of a tile lies at place c ^ order(i) of the row.
+  auto order = [](int i) { return C == 8 ? (i >> 1) & 7 : (i >> 2) & 3; };
+  const __bf16 *x[kXLoads], *w[kWLoads];
+  int chunk[2];  // loads of even and odd index
 #pragma unroll
-  for (int t = 0; t < RT; ++t) x[t] = s.x + lists.row(tile.first + min(16 * t + m, tile.count - 1)) * s.ldx + 8 * g;
+  for (int l = 0; l < 2; ++l) chunk[l] = lane % C ^ order(l * R + lane / C);
 #pragma unroll
-  for (int n = 0; n < NT; ++n) w[n] = s.a + ((size_t)tile.adapter * s.rank + min(16 * n + m, s.rank - 1)) * s.d_in + 8 * g;
+  for (int l = 0; l < kXLoads; ++l)
+    x[l] = s.x + lists.row(tile.first + min(l * R + lane / C, tile.count - 1)) * s.ldx + 8 * chunk[l & 1];
+#pragma unroll
+  for (int l = 0; l < kWLoads; ++l)
+    w[l] = s.a + ((size_t)tile.adapter * s.rank + min(l * R + lane / C, s.rank - 1)) * s.d_in + 8 * chunk[l & 1];
   struct Unit {
-    bf16x8 w[kHalves][NT], x[kHalves][RT];
+    uint4 x[kXLoads], w[kWLoads];
   };
   f32x4 acc[RT][NT] = {};
   auto load = [&](int u, Unit& f) {
 #pragma unroll
-    for (int half = 0; half < kHalves; ++half) {
+    for (int l = 0; l < kXLoads; ++l) f.x[l] = *reinterpret_cast<const uint4*>(x[l] + u * kUnit);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) f.w[half][n] = load8(w[n] + u * kUnit + 32 * half);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) f.x[half][t] = load8(x[t] + u * kUnit + 32 * half);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    for (int l = 0; l < kWLoads; ++l) f.w[l] = *reinterpret_cast<const uint4*>(w[l] + u * kUnit);
   };
-  auto multiply = [&](const Unit& f) {
+  auto place = [&](const Unit& f) {
 #pragma unroll
-    for (int half = 0; half < kHalves; ++half)
+    for (int l = 0; l < kXLoads; ++l) own[l * 64 + lane] = f.x[l];
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
+    for (int l = 0; l < kWLoads; ++l) own[(kXLoads + l) * 64 + lane] = f.w[l];
+  };
+  auto multiply = [&] {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[half][n], f.x[half][t], acc[t][n], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int half = 0; half < kHalves; ++half) {
+      const uint4* at = own + m * C + ((4 * half + g) ^ order(m));
+      bf16x8 wv[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wv[n] = __builtin_bit_cast(bf16x8, at[(RT + n) * 16 * C]);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const bf16x8 xv = __builtin_bit_cast(bf16x8, at[t * 16 * C]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[n], xv, acc[t][n], 0, 0, 0);
+      }
+    }
   };
   const int whole = min(u1, s.d_in / kUnit);  // the last unit may be cut off, at a multiple of 8 columns
+  Unit f;
   if (u0 < whole) {
-    const int n = (whole - u0 + 3) / 4;
-    Unit even, odd;
-    load(u0, even);
-    for (int i = 0; i + 2 <= n; i += 2) {
-      load(u0 + 4 * (i + 1), odd);
-      multiply(even);
-      load(u0 + 4 * min(i + 2, n - 1), even);
-      multiply(odd);
+    load(u0, f);
+    for (int u = u0; u < whole; u += 4) {
+      place(f);
+      load(u + 4 < whole ? u + 4 : u0, f);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply();
     }
-    if (n & 1) multiply(even);
   }
   if (whole < u1 && (whole - u0) % 4 == 0) {
-    Unit cut;
 #pragma unroll
-    for (int half = 0; half < kHalves; ++half) {
-      const int k = whole * kUnit + 32 * half;
-      const bool in = k + 8 * g < s.d_in;
+    for (int l = 0; l < kXLoads; ++l) f.x[l] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) cut.w[half][n] = in ? load8(w[n] + k) : zero8();
+    for (int l = 0; l < kWLoads; ++l) f.w[l] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) cut.x[half][t] = in ? load8(x[t] + k) : zero8();
-    }
-    multiply(cut);
+    for (int odd = 0; odd < 2; ++odd)
+      if (whole * kUnit + 8 * chunk[odd] < s.d_in) {
+#pragma unroll
+        for (int l = odd; l < kXLoads; l += 2) f.x[l] = *reinterpret_cast<const uint4*>(x[l] + whole * kUnit);
+#pragma unroll
+        for (int l = odd; l < kWLoads; l += 2) f.w[l] = *reinterpret_cast<const uint4*>(w[l] + whole * kUnit);
+      }
+    place(f);
+    multiply();
   }
+  __syncthreads();
+  f32x4(*sums)[RT * NT][64] = reinterpret_cast<f32x4(*)[RT * NT][64]>(lds);
   auto put = [&](int b) {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -166,13 +197,13 @@ __device__ __forceinline__ void down_part(const LoraArgs& s, const Lists& lists,
 // two bf16 (its value and what that leaves out, 16 bits together).
 template <int NT, typename Lists>
 __global__ __launch_bounds__(256) void lora_down(LoraArgs s, Lists lists) {
-  __shared__ f32x4 sums[2][kRowTiles * NT][64];
+  __shared__ uint4 lds[Down<NT>::kLds * 64];
   __shared__ int last;
   const LoraTile tile = lists.tile(blockIdx.x);
   if (tile.adapter < 0) return;
-  if (tile.count > 32) down_part<NT, 4>(s, lists, tile, sums);
-  else if (tile.count > 16) down_part<NT, 2>(s, lists, tile, sums);
-  else down_part<NT, 1>(s, lists, tile, sums);
+  if (tile.count > 32) down_part<NT, 4>(s, lists, tile, lds);
+  else if (tile.count > 16) down_part<NT, 2>(s, lists, tile, lds);
+  else down_part<NT, 1>(s, lists, tile, lds);
   if (Lists::kPassed) return;
   if (threadIdx.x < 64) {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's stores have completed
@@ -204,70 +235,72 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s, Lists lists) {
   }
 }
 
-// out of 16 RT rows of a tile from row0 on, 64 columns at a time, every col_step-th from col0 on.  Ranks up to 16 (STEPS 0)
-// take h's two halves and B twice along one MFMA, [h_hi | h_lo] times [B | B]; others STEPS times 32 ranks, B for both
-// halves.  The 16 columns of an MFMA are taken in fours out of 32, so that two MFMAs give a lane eight neighbours.  The next
-// columns' base is read ahead of the products.
-template <int STEPS, int RT, typename Lists>
-__device__ __forceinline__ void up_rows(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int row0, int col0, int col_step) {
-  constexpr int kSteps = STEPS ? STEPS : 1, kParts = STEPS ? 2 : 1;
+// h of row i of the list for STEPS times 32 ranks, as its value and what that leaves out, in an MFMA operand's shape; ranks up to
+// 16 (STEPS 0) have both along one MFMA.
+template <int STEPS>
+struct H {
+  static constexpr int kSteps = STEPS ? STEPS : 1, kParts = STEPS ? 2 : 1;
+  bf16x8 v[kSteps][kParts];
+};
+template <int STEPS, typename Lists>
+__device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile, int i) {
+  constexpr int kParts = H<STEPS>::kParts;
+  const int g = (threadIdx.x & 63) >> 4, chunks = s.rank / 8;
+  const float scale = Lists::kPassed && s.scale ? s.scale[tile.adapter] : 1.f;
+  H<STEPS> h;
+#pragma unroll
+  for (int st = 0; st < H<STEPS>::kSteps; ++st) {
+    const int q = 4 * st + g;
+    if (q >= (STEPS ? chunks : 2 * chunks)) {
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) h.v[st][p] = zero8();
+    } else if (!Lists::kPassed) {
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) h.v[st][p] = load8(s.h + ((size_t)i * 2 + p) * s.rank + 8 * q);
+    } else {  // the parts of h, in their order
+      const bool low = !STEPS && q >= chunks;
+      const float* part = s.part + (size_t)i * s.rank + 8 * (low ? q - chunks : q);
+      const size_t step = (size_t)s.tokens * s.rank;
+      f32x4 sum[2] = {};
+      for (int p = 0; p < s.parts; ++p)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sum[k] += *reinterpret_cast<const f32x4*>(part + p * step + 4 * k);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        __bf16 hi, lo;
+        split(sum[e / 4][e % 4] * scale, &hi, &lo);
+        h.v[st][0][e] = low ? lo : hi;
+        if (kParts == 2) h.v[st][kParts - 1][e] = lo;
+      }
+    }
+  }
+  return h;
+}
+
+// out of a tile of up to 16 rows, 64 columns a wave at a time, every col_step-th from col0 on.  The 16 columns of an MFMA are
+// taken in fours out of 32, so that two MFMAs give a lane eight neighbours.  The next columns' base is read ahead of the
+// products.
+template <int STEPS, typename Lists>
+__device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int col0, int col_step) {
+  constexpr int kSteps = H<STEPS>::kSteps, kParts = H<STEPS>::kParts;
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0;
   if (col0 >= s.d_out) return;
-  const __bf16* base[RT];
-  int index[RT];
-  __bf16* out[RT];
+  const int i = tile.first + min(m, tile.count - 1);
+  const long long row = lists.row(i);
+  const __bf16* base = s.base + row * s.ldb;
+  __bf16* out = s.out + row * s.ldo;
+  auto read = [&](int c0, bf16x8* v) {  // past the last column: the last eight again
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int i = tile.first + min(row0 + 16 * t + m, tile.count - 1);
-    const long long row = lists.row(i);
-    index[t] = i;
-    base[t] = s.base + row * s.ldb;
-    out[t] = s.out + row * s.ldo;
-  }
-  auto read = [&](int c0, bf16x8 (*v)[2]) {  // past the last column: the last eight again
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) v[t][p] = load8(base[t] + min(c0 + 32 * p + 8 * g, s.d_out - 8));
+    for (int p = 0; p < 2; ++p) v[p] = load8(base + min(c0 + 32 * p + 8 * g, s.d_out - 8));
   };
-  bf16x8 now[RT][2], next[RT][2];
+  bf16x8 now[2], next[2];
   read(col0, now);
-  bf16x8 hv[kSteps][kParts][RT];
-  if (some) {
-    const float scale = Lists::kPassed && s.scale ? s.scale[tile.adapter] : 1.f;
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const int q = 4 * st + g;
-        if (q >= (STEPS ? chunks : 2 * chunks)) {
-#pragma unroll
-          for (int p = 0; p < kParts; ++p) hv[st][p][t] = zero8();
-        } else if (!Lists::kPassed) {
-#pragma unroll
-          for (int p = 0; p < kParts; ++p) hv[st][p][t] = load8(s.h + ((size_t)index[t] * 2 + p) * s.rank + 8 * q);
-        } else {  // the parts of h, in their order
-          const bool low = !STEPS && q >= chunks;
-          const float* part = s.part + (size_t)index[t] * s.rank + 8 * (low ? q - chunks : q);
-          const size_t step = (size_t)s.tokens * s.rank;
-          f32x4 h[2] = {};
-          for (int p = 0; p < s.parts; ++p)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) h[i] += *reinterpret_cast<const f32x4*>(part + p * step + 4 * i);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            __bf16 hi, lo;
-            split(h[e / 4][e % 4] * scale, &hi, &lo);
-            hv[st][0][t][e] = low ? lo : hi;
-            if (kParts == 2) hv[st][kParts - 1][t][e] = lo;
-          }
-        }
-      }
-  }
+  H<STEPS> h;
+  if (some) h = h_of<STEPS, Lists>(s, tile, i);
   const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
   for (int c0 = col0; c0 < s.d_out; c0 += col_step) {
-    f32x4 acc[RT][4] = {};
+    f32x4 acc[4] = {};
     if (some) {
       bf16x8 wv[kSteps][4];
 #pragma unroll
@@ -285,38 +318,109 @@ __device__ __forceinline__ void up_rows(const LoraArgs& s, const Lists& lists, c
 #pragma unroll
         for (int p = 0; p < kParts; ++p)
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-              acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], hv[st][p][t], acc[t][n], 0, 0, 0);
+          for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], h.v[st][p], acc[n], 0, 0, 0);
     } else {
       read(c0 + col_step, next);
     }
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+    for (int p = 0; p < 2; ++p) {
+      bf16x8 o = now[p];
+      if (some)
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        bf16x8 o = now[t][p];
-        if (some)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            o[e] = static_cast<__bf16>(static_cast<float>(o[e]) + acc[t][2 * p + e / 4][e % 4]);
-        const int c = c0 + 32 * p + 8 * g;
-        if (row0 + 16 * t + m < tile.count && c < s.d_out) *reinterpret_cast<bf16x8*>(out[t] + c) = o;
-        now[t][p] = next[t][p];
-      }
+        for (int e = 0; e < 8; ++e) o[e] = static_cast<__bf16>(static_cast<float>(o[e]) + acc[2 * p + e / 4][e % 4]);
+      const int c = c0 + 32 * p + 8 * g;
+      if (m < tile.count && c < s.d_out) *reinterpret_cast<bf16x8*>(out + c) = o;
+      now[p] = next[p];
+    }
   }
 }
 
-// A wave takes 32 rows of a tile: two waves the rows of one that holds more, so two 64-column blocks at a time for the
-// workgroup, else four.
+// out of a larger tile, a wave 16 rows and the workgroup 128 columns at a time, every `ways`-th from the way-th on.  h is the first
+// operand here: with the columns of MFMA n taken as 8 j + n, lane j has eight neighbours of a row after eight MFMAs, and the 16
+// lanes of a row 256 bytes.  B's columns, which the waves share, go through LDS, eight of them and 16 bytes apart, so that
+// those 16 lanes meet all banks.  The next columns' base and B are read ahead of the products.
+template <int STEPS>
+constexpr int kMostRank = STEPS ? 32 * STEPS : 16;
+template <int STEPS, typename Lists>
+__device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int way, int ways, uint4* lds) {
+  constexpr int kSteps = H<STEPS>::kSteps, kParts = H<STEPS>::kParts, kUnits = 128 * kMostRank<STEPS> / 8 / 256;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, j = lane & 15, g = lane >> 4, chunks = s.rank / 8;
+  const bool some = tile.adapter >= 0, rows = 16 * wave < tile.count;
+  const __bf16* base[4];
+  __bf16* out[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long row = lists.row(tile.first + min(16 * wave + 4 * g + i, tile.count - 1));
+    base[i] = s.base + row * s.ldb;
+    out[i] = s.out + row * s.ldo;
+  }
+  const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
+  // This thread's 16-byte units of 128 columns of B, which lie one after the other, and their places.
+  int place[kUnits];
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) place[k] = k * 256 + tid + (k * 256 + tid) / (8 * chunks);
+  bf16x8 b[kUnits], now[4], next[4];
+  auto read = [&](int c0, bf16x8* v) {  // past the last column: the last eight again
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = load8(base[i] + min(c0 + 8 * j, s.d_out - 8));
+  };
+  auto read_b = [&](int c0) {
+    const int left = (min(c0 + 128, s.d_out) - c0) * chunks;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) b[k] = k * 256 + tid < left ? load8(w + (size_t)c0 * s.rank + 8 * (k * 256 + tid)) : zero8();
+  };
+  const int step = 128 * ways;
+  int c0 = 128 * way;
+  if (c0 >= s.d_out) return;
+  if (rows) read(c0, now);
+  if (some) read_b(c0);
+  H<STEPS> h;
+  if (some) h = h_of<STEPS, Lists>(s, tile, tile.first + min(16 * wave + j, tile.count - 1));
+  for (; c0 < s.d_out; c0 += step) {
+    f32x4 acc[8] = {};
+    if (some) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k)
+        if (k * 256 + tid < 128 * chunks) lds[place[k]] = __builtin_bit_cast(uint4, b[k]);
+      __syncthreads();
+      if (c0 + step < s.d_out) read_b(c0 + step);
+    }
+    if (!rows) continue;
+    read(c0 + step, next);
+    if (some) {
+      const uint4* own = lds + j * (8 * chunks + 1);
+      const bool partial = STEPS ? chunks < 4 * STEPS : chunks < 2;  // zeros past the rank's end
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        const int q = STEPS || g < chunks ? 4 * st + g : g - chunks;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          bf16x8 wv = __builtin_bit_cast(bf16x8, own[n * chunks + min(q, chunks - 1)]);
+          if (partial && q >= chunks) wv = zero8();
+#pragma unroll
+          for (int p = 0; p < kParts; ++p) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.v[st][p], wv, acc[n], 0, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x8 o = now[i];
+      if (some)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) o[n] = static_cast<__bf16>(static_cast<float>(o[n]) + acc[n][i]);
+      if (16 * wave + 4 * g + i < tile.count && c0 + 8 * j < s.d_out) *reinterpret_cast<bf16x8*>(out[i] + c0 + 8 * j) = o;
+      now[i] = next[i];
+    }
+  }
+}
+
 template <int STEPS, typename Lists>
 __global__ __launch_bounds__(256) void lora_up(LoraArgs s, Lists lists) {
+  __shared__ uint4 lds[128 * kMostRank<STEPS> / 8 + 16];
   const LoraTile tile = lists.tile(blockIdx.x);
-  const int wave = threadIdx.x >> 6;
-  if (tile.count > 32) up_rows<STEPS, 2>(s, lists, tile, 32 * (wave & 1), (blockIdx.y * 2 + (wave >> 1)) * 64, gridDim.y * 128);
-  else if (tile.count > 16) up_rows<STEPS, 2>(s, lists, tile, 0, (blockIdx.y * 4 + wave) * 64, gridDim.y * 256);
-  else up_rows<STEPS, 1>(s, lists, tile, 0, (blockIdx.y * 4 + wave) * 64, gridDim.y * 256);
+  if (tile.count > 16) up_many<STEPS>(s, lists, tile, blockIdx.y, gridDim.y, lds);
+  else up_few<STEPS>(s, lists, tile, (blockIdx.y * 4 + (threadIdx.x >> 6)) * 64, gridDim.y * 256);
 }
 
 }  // namespace
