@@ -254,9 +254,8 @@ struct LoraArgs {
   int32_t n_tiles, parts, tokens, rank, d_in, d_out;
 };
 // Parts of the input's columns, each a workgroup a tile: as many as give some 160 workgroups, with four 64-column units at
-// least.  More cost their merge.  us of the down product with 1 / 2 / 4 / 8 / 16 parts: 17 tiles of a few rows, 4096
-// columns, rank 16, 11.3 / 8.0 / 6.7 / 6.6 / 7.6; 41 tiles (2112 rows) 25 / 16 / 12 / 16 / 14; 100 tiles (6400 rows) of 14336
-// columns, rank 64, 115 / 68 / 73 / 80 / 83.
+// least.  More cost their merge.  us of the down product with 1 / 2 / 4 / 8 parts: 17 tiles of a few rows, 4096 columns, rank
+// 16, 8.0 / 5.4 / 4.5 / 4.0; 41 tiles (2112 rows) 20 / 14 / 11 / 12; 100 tiles (6400 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 69.
 constexpr int kLoraMaxParts = 8;
 int lora_parts(int tokens, int d_in);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);

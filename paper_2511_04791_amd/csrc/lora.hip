@@ -440,8 +440,10 @@ hipError_t launch(const LoraArgs& a, const Lists& lists, hipStream_t s) {
   else hipLaunchKernelGGL((lora_down<8, Lists>), down, block, 0, s, a, lists);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // Workgroups a tile: some 512 in all (us with 256 / 512 / 1024 / 3000: 41 tiles of 28672 columns, rank 16, 59 / 53 / 57 / 53; 100
+  // of 4096, rank 64, 37 / 25 / 30 / 30).
   const int blocks = (a.d_out + 127) / 128;
-  const dim3 up(a.n_tiles, std::max(1, std::min(blocks, 2048 / a.n_tiles)));
+  const dim3 up(a.n_tiles, std::max(1, std::min(blocks, 512 / a.n_tiles)));
   if (a.rank <= 16) hipLaunchKernelGGL((lora_up<0, Lists>), up, block, 0, s, a, lists);
   else if (a.rank <= 32) hipLaunchKernelGGL((lora_up<1, Lists>), up, block, 0, s, a, lists);
   else if (a.rank <= 64) hipLaunchKernelGGL((lora_up<2, Lists>), up, block, 0, s, a, lists);
