@@ -235,11 +235,11 @@ struct RopeSplitArgs {
 constexpr int kRopeTable = 256;
 hipError_t launch_rope_split(const RopeSplitArgs& a, const int4* requests, hipStream_t s);  // requests: the batch, on the host
 
-// out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).  The rows are listed by adapter and taken in
-// tiles: rows[first] .. rows[first + count - 1] have this adapter (-1: none).
+// out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).  The rows are taken by adapter in tiles; row i of a
+// tile is rows + i, or entry ~rows + i of a list where the tile's rows do not follow each other.
 constexpr int kLoraTileRows = 64;
 struct LoraTile {
-  int32_t adapter, first, count, pad;
+  int32_t adapter, first, count, rows;  // -1: none; the tiles' rows before this one; its rows
 };
 struct LoraArgs {
   const __bf16 *x, *base, *a, *b;  // x [T, d_in], base [T, d_out], a [N, rank, d_in], b [N, d_out, rank]
@@ -249,15 +249,17 @@ struct LoraArgs {
   __bf16* h;                       // [T, 2 rank]: h and the rounding it leaves out
   int32_t* done;                   // [tiles] parts finished; zero before the call
   const LoraTile* tiles;
-  const int32_t* rows;             // [T]
+  const int32_t* rows;             // the list
   long long ldx, ldb, ldo;
   int32_t n_tiles, parts, tokens, rank, d_in, d_out;
 };
-// Parts of the input's columns, each a workgroup a tile: as many as give some 160 workgroups, with four 64-column units at
-// least.  More cost their merge.  us of the down product with 1 / 2 / 4 / 8 parts: 17 tiles of a few rows, 4096 columns, rank
-// 16, 8.0 / 5.4 / 4.5 / 4.0; 41 tiles (2112 rows) 20 / 14 / 11 / 12; 100 tiles (6400 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 69.
+// Parts of the input's columns, each a workgroup a tile.  A CU pulls at most some 30 GB/s of its own from memory, so the 256 CUs'
+// largest share counts, and a little for each part's merge; at least four 64-column units a part.  us of the down product with
+// 1 / 2 / 4 / 5 / 6 / 8 parts: 17 tiles of a few rows, 4096 columns, rank 16, 8.0 / 5.4 / 4.5 / . / 4.5 / 4.0; 41 tiles (2112 rows)
+// 20 / 14 / 11 / . / 11 / 12; 100 tiles (6400 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 53 / 73 / 69.
 constexpr int kLoraMaxParts = 8;
-int lora_parts(int tokens, int d_in);
+int lora_most_parts(int tokens, int d_in);
+int lora_parts(int tiles, int most);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
 // The same for few rows: a.tiles, a.rows, a.h and a.done are not used.
 constexpr int kLoraPassedTiles = 64, kLoraPassedRows = 256;

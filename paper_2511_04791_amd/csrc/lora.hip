@@ -49,14 +49,14 @@ struct Uploaded {
   const LoraTile* tiles;
   const int32_t* rows;
   __device__ __forceinline__ LoraTile tile(int i) const { return tiles[i]; }
-  __device__ __forceinline__ int row(int i) const { return rows[i]; }
+  __device__ __forceinline__ int row(const LoraTile& t, int i) const { return t.rows >= 0 ? t.rows + i : rows[~t.rows + i]; }
 };
 struct Passed {
   static constexpr bool kPassed = true;
   LoraTile tiles[kLoraPassedTiles];
   int32_t rows[kLoraPassedRows];
   __device__ __forceinline__ LoraTile tile(int i) const { return tiles[i]; }
-  __device__ __forceinline__ int row(int i) const { return rows[i]; }
+  __device__ __forceinline__ int row(const LoraTile& t, int i) const { return t.rows >= 0 ? t.rows + i : rows[~t.rows + i]; }
 };
 
 // h and what its rounding to bf16 leaves out (16 bits together).
@@ -97,7 +97,7 @@ __device__ __forceinline__ void down_part(const LoraArgs& s, const Lists& lists,
   for (int l = 0; l < 2; ++l) chunk[l] = lane % C ^ order(l * R + lane / C);
 #pragma unroll
   for (int l = 0; l < kXLoads; ++l)
-    x[l] = s.x + lists.row(tile.first + min(l * R + lane / C, tile.count - 1)) * s.ldx + 8 * chunk[l & 1];
+    x[l] = s.x + lists.row(tile, min(l * R + lane / C, tile.count - 1)) * s.ldx + 8 * chunk[l & 1];
 #pragma unroll
   for (int l = 0; l < kWLoads; ++l)
     w[l] = s.a + ((size_t)tile.adapter * s.rank + min(l * R + lane / C, s.rank - 1)) * s.d_in + 8 * chunk[l & 1];
@@ -286,8 +286,8 @@ __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, co
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0;
   if (col0 >= s.d_out) return;
-  const int i = tile.first + min(m, tile.count - 1);
-  const long long row = lists.row(i);
+  const int i = min(m, tile.count - 1);
+  const long long row = lists.row(tile, i);
   const __bf16* base = s.base + row * s.ldb;
   __bf16* out = s.out + row * s.ldo;
   auto read = [&](int c0, bf16x8* v) {  // past the last column: the last eight again
@@ -297,7 +297,7 @@ __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, co
   bf16x8 now[2], next[2];
   read(col0, now);
   H<STEPS> h;
-  if (some) h = h_of<STEPS, Lists>(s, tile, i);
+  if (some) h = h_of<STEPS, Lists>(s, tile, tile.first + i);
   const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
   for (int c0 = col0; c0 < s.d_out; c0 += col_step) {
     f32x4 acc[4] = {};
@@ -350,7 +350,7 @@ __device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, c
   __bf16* out[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const long long row = lists.row(tile.first + min(16 * wave + 4 * g + i, tile.count - 1));
+    const long long row = lists.row(tile, min(16 * wave + 4 * g + i, tile.count - 1));
     base[i] = s.base + row * s.ldb;
     out[i] = s.out + row * s.ldo;
   }
@@ -425,9 +425,19 @@ __global__ __launch_bounds__(256) void lora_up(LoraArgs s, Lists lists) {
 
 }  // namespace
 
-int lora_parts(int tokens, int d_in) {
+int lora_most_parts(int tokens, int d_in) {
   const int tiles = std::max(1, (tokens + kLoraTileRows - 1) / kLoraTileRows), units = (d_in + 63) / 64;
-  return std::max(1, std::min({kLoraMaxParts, (160 + tiles - 1) / tiles, (units + 3) / 4}));
+  return std::max(1, std::min({kLoraMaxParts, 2048 / tiles, (units + 3) / 4}));
+}
+
+int lora_parts(int tiles, int most) {
+  int best = 1;
+  double least = 1e9;
+  for (int p = 1; p <= most; ++p) {
+    const double cost = (double)((tiles * (long long)p + 255) / 256) / p + 0.01 * p;
+    if (cost < least) least = cost, best = p;
+  }
+  return best;
 }
 
 namespace {

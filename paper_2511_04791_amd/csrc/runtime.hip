@@ -1340,11 +1340,11 @@ LoraLayout lora_layout(const duet_lora* l, const duet_batch* b, int32_t tokens) 
   L.rows = L.tiles + align_up(most * sizeof(LoraTile));
   L.h = L.rows + align_up((size_t)tokens * sizeof(int32_t));
   L.part = L.h + align_up((size_t)tokens * 2 * l->rank * sizeof(__bf16));
-  L.total = L.part + align_up((size_t)lora_parts(tokens, l->d_in) * tokens * l->rank * sizeof(float));
+  L.total = L.part + align_up((size_t)lora_most_parts(tokens, l->d_in) * tokens * l->rank * sizeof(float));
   return L;
 }
 
-// The batch's rows by adapter (in order within each), and their tiles; rows without one only if `with_none`.
+// The tiles of the batch's rows by adapter (in order within each), and their list; rows without an adapter only if `with_none`.
 int lora_lists(const duet_lora* l, const duet_batch* b, const int32_t* ids, bool with_none, std::vector<LoraTile>* tiles,
                std::vector<int32_t>* rows) {
   try {
@@ -1352,15 +1352,28 @@ int lora_lists(const duet_lora* l, const duet_batch* b, const int32_t* ids, bool
     for (int r = 0; r < b->num_reqs; ++r)
       if (ids[r] >= 0 || with_none) order.push_back(r);
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return ids[x] < ids[y]; });
+    int first = 0;
     for (size_t i = 0; i < order.size();) {
       const int id = ids[order[i]];
-      int first = (int)rows->size();
+      // The adapter's rows, tile by tile; a tile's go into the list only if they do not follow each other.
+      int32_t tile[kLoraTileRows];
+      int n = 0;
+      auto close = [&] {
+        if (n == 0) return;
+        const bool run = tile[n - 1] - tile[0] == n - 1;  // rows rise within an adapter
+        tiles->push_back(LoraTile{id, first, n, run ? tile[0] : ~(int32_t)rows->size()});
+        if (!run) rows->insert(rows->end(), tile, tile + n);
+        first += n;
+        n = 0;
+      };
       for (; i < order.size() && ids[order[i]] == id; ++i) {
         const duet_seq_meta& m = b->reqs[order[i]];
-        for (int t = 0; t < m.q_len; ++t) rows->push_back(m.q_start + t);
+        for (int t = 0; t < m.q_len; ++t) {
+          tile[n++] = m.q_start + t;
+          if (n == kLoraTileRows) close();
+        }
       }
-      for (; first < (int)rows->size(); first += kLoraTileRows)
-        tiles->push_back(LoraTile{id, first, std::min(kLoraTileRows, (int)rows->size() - first), 0});
+      close();
     }
     return DUET_OK;
   } catch (const std::bad_alloc&) {
@@ -1979,7 +1992,7 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   char* ws = static_cast<char*>(workspace);
   if (tiles.empty()) return DUET_OK;
   a.n_tiles = (int)tiles.size();
-  a.parts = lora_parts(a.tokens, lora->d_in);
+  a.parts = lora_parts(a.n_tiles, lora_most_parts(a.tokens, lora->d_in));
   a.part = reinterpret_cast<float*>(ws + L.part);
   if (tiles.size() <= kLoraPassedTiles && rows.size() <= kLoraPassedRows) {
     HIP_TRY(launch_lora_passed(a, tiles.data(), rows.data(), (int)rows.size(), st));
