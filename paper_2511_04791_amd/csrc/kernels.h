@@ -245,24 +245,22 @@ struct LoraArgs {
   const __bf16 *x, *base, *a, *b;  // x [T, d_in], base [T, d_out], a [N, rank, d_in], b [N, d_out, rank]
   __bf16* out;                     // [T, d_out]
   const float* scale;              // [N], or null: 1
-  float* part;                     // [parts, T, rank], rows in the order of the list
-  __bf16* h;                       // [T, 2 rank]: h and the rounding it leaves out
-  int32_t* done;                   // [tiles] parts finished; zero before the call
+  float* part;                     // [parts, T, rank], rows in the tiles' order
   const LoraTile* tiles;
   const int32_t* rows;             // the list
   long long ldx, ldb, ldo;
   int32_t n_tiles, parts, tokens, rank, d_in, d_out;
 };
 // Parts of the input's columns, each a workgroup a tile.  A CU pulls at most some 30 GB/s of its own from memory, so the 256 CUs'
-// largest share counts, and a little for each part's merge; at least four 64-column units a part.  us of the down product with
+// largest share counts, and a little for each part; at least four 64-column units a part.  us of the down product with
 // 1 / 2 / 4 / 5 / 6 / 8 parts: 17 tiles of a few rows, 4096 columns, rank 16, 8.0 / 5.4 / 4.5 / . / 4.5 / 4.0; 41 tiles (2112 rows)
 // 20 / 14 / 11 / . / 11 / 12; 100 tiles (6400 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 53 / 73 / 69.
 constexpr int kLoraMaxParts = 8;
 int lora_most_parts(int tokens, int d_in);
 int lora_parts(int tiles, int most);
 hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
-// The same for few rows: a.tiles, a.rows, a.h and a.done are not used.
-constexpr int kLoraPassedTiles = 64, kLoraPassedRows = 256;
+// The same with the lists on the host: a.tiles and a.rows are not used.
+constexpr int kLoraPassedTiles = 128, kLoraPassedRows = 256;
 hipError_t launch_lora_passed(const LoraArgs& a, const LoraTile* tiles, const int32_t* rows, int n_rows, hipStream_t s);
 
 // One token from each row of logits (sample.hip); the parameters' arrays may be null.

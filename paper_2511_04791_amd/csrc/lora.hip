@@ -1,11 +1,10 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   out[t] = base[t] + scale_a B_a (A_a x[t]),  a the adapter of token t's request.
-// Two kernels: h = scale_a A_a x into the workspace, then out = base + B_a h with one rounding to bf16.
+// Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h with one rounding to bf16.
 // Both are bound by memory: x, base and out pass once, the adapters are a few MB.
 //
-// Few rows and tiles (kLoraPassedRows, kLoraPassedTiles) travel with the launches' arguments and the second kernel adds the
-// parts of h itself; otherwise they are uploaded, with the counters by which the last part to finish does: a third launch, which
-// the host and the GPU pay for (64 rows of 16 adapters, 4096 to 6144 columns, rank 16: 20.5 us a call with it, 14.9 without).
+// The lists of up to kLoraPassedTiles tiles travel with the launches' arguments; longer ones are uploaded, a launch of its own
+// (64 rows of 16 adapters, 4096 to 6144 columns, rank 16: 20.5 us a call with it, 14.9 without).
 //
 // Rows of one adapter, wherever in the batch they stand, are taken in tiles of up to kTileRows, so its weights are
 // read once a tile and a decode batch of a few adapters costs a few tiles.  Matrix products run on 16x16x32 MFMAs
@@ -21,7 +20,6 @@ namespace duet {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRowTiles = kLoraTileRows / 16;
@@ -29,30 +27,14 @@ constexpr int kRowTiles = kLoraTileRows / 16;
 __device__ __forceinline__ bf16x8 load8(const __bf16* p) { return *reinterpret_cast<const bf16x8*>(p); }
 __device__ __forceinline__ bf16x8 zero8() { return __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0)); }
 
-// Four values that another workgroup, on whatever XCD, reads or wrote within the launch: device-scope accesses go
-// past the XCD's L2, without the write-back and invalidation of all of it that a device-scope fence costs.
-__device__ __forceinline__ void store_shared(float* p, f32x4 v) {
-  const ulonglong2 u = __builtin_bit_cast(ulonglong2, v);
-  unsigned long long* q = reinterpret_cast<unsigned long long*>(p);
-  __hip_atomic_store(q, u.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store(q + 1, u.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x4 load_shared(const float* p) {
-  const unsigned long long* q = reinterpret_cast<const unsigned long long*>(p);
-  return __builtin_bit_cast(f32x4, make_ulonglong2(__hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-                                                   __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)));
-}
-
 // The tiles and rows as the kernels read them.
 struct Uploaded {
-  static constexpr bool kPassed = false;
   const LoraTile* tiles;
   const int32_t* rows;
   __device__ __forceinline__ LoraTile tile(int i) const { return tiles[i]; }
   __device__ __forceinline__ int row(const LoraTile& t, int i) const { return t.rows >= 0 ? t.rows + i : rows[~t.rows + i]; }
 };
 struct Passed {
-  static constexpr bool kPassed = true;
   LoraTile tiles[kLoraPassedTiles];
   int32_t rows[kLoraPassedRows];
   __device__ __forceinline__ LoraTile tile(int i) const { return tiles[i]; }
@@ -186,67 +168,32 @@ __device__ __forceinline__ void down_part(const LoraArgs& s, const Lists& lists,
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank) {
-        float* to = part + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g;
-        if (Lists::kPassed) *reinterpret_cast<f32x4*>(to) = acc[t][n];
-        else store_shared(to, acc[t][n]);
-      }
+      if (16 * t + m < tile.count && 16 * n + 4 * g < s.rank)
+        *reinterpret_cast<f32x4*>(part + (size_t)(16 * t + m) * s.rank + 16 * n + 4 * g) = acc[t][n];
 }
 
-// The part of a tile that finishes last adds all of them in their order and writes h for the second kernel: scaled, as
-// two bf16 (its value and what that leaves out, 16 bits together).
 template <int NT, typename Lists>
 __global__ __launch_bounds__(256) void lora_down(LoraArgs s, Lists lists) {
   __shared__ uint4 lds[Down<NT>::kLds * 64];
-  __shared__ int last;
   const LoraTile tile = lists.tile(blockIdx.x);
   if (tile.adapter < 0) return;
   if (tile.count > 32) down_part<NT, 4>(s, lists, tile, lds);
   else if (tile.count > 16) down_part<NT, 2>(s, lists, tile, lds);
   else down_part<NT, 1>(s, lists, tile, lds);
-  if (Lists::kPassed) return;
-  if (threadIdx.x < 64) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's stores have completed
-    if (threadIdx.x == 0) last = atomicAdd(s.done + blockIdx.x, 1) == s.parts - 1;
-  }
-  __syncthreads();
-  if (!last) return;
-  const float scale = s.scale ? s.scale[tile.adapter] : 1.f;
-  const size_t step = (size_t)s.tokens * s.rank, at = (size_t)tile.first * s.rank;
-  for (int i = threadIdx.x; i < tile.count * s.rank / 4; i += 256) {
-    f32x4 v[kLoraMaxParts];
-#pragma unroll
-    for (int p = 0; p < kLoraMaxParts; ++p) v[p] = load_shared(s.part + min(p, s.parts - 1) * step + at + 4 * i);
-    f32x4 h = v[0];
-#pragma unroll
-    for (int p = 1; p < kLoraMaxParts; ++p)
-      if (p < s.parts) h += v[p];
-    h *= scale;
-    bf16x4 hi, lo;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      __bf16 a, b;
-      split(h[e], &a, &b);
-      hi[e] = a, lo[e] = b;
-    }
-    __bf16* to = s.h + (size_t)(tile.first + 4 * i / s.rank) * 2 * s.rank + 4 * i % s.rank;
-    *reinterpret_cast<bf16x4*>(to) = hi;
-    *reinterpret_cast<bf16x4*>(to + s.rank) = lo;
-  }
 }
 
-// h of row i of the list for STEPS times 32 ranks, as its value and what that leaves out, in an MFMA operand's shape; ranks up to
-// 16 (STEPS 0) have both along one MFMA.
+// h of the i-th of the tiles' rows for STEPS times 32 ranks: the sum of its parts in their order, scaled, as its value in bf16 and
+// what that leaves out (16 bits together), in an MFMA operand's shape.  Ranks up to 16 (STEPS 0) have both along one MFMA.
 template <int STEPS>
 struct H {
   static constexpr int kSteps = STEPS ? STEPS : 1, kParts = STEPS ? 2 : 1;
   bf16x8 v[kSteps][kParts];
 };
-template <int STEPS, typename Lists>
+template <int STEPS>
 __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile, int i) {
   constexpr int kParts = H<STEPS>::kParts;
   const int g = (threadIdx.x & 63) >> 4, chunks = s.rank / 8;
-  const float scale = Lists::kPassed && s.scale ? s.scale[tile.adapter] : 1.f;
+  const float scale = s.scale ? s.scale[tile.adapter] : 1.f;
   H<STEPS> h;
 #pragma unroll
   for (int st = 0; st < H<STEPS>::kSteps; ++st) {
@@ -254,10 +201,7 @@ __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile
     if (q >= (STEPS ? chunks : 2 * chunks)) {
 #pragma unroll
       for (int p = 0; p < kParts; ++p) h.v[st][p] = zero8();
-    } else if (!Lists::kPassed) {
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) h.v[st][p] = load8(s.h + ((size_t)i * 2 + p) * s.rank + 8 * q);
-    } else {  // the parts of h, in their order
+    } else {
       const bool low = !STEPS && q >= chunks;
       const float* part = s.part + (size_t)i * s.rank + 8 * (low ? q - chunks : q);
       const size_t step = (size_t)s.tokens * s.rank;
@@ -297,7 +241,7 @@ __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, co
   bf16x8 now[2], next[2];
   read(col0, now);
   H<STEPS> h;
-  if (some) h = h_of<STEPS, Lists>(s, tile, tile.first + i);
+  if (some) h = h_of<STEPS>(s, tile, tile.first + i);
   const __bf16* w = s.b + (size_t)max(tile.adapter, 0) * s.d_out * s.rank;
   for (int c0 = col0; c0 < s.d_out; c0 += col_step) {
     f32x4 acc[4] = {};
@@ -375,7 +319,7 @@ __device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, c
   if (rows) read(c0, now);
   if (some) read_b(c0);
   H<STEPS> h;
-  if (some) h = h_of<STEPS, Lists>(s, tile, tile.first + min(16 * wave + j, tile.count - 1));
+  if (some) h = h_of<STEPS>(s, tile, tile.first + min(16 * wave + j, tile.count - 1));
   for (; c0 < s.d_out; c0 += step) {
     f32x4 acc[8] = {};
     if (some) {

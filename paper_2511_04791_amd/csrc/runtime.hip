@@ -1285,15 +1285,15 @@ int batch_tokens(const duet_batch* b, int32_t* tokens) {
 // A workspace that holds an error word and a table of the requests only.
 size_t request_table_bytes(const duet_batch* b) { return kAlign + align_up((size_t)b->num_reqs * sizeof(int4)); }
 
-// Parts of a workspace whose first `zero` bytes the upload clears, in rising order.
+// Parts of a workspace whose first kAlign bytes the upload clears, in rising order.
 struct UploadPart {
   const void* data;
   size_t bytes, at;
 };
-int upload_parts(duet_ctx* ctx, size_t zero, const UploadPart* parts, int n, char* ws, hipStream_t st) {
+int upload_parts(duet_ctx* ctx, const UploadPart* parts, int n, char* ws, hipStream_t st) {
   try {
     const size_t bytes = align_up(parts[n - 1].at + parts[n - 1].bytes);
-    return stage_bytes(ctx, zero, bytes, [&](char* h) {
+    return stage_bytes(ctx, kAlign, bytes, [&](char* h) {
       for (int i = 0; i < n; ++i)
         if (parts[i].bytes) std::memcpy(h + parts[i].at, parts[i].data, parts[i].bytes);
     }, ws, st);
@@ -1327,19 +1327,17 @@ int check_lora(const duet_lora* l) {
   return DUET_OK;
 }
 
-// Workspace of duet_lora_add: a head and the tiles' counters, which the upload clears, the tiles, the rows by adapter, h
-// and its parts.  There are at most as
-// many tiles that are not full as adapters and requests (and one of rows without an adapter).
+// Workspace of duet_lora_add: a head, the tiles, their list of rows, the parts of h.  There are at most as many tiles that
+// are not full as adapters and requests (and one of rows without an adapter).
 struct LoraLayout {
-  size_t tiles, rows, h, part, total;
+  size_t tiles, rows, part, total;
 };
 LoraLayout lora_layout(const duet_lora* l, const duet_batch* b, int32_t tokens) {
   const size_t most = (size_t)tokens / kLoraTileRows + std::min(l->num_adapters + 1, b->num_reqs);
   LoraLayout L;
-  L.tiles = kAlign + align_up(most * sizeof(int32_t));
+  L.tiles = kAlign;
   L.rows = L.tiles + align_up(most * sizeof(LoraTile));
-  L.h = L.rows + align_up((size_t)tokens * sizeof(int32_t));
-  L.part = L.h + align_up((size_t)tokens * 2 * l->rank * sizeof(__bf16));
+  L.part = L.rows + align_up((size_t)tokens * sizeof(int32_t));
   L.total = L.part + align_up((size_t)lora_most_parts(tokens, l->d_in) * tokens * l->rank * sizeof(float));
   return L;
 }
@@ -1925,7 +1923,7 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   char* ws = static_cast<char*>(workspace);
   static_assert(sizeof(duet_seq_meta) == sizeof(int4), "the kernels read the requests as they are");
   const UploadPart table{batch->reqs, batch->num_reqs * sizeof(int4), kAlign};
-  if (batch->num_reqs > kRopeTable && (rc = upload_parts(ctx, kAlign, &table, 1, ws, st))) return rc;
+  if (batch->num_reqs > kRopeTable && (rc = upload_parts(ctx, &table, 1, ws, st))) return rc;
   a.meta = reinterpret_cast<const int4*>(ws + kAlign);
   a.err = reinterpret_cast<int32_t*>(ws);
   HIP_TRY(launch_rope_split(a, reinterpret_cast<const int4*>(batch->reqs), st));
@@ -2000,11 +1998,9 @@ int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t l
   }
   const UploadPart parts[2] = {{tiles.data(), tiles.size() * sizeof(LoraTile), L.tiles},
                                {rows.data(), rows.size() * sizeof(int32_t), L.rows}};
-  if ((rc = upload_parts(ctx, L.tiles, parts, 2, ws, st))) return rc;
-  a.done = reinterpret_cast<int32_t*>(ws + kAlign);
+  if ((rc = upload_parts(ctx, parts, 2, ws, st))) return rc;
   a.tiles = reinterpret_cast<const LoraTile*>(ws + L.tiles);
   a.rows = reinterpret_cast<const int32_t*>(ws + L.rows);
-  a.h = reinterpret_cast<__bf16*>(ws + L.h);
   HIP_TRY(launch_lora(a, st));
   return DUET_OK;
 }
