@@ -276,7 +276,8 @@ int duet_qkv_split(duet_ctx* ctx, const duet_shape* shape, const void* qkv, void
                    const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- token-level operators of a served model.  No passage of the paper: what a serving step needs beside
- * the operators above.  Work is enqueued on `stream`; under capture a call goes into the graph with its batch. ---- */
+ * the operators above.  Work is enqueued on `stream`; under capture a call goes into the graph with its batch.  A workspace
+ * needs no preparation and may serve any calls after each other on a stream, captured ones too, but no two at once. ---- */
 
 /* Rotary position embedding of a head's first rot_dim dimensions: pair i, (a, b), turns by t = p f_i to
  * (a cos t - b sin t, a sin t + b cos t), p the token's position on the pair's axis. */
@@ -295,7 +296,7 @@ int duet_rope_workspace_bytes(const duet_batch* batch, size_t* bytes);
  * or fp32 (qkv, q and both caches).  positions [axes, T] int32 (device), row a for axis a in seq_meta order, any
  * values; NULL: every axis takes the token's place in its request's cache, cached_len + its index.  Angles are formed
  * in 64 bits, the rotation in fp32 with one rounding.  qkv, q, the caches and the workspace lie on 16 bytes; q
- * may not be qkv.  Requests must not share the pages that they write.  At most 2^22 tokens.  Page ids outside the pool are not
+ * may not be qkv.  No page may be written through two entries of the table.  At most 2^22 tokens.  Page ids outside the pool are not
  * written and set the error word (duet_check_device_error). */
 int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope* rope, const void* qkv,
                         const int32_t* positions, void* q, void* k_cache, void* v_cache, int64_t num_phys_pages,

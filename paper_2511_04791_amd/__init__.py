@@ -622,6 +622,15 @@ class Context:
                                torch.cuda.default_stream(self._dev)):
             return torch.empty(shape, dtype=dtype, device=self._dev)
 
+    def _space(self, workspace, need: int, stream):
+        """A workspace of `need` bytes for a call on `stream`, or the caller's."""
+        import torch
+        if workspace is None:
+            return self._empty(need, torch.uint8, stream)
+        if not (workspace.is_cuda and workspace.get_device() == self.device and workspace.is_contiguous()):
+            raise ValueError(f"workspace must be a contiguous tensor on cuda:{self.device}")
+        return workspace
+
     def _check_on(self, t, name, dtype, shape):
         """A contiguous tensor of this context's device."""
         if not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == self.device and t.is_contiguous()):
@@ -659,17 +668,16 @@ class Context:
             q = self._empty((T, hq, d), dt, stream)
         else:
             self._check_on(q, "q", dt, (T, hq, d))
-        if workspace is None:
-            n = ctypes.c_size_t()
-            N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
-            workspace = self._empty(n.value, torch.uint8, stream)
+        n = ctypes.c_size_t()
+        N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+        workspace = self._space(workspace, n.value, stream)
         if T == 0:
             return q
         st = self._current(stream)
         N.check(lib.duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
                                         positions.data_ptr() if positions is not None else None, q.data_ptr(),
                                         k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(), table[1],
-                                        ctypes.byref(b.c), workspace.data_ptr(), workspace.numel(), st), "duet_qkv_rope_split")
+                                        ctypes.byref(b.c), workspace.data_ptr(), workspace.nbytes, st), "duet_qkv_rope_split")
         if check_errors:
             N.check(lib.duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
         return q
@@ -692,16 +700,15 @@ class Context:
             ld.append(t.stride(0) if T > 1 else width)
         if lora.a.get_device() != self.device:
             raise ValueError(f"the adapters must lie on cuda:{self.device}")
-        if workspace is None:
-            n = ctypes.c_size_t()
-            N.check(lib.duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
-                    "duet_lora_workspace_bytes")
-            workspace = self._empty(n.value, torch.uint8, stream)
+        n = ctypes.c_size_t()
+        N.check(lib.duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
+                "duet_lora_workspace_bytes")
+        workspace = self._space(workspace, n.value, stream)
         if T == 0:
             return out
         N.check(lib.duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld[0], base.data_ptr(), ld[1],
                                   out.data_ptr(), ld[2], ctypes.byref(b.c), ids.ctypes.data, workspace.data_ptr(),
-                                  workspace.numel(), self._current(stream)), "duet_lora_add")
+                                  workspace.nbytes, self._current(stream)), "duet_lora_add")
         return out
 
     def sample(self, logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None,
@@ -732,13 +739,12 @@ class Context:
         if rows == 0:
             return out, probs
         stride, lib = vocab if rows == 1 else logits.stride(0), N.lib()
-        if workspace is None:
-            n = ctypes.c_size_t()
-            N.check(lib.duet_sample_workspace_bytes(rows, vocab, ctypes.byref(n)), "duet_sample_workspace_bytes")
-            workspace = self._empty(n.value, torch.uint8, stream)
+        n = ctypes.c_size_t()
+        N.check(lib.duet_sample_workspace_bytes(rows, vocab, ctypes.byref(n)), "duet_sample_workspace_bytes")
+        workspace = self._space(workspace, n.value, stream)
         N.check(lib.duet_sample(self.handle, logits.data_ptr(), BF16 if logits.dtype == torch.bfloat16 else F32, rows,
                                 vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
-                                workspace.data_ptr(), workspace.numel(), self._current(stream)), "duet_sample")
+                                workspace.data_ptr(), workspace.nbytes, self._current(stream)), "duet_sample")
         return out, probs
 
     def attn_iteration(self, qs, k_caches, v_caches, page_table, seq_meta, cu_split: CuSplit = CuSplit.agg(), *,

@@ -2032,6 +2032,8 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
   if ((rc = check_device_ptr(logits, "logits")) || (rc = check_device_ptr(u, "u")) || (rc = check_device_ptr(ids, "ids")))
     return rc;
   if (dtype != DUET_BF16 && dtype != DUET_F32) return fail(DUET_EUNSUPPORTED, "dtype must be bf16 or f32");
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == DUET_BF16 ? 2 : 4))
+    return fail(DUET_EINVAL, "the logits must lie on their type's size");
   if ((rc = check_sample(rows, vocab))) return rc;
   const size_t need = sample_workspace(rows, vocab);
   if (need && !workspace) return fail(DUET_EINVAL, "workspace is NULL");

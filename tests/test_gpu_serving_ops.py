@@ -466,3 +466,48 @@ def test_calls_on_two_streams_at_once(ctx):
     torch.cuda.synchronize()
     for i in (0, 1):
         assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_one_workspace_for_all(ctx):
+    """A workspace of the caller's that holds anything, for every operator in turn and in two graphs."""
+    import paper_2511_04791_amd as duet
+    sh, rope = duet.AttnShape(8, 2, 64, "bf16"), duet.Rope.base(10000.0, 64)
+
+    def make(reqs, seed):
+        b, qkv, kc, vc = _rope_inputs(sh, reqs, seed)
+        meta, ids, x, base, la, lb, scale = _lora_case(seed + 1, 256, 136, 16, 3, reqs)
+        table, lora = torch.as_tensor(b.page_table, device="cuda"), duet.Lora(la.cuda(), lb.cuda(), scale.cuda())
+        qkv, kc, vc, x, base = (t.cuda() for t in (qkv, kc, vc, x, base))
+        logits = _randn(seed + 2, len(reqs), 70000, scale=2.0, dtype=torch.float32).cuda()
+        u = torch.rand(len(reqs), generator=torch.Generator().manual_seed(seed)).cuda()
+
+        def call(workspace=None):
+            q = ctx.qkv_rope_split(qkv, kc, vc, table, meta, sh, rope, workspace=workspace)
+            out = ctx.lora_add(x, base, lora, meta, ids, workspace=workspace)
+            return (q, out) + ctx.sample(logits, u, workspace=workspace)
+        return call
+
+    # Requests past and within those that travel with the arguments; adapters whose rows lie in one run and in none.
+    calls = [make([(0, 40, 7)] + [(1, 1, i) for i in range(300)], 8500), make([(1, 1, 9 * i) for i in range(30)], 8600)]
+    want = [c() for c in calls]
+    ws = torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")
+    for turn in range(2):
+        got = [c(ws) for c in calls]
+        assert all(torch.equal(g, w) for a, b in zip(got, want) for g, w in zip(a, b)), turn
+    graphs, outs = [], []
+    for c in calls:
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c(ws))
+        graphs.append(g)
+    for turn in range(3):
+        ws.fill_(255 - turn)
+        for o in outs:
+            for t in o:
+                t.zero_()
+        for g in graphs:
+            g.replay()
+        calls[turn % 2](ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for a, b in zip(outs, want) for g, w in zip(a, b)), turn

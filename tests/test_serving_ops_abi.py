@@ -150,7 +150,7 @@ class TestWithContext:
         big = dict(vocab=100000, stride=100000)
         for kw, code in ((dict(logits=None), -1), (dict(u=None), -1), (dict(ids=None), -1), (dict(dtype=2), -2), (dict(rows=-1), -1),
                          (dict(rows=(1 << 20) + 1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 18) + 1, stride=1 << 19), -2),
-                         (dict(stride=9), -1), (dict(big), -1), (dict(big, ws=16, nbytes=4096), -3),
+                         (dict(stride=9), -1), (dict(logits=17), -1), (dict(logits=18, dtype=1), -1), (dict(big), -1), (dict(big, ws=16, nbytes=4096), -3),
                          (dict(big, ws=24, nbytes=1 << 20), -1)):
             assert call(**kw) == code, kw
             assert native.duet_last_error()
@@ -170,7 +170,17 @@ class TestWithContext:
             with pytest.raises(ValueError):
                 ctx.qkv_rope_split(kw["qkv"], kw["kc"], kw["vc"], kw["table"], meta, sh, rope, q=kw.get("q"),
                                    positions=kw.get("positions"))
+        far = torch.zeros(1 << 20, dtype=torch.uint8)
+        with pytest.raises(ValueError):
+            ctx.qkv_rope_split(qkv, kc, vc, table, meta, sh, rope, workspace=far)
         lora = duet.Lora(z(2, 8, 16), z(2, 24, 8))
+        for ws in (far, z(1 << 20)[::2]):
+            with pytest.raises(ValueError):
+                ctx.lora_add(z(1, 16), z(1, 24), lora, meta, [0], workspace=ws)
+        with pytest.raises(duet.DuetError):
+            ctx.lora_add(z(1, 16), z(1, 24), lora, meta, [0], workspace=z(8))
+        with pytest.raises(ValueError):
+            ctx.sample(z(4, 100), z(4, dt=torch.float32), workspace=far)
         for x, base, ids, out in ((z(1, 24), z(1, 24), [0], None), (z(1, 16), z(2, 24), [0], None), (z(1, 16), z(1, 24), [0, 1], None),
                                   (z(1, 16), z(1, 24), [0], z(1, 24, dt=torch.float32)), (z(1, 16).cpu(), z(1, 24), [0], None)):
             with pytest.raises(ValueError):
