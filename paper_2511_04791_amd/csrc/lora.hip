@@ -1,7 +1,9 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   out[t] = base[t] + scale_a B_a (A_a x[t]),  a the adapter of token t's request.
 // Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h with one rounding to bf16.
-// Both are bound by memory: x, base and out pass once, the adapters are a few MB.
+// Both are bound by memory: x, base and out pass once, the adapters are a few MB.  us of the two: 64 rows, 4096 to 6144 columns,
+// rank 16, 4.2 + 5.9 (latency); 2112 rows, 4096 to 28672, rank 16, 8 + 55 (4.4 TB/s); 6400 rows, 14336 to 4096, rank 64, 47 + 28
+// (3.9 and 3.8 TB/s of x, base and out; the first has 500 workgroups for 256 CUs, which read A again for each tile).
 //
 // The lists of up to kLoraPassedTiles tiles travel with the launches' arguments; longer ones are uploaded, a launch of its own
 // (64 rows of 16 adapters, 4096 to 6144 columns, rank 16: 20.5 us a call with it, 14.9 without).
@@ -286,7 +288,8 @@ __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, co
 template <int STEPS>
 constexpr int kMostRank = STEPS ? 32 * STEPS : 16;
 template <int STEPS, typename Lists>
-__device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int way, int ways, uint4* lds) {
+__device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int way, int ways,
+                                        uint4* lds) {
   constexpr int kSteps = H<STEPS>::kSteps, kParts = H<STEPS>::kParts, kUnits = 128 * kMostRank<STEPS> / 8 / 256;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, j = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0, rows = 16 * wave < tile.count;

@@ -16,6 +16,9 @@
 // Request r (rows q_start .. q_start + q_len - 1) has the page groups from q_start / 16 + 2 r on: more than it needs,
 // whatever its first slot, and groups past its last page end at once.
 //
+// 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.3 TB/s; a large copy reaches 5.1), 256 decode rows of
+// 32 + 2 x 8 heads 9, one 4.8.
+//
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
 // much on the host: one decode row 15.8 us a call with it, 10.3 without).  The upload clears the error word; without it one more
 // workgroup reads the page ids of the whole batch and stores the word.

@@ -16,6 +16,10 @@
 //
 // A row is read twice (its maximum, the histogram), a third time where the places lie past the largest few hundred tokens,
 // which the second pass lists as it goes; by one workgroup, or in slices by several where there are few rows.
+//
+// us of the steps for 256 float32 rows of 128256 logits, a CU each, 76 a call: maximum 16 (131 MB, 8 TB/s), histogram 19,
+// its sums 5, third pass 15, sorting 2, the answer 4.  One row alone: 6, 18, 5, 9 to 15, 2, 4: the histogram is bound by its LDS
+// additions (12 us without any arithmetic) and the arithmetic in 64 bits (16 without additions), the rest by latency.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -65,6 +69,7 @@ struct Shared {
   };
   uint32_t before[kBins + 1];  // tokens before each bin
   u64 list[kList];             // (~key, index): in rank order when sorted
+  uint32_t guesses[kList + 1];
   union {
     Run runs[kWaves];
     struct {
@@ -405,15 +410,27 @@ __device__ void sort_list(Shared& s, int n) {
 
 __device__ __forceinline__ u64 entry(float v, int i) { return (u64)(~key_of(v)) << 32 | (uint32_t)i; }
 
-// Those of a wave's tokens that are `in` to the list's end.
-__device__ __forceinline__ void put(Shared& s, bool in, float v, int i) {
-  const u64 all = __ballot(in);
-  if (!all) return;
-  const int lane = threadIdx.x & 63, leader = __ffsll((long long)all) - 1;
-  uint32_t at = 0;
-  if (lane == leader) at = atomicAdd(&s.listed, (uint32_t)__popcll(all));
-  at = __builtin_amdgcn_readlane(at, leader) + __popcll(all & ((1ull << lane) - 1));
-  if (in && at < kList) s.list[at] = entry(v, i);
+// Lanes of the mask before this one.
+__device__ __forceinline__ uint32_t lanes_before(u64 mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Of a wave's N tokens a lane, token(e), those that are in[e], to the list's end.
+template <int N, typename F>
+__device__ __forceinline__ void put(Shared& s, const bool* in, F token) {
+  u64 all[N];
+  uint32_t n = 0, at = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) all[e] = __ballot(in[e]), n += __popcll(all[e]);
+  if (!n) return;
+  if ((threadIdx.x & 63) == 0) at = atomicAdd(&s.listed, n);
+  at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const uint32_t to = at + lanes_before(all[e]);
+    if (in[e] && to < kList) s.list[to] = token(e);
+    at += __popcll(all[e]);
+  }
 }
 
 // The bins that a row's places may lie in: those of top-k's end, top-p's, min-p's and the token's.
@@ -633,8 +650,8 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int r, doub
 }
 
 // A slice's largest logit (and, for the first rank alone, its lowest index), and the smallest of the maxima of groups of 32
-// threads, or of `waves` waves (a power of two): some 130 tokens of a row lie above the smallest of 32 such, 32 at least if the groups have a
-// token each.
+// threads, or of `waves` waves (a power of two): some 130 tokens of a row lie above the smallest of 32 such, 32 at least if
+// the groups have a token each.
 struct Part {
   float max, low;
   int index, pad;
@@ -687,7 +704,6 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int r, int index, fl
 constexpr int kWaveList = kList / kWaves;
 template <typename T>
 __device__ int count(Shared& s, const Logits<T>& x, int first, const Row& row, float low) {
-  const int lane = threadIdx.x & 63;
   u64* list = s.list + (threadIdx.x >> 6) * kWaveList;
   int n = 0;
   x.template fours<4>([&](const float* v, int i) {
@@ -698,12 +714,13 @@ __device__ int count(Shared& s, const Logits<T>& x, int first, const Row& row, f
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (d[e] < kBins) atomicAdd(&s.hist[(int)d[e]], bits[e]);
-    if (__ballot(v[0] >= low || v[1] >= low || v[2] >= low || v[3] >= low))
+    if (__ballot(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= low))
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool in = v[e] >= low && d[e] < kBins;
         const u64 all = __ballot(in);
-        const int at = n + __popcll(all & ((1ull << lane) - 1));
+        if (!all) continue;
+        const int at = n + lanes_before(all);
         if (in && at < kWaveList) list[at] = entry(v[e], first + i + e);
         n += __popcll(all);
       }
@@ -711,20 +728,41 @@ __device__ int count(Shared& s, const Logits<T>& x, int first, const Row& row, f
   return n;
 }
 
-// The wanted bins fall with the logits, so their `n` runs are runs of logits, from .. to.  Lane 2 q (and 2 q + 1) of each wave
-// finds by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
+// The wanted bins as `n` runs apart from each other, in rank order.  The bins fall with the logits, so a run is one of logits,
+// from .. to; its tokens take the places start .. start + tokens - 1 among all of the runs' and its bins begin at `bin`, with
+// `slope` tokens each.
 struct Edges {
-  float from[4], to[4];
-  int n, pad;
+  float from[4], to[4], slope[4];
+  int bin[4];
+  uint32_t start[5];
+  int n, pad[2];
 };
-__device__ Edges edges_of(const Row& row, const Wanted& w) {
+// Lane 2 q (and 2 q + 1) of each wave finds by bisection the smallest key of run q (past it), that is with bins below hi + 1 (lo).
+__device__ Edges edges_of(const Shared& s, const Row& row, const Wanted& w) {
   const int lane = threadIdx.x & 63;
+  int lo[4], hi[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) lo[q] = w.hi[q] < w.lo[q] ? kBins : w.lo[q], hi[q] = w.hi[q] < w.lo[q] ? kBins - 1 : w.hi[q];
+  auto order = [&](int i, int j) {
+    if (lo[j] < lo[i]) {
+      const int l = lo[i], h = hi[i];
+      lo[i] = lo[j], hi[i] = hi[j], lo[j] = l, hi[j] = h;
+    }
+  };
+  order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
+  // Runs that meet become one, in the last of them; empty ones stand behind all others.
+#pragma unroll
+  for (int q = 1; q < 4; ++q)
+    if (lo[q] < kBins && lo[q] <= hi[q - 1] + 1) {
+      lo[q] = lo[q - 1], hi[q] = max(hi[q], hi[q - 1]);
+      lo[q - 1] = kBins, hi[q - 1] = kBins - 1;
+    }
   uint32_t below = 0, at = 0xff800000u;  // the keys of masked tokens, and past every finite logit's
   int edge = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    if (lane == 2 * q) edge = w.hi[q] < w.lo[q] ? -1 : w.hi[q] + 1;
-    if (lane == 2 * q + 1) edge = w.hi[q] < w.lo[q] ? -1 : w.lo[q];
+    if (lane == 2 * q) edge = lo[q] == kBins ? -1 : hi[q] + 1;
+    if (lane == 2 * q + 1) edge = lo[q] == kBins ? -1 : lo[q];
   }
   // The key of the edge's place on the scale, if rounding left it near enough; else all of them.
   const uint32_t near = key_of((float)(row.max - edge / row.scale));
@@ -736,19 +774,102 @@ __device__ Edges edges_of(const Row& row, const Wanted& w) {
     else below = mid;
   }
   Edges e;
-  e.n = e.pad = 0;
+  e.n = e.pad[0] = e.pad[1] = 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) e.from[q] = e.to[q] = INFINITY;  // holds no finite logit
+  for (int q = 0; q < 4; ++q) e.from[q] = e.to[q] = INFINITY, e.slope[q] = 0, e.bin[q] = 0;  // holds no finite logit
+  uint32_t start = 0;
+#pragma unroll
+  for (int q = 0; q < 5; ++q) e.start[q] = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t from = __shfl(at, 2 * q), to = __shfl(at, 2 * q + 1) - 1;
-    if (w.hi[q] < w.lo[q] || to < from) continue;  // min-p's bin may have room for no logit
+    if (lo[q] == kBins || to < from) continue;  // min-p's bin may have room for no logit
+    const uint32_t tokens = s.before[hi[q] + 1] - s.before[lo[q]];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (i == e.n) e.from[i] = of_key(from), e.to[i] = of_key(to);
+      if (i == e.n) {
+        e.from[i] = of_key(from), e.to[i] = of_key(to), e.bin[i] = lo[q], e.start[i] = start;
+        e.slope[i] = (float)tokens / (hi[q] + 1 - lo[q]);
+      }
+    start += tokens;
     ++e.n;
+#pragma unroll
+    for (int i = 1; i < 5; ++i)
+      if (i >= e.n) e.start[i] = start;
   }
   return e;
+}
+
+// The list of the runs' n tokens into rising order: a token's place is guessed, as if its run's were spread evenly over its
+// bins (and, where T is bf16, those of one logit, by their index, over the gap to the next), and the few tokens with one guess
+// are put in order by comparing them all; by sort_list where more than kAlike have one.  us of 25 / 480 / 900 tokens:
+// 1.8 / 2.1 / 2.4, by sort_list 1.2 / 4.1 / 6.5.
+constexpr uint32_t kAlike = 64;
+template <typename T>
+__device__ void sort_runs(Shared& s, int n, const Row& row, const Edges& edges, int vocab) {
+  constexpr int P = kListPerThread;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  u64 v[P];
+  uint32_t guess[P], slot[P];
+#pragma unroll
+  for (int j = 0; j < P; ++j) s.guesses[tid + j * kThreads] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (tid + j * kThreads >= n) continue;
+    v[j] = s.list[tid + j * kThreads];
+    const uint32_t key = ~(uint32_t)(v[j] >> 32);
+    const double d = row.bins_of_key(key);
+    float slope = edges.slope[0];
+    int bin = edges.bin[0];
+    uint32_t start = edges.start[0], end = edges.start[1];
+#pragma unroll
+    for (int q = 1; q < 4; ++q)
+      if (q < edges.n && d >= edges.bin[q])
+        slope = edges.slope[q], bin = edges.bin[q], start = edges.start[q], end = edges.start[q + 1];
+    float x = (float)(d - bin) * slope;
+    if (std::is_same<T, __bf16>::value) {
+      const float next = fminf((float)(row.bins_of_key(key - 0x10000u) - bin) * slope, (float)(end - start));
+      x = fminf(fmaf(next - x, (float)(int)(uint32_t)v[j] / (float)vocab, x), next);
+    }
+    guess[j] = min(start + (uint32_t)x, min(end, (uint32_t)kList) - 1);
+    slot[j] = atomicAdd(&s.guesses[guess[j]], 1u);
+  }
+  __syncthreads();
+  // Tokens before each guess.
+  uint32_t c[P], sum = 0, most = 0;
+#pragma unroll
+  for (int j = 0; j < P; ++j) c[j] = s.guesses[P * tid + j], sum += c[j], most = max(most, c[j]);
+  uint32_t in = sum;
+  scan_steps([&](auto ctrl, auto rows) { in += before_in_wave<decltype(ctrl)::value, decltype(rows)::value>(in); });
+  if (lane == 63) s.wave_count[wave] = in;
+  if (__syncthreads_or(most > kAlike)) return sort_list(s, n);
+  uint32_t before = in - sum;
+  for (int w = 0; w < wave; ++w) before += s.wave_count[w];
+#pragma unroll
+  for (int j = 0; j < P; ++j) s.guesses[P * tid + j] = before, before += c[j];
+  if (tid == kThreads - 1) s.guesses[kList] = before;
+  __syncthreads();
+  uint32_t from[P], to[P];
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (tid + j * kThreads >= n) continue;
+    from[j] = s.guesses[guess[j]], to[j] = s.guesses[guess[j] + 1];
+    s.list[from[j] + slot[j]] = v[j];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (tid + j * kThreads >= n) continue;
+    uint32_t at = from[j];
+    for (uint32_t i = from[j]; i < to[j]; ++i) at += s.list[i] < v[j];
+    slot[j] = at;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < P; ++j)
+    if (tid + j * kThreads < n) s.list[slot[j]] = v[j];
+  __syncthreads();
 }
 
 // The slice's tokens within the N runs into s.list.
@@ -761,9 +882,8 @@ __device__ __forceinline__ void gather_runs(Shared& s, const Logits<T>& x, int f
       for (int q = 0; q < N; ++q) any |= __builtin_amdgcn_fmed3f(v[e], edges.from[q], edges.to[q]) == v[e];
       return any;
     };
-    if (__ballot(in(0) || in(1) || in(2) || in(3)))
-#pragma unroll
-      for (int e = 0; e < 4; ++e) put(s, in(e), v[e], first + i + e);
+    const bool wanted[4] = {in(0), in(1), in(2), in(3)};
+    put<4>(s, wanted, [&](int e) { return entry(v[e], first + i + e); });
   });
 }
 template <typename T>
@@ -788,11 +908,10 @@ __device__ void keep_wanted(Shared& s, int n, const Row& row, const Wanted& w) {
     v[j] = lane + 64 * j < n ? s.list[(threadIdx.x >> 6) * kWaveList + lane + 64 * j] : ~0ull;
   if (threadIdx.x == 0) s.listed = 0;
   __syncthreads();
+  bool in[kWaveList / 64];
 #pragma unroll
-  for (int j = 0; j < kWaveList / 64; ++j) {
-    const float x = of_key(~(uint32_t)(v[j] >> 32));
-    put(s, v[j] != ~0ull && w.has((int)row.bins(x)), x, (int)(uint32_t)v[j]);
-  }
+  for (int j = 0; j < kWaveList / 64; ++j) in[j] = v[j] != ~0ull && w.has((int)row.bins_of_key(~(uint32_t)(v[j] >> 32)));
+  put<kWaveList / 64>(s, in, [&](int j) { return v[j]; });
   __syncthreads();
 }
 
@@ -817,18 +936,19 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleArgs a) {
   const Wanted w = decide(s, c);
   if (whole && list_serves(row, w, low)) {
     keep_wanted(s, listed, row, w);
+    sort_list(s, s.listed);
   } else if (s.wanted > kList) {
     const Pick pick = narrow(s, x, row, c);
     return answer(a, r, pick.index, pick.prob);
   } else {
-    const Edges edges = edges_of(row, w);
+    const Edges edges = edges_of(s, row, w);
     if (tid == 0) s.listed = 0;
     __syncthreads();
     gather(s, x, 0, edges);
     __syncthreads();
+    sort_runs<T>(s, s.listed, row, edges, x.n);
   }
   const int n = s.listed;
-  sort_list(s, n);
   const Pick pick = finish(s, n, row, c, w, [&](int b) { return Place{s.before[b], s.mass[b]}; });
   answer(a, r, pick.index, pick.prob);
 }
@@ -872,7 +992,8 @@ __device__ void send_list(Split* row, const u64* list, int n, int room) {
   const int lane = threadIdx.x & 63;
   if (n == 0) return;
   uint32_t at = 0;
-  if (lane == 0) at = __hip_atomic_fetch_add(&row->listed, (uint32_t)(n > room ? kList + 1 : n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint32_t more = n > room ? kList + 1 : n;
+  if (lane == 0) at = __hip_atomic_fetch_add(&row->listed, more, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   at = __builtin_amdgcn_readfirstlane(at);
   for (int i = lane; i < min(n, room); i += 64)
     if (at + i < kList) store_shared(&row->list[at + i], list[i]);
@@ -968,7 +1089,7 @@ __global__ __launch_bounds__(kThreads) void sample_count(SampleArgs a, Split* sp
     const Pick pick = narrow(s, x, scale, c);
     return answer(a, r, pick.index, pick.prob);
   }
-  const Edges edges = edges_of(scale, w);
+  const Edges edges = edges_of(s, scale, w);
   for (int i = tid; i < kBins; i += kThreads) row->mass[i] = s.mass[i], row->before[i] = s.before[i];
   if (tid == 0) row->edges = edges, row->wanted = w, row->listed = 0, row->open = 1;
 }
@@ -988,13 +1109,14 @@ __global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* spl
   const Row scale{x.plain(p.max), inv_t * kBinsPerUnit};
   if (tid == 0) s.listed = 0;
   __syncthreads();
-  gather(s, x, first, row->edges);
+  const Edges edges = row->edges;
+  gather(s, x, first, edges);
   __syncthreads();
   const int each = (s.listed + kWaves - 1) / kWaves, from = (tid >> 6) * each;
   send_list(row, s.list + from, max(0, min(each, (int)s.listed - from)), kList);
   if (!last_of_row(s, row, &row->gathered)) return;
   const int n = s.listed;
-  sort_list(s, n);
+  sort_runs<T>(s, n, scale, edges, a.vocab);
   const Wanted w = row->wanted;
   const Pick pick = finish(s, n, scale, c, w, [&](int b) { return Place{row->before[b], row->mass[b]}; });
   answer(a, r, pick.index, pick.prob);
@@ -1003,8 +1125,8 @@ __global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* spl
 }  // namespace
 
 // Slices of a row.  One workgroup pays for no hand-over; several share the passes.  us of a call with 1 / 2 / 4 / 8 / 16, top-p
-// of float32 rows: 128256 logits, 1 row 65 / 55 / 46 / 44 / 45, 32 rows 74 / 66 / 56 / 55 / 73, 64 rows 77 / 70 / 64 / 77 / 112,
-// 128 rows 79 / 81 / 94 / 129; 50000 logits, 1 row 30 / 35 / 33 / 31 / 33, 64 rows 39 / 45 / 42 / 60; 16384, 1 row 21 / 30.
+// of float32 rows: 128256 logits, 1 row 50 / 45 / 38 / 35 / 36, 32 rows 58 / 52 / 44 / 44 / 71, 64 rows 61 / 56 / 51 / 76 / 123,
+// 128 rows 64 / 68 / 89 / 139; 50000 logits, 1 row 31 / 35 / 32 / 33 / 35, 64 rows 35 / 41 / 40 / 66; 16384, 1 row 21 / 29.
 int sample_slices(int rows, int vocab) {
   if (vocab < (1 << 16) || rows > 64) return 1;
   return rows > 32 ? 4 : 8;

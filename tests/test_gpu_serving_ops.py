@@ -316,6 +316,24 @@ def test_sample_rows(ctx, name, dtype, vocab):
     _check_sample(ctx, x, u)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [9001, 70001])
+@pytest.mark.parametrize("ties", ["scattered", "in blocks", "at one end"])
+def test_sample_places_among_many_ties(ctx, dtype, vocab, ties):
+    """Hundreds of tokens of one logit, spread over the row, one behind the other, or crowded beside a few far ones: their order is
+    that of the index whatever way they are listed."""
+    rows, i = 24, torch.arange(vocab)
+    x = {"scattered": torch.round(_randn(7250, vocab, dtype=torch.float32) * 16) / 16,
+         "in blocks": -(i // 150 % 60) * 0.0625,
+         "at one end": torch.where(i % 1500 == 7, 2.0, torch.where(i < 900, 1.0, -0.5 - (i % 64) * 0.0625))}[ties]
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).repeat(rows, 1)
+    u = (torch.arange(rows) + 0.37) / rows
+    for params in (dict(top_p=torch.linspace(0.05, 0.95, rows)), dict(top_k=torch.arange(rows, dtype=torch.int32) * 67 + 3),
+                   dict(top_p=torch.full((rows,), 0.9), min_p=torch.linspace(0.01, 0.9, rows)),
+                   dict(temperature=torch.linspace(0.1, 1.5, rows), top_k=torch.full((rows,), 1000, dtype=torch.int32))):
+        _check_sample(ctx, x, u, **params)
+
+
 def test_sample_odd_parameters(ctx):
     """NaN and infinities among the parameters."""
     rows, nan, inf = 12, float("nan"), float("inf")
