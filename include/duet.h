@@ -289,7 +289,9 @@ typedef struct {
   const uint8_t* pair_axis; /* host, [rot_dim / 2]: the axis of each pair, below axes; NULL: axis 0 */
 } duet_rope;
 
-/* Workspace of duet_qkv_rope_split: an error word and the table of the requests.  Host only. */
+/* Workspace of duet_qkv_rope_split: an error word and the table of the requests.  Host only.  Up to this many requests travel
+ * with the launch, and the workspace may then be NULL: page ids outside the pool are not reported. */
+#define DUET_ROPE_NO_WORKSPACE 256
 int duet_rope_workspace_bytes(const duet_batch* batch, size_t* bytes);
 /* duet_qkv_split with the rotation on the way: the query and key columns of qkv [T, (h_q + 2 h_kv) d] are
  * turned by their token's position before they go to q and k_cache; values are copied.  shape.dtype bf16

@@ -437,7 +437,7 @@ class Context:
         else:
             N.check(N.lib().duet_init_with_model(device, model_path.encode(), ctypes.byref(h)), "duet_init_with_model")
         self.handle = h
-        self._dev = torch.device("cuda", device)
+        self._torch, self._dev = torch, torch.device("cuda", device)
         self.model = Model(N.lib().duet_ctx_model(h), owner=self)
         self._ws = None
 
@@ -615,7 +615,7 @@ class Context:
     def _empty(self, shape, dtype, stream):
         """Memory for one call that runs on `stream` (None: the current one): the allocator hands it to no later
         work before the call's, and under capture it belongs to the graph."""
-        import torch
+        torch = self._torch
         if stream is None:
             return torch.empty(shape, dtype=dtype, device=self._dev)
         with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self._dev) if stream else
@@ -624,31 +624,29 @@ class Context:
 
     def _space(self, workspace, need: int, stream):
         """A workspace of `need` bytes for a call on `stream`, or the caller's."""
-        import torch
         if workspace is None:
-            return self._empty(need, torch.uint8, stream)
+            return self._empty(need, self._torch.uint8, stream)
         if not (workspace.is_cuda and workspace.get_device() == self.device and workspace.is_contiguous()):
             raise ValueError(f"workspace must be a contiguous tensor on cuda:{self.device}")
         return workspace
 
     def _check_on(self, t, name, dtype, shape):
         """A contiguous tensor of this context's device."""
-        if not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == self.device and t.is_contiguous()):
+        if not (t.dtype is dtype and t.shape == shape and t.get_device() == self.device and t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{self.device}")
 
     def _current(self, stream) -> int:
         """The caller's stream, or torch's current one on this context's device."""
         if stream is not None:
             return stream
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 1.7 us less than a Stream object
-        return raw(self.device) if raw else torch.cuda.current_stream(self._dev).cuda_stream
+        raw = getattr(self._torch._C, "_cuda_getCurrentRawStream", None)  # 1.7 us less than a Stream object
+        return raw(self.device) if raw else self._torch.cuda.current_stream(self._dev).cuda_stream
 
     def qkv_rope_split(self, qkv, k_cache, v_cache, page_table, seq_meta, shape: AttnShape, rope: Rope, *, positions=None,
                        q=None, workspace=None, stream=None, check_errors: bool = False):
         """duet_qkv_rope_split: the rotated query rows out of qkv [T, (h_q + 2 h_kv) d], rotated keys and values into the
         cache.  positions: int32 [axes, T] ([T] for one axis); None: the tokens' places in the cache."""
-        import torch
+        torch = self._torch
         lib, b = N.lib(), _BatchC(seq_meta)
         T = b.end_row()
         dt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
@@ -668,24 +666,27 @@ class Context:
             q = self._empty((T, hq, d), dt, stream)
         else:
             self._check_on(q, "q", dt, (T, hq, d))
-        n = ctypes.c_size_t()
-        N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
-        workspace = self._space(workspace, n.value, stream)
+        ws = (None, 0)  # nobody would read the error word
+        if workspace is not None or check_errors or len(b.rows) > N.ROPE_NO_WORKSPACE:
+            n = ctypes.c_size_t()
+            N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+            workspace = self._space(workspace, n.value, stream)
+            ws = (workspace.data_ptr(), workspace.nbytes)
         if T == 0:
             return q
         st = self._current(stream)
         N.check(lib.duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
                                         positions.data_ptr() if positions is not None else None, q.data_ptr(),
                                         k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(), table[1],
-                                        ctypes.byref(b.c), workspace.data_ptr(), workspace.nbytes, st), "duet_qkv_rope_split")
+                                        ctypes.byref(b.c), *ws, st), "duet_qkv_rope_split")
         if check_errors:
-            N.check(lib.duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
+            N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
         return q
 
     def lora_add(self, x, base, lora: Lora, seq_meta, adapter_ids, *, out=None, workspace=None, stream=None):
         """duet_lora_add: base [T, d_out] plus each request's adapter applied to x [T, d_in] (bf16, rows may be strided).
         adapter_ids: one int per request, -1 for none.  out may be base."""
-        import torch
+        torch = self._torch
         lib, b = N.lib(), _BatchC(seq_meta)
         T = b.end_row()
         ids = np.ascontiguousarray(adapter_ids, dtype=np.int32)
@@ -716,7 +717,7 @@ class Context:
         """duet_sample: (ids int32 [rows], probs float32 [rows]), one token for each row of logits [rows, vocab] (bf16 or
         float32, rows may be strided) from the given random numbers u [rows] float32 in [0, 1).  temperature, top_p,
         min_p: float32 [rows]; top_k: int32 [rows]; None: off."""
-        import torch
+        torch = self._torch
         if not (logits.is_cuda and logits.get_device() == self.device and logits.dim() == 2 and
                 logits.dtype in (torch.bfloat16, torch.float32) and (logits.stride(1) == 1 or logits.shape[1] == 1)):
             raise ValueError(f"logits must be a bf16 or float32 tensor [rows, vocab] on cuda:{self.device} with contiguous rows")

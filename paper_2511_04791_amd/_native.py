@@ -15,6 +15,7 @@ ERRORS = {-1: "EINVAL", -2: "EUNSUPPORTED", -3: "EWORKSPACE", -4: "EHIP", -5: "E
 BF16, F32 = 0, 1
 KIND_PREFILL, KIND_DECODE = 0, 1
 AGG, SPLIT, CONCURRENT = 0, 1, 2
+ROPE_NO_WORKSPACE = 256
 STATUS_SLO_INFEASIBLE, STATUS_UNCALIBRATED = 1, 2
 TOTAL_CUS, CU_STEP, SPLIT_STEP = 256, 8, 32
 

@@ -226,13 +226,13 @@ struct RopeSplitArgs {
   const int32_t* page_table;
   const int32_t* positions;  // [axes, T], or null: the tokens' places in the cache
   long long num_phys_pages;
-  int32_t* err;
+  int32_t* err;            // may be null for up to kRopeTable requests
   int32_t num_reqs, max_pages, h_q, h_kv, head_dim, dtype, tokens;
   int32_t rot_dim, adjacent;
   double turns[64];        // turns per position of each pair (frequency / 2 pi)
   uint8_t pair_axis[64];
 };
-constexpr int kRopeTable = 256;
+constexpr int kRopeTable = DUET_ROPE_NO_WORKSPACE;
 hipError_t launch_rope_split(const RopeSplitArgs& a, const int4* requests, hipStream_t s);  // requests: the batch, on the host
 
 // out = base + scale_a B_a (A_a x) of each token's adapter a (lora.hip).  The rows are taken by adapter in tiles; row i of a

@@ -20,8 +20,8 @@
 // 32 + 2 x 8 heads 9, one 4.8.
 //
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
-// much on the host: one decode row 15.8 us a call with it, 10.3 without).  The upload clears the error word; without it one more
-// workgroup reads the page ids of the whole batch and stores the word.
+// much on the host: one decode row 15.8 us a call with it, 10.3 without, 8.5 also without a workspace).  The upload clears the error word; without it one more
+// workgroup reads the page ids of the whole batch and stores the word, if the caller has a workspace for it.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -106,10 +106,11 @@ __global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s, Table request
   __shared__ float2 turn[16][kMaxPairs];
   const int d = s.head_dim, pairs = s.rot_dim / 2, tid = threadIdx.x;
   int group = blockIdx.x;
-  if constexpr (kPassed) {
-    static_assert(sizeof(requests.at) <= sizeof(turn), "the check keeps the requests where the sines go");
+  if (kPassed && s.err) {
+    static_assert(sizeof(Passed::at) <= sizeof(turn), "the check keeps the requests where the sines go");
     if (group == 0) {
-      if (blockIdx.y == 0) check_pages(s, requests, reinterpret_cast<int2*>(turn));
+      if constexpr (kPassed)
+        if (blockIdx.y == 0) check_pages(s, requests, reinterpret_cast<int2*>(turn));
       return;
     }
     --group;
@@ -234,7 +235,7 @@ hipError_t launch(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
     Passed p;
     for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);
     p.at[a.num_reqs] = make_int2(a.tokens, 0);
-    hipLaunchKernelGGL((rope_split<T, Passed>), dim3(groups + 1, columns), dim3(256), 0, s, a, p);
+    hipLaunchKernelGGL((rope_split<T, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, a, p);
   } else {
     hipLaunchKernelGGL((rope_split<T, Uploaded>), dim3(groups, columns), dim3(256), 0, s, a, Uploaded{a.meta});
   }

@@ -1887,13 +1887,15 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   const void* v_l[1] = {v_cache};
   const void* o_l[1] = {q};
   rc = check_call(ctx, shape, 1, q_l, k_l, v_l, num_phys_pages, page_table, max_pages_per_req, batch,
-                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace, o_l, 0);
+                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace ? workspace : ctx, o_l, 0);
   if (rc) return rc;
   for (const void* p : {qkv, static_cast<const void*>(q), static_cast<const void*>(k_cache),
                         static_cast<const void*>(v_cache)})
     if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "qkv, q and the caches must lie on 16 bytes");
   if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
-  if (workspace_bytes < request_table_bytes(batch))
+  if (!workspace && batch->num_reqs > kRopeTable)
+    return fail(DUET_EINVAL, "workspace is NULL with more than %d requests", kRopeTable);
+  if (workspace && workspace_bytes < request_table_bytes(batch))
     return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, request_table_bytes(batch));
   RopeSplitArgs a{};
   if ((rc = batch_tokens(batch, &a.tokens))) return rc;
@@ -1924,7 +1926,7 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   static_assert(sizeof(duet_seq_meta) == sizeof(int4), "the kernels read the requests as they are");
   const UploadPart table{batch->reqs, batch->num_reqs * sizeof(int4), kAlign};
   if (batch->num_reqs > kRopeTable && (rc = upload_parts(ctx, &table, 1, ws, st))) return rc;
-  a.meta = reinterpret_cast<const int4*>(ws + kAlign);
+  if (ws) a.meta = reinterpret_cast<const int4*>(ws + kAlign);
   a.err = reinterpret_cast<int32_t*>(ws);
   HIP_TRY(launch_rope_split(a, reinterpret_cast<const int4*>(batch->reqs), st));
   return DUET_OK;

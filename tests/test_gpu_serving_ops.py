@@ -146,6 +146,18 @@ def test_rope_pages_outside_the_pool(ctx, name):
     ctx.qkv_rope_split(qkv.cuda(), kg, vg, torch.as_tensor(b.page_table, device="cuda"), *args, workspace=ws, check_errors=True)
 
 
+def test_rope_pages_outside_the_pool_without_a_workspace(ctx):
+    """Skipped all the same; nobody is told."""
+    import paper_2511_04791_amd as duet
+    sh = duet.AttnShape(4, 2, 64, "f32")
+    b, qkv, kc, vc = _rope_inputs(sh, REQUESTS["pages"], 6350)
+    table = b.page_table.copy()
+    table[0, 0], table[1, 3], table[len(table) - 1, 0] = -1, b.num_phys_pages, 2 ** 31 - 1
+    kg, vg = kc.cuda(), vc.cuda()
+    q = ctx.qkv_rope_split(qkv.cuda(), kg, vg, torch.as_tensor(table, device="cuda"), b.seq_meta, sh, duet.Rope(_freq(64)))
+    _check_rope(sh, b, qkv, kc, vc, (q, kg, vg), (_freq(64), False, None, None), table)
+
+
 # ---- adapters -------------------------------------------------------------------------------------
 
 

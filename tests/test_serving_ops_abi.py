@@ -122,7 +122,8 @@ class TestWithContext:
         def call(qkv=16, q=32, kc=48, vc=64, pages=10, table=80, max_pages=4, ws=96, nbytes=1 << 20, batch=b, shape=SHAPE):
             return native.duet_qkv_rope_split(ctx.handle, B(shape), B(_rope()), qkv, None, q, kc, vc, pages, table, max_pages,
                                               B(batch), ws, nbytes, None)
-        for kw, code in ((dict(qkv=None), -1), (dict(q=None), -1), (dict(kc=None), -1), (dict(vc=None), -1), (dict(ws=None), -1),
+        for kw, code in ((dict(qkv=None), -1), (dict(q=None), -1), (dict(kc=None), -1), (dict(vc=None), -1),
+                         (dict(ws=None, batch=_batch([(1, r, 1, 10) for r in range(257)])[1]), -1),
                          (dict(table=None), -1), (dict(q=16), -1), (dict(q=40), -1), (dict(kc=52), -1), (dict(ws=100), -1),
                          (dict(pages=0), -1), (dict(max_pages=0), -1), (dict(nbytes=256), -3),
                          (dict(shape=N.Shape(8, 2, 96, 16, N.BF16, 1)), -2), (dict(shape=N.Shape(8, 3, 64, 16, N.BF16, 1)), -2),
