@@ -20,8 +20,9 @@
 // 32 + 2 x 8 heads 9, one 4.8.
 //
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
-// much on the host: one decode row 15.8 us a call with it, 10.3 without, 8.5 also without a workspace).  The upload clears the error word; without it one more
-// workgroup reads the page ids of the whole batch and stores the word, if the caller has a workspace for it.
+// much on the host).  The upload clears the error word; without it one more workgroup reads the page ids of the whole batch
+// and stores the word, if the caller has a workspace for it.  One decode row: 15.8 us a call with the upload, 10.3 with the
+// workgroup, 8.5 without a workspace.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

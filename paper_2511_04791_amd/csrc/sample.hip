@@ -17,9 +17,9 @@
 // A row is read twice (its maximum, the histogram), a third time where the places lie past the largest few hundred tokens,
 // which the second pass lists as it goes; by one workgroup, or in slices by several where there are few rows.
 //
-// us of the steps for 256 float32 rows of 128256 logits, a CU each, 76 a call: maximum 16 (131 MB, 8 TB/s), histogram 19,
-// its sums 5, third pass 15, sorting 2, the answer 4.  One row alone: 6, 18, 5, 9 to 15, 2, 4: the histogram is bound by its LDS
-// additions (12 us without any arithmetic) and the arithmetic in 64 bits (16 without additions), the rest by latency.
+// us of the steps for 256 float32 rows of 128256 logits, a CU each, 68 a call: maximum 17 (131 MB, 7.7 TB/s), histogram 19,
+// its sums 5, third pass 15, sorting 2, the answer 3.  One row on one CU: 5, 18, 5, 9 to 13, 2, 3: the histogram is bound by its
+// LDS additions (12 us without any arithmetic) and the arithmetic in 64 bits (16 without additions), the rest by latency.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -343,7 +343,7 @@ struct Pick {
 };
 
 template <typename T>
-__device__ __attribute__((noinline)) Pick narrow(Shared& s, const Logits<T>& x, const Row& row, const Settings& c) {
+__device__ __attribute__((noinline)) Pick narrow(Shared& s, Logits<T> x, Row row, Settings c) {
   const uint32_t k = c.top_k ? c.top_k : 0xffffffffu;
   Place kept = find(s, x, row, [&](const Place& p) { return p.n >= k; }).end;
   if (c.top_p < 1) {
@@ -427,6 +427,7 @@ __device__ __forceinline__ void put(Shared& s, const bool* in, F token) {
   at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
   for (int e = 0; e < N; ++e) {
+    if (!all[e]) continue;
     const uint32_t to = at + lanes_before(all[e]);
     if (in[e] && to < kList) s.list[to] = token(e);
     at += __popcll(all[e]);
@@ -595,6 +596,11 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
   if (last >= 0 && !(__ballot(last >= 0) >> lane >> 1)) atomicMax(&s.last_pos, last);
   __syncthreads();
   Place kept{k ? c.top_k : w.all.n, s.value};
+  auto leave = [&](int at) {  // an index known when compiled keeps the array in registers
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+      if (at == tid * P + j) s.place = high[j];
+  };
   // The first listed rank at or past a place, the last one where none is.
   auto first = [&](auto reached) {
     int i = 1 << 30;
@@ -605,7 +611,7 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
     if (i < 1 << 30 && !(some & ((1ull << lane) - 1))) atomicMin(&s.pos, i);
     __syncthreads();
     const int at = s.pos == 1 << 30 ? s.last_pos : s.pos;
-    if (at / P == tid) s.place = high[at % P];
+    leave(at);
     __syncthreads();
     if (tid == 0) s.pos = 1 << 30;
     return at;
@@ -623,7 +629,7 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
       if (listed(j) && bin[j] == w.lo[2] && weight_of(d[j]) >= c.min_p) own = tid * P + j;
     if (own >= 0) atomicMax(&s.at, own);
     __syncthreads();
-    if (s.at >= 0 && s.at / P == tid) s.place = high[s.at % P];
+    leave(s.at);
     if (s.at < 0 && tid == 0) s.place = before_bin(w.lo[2]);
     __syncthreads();
     if (s.place.n < kept.n) kept = s.place;
@@ -631,7 +637,9 @@ __device__ Pick finish(Shared& s, int n, const Row& row, const Settings& c, cons
   }
   const double target = c.u * kept.mass;
   const int at = first([&](const Place& p) { return p.mass > target; });
-  if (at / P == tid) s.value = weight_of(d[at % P]);
+#pragma unroll
+  for (int j = 0; j < P; ++j)
+    if (at == tid * P + j) s.value = weight_of(d[j]);
   __syncthreads();
   return Pick{(int)(uint32_t)s.list[at], (float)(s.value / kept.mass)};
 }
@@ -1125,8 +1133,8 @@ __global__ __launch_bounds__(kThreads) void sample_list(SampleArgs a, Split* spl
 }  // namespace
 
 // Slices of a row.  One workgroup pays for no hand-over; several share the passes.  us of a call with 1 / 2 / 4 / 8 / 16, top-p
-// of float32 rows: 128256 logits, 1 row 50 / 45 / 38 / 35 / 36, 32 rows 58 / 52 / 44 / 44 / 71, 64 rows 61 / 56 / 51 / 76 / 123,
-// 128 rows 64 / 68 / 89 / 139; 50000 logits, 1 row 31 / 35 / 32 / 33 / 35, 64 rows 35 / 41 / 40 / 66; 16384, 1 row 21 / 29.
+// of float32 rows: 128256 logits, 1 row 49 / 44 / 36 / 33 / 35, 32 rows 56 / 49 / 41 / 40 / 67, 64 rows 57 / 52 / 46 / 69 / 114,
+// 128 rows 61 / 62 / 81 / 125; 50000 logits, 1 row 27 / 31 / 29 / 30 / 32, 64 rows 32 / 37 / 37 / 60; 16384, 1 row 20 / 27.
 int sample_slices(int rows, int vocab) {
   if (vocab < (1 << 16) || rows > 64) return 1;
   return rows > 32 ? 4 : 8;
