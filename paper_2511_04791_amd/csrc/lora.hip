@@ -15,7 +15,7 @@
 
 #include <algorithm>
 
-#include "kernels.h"
+#include "serving_ops.h"
 #include "wave_ops.h"
 
 namespace duet {

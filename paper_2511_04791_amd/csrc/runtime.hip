@@ -29,6 +29,7 @@
 #include "duet_internal.h"
 #include "gemm.h"
 #include "kernels.h"
+#include "serving_ops.h"
 
 namespace {
 

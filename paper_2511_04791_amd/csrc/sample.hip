@@ -24,7 +24,7 @@
 
 #include <type_traits>
 
-#include "kernels.h"
+#include "serving_ops.h"
 #include "wave_ops.h"
 
 namespace duet {
