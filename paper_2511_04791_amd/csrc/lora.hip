@@ -2,7 +2,7 @@
 //   out[t] = base[t] + scale_a B_a (A_a x[t]),  a the adapter of token t's request.
 // Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h with one rounding to bf16.
 // Both are bound by memory: x, base and out pass once, the adapters are a few MB.  us of the two: 64 rows, 4096 to 6144 columns,
-// rank 16, 4.2 + 5.9 (latency); 2112 rows, 4096 to 28672, rank 16, 8 + 55 (4.4 TB/s); 6400 rows, 14336 to 4096, rank 64, 47 + 28
+// rank 16, 4.2 + 5.9 (latency); 2112 rows, 4096 to 28672, rank 16, 8 + 55 (4.4 TB/s); 6298 rows, 14336 to 4096, rank 64, 47 + 28
 // (3.9 and 3.8 TB/s of x, base and out; the first has 500 workgroups for 256 CUs, which read A again for each tile).
 //
 // The lists of up to kLoraPassedTiles tiles travel with the launches' arguments; longer ones are uploaded, a launch of its own
@@ -55,7 +55,7 @@ __device__ __forceinline__ void split(float h, __bf16* hi, __bf16* lo) {
 // An MFMA operand wants a row a lane, and a load of that shape costs the address unit 82 cycles (neighbouring lanes lie in
 // different rows); a load whose neighbours lie in one row costs 19.  So a unit's rows are loaded 64 or 128 bytes by
 // neighbours, put into the wave's part of LDS and read from there in the operands' shape, a row's 16-byte chunks in an order
-// by which the 16 lanes of a read meet all banks.  us of 6400 rows of 14336 columns, rank 64: 67 without this.
+// by which the 16 lanes of a read meet all banks.  us of 6298 rows of 14336 columns, rank 64: 67 without this.
 template <int NT>
 struct Down {
   static constexpr int kHalves = NT == 8 ? 1 : 2, kUnit = 32 * kHalves;

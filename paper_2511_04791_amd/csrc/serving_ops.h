@@ -48,7 +48,7 @@ struct LoraArgs {
 // Parts of the input's columns, each a workgroup a tile.  A CU pulls at most some 30 GB/s of its own from memory, so the 256 CUs'
 // largest share counts, and a little for each part; at least four 64-column units a part.  us of the down product with
 // 1 / 2 / 4 / 5 / 6 / 8 parts: 17 tiles of a few rows, 4096 columns, rank 16, 8.0 / 5.4 / 4.5 / . / 4.5 / 4.0; 41 tiles (2112 rows)
-// 20 / 14 / 11 / . / 11 / 12; 100 tiles (6400 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 53 / 73 / 69.
+// 20 / 14 / 11 / . / 11 / 12; 100 tiles (6298 rows) of 14336 columns, rank 64, 82 / 56 / 59 / 53 / 73 / 69.
 constexpr int kLoraMaxParts = 8;
 int lora_most_parts(int tokens, int d_in);
 int lora_parts(int tiles, int most);
