@@ -46,7 +46,8 @@ struct Passed {
 // h and what its rounding to bf16 leaves out (16 bits together).
 __device__ __forceinline__ void split(float h, __bf16* hi, __bf16* lo) {
   *hi = static_cast<__bf16>(h);
-  *lo = static_cast<__bf16>(__builtin_isfinite(h) ? h - static_cast<float>(*hi) : 0.f);
+  const float r = static_cast<float>(*hi);
+  *lo = static_cast<__bf16>(__builtin_isfinite(r) ? h - r : 0.f);
 }
 
 // Partial sums of h of a tile's 16 RT rows over the columns of one part: four waves take its units of kUnit columns in

@@ -47,7 +47,8 @@ def _rope_inputs(sh, reqs, seed):
     b = wl.make_batch(sh, reqs, page_seed=seed)
     dt = torch.bfloat16 if sh.dtype == "bf16" else torch.float32
     P = b.num_phys_pages
-    kc, vc = _randn(seed + 1, P, sh.num_kv_heads, 16, sh.head_dim, dtype=dt), _randn(seed + 2, P, sh.num_kv_heads, sh.head_dim, 16, dtype=dt)
+    kc = _randn(seed + 1, P, sh.num_kv_heads, 16, sh.head_dim, dtype=dt)
+    vc = _randn(seed + 2, P, sh.num_kv_heads, sh.head_dim, 16, dtype=dt)
     qkv = _randn(seed + 3, b.num_tokens, (sh.num_q_heads + 2 * sh.num_kv_heads) * sh.head_dim, dtype=dt)
     return b, qkv, kc, vc
 
@@ -240,6 +241,18 @@ def test_lora_keeps_what_is_not_finite_to_its_own_rows(ctx):
     assert torch.equal(got[1:], clean[1:])
 
 
+def test_lora_beyond_the_largest_bf16(ctx):
+    """A hidden value between bf16's largest and fp32's gives infinities, not NaN."""
+    import paper_2511_04791_amd as duet
+    x, base = torch.ones(2, 8, dtype=torch.bfloat16), torch.ones(2, 16, dtype=torch.bfloat16)
+    x[0, 0], x[0, 1], x[0, 2:] = torch.finfo(torch.bfloat16).max, 1.5 * 2.0 ** 119, 0
+    a, b = torch.ones(1, 8, 8, dtype=torch.bfloat16), torch.ones(1, 16, 8, dtype=torch.bfloat16)
+    h = x[0].float().sum()
+    assert torch.isfinite(h) and torch.isinf(h.to(torch.bfloat16))
+    got = ctx.lora_add(x.cuda(), base.cuda(), duet.Lora(a.cuda(), b.cuda()), [(0, 2, 0)], [0]).cpu()
+    assert (got[0] == float("inf")).all() and (got[1] == 65).all()
+
+
 # ---- sampling ---------------------------------------------------------------------------------------
 
 
@@ -300,7 +313,8 @@ ROWS = {
     "few values": lambda v: (torch.arange(v) % 5).float() * 0.25,
     "one finite": lambda v: torch.full((v,), -float("inf")).index_fill(0, torch.tensor([v // 2]), -1e30),
     "masked": lambda v: _randn(1, v, dtype=torch.float32).masked_fill(torch.arange(v) % 7 != 3, -float("inf")),
-    "masked with the lowest": lambda v: _randn(2, v, dtype=torch.float32).masked_fill(torch.arange(v) % 7 != 3, torch.finfo(torch.float32).min),
+    "masked with the lowest": lambda v: _randn(2, v, dtype=torch.float32).masked_fill(torch.arange(v) % 7 != 3,
+                                                                                      torch.finfo(torch.float32).min),
     "all the lowest": lambda v: torch.full((v,), torch.finfo(torch.float32).min),
     "nothing": lambda v: torch.full((v,), -float("inf")),
     "NaN": lambda v: torch.full((v,), float("nan")),
@@ -326,6 +340,16 @@ def test_sample_rows(ctx, name, dtype, vocab):
     _check_sample(ctx, x, u, **_mixed_params(7201, rows))
     _check_sample(ctx, x, u, top_p=torch.full((rows,), 0.5))
     _check_sample(ctx, x, u)
+
+
+@pytest.mark.parametrize("name", list(ROWS))
+def test_sample_rows_in_more_slices(ctx, name):
+    """Fewer rows go to more workgroups each."""
+    rows = 9
+    x = ROWS[name](70001).repeat(rows, 1)
+    u = torch.linspace(0, 1, rows)
+    _check_sample(ctx, x, u, **_mixed_params(7221, rows))
+    _check_sample(ctx, x, u, top_p=torch.full((rows,), 0.7), top_k=torch.full((rows,), 3000, dtype=torch.int32))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

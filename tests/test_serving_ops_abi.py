@@ -151,8 +151,8 @@ class TestWithContext:
         big = dict(vocab=100000, stride=100000)
         for kw, code in ((dict(logits=None), -1), (dict(u=None), -1), (dict(ids=None), -1), (dict(dtype=2), -2), (dict(rows=-1), -1),
                          (dict(rows=(1 << 20) + 1), -1), (dict(vocab=0), -1), (dict(vocab=(1 << 18) + 1, stride=1 << 19), -2),
-                         (dict(stride=9), -1), (dict(logits=17), -1), (dict(logits=18, dtype=1), -1), (dict(big), -1), (dict(big, ws=16, nbytes=4096), -3),
-                         (dict(big, ws=24, nbytes=1 << 20), -1)):
+                         (dict(stride=9), -1), (dict(logits=17), -1), (dict(logits=18, dtype=1), -1), (dict(big), -1),
+                         (dict(big, ws=16, nbytes=4096), -3), (dict(big, ws=24, nbytes=1 << 20), -1)):
             assert call(**kw) == code, kw
             assert native.duet_last_error()
         assert call(rows=0) == 0
