@@ -9,15 +9,17 @@
 //
 // Bound by memory: the projection is read once, the same bytes are written.  A workgroup takes the rows of one request
 // whose positions lie on one page (up to 16; one decode row), forms their sines and cosines once in LDS (all heads turn
-// alike), and then some of the columns of all of them: a thread a unit of 32 bytes a row (of queries and keys the two
-// 16-byte chunks that turn together), eight rows in flight.  Values go to a dim-major page, a whole page's 32 or 64
+// alike), and moves some of the columns of all of them: a thread a unit of 32 bytes a row (of queries and keys two 16-byte
+// chunks, eight rows in flight, neighbours at neighbouring chunks: with the two side by side a kernel that only copied took twice
+// as long).  The first loads go out before the sines are formed.  Values go to a dim-major page, a whole page's 32 or 64
 // contiguous bytes a dim, of a page that the chunk covers in part, value by value.
 //
 // Request r (rows q_start .. q_start + q_len - 1) has the page groups from q_start / 16 + 2 r on: more than it needs,
 // whatever its first slot, and groups past its last page end at once.
 //
-// 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.3 TB/s; a large copy reaches 5.1), 256 decode rows of
-// 32 + 2 x 8 heads 9, one 4.8.
+// 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.3 TB/s; a large copy reaches 5.1), 2112 rows of 32 + 2 x 8 heads
+// 15 (3.4 TB/s: a chain of latencies of 3 us before the first store), 256 decode rows of those 8.7, one 3.8.  One kernel for
+// both orders of pairs took 1.2 us more for the 2112 rows.
 //
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
 // much on the host).  The upload clears the error word; without it one more workgroup reads the page ids of the whole batch
@@ -100,7 +102,7 @@ __device__ void check_pages(const RopeSplitArgs& s, const Passed& requests, int2
   if (threadIdx.x == 0) *s.err = bad;
 }
 
-template <typename T, typename Table>
+template <typename T, bool ADJACENT, typename Table>
 __global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s, Table requests) {
   constexpr int N = Chunk<T>::N;
   constexpr bool kPassed = std::is_same<Table, Passed>::value;
@@ -123,111 +125,132 @@ __global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s, Table request
   const int id = s.page_table[(size_t)r * s.max_pages + at.page];
   const bool ok = page_ok(id, s.num_phys_pages);
   if (!kPassed && !ok && blockIdx.y == 0 && tid == 0) atomicOr(s.err, 1);
-  for (int i = tid; i < n * pairs; i += 256) {
-    const int t = i / pairs, pair = i - t * pairs;
-    const int p = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
-    turn[t][pair] = cos_sin_of(p * s.turns[pair]);
-  }
-  __syncthreads();
+  // The thread's unit.  Its first loads, 16 of 16 bytes, go out before the sines are formed and wait for neither the page id nor
+  // those: eight rows of a unit of queries or keys, all sixteen of one of values.
   const int units = d / (2 * N), nqk = s.h_q + s.h_kv, width = (nqk + s.h_kv) * d;
-  const int qk_units = nqk * units, all = qk_units + s.h_kv * d / N;
+  const int qk_units = nqk * units, all = qk_units + s.h_kv * d / N, u = blockIdx.y * 256 + tid;
   const T* src = static_cast<const T*>(s.qkv) + (size_t)row * width;
-  for (int u = blockIdx.y * 256 + tid; u < all; u += gridDim.y * 256) {
-    if (u < qk_units) {
-      const int head = u / units, k = u - head * units, turned = pairs / N;  // units that turn
-      const bool is_q = head < s.h_q;
-      if (!is_q && !ok) continue;
-      // The unit's two chunks, and the pair of its first element(s).
-      const bool halves = k < turned && !s.adjacent;
-      const int c0 = halves ? k * N : 2 * k * N, c1 = halves ? c0 + pairs : c0 + N;
-      const T* x = src + head * d;
-      T* dst;
-      size_t stride;
-      if (is_q) {
-        dst = static_cast<T*>(s.q) + ((size_t)row * s.h_q + head) * d;
-        stride = (size_t)s.h_q * d;
-      } else {
-        dst = static_cast<T*>(s.k_cache) + (((size_t)id * s.h_kv + head - s.h_q) * 16 + slot) * d;
-        stride = d;
-      }
-      const bool turns = k < turned;
+  const bool qk = u < qk_units, there = u < all;
+  const int head = u / units, k = u - head * units;
+  // A unit's two chunks: those that turn together, of halves, else two half a head apart or half of what is copied; so that
+  // neighbours take neighbouring chunks.  A column of values.
+  const bool together = !ADJACENT && k < pairs / N;
+  const int from = ADJACENT || together ? 0 : s.rot_dim - pairs, half = ADJACENT ? d / 2 : together ? pairs : (d - s.rot_dim) / 2;
+  const int c0 = from + k * N, c1 = c0 + half;
+  const int col = (u - qk_units) * N;
+  uint4 a[16];
+  auto load = [&](int t0, uint4* v) {
 #pragma unroll
-      for (int t0 = 0; t0 < 16; t0 += 8) {
-        if (t0 >= n) break;
-        uint4 a[8], b[8];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const T* y = x + (size_t)min(t0 + t, n - 1) * width;
-          a[t] = *reinterpret_cast<const uint4*>(y + c0);
-          b[t] = *reinterpret_cast<const uint4*>(y + c1);
-        }
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          if (t0 + t >= n) break;
-          if (turns) {
-            Chunk<T> p = __builtin_bit_cast(Chunk<T>, a[t]), q = __builtin_bit_cast(Chunk<T>, b[t]);
-            const float2* cs = turn[t0 + t] + k * N;
-            if (s.adjacent) {
-#pragma unroll
-              for (int e = 0; e < N / 2; ++e)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  T* w = h ? q.v : p.v;
-                  const float2 z = cs[h * N / 2 + e];
-                  const float v0 = static_cast<float>(w[2 * e]), v1 = static_cast<float>(w[2 * e + 1]);
-                  w[2 * e] = static_cast<T>(v0 * z.x - v1 * z.y);
-                  w[2 * e + 1] = static_cast<T>(v0 * z.y + v1 * z.x);
-                }
-            } else {
-#pragma unroll
-              for (int e = 0; e < N; ++e) {
-                const float2 z = cs[e];
-                const float v0 = static_cast<float>(p.v[e]), v1 = static_cast<float>(q.v[e]);
-                p.v[e] = static_cast<T>(v0 * z.x - v1 * z.y);
-                q.v[e] = static_cast<T>(v0 * z.y + v1 * z.x);
-              }
-            }
-            a[t] = __builtin_bit_cast(uint4, p);
-            b[t] = __builtin_bit_cast(uint4, q);
-          }
-          T* y = dst + (t0 + t) * stride;
-          *reinterpret_cast<uint4*>(y + c0) = a[t];
-          *reinterpret_cast<uint4*>(y + c1) = b[t];
-        }
-      }
-      continue;
+    for (int t = 0; t < 8; ++t) {
+      const T* y = src + (size_t)min(t0 + t, n - 1) * width + head * d;
+      v[t] = *reinterpret_cast<const uint4*>(y + c0);
+      v[8 + t] = *reinterpret_cast<const uint4*>(y + c1);
     }
-    if (!ok) continue;
-    const int col = (u - qk_units) * N;
-    T* v = static_cast<T*>(s.v_cache) + (((size_t)id * s.h_kv + col / d) * d + col % d) * 16 + slot;
-    Chunk<T> x[16];
+  };
+  constexpr int J = 16 * kMaxPairs / 256;
+  int p[J];
+  double f[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    if (256 * j >= n * pairs) break;
+    const int i = min(tid + 256 * j, n * pairs - 1), t = i / pairs, pair = i - t * pairs;
+    p[j] = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
+    f[j] = s.turns[pair];
+  }
+  if (qk) {
+    load(0, a);
+  } else if (there) {
 #pragma unroll
     for (int t = 0; t < 16; ++t)
-      x[t] = __builtin_bit_cast(Chunk<T>, *reinterpret_cast<const uint4*>(src + (size_t)min(t, n - 1) * width + nqk * d + col));
-    if (n < 16) {
-#pragma unroll
-      for (int t = 0; t < 16; ++t)
-        if (t < n)
-#pragma unroll
-          for (int e = 0; e < N; ++e) v[e * 16 + t] = x[t].v[e];
-      continue;
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-#pragma unroll
-      for (int t = 0; t < 16; t += N) {
-        Chunk<T> y;
-#pragma unroll
-        for (int i = 0; i < N; ++i) y.v[i] = x[t + i].v[e];
-        *reinterpret_cast<uint4*>(v + e * 16 + t) = __builtin_bit_cast(uint4, y);
-      }
+      a[t] = *reinterpret_cast<const uint4*>(src + (size_t)min(t, n - 1) * width + nqk * d + col);
   }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    if (256 * j >= n * pairs) break;
+    const int i = min(tid + 256 * j, n * pairs - 1), t = i / pairs;
+    turn[t][i - t * pairs] = cos_sin_of(p[j] * f[j]);
+  }
+  __syncthreads();
+  if (!there) return;
+  if (qk) {
+    const bool is_q = head < s.h_q;
+    if (!is_q && !ok) return;
+    T* dst;
+    size_t stride;
+    if (is_q) {
+      dst = static_cast<T*>(s.q) + ((size_t)row * s.h_q + head) * d;
+      stride = (size_t)s.h_q * d;
+    } else {
+      dst = static_cast<T*>(s.k_cache) + (((size_t)id * s.h_kv + head - s.h_q) * 16 + slot) * d;
+      stride = d;
+    }
+    auto store = [&](int t0, uint4* v) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if (t0 + t >= n) break;
+        const float2* turns = turn[t0 + t];
+        if constexpr (ADJACENT) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int c = h ? c1 : c0;
+            if (c >= s.rot_dim) continue;
+            Chunk<T> x = __builtin_bit_cast(Chunk<T>, v[8 * h + t]);
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+              const float2 z = turns[(c + e) / 2];
+              const float v0 = static_cast<float>(x.v[e]), v1 = static_cast<float>(x.v[e + 1]);
+              x.v[e] = static_cast<T>(v0 * z.x - v1 * z.y);
+              x.v[e + 1] = static_cast<T>(v0 * z.y + v1 * z.x);
+            }
+            v[8 * h + t] = __builtin_bit_cast(uint4, x);
+          }
+        } else if (together) {
+          Chunk<T> x = __builtin_bit_cast(Chunk<T>, v[t]), y = __builtin_bit_cast(Chunk<T>, v[8 + t]);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float2 z = turns[c0 + e];
+            const float v0 = static_cast<float>(x.v[e]), v1 = static_cast<float>(y.v[e]);
+            x.v[e] = static_cast<T>(v0 * z.x - v1 * z.y);
+            y.v[e] = static_cast<T>(v0 * z.y + v1 * z.x);
+          }
+          v[t] = __builtin_bit_cast(uint4, x);
+          v[8 + t] = __builtin_bit_cast(uint4, y);
+        }
+        T* y = dst + (t0 + t) * stride;
+        *reinterpret_cast<uint4*>(y + c0) = v[t];
+        *reinterpret_cast<uint4*>(y + c1) = v[8 + t];
+      }
+    };
+    store(0, a);
+    if (n > 8) load(8, a), store(8, a);
+    return;
+  }
+  if (!ok) return;
+  T* v = static_cast<T*>(s.v_cache) + (((size_t)id * s.h_kv + col / d) * d + col % d) * 16 + slot;
+  Chunk<T> x[16];
+#pragma unroll
+  for (int t = 0; t < 16; ++t) x[t] = __builtin_bit_cast(Chunk<T>, a[t]);
+  if (n < 16) {
+#pragma unroll
+    for (int t = 0; t < 16; ++t)
+      if (t < n)
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e * 16 + t] = x[t].v[e];
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+#pragma unroll
+    for (int t = 0; t < 16; t += N) {
+      Chunk<T> y;
+#pragma unroll
+      for (int i = 0; i < N; ++i) y.v[i] = x[t + i].v[e];
+      *reinterpret_cast<uint4*>(v + e * 16 + t) = __builtin_bit_cast(uint4, y);
+    }
 }
 
-}  // namespace
-
-namespace {
-template <typename T>
+template <typename T, bool ADJACENT>
 hipError_t launch(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
   const int n = 16 / sizeof(T), d = a.head_dim;
   const int units = (a.h_q + a.h_kv) * d / (2 * n) + a.h_kv * d / n;
@@ -236,12 +259,17 @@ hipError_t launch(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
     Passed p;
     for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);
     p.at[a.num_reqs] = make_int2(a.tokens, 0);
-    hipLaunchKernelGGL((rope_split<T, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, a, p);
+    hipLaunchKernelGGL((rope_split<T, ADJACENT, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, a, p);
   } else {
-    hipLaunchKernelGGL((rope_split<T, Uploaded>), dim3(groups, columns), dim3(256), 0, s, a, Uploaded{a.meta});
+    hipLaunchKernelGGL((rope_split<T, ADJACENT, Uploaded>), dim3(groups, columns), dim3(256), 0, s, a, Uploaded{a.meta});
   }
   return hipGetLastError();
 }
+template <typename T>
+hipError_t launch(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {
+  return a.adjacent ? launch<T, true>(a, requests, s) : launch<T, false>(a, requests, s);
+}
+
 }  // namespace
 
 hipError_t launch_rope_split(const RopeSplitArgs& a, const int4* requests, hipStream_t s) {

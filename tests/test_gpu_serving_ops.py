@@ -87,7 +87,9 @@ def _freq(rot, theta=10000.0):
 @pytest.mark.parametrize("name", list(REQUESTS))
 @pytest.mark.parametrize("heads,dtype,rot,adjacent", [((4, 2, 128), "bf16", 128, False), ((6, 3, 64), "bf16", 64, True),
                                                       ((20, 4, 128), "bf16", 48, False), ((2, 2, 64), "f32", 64, False),
-                                                      ((5, 1, 64), "f32", 16, True), ((4, 2, 128), "f32", 112, True)])
+                                                      ((5, 1, 64), "f32", 16, True), ((4, 2, 128), "f32", 112, True),
+                                                      ((8, 1, 128), "bf16", 80, True), ((4, 4, 64), "f32", 48, False),
+                                                      ((2, 1, 64), "bf16", 16, False)])
 def test_rope_split(ctx, name, heads, dtype, rot, adjacent):
     import paper_2511_04791_amd as duet
     sh = duet.AttnShape(*heads, dtype)
