@@ -692,11 +692,12 @@ class Context:
         ids = np.ascontiguousarray(adapter_ids, dtype=np.int32)
         if ids.shape != (len(b.rows),):
             raise ValueError(f"adapter_ids must hold {len(b.rows)} values, one per request")
+        ids = (ctypes.c_int32 * len(ids)).from_buffer_copy(ids) if len(ids) else None
         if out is None:
             out = self._empty((T, lora.c.d_out), torch.bfloat16, stream)
         dt, ld = torch.bfloat16, []
         for t, name, width in ((x, "x", lora.c.d_in), (base, "base", lora.c.d_out), (out, "out", lora.c.d_out)):
-            if not (t.dtype is dt and t.shape == (T, width) and t.is_cuda and t.get_device() == self.device and t.stride(1) == 1):
+            if not (t.dtype is dt and t.shape == (T, width) and t.get_device() == self.device and t.stride(1) == 1):
                 raise ValueError(f"{name} must be a bf16 tensor [{T}, {width}] on cuda:{self.device} with contiguous rows")
             ld.append(t.stride(0) if T > 1 else width)
         if lora.a.get_device() != self.device:
@@ -708,7 +709,7 @@ class Context:
         if T == 0:
             return out
         N.check(lib.duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld[0], base.data_ptr(), ld[1],
-                                  out.data_ptr(), ld[2], ctypes.byref(b.c), ids.ctypes.data, workspace.data_ptr(),
+                                  out.data_ptr(), ld[2], ctypes.byref(b.c), ids, workspace.data_ptr(),
                                   workspace.nbytes, self._current(stream)), "duet_lora_add")
         return out
 
