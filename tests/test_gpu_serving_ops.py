@@ -567,3 +567,34 @@ def test_one_workspace_for_all(ctx):
         calls[turn % 2](ws)
         torch.cuda.synchronize()
         assert all(torch.equal(g, w) for a, b in zip(outs, want) for g, w in zip(a, b)), turn
+
+
+def test_offsets_past_32_bits(ctx):
+    """Pages, rows and logits more than 2^31 elements from the start."""
+    import paper_2511_04791_amd as duet
+    far = 1 << 30
+    # The last pages of a large pool.
+    sh = duet.AttnShape(8, 8, 128, "bf16")
+    b, qkv, kc, vc = _rope_inputs(sh, [(0, 33, 5), (1, 1, 40)], 8700)
+    P, pages = kc.shape[0], far * 2 // (8 * 16 * 128) + 64
+    big = [torch.empty(pages, *c.shape[1:], dtype=torch.bfloat16, device="cuda") for c in (kc, vc)]
+    for c, at in zip((kc, vc), big):
+        at[pages - P:] = c.cuda()
+    table = torch.as_tensor(np.where(b.page_table >= 0, b.page_table + pages - P, -1).astype(np.int32), device="cuda")
+    q = ctx.qkv_rope_split(qkv.cuda(), big[0], big[1], table, b.seq_meta, sh, duet.Rope(_freq(128)), check_errors=True)
+    _check_rope(sh, b, qkv, kc, vc, (q, big[0][pages - P:], big[1][pages - P:]), (_freq(128), False, None, None))
+    del big
+    # Rows far apart.
+    meta, ids, x, base, la, lb, scale = _lora_case(8710, 72, 80, 16, 2, [(1, 1, 0)] * 3, [1, 0, 1])
+    room = torch.empty(2 * far + 1024, dtype=torch.bfloat16, device="cuda")
+    rows = lambda at, n: torch.as_strided(room, (3, n), (far, 1), at)  # noqa: E731
+    xs, bases, out = rows(0, 72), rows(128, 80), rows(256, 80)
+    xs.copy_(x), bases.copy_(base)
+    ctx.lora_add(xs, bases, duet.Lora(la.cuda(), lb.cuda(), scale.cuda()), meta, ids, out=out)
+    _check_lora(out, meta, ids, x, base, la, lb, scale)
+    logits = _randn(8720, 3, 900, scale=2.0)
+    rows(0, 900).copy_(logits)
+    u = torch.tensor([0.1, 0.5, 0.9])
+    ids, probs = ctx.sample(rows(0, 900), u.cuda())
+    want = ctx.sample(logits.cuda(), u.cuda())
+    assert torch.equal(ids, want[0]) and torch.equal(probs, want[1])
