@@ -18,8 +18,9 @@
 // whatever its first slot, and groups past its last page end at once.
 //
 // 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.3 TB/s; a large copy reaches 5.1), 2112 rows of 32 + 2 x 8 heads
-// 15 (3.4 TB/s: a chain of latencies of 3 us before the first store), 256 decode rows of those 8.7, one 3.8.  One kernel for
-// both orders of pairs took 1.2 us more for the 2112 rows.
+// 15 (3.4 TB/s: a chain of latencies of 3 us before the first store), 256 decode rows of those 7.9, one 3.5.  One kernel for
+// both orders of pairs took 1.2 us more for the 2112 rows.  Rows past the last are loaded as that again: with branches around
+// the loads those waited for each other (8224 rows 159 us).  A single row alone is told apart (256 decode rows 8.9 us without).
 //
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
 // much on the host).  The upload clears the error word; without it one more workgroup reads the page ids of the whole batch
@@ -157,7 +158,11 @@ __global__ __launch_bounds__(256) void rope_split(RopeSplitArgs s, Table request
     p[j] = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
     f[j] = s.turns[pair];
   }
-  if (qk) {
+  if (n == 1) {
+    const T* y = src + (qk ? head * d + c0 : nqk * d + col);
+    if (there) a[0] = *reinterpret_cast<const uint4*>(y);
+    if (qk) a[8] = *reinterpret_cast<const uint4*>(y + half);
+  } else if (qk) {
     load(0, a);
   } else if (there) {
 #pragma unroll
