@@ -43,10 +43,13 @@ struct Passed {
   __device__ __forceinline__ int row(const LoraTile& t, int i) const { return t.rows >= 0 ? t.rows + i : rows[~t.rows + i]; }
 };
 
-// h and what its rounding to bf16 leaves out (16 bits together).
+// h and what its rounding to bf16 leaves out (16 bits together).  Finite values that would round to infinity are bf16's
+// largest and the rest; nothing is left of an infinity.
 __device__ __forceinline__ void split(float h, __bf16* hi, __bf16* lo) {
-  *hi = static_cast<__bf16>(h);
-  const float r = static_cast<float>(*hi);
+  constexpr float kMost = 0x1.fep127f;
+  float r = static_cast<float>(static_cast<__bf16>(h));
+  if (__builtin_isinf(r) && !__builtin_isinf(h)) r = __builtin_copysignf(kMost, h);
+  *hi = static_cast<__bf16>(r);
   *lo = static_cast<__bf16>(__builtin_isfinite(r) ? h - r : 0.f);
 }
 

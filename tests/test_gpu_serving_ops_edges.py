@@ -1,0 +1,43 @@
+"""GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
+hidden values past bf16's largest."""
+import numpy as np
+import pytest
+
+from _helpers import to64
+from test_gpu_serving_ops import E, U, _check_lora, _lora_case, _randn
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2511_04791_amd as duet
+    c = duet.Context(0)
+    yield c
+    c.close()
+
+
+# Of the adapters' second product: ranks of each of its kernels, padded ones among them, and tiles of few rows and of many.
+UP = [(rank, rows) for rank in (8, 16, 24, 64, 128) for rows in (3, 40)]
+
+
+@pytest.mark.parametrize("rank,rows", UP)
+def test_lora_hidden_values_past_the_largest_bf16(ctx, rank, rows):
+    """h between bf16's largest and fp32's, of both signs, times weights that bring the result back: finite in fp32, so here too."""
+    import paper_2511_04791_amd as duet
+    x = torch.zeros(rows, 16, dtype=torch.bfloat16)
+    x[:, 0] = torch.finfo(torch.bfloat16).max
+    x[:, 1] = torch.linspace(1.0, 1.75, rows) * 2.0 ** 119
+    x[1::2] = -x[1::2]
+    a = torch.zeros(1, rank, 16, dtype=torch.bfloat16)
+    a[:, :, :2] = 1
+    b = (_randn(9000 + rank, 1, 72, rank) * 2.0 ** -20).to(torch.bfloat16)
+    h = x.float() @ a[0].float().t()
+    assert torch.isfinite(h).all() and torch.isinf(h.to(torch.bfloat16)).all()
+    base = _randn(9001, rows, 72)
+    got = ctx.lora_add(x.cuda(), base.cuda(), duet.Lora(a.cuda(), b.cuda()), [(0, rows, 0)], [0])
+    _check_lora(got, np.array([[0, 0, rows, 0]]), [0], x, base, a, b, None)
