@@ -188,28 +188,25 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s, Lists lists) {
   else down_part<NT, 1>(s, lists, tile, lds);
 }
 
-// h of the i-th of the tiles' rows for STEPS times 32 ranks: the sum of its parts in their order, scaled, as its value in bf16 and
-// what that leaves out (16 bits together), in an MFMA operand's shape.  Ranks up to 16 (STEPS 0) have both along one MFMA.
+// h of the i-th of the tiles' rows for STEPS times 32 ranks (0: up to 16): the sum of its parts in their order, scaled, as its value
+// in bf16 and what that leaves out (16 bits together), in an MFMA operand's shape.
 template <int STEPS>
 struct H {
-  static constexpr int kSteps = STEPS ? STEPS : 1, kParts = STEPS ? 2 : 1;
-  bf16x8 v[kSteps][kParts];
+  static constexpr int kSteps = STEPS ? STEPS : 1;
+  bf16x8 high[kSteps], low[kSteps];
 };
 template <int STEPS>
 __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile, int i) {
-  constexpr int kParts = H<STEPS>::kParts;
   const int g = (threadIdx.x & 63) >> 4, chunks = s.rank / 8;
   const float scale = s.scale ? s.scale[tile.adapter] : 1.f;
   H<STEPS> h;
 #pragma unroll
   for (int st = 0; st < H<STEPS>::kSteps; ++st) {
     const int q = 4 * st + g;
-    if (q >= (STEPS ? chunks : 2 * chunks)) {
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) h.v[st][p] = zero8();
+    if (q >= chunks) {
+      h.high[st] = h.low[st] = zero8();
     } else {
-      const bool low = !STEPS && q >= chunks;
-      const float* part = s.part + (size_t)i * s.rank + 8 * (low ? q - chunks : q);
+      const float* part = s.part + (size_t)i * s.rank + 8 * q;
       const size_t step = (size_t)s.tokens * s.rank;
       f32x4 sum[2] = {};
       for (int p = 0; p < s.parts; ++p)
@@ -217,14 +214,25 @@ __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile
         for (int k = 0; k < 2; ++k) sum[k] += *reinterpret_cast<const f32x4*>(part + p * step + 4 * k);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        __bf16 hi, lo;
-        split(sum[e / 4][e % 4] * scale, &hi, &lo);
-        h.v[st][0][e] = low ? lo : hi;
-        if (kParts == 2) h.v[st][kParts - 1][e] = lo;
+        __bf16 high, low;
+        split(sum[e / 4][e % 4] * scale, &high, &low);
+        h.high[st][e] = high;
+        h.low[st][e] = low;
       }
     }
   }
   return h;
+}
+
+// The sum over h's low parts, as a finite number.  One that is not has an infinite or NaN weight in it, or weights so large that the
+// high parts' products (2^8 times the low ones' and more, of up to 128) are infinite: the high parts then give the infinity or NaN
+// that is B h's, where a low part, zero or of the other sign, would have made NaN of an infinity.  A median with a NaN is the
+// smallest of the others.
+__device__ __forceinline__ f32x4 finite(f32x4 v) {
+  constexpr float kMost = 0x1.fffffep127f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i], -kMost, kMost);
+  return v;
 }
 
 // out of a tile of up to 16 rows, 64 columns a wave at a time, every col_step-th from col0 on.  The 16 columns of an MFMA are
@@ -232,7 +240,7 @@ __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile
 // products.
 template <int STEPS, typename Lists>
 __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int col0, int col_step) {
-  constexpr int kSteps = H<STEPS>::kSteps, kParts = H<STEPS>::kParts;
+  constexpr int kSteps = H<STEPS>::kSteps;
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0;
   if (col0 >= s.d_out) return;
@@ -258,17 +266,19 @@ __device__ __forceinline__ void up_few(const LoraArgs& s, const Lists& lists, co
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const int q = 4 * st + g, c = min(c0 + 32 * (n / 2) + 8 * (m / 4) + 4 * (n % 2) + m % 4, s.d_out - 1);
-          const __bf16* wc = w + (size_t)c * s.rank;
-          if (STEPS) wv[st][n] = q < chunks ? load8(wc + 8 * q) : zero8();
-          else wv[st][n] = q < 2 * chunks ? load8(wc + 8 * (q < chunks ? q : q - chunks)) : zero8();
+          wv[st][n] = q < chunks ? load8(w + (size_t)c * s.rank + 8 * q) : zero8();
         }
       read(c0 + col_step, next);
 #pragma unroll
       for (int st = 0; st < kSteps; ++st)
 #pragma unroll
-        for (int p = 0; p < kParts; ++p)
+        for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], h.low[st], acc[n], 0, 0, 0);
 #pragma unroll
-          for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], h.v[st][p], acc[n], 0, 0, 0);
+      for (int n = 0; n < 4; ++n) acc[n] = finite(acc[n]);
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[st][n], h.high[st], acc[n], 0, 0, 0);
     } else {
       read(c0 + col_step, next);
     }
@@ -294,7 +304,7 @@ constexpr int kMostRank = STEPS ? 32 * STEPS : 16;
 template <int STEPS, typename Lists>
 __device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, const LoraTile& tile, int way, int ways,
                                         uint4* lds) {
-  constexpr int kSteps = H<STEPS>::kSteps, kParts = H<STEPS>::kParts, kUnits = 128 * kMostRank<STEPS> / 8 / 256;
+  constexpr int kSteps = H<STEPS>::kSteps, kUnits = 128 * kMostRank<STEPS> / 8 / 256;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, j = lane & 15, g = lane >> 4, chunks = s.rank / 8;
   const bool some = tile.adapter >= 0, rows = 16 * wave < tile.count;
   const __bf16* base[4];
@@ -341,17 +351,21 @@ __device__ __forceinline__ void up_many(const LoraArgs& s, const Lists& lists, c
     read(c0 + step, next);
     if (some) {
       const uint4* own = lds + j * (8 * chunks + 1);
-      const bool partial = STEPS ? chunks < 4 * STEPS : chunks < 2;  // zeros past the rank's end
+      const bool partial = chunks < 4 * kSteps;  // zeros past the rank's end
 #pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const int q = STEPS || g < chunks ? 4 * st + g : g - chunks;
+      for (int n = 0; n < 8; ++n) {
+        bf16x8 wv[kSteps];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-          bf16x8 wv = __builtin_bit_cast(bf16x8, own[n * chunks + min(q, chunks - 1)]);
-          if (partial && q >= chunks) wv = zero8();
-#pragma unroll
-          for (int p = 0; p < kParts; ++p) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.v[st][p], wv, acc[n], 0, 0, 0);
+        for (int st = 0; st < kSteps; ++st) {
+          const int q = 4 * st + g;
+          wv[st] = __builtin_bit_cast(bf16x8, own[n * chunks + min(q, chunks - 1)]);
+          if (partial && q >= chunks) wv[st] = zero8();
         }
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.low[st], wv[st], acc[n], 0, 0, 0);
+        acc[n] = finite(acc[n]);
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.high[st], wv[st], acc[n], 0, 0, 0);
       }
     }
 #pragma unroll

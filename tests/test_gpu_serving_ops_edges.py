@@ -1,5 +1,5 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
-hidden values past bf16's largest."""
+hidden values past bf16's largest, infinite weights."""
 import numpy as np
 import pytest
 
@@ -41,3 +41,26 @@ def test_lora_hidden_values_past_the_largest_bf16(ctx, rank, rows):
     base = _randn(9001, rows, 72)
     got = ctx.lora_add(x.cuda(), base.cuda(), duet.Lora(a.cuda(), b.cuda()), [(0, rows, 0)], [0])
     _check_lora(got, np.array([[0, 0, rows, 0]]), [0], x, base, a, b, None)
+
+
+@pytest.mark.parametrize("rank,rows", UP)
+def test_lora_infinite_weights(ctx, rank, rows):
+    """An infinity of B gives one of h's sign (NaN beside another of the other sign, or where h is zero), whatever h's own
+    rounding to bf16 leaves out; the other columns are as without it."""
+    import paper_2511_04791_amd as duet
+    meta, ids, x, base, a, b, _ = _lora_case(9100 + rank, 40, 136, rank, 2, [(0, rows, 0)], [1])
+    inf = float("inf")
+    a[1, 1] = 0  # a hidden value of zero
+    a[1, 2], a[1, 2, 0] = 0, 1
+    x[1, 0] = 3.0  # one that bf16 holds
+    b[1, 5, 0], b[1, 6, 2], b[1, 70, 2], b[1, 71, 0], b[1, 71, 2] = inf, inf, -inf, inf, -inf
+    b[1, 130, 1], b[1, 131, 3] = inf, float("nan")
+    lora = duet.Lora(a.cuda(), b.cuda())
+    got = to64(ctx.lora_add(x.cuda(), base.cuda(), lora, meta, ids))
+    with np.errstate(invalid="ignore"):
+        h = to64(x) @ to64(a)[1].T
+        want = to64(base) + (h[:, None] * to64(b)[1]).sum(-1)
+    special = [5, 6, 70, 71, 130, 131]
+    assert np.array_equal(got[:, special], want[:, special], equal_nan=True) and not np.isfinite(want[:, special]).any()
+    rest = [i for i in range(136) if i not in special]
+    _check_lora(torch.from_numpy(got[:, rest]), meta, ids, x, base[:, rest], a, b[:, rest], None)
