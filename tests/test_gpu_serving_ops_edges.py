@@ -1,5 +1,5 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
-hidden values past bf16's largest, infinite weights."""
+hidden values past bf16's largest, infinite weights, batches of no requests."""
 import numpy as np
 import pytest
 
@@ -64,3 +64,36 @@ def test_lora_infinite_weights(ctx, rank, rows):
     assert np.array_equal(got[:, special], want[:, special], equal_nan=True) and not np.isfinite(want[:, special]).any()
     rest = [i for i in range(136) if i not in special]
     _check_lora(torch.from_numpy(got[:, rest]), meta, ids, x, base[:, rest], a, b[:, rest], None)
+
+
+@pytest.mark.parametrize("workspace", [False, True])
+def test_empty_batches(ctx, workspace):
+    """A batch of no requests does nothing; a workspace's error word is cleared."""
+    import ctypes
+
+    import paper_2511_04791_amd as duet
+    from paper_2511_04791_amd import _native as N
+    lib, B = N.lib(), ctypes.byref
+    buf = torch.full((1 << 16,), 255, dtype=torch.uint8, device="cuda")
+    p = [buf.data_ptr() + 4096 * i for i in range(8)]
+    ws, st = p[6] if workspace else None, torch.cuda.current_stream().cuda_stream
+    none = N.Batch((N.SeqMeta * 1)(), 0)
+    rope = duet.Rope.base(10000.0, 64)
+    n = ctypes.c_size_t()
+    assert lib.duet_rope_workspace_bytes(B(none), B(n)) == 0 and n.value <= 4096
+    assert lib.duet_qkv_rope_split(ctx.handle, B(N.Shape(8, 2, 64, 16, N.BF16, 1)), B(rope.c), p[0], None, p[1], p[2], p[3], 1, p[4],
+                                   1, B(none), ws, 4096 if workspace else 0, st) == 0, lib.duet_last_error()
+    if workspace:
+        assert lib.duet_check_device_error(ctx.handle, ws, st) == 0
+    lora = N.Lora(p[0], p[1], None, 1, 8, 8, 8)
+    assert lib.duet_lora_workspace_bytes(B(lora), B(none), B(n)) == 0 and n.value <= 4096
+    assert lib.duet_lora_add(ctx.handle, B(lora), p[2], 8, p[3], 8, p[4], 8, B(none), None, p[6], 4096, st) == 0
+    assert lib.duet_sample(ctx.handle, p[0], N.BF16, 0, 8, 8, None, p[1], p[2], p[3], None, 0, st) == 0
+    torch.cuda.synchronize()
+    kept = buf.cpu().numpy()
+    kept[4096 * 6:4096 * 6 + 4] = 255
+    assert (kept == 255).all()
+    kc, vc = torch.zeros(1, 2, 16, 64, device="cuda"), torch.zeros(1, 2, 64, 16, device="cuda")
+    q = ctx.qkv_rope_split(torch.zeros(0, 768, device="cuda"), kc, vc, torch.zeros(0, 1, dtype=torch.int32, device="cuda"),
+                           np.zeros((0, 4), np.int32), duet.AttnShape(8, 2, 64, "f32"), rope)
+    assert q.shape == (0, 8, 64)
