@@ -1036,7 +1036,7 @@ __global__ __launch_bounds__(kThreads) void sample_max(SampleArgs a, Split* spli
   int first;
   const Logits<T> x = slice_of<T>(a, r, &first);
   Part p = largest(s, x, gridDim.x / 2, greedy);
-  p.index += first;
+  if (p.max > -INFINITY) p.index += first;  // a slice without a token keeps the index past all others
   if (tid == 0) row->part[blockIdx.x] = p;
 }
 

@@ -1,5 +1,5 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
-hidden values past bf16's largest, infinite weights, batches of no requests."""
+hidden values past bf16's largest, infinite weights, batches of no requests, masked slices."""
 import numpy as np
 import pytest
 
@@ -97,3 +97,21 @@ def test_empty_batches(ctx, workspace):
     q = ctx.qkv_rope_split(torch.zeros(0, 768, device="cuda"), kc, vc, torch.zeros(0, 1, dtype=torch.int32, device="cuda"),
                            np.zeros((0, 4), np.int32), duet.AttnShape(8, 2, 64, "f32"), rope)
     assert q.shape == (0, 8, 64)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sample_greedy_rows_with_masked_slices(ctx, rows, dtype):
+    """Rows that several workgroups share, where the mask leaves some of them no token: the lowest index of the largest logit."""
+    vocab = 70001
+    for kept in ([vocab - 1], [vocab - 3, vocab - 1], [0], [0, vocab - 1], [35000, 35001, vocab - 1], []):
+        x = torch.full((rows, vocab), -float("inf"))
+        for i in kept:
+            x[:, i] = -7.5
+        x = x.to(dtype)
+        want = kept[0] if kept else -1
+        u = torch.full((rows,), 0.5, device="cuda")
+        for params in (dict(temperature=torch.zeros(rows)), dict(top_k=torch.ones(rows, dtype=torch.int32)),
+                       dict(top_p=torch.zeros(rows))):
+            ids, probs = ctx.sample(x.cuda(), u, **{k: v.cuda() for k, v in params.items()})
+            assert (ids == want).all() and (probs == (1.0 if kept else 0.0)).all(), (kept, params)
