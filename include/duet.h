@@ -343,8 +343,8 @@ int duet_sample_workspace_bytes(int32_t rows, int32_t vocab, size_t* bytes);
  * first rank whose cumulative kept weight exceeds u[row] times all of it, probs[row] (may be NULL) its weight's
  * share of it.  u is a given random number in [0, 1); others are taken as 0 or the largest below 1.  NaN and -inf are
  * tokens that a mask took out; a row of nothing else gives -1 with probability 0.  +inf outweighs all finite
- * logits.  params NULL: all off.  The workspace lies on 16 bytes (NULL where none is needed).  The result does not depend
- * on other rows nor on the stream. */
+ * logits.  params NULL: all off.  ids and probs overlap neither each other nor an input.  The workspace lies on 16 bytes (NULL
+ * where none is needed).  The result does not depend on other rows nor on the stream. */
 int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
                 const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* workspace,
                 size_t workspace_bytes, void* stream);

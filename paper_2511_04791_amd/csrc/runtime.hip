@@ -2043,15 +2043,21 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
   if (workspace_bytes < need) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, need);
   if (need && reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
   if (row_stride < vocab) return fail(DUET_EINVAL, "row_stride %lld < vocab %d", (long long)row_stride, vocab);
+  if (rows == 0) return DUET_OK;
+  if (static_cast<const void*>(ids) == probs) return fail(DUET_EINVAL, "ids and probs are one");
+  const duet_sampling none{};
+  const duet_sampling& par = params ? *params : none;
+  for (const void* in : {logits, static_cast<const void*>(u), static_cast<const void*>(par.temperature),
+                         static_cast<const void*>(par.top_k), static_cast<const void*>(par.top_p),
+                         static_cast<const void*>(par.min_p)})
+    if (in && (in == ids || in == probs)) return fail(DUET_EINVAL, "ids or probs alias an input");
   SampleArgs a{};
   a.logits = logits;
   a.row_stride = row_stride;
-  if (params) {
-    a.temperature = params->temperature;
-    a.top_k = params->top_k;
-    a.top_p = params->top_p;
-    a.min_p = params->min_p;
-  }
+  a.temperature = par.temperature;
+  a.top_k = par.top_k;
+  a.top_p = par.top_p;
+  a.min_p = par.min_p;
   a.u = u;
   a.ids = ids;
   a.probs = probs;

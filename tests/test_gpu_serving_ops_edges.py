@@ -1,5 +1,6 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
-hidden values past bf16's largest, infinite weights, batches of no requests, masked slices."""
+hidden values past bf16's largest, infinite weights, batches of no requests, masked slices,
+results in the place of inputs."""
 import numpy as np
 import pytest
 
@@ -115,3 +116,24 @@ def test_sample_greedy_rows_with_masked_slices(ctx, rows, dtype):
                        dict(top_p=torch.zeros(rows))):
             ids, probs = ctx.sample(x.cuda(), u, **{k: v.cuda() for k, v in params.items()})
             assert (ids == want).all() and (probs == (1.0 if kept else 0.0)).all(), (kept, params)
+
+
+def test_sample_results_in_the_place_of_others(ctx):
+    """ids and probs are refused where they are each other or an input; nothing is written then."""
+    import paper_2511_04791_amd as duet
+    rows = 4
+    x = _randn(9200, rows, 100, dtype=torch.float32).cuda()
+    f = lambda v: torch.full((rows,), v, device="cuda")  # noqa: E731
+    u, p, t, m = f(0.5), f(0.9), f(0.7), f(0.1)
+    k, ids = torch.full((rows,), 7, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    as_int = lambda v: v.view(torch.int32)  # noqa: E731
+    params = dict(temperature=t, top_k=k, top_p=p, min_p=m)
+    inputs = [v.clone() for v in (x, u, t, k, p, m, ids)]
+    for kw in (dict(out=ids, probs=ids.view(torch.float32)), dict(out=k), dict(out=as_int(u)), dict(probs=u), dict(probs=t),
+               dict(probs=p), dict(out=as_int(m)), dict(probs=x.view(-1)[:rows])):
+        with pytest.raises(duet.DuetError) as e:
+            ctx.sample(x, u, **params, **kw)
+        assert e.value.code == -1
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(inputs, (x, u, t, k, p, m, ids)))
+    ctx.sample(x, u, **params, out=ids)
