@@ -672,7 +672,7 @@ class Context:
             N.check(lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
             workspace = self._space(workspace, n.value, stream)
             ws = (workspace.data_ptr(), workspace.nbytes)
-        if T == 0:
+        if len(b.rows) == 0:
             return q
         st = self._current(stream)
         N.check(lib.duet_qkv_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(rope.c), qkv.data_ptr(),
@@ -706,7 +706,7 @@ class Context:
         N.check(lib.duet_lora_workspace_bytes(ctypes.byref(lora.c), ctypes.byref(b.c), ctypes.byref(n)),
                 "duet_lora_workspace_bytes")
         workspace = self._space(workspace, n.value, stream)
-        if T == 0:
+        if len(b.rows) == 0:
             return out
         N.check(lib.duet_lora_add(self.handle, ctypes.byref(lora.c), x.data_ptr(), ld[0], base.data_ptr(), ld[1],
                                   out.data_ptr(), ld[2], ctypes.byref(b.c), ids, workspace.data_ptr(),

@@ -1,6 +1,6 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
 hidden values past bf16's largest, infinite weights, batches of no requests, masked slices,
-results in the place of inputs."""
+results in the place of inputs, broken batches."""
 import numpy as np
 import pytest
 
@@ -137,3 +137,18 @@ def test_sample_results_in_the_place_of_others(ctx):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(inputs, (x, u, t, k, p, m, ids)))
     ctx.sample(x, u, **params, out=ids)
+
+
+@pytest.mark.parametrize("meta", [[[1, 0, 1, 5], [1, -1, 1, 5]], [[0, 0, 0, 5]], [[1, 0, 2, 0], [0, 5, -5, 0]]])
+def test_broken_batches_that_end_at_row_zero(ctx, meta):
+    """Requests whose rows are not packed, or are none, are refused also where the last of them ends at row 0."""
+    import paper_2511_04791_amd as duet
+    meta = np.array(meta, np.int32)
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    with pytest.raises(duet.DuetError) as e:
+        ctx.qkv_rope_split(z(0, 768), z(3, 2, 16, 64), z(3, 2, 64, 16), z(2, 4, dt=torch.int32), meta,
+                           duet.AttnShape(8, 2, 64, "bf16"), duet.Rope.base(10000.0, 64))
+    assert e.value.code == -1 and "request" in str(e.value)
+    with pytest.raises(duet.DuetError) as e:
+        ctx.lora_add(z(0, 16), z(0, 24), duet.Lora(z(2, 8, 16), z(2, 24, 8)), meta, [0] * len(meta))
+    assert e.value.code == -1 and "request" in str(e.value)
