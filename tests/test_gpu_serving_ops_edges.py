@@ -1,6 +1,7 @@
 """GPU tests of the rotating QKV split, the adapters and sampling at values and batches where ordinary inputs do not reach:
 hidden values past bf16's largest, infinite weights, batches of no requests, masked slices,
-results in the place of inputs, broken batches."""
+results in the place of inputs, broken batches, adapters whose lists are
+uploaded."""
 import numpy as np
 import pytest
 
@@ -152,3 +153,65 @@ def test_broken_batches_that_end_at_row_zero(ctx, meta):
     with pytest.raises(duet.DuetError) as e:
         ctx.lora_add(z(0, 16), z(0, 24), duet.Lora(z(2, 8, 16), z(2, 24, 8)), meta, [0] * len(meta))
     assert e.value.code == -1 and "request" in str(e.value)
+
+
+# ---- adapters whose lists do not travel with the launch ---------------------------------------------
+
+
+def _lora_lists(reqs, ids):
+    """(tiles, listed rows) of the rows by adapter: tiles of up to 64 rows, listed where they do not follow each other."""
+    starts = np.concatenate([[0], np.cumsum([q for _, q, _ in reqs])])
+    tiles = listed = 0
+    for a in np.unique(ids):
+        rows = np.concatenate([np.arange(starts[r], starts[r + 1]) for r in range(len(reqs)) if ids[r] == a])
+        for i in range(0, len(rows), 64):
+            tile = rows[i:i + 64]
+            tiles += 1
+            listed += len(tile) if tile[-1] - tile[0] != len(tile) - 1 else 0
+    return tiles, listed
+
+
+def _interleaved(counts):
+    """Single rows of adapters 0, 1, ..., counts[a] of each, none beside its like as far as that goes."""
+    order = sorted((((i + 0.5) / n, a) for a, n in enumerate(counts) for i in range(n)))
+    return [(1, 1, 0)] * len(order), [a for _, a in order]
+
+
+LISTS = {
+    # Up to 128 tiles and 256 listed rows travel with the launch; both sides of each limit.
+    "256 listed": (_interleaved([128, 128]), (4, 256)),
+    "257 listed": (_interleaved([128, 126, 3]), (5, 257)),
+    "128 tiles": (([(1, 1, 0)] * 128, list(range(128))), (128, 0)),
+    "129 tiles": (([(1, 1, 0)] * 129, list(range(129))), (129, 0)),
+    # A running batch, rows without an adapter among them; long and short tiles, in runs and not; more tiles than 512.
+    "decode": (([(1, 1, 0)] * 431, [(i * 7) % 5 - 1 for i in range(431)]), None),
+    "mixed": (([(1, 1, 0)] * 300 + [(0, 130, 0), (0, 17, 3), (0, 64, 0), (0, 70, 1)],
+               [i % 3 for i in range(300)] + [0, 3, 2, 3]), None),
+    "many adapters": (([(1, 1, 0), (0, 2, 0)] * 300, list(range(600))), (600, 0)),
+}
+
+
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 64, 88, 128])
+@pytest.mark.parametrize("name", list(LISTS))
+def test_lora_lists(ctx, name, rank):
+    import paper_2511_04791_amd as duet
+    (reqs, ids), counts = LISTS[name]
+    tiles, listed = _lora_lists(reqs, np.asarray(ids))
+    assert (counts is None and (tiles > 128 or listed > 256)) or (tiles, listed) == counts
+    meta, ids, x, base, a, b, scale = _lora_case(9300 + rank, 72, 136, rank, max(ids) + 1, reqs, ids)
+    none = np.repeat(np.asarray(ids) < 0, meta[:, 2])
+    for in_place in (False, True):
+        given = base.cuda()
+        got = ctx.lora_add(x.cuda(), given, duet.Lora(a.cuda(), b.cuda(), scale.cuda()), meta, ids, out=given if in_place else None)
+        _check_lora(got, meta, ids, x, base, a, b, scale)
+        assert torch.equal(got.cpu()[none], base[none]) and (in_place or torch.equal(given.cpu(), base))
+
+
+@pytest.mark.parametrize("rank", [16, 64, 128])
+def test_lora_lists_of_wide_projections(ctx, rank):
+    """Uploaded lists with several parts of the input and several workgroups a tile."""
+    import paper_2511_04791_amd as duet
+    reqs = [(1, 1, 0)] * 290 + [(0, 200, 0)]
+    meta, ids, x, base, a, b, scale = _lora_case(9400 + rank, 4104, 1544, rank, 4, reqs, [i % 4 for i in range(290)] + [2])
+    got = ctx.lora_add(x.cuda(), base.cuda(), duet.Lora(a.cuda(), b.cuda(), scale.cuda()), meta, ids)
+    _check_lora(got, meta, ids, x, base, a, b, scale)
