@@ -515,7 +515,9 @@ __device__ Wanted decide(Shared& s, const Settings& c) {
     __syncthreads();
     plo = min(kb, s.found[1]), phi = min(kb, s.found[2]);
   }
-  if (c.min_p > 0) mb = min((int)((2e-16 - log(c.min_p)) * kBinsPerUnit), kBins - 1);  // weights that round to min-p count
+  // The bin that weights of min-p lie in.  No float's logarithm is nearer to a bin's edge than 1.7e-10 bins, and the roundings of a
+  // token's and of this are under 1e-11: tokens of earlier bins weigh more than min-p and those of later ones less.
+  if (c.min_p > 0) mb = min((int)(-log(c.min_p) * kBinsPerUnit), kBins - 1);
   const int elo = min(min(kb, plo), mb), ehi = min(min(kb, phi), mb);
   const double tlo = c.u * s.mass[elo], thi = c.u * s.mass[ehi + 1];
   look(3, [&](const Place& q) { return q.mass > tlo; });
