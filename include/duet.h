@@ -310,7 +310,7 @@ typedef struct {
   const void* a;       /* [num_adapters, rank, d_in] */
   const void* b;       /* [num_adapters, d_out, rank] */
   const float* scale;  /* [num_adapters] (device), or NULL: 1 */
-  int32_t num_adapters;
+  int32_t num_adapters; /* at most 2^20 */
   int32_t rank;        /* a multiple of 8 in [8, 128]; smaller ones are padded with zeros */
   int32_t d_in, d_out; /* multiples of 8, at most 2^20 */
 } duet_lora;
@@ -320,8 +320,10 @@ int duet_lora_workspace_bytes(const duet_lora* lora, const duet_batch* batch, si
 /* out[t] = base[t] + scale_a B_a (A_a x[t]) for the tokens t of every request with adapter a =
  * adapter_ids[r] (host, [num_reqs]), out[t] = base[t] where it is -1: x [T, d_in] the projection's input, base
  * [T, d_out] its output, rows in seq_meta order, ldx, ld_base and ld_out elements apart (multiples of 8).
- * bf16, fp32 sums, one rounding.  out may be base; otherwise it overlaps no input.  base and out may be some of the columns
- * of a wider projection.  The workspace lies on 16 bytes.  At most 2^22 tokens. */
+ * bf16, sums in fp32, out rounded once.  scale_a A_a x goes into the second product as two bf16 values, within 2^-17 of each of its
+ * elements, so out is off by its rounding and 2^-17 of the sum of the products' magnitudes (and the fp32 sums' errors).  out may be
+ * base; otherwise it overlaps no input.  base and out may be some of the columns of a wider projection.  The workspace lies on
+ * 16 bytes.  At most 2^22 tokens. */
 int duet_lora_add(duet_ctx* ctx, const duet_lora* lora, const void* x, int64_t ldx, const void* base, int64_t ld_base,
                   void* out, int64_t ld_out, const duet_batch* batch, const int32_t* adapter_ids, void* workspace,
                   size_t workspace_bytes, void* stream);

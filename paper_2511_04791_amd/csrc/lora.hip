@@ -1,9 +1,11 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   out[t] = base[t] + scale_a B_a (A_a x[t]),  a the adapter of token t's request.
-// Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h with one rounding to bf16.
+// Two kernels: h = A_a x in fp32 parts into the workspace, then out = base + scale_a B_a h, scale_a h as two bf16 (2^-17 of it
+// off at most), sums in fp32, rounded to bf16 once.
 // Both are bound by memory: x, base and out pass once, the adapters are a few MB.  us of the two: 64 rows, 4096 to 6144 columns,
-// rank 16, 4.2 + 5.9 (latency); 2112 rows, 4096 to 28672, rank 16, 8 + 55 (4.4 TB/s); 6298 rows, 14336 to 4096, rank 64, 47 + 28
-// (3.9 and 3.8 TB/s of x, base and out; the first has 500 workgroups for 256 CUs, which read A again for each tile).
+// rank 16, 4.1 + 6.1 (latency); 2112 rows, 4096 to 28672, rank 16, 8 + 56 (4.4 TB/s); 6298 rows, 14336 to 4096, rank 64, 47 + 29
+// (3.9 TB/s of x, and of base and out; the first has 500 workgroups for 256 CUs, which read A again for each tile: 364 MB in all,
+// of which 224 come from past the L2).  64 and 2112 rows, 4096 to 6144, rank 128: 7 + 19 and 14 + 30.
 //
 // The lists of up to kLoraPassedTiles tiles travel with the launches' arguments; longer ones are uploaded, a launch of its own
 // (64 rows of 16 adapters, 4096 to 6144 columns, rank 16: 20.5 us a call with it, 14.9 without).
@@ -188,8 +190,8 @@ __global__ __launch_bounds__(256) void lora_down(LoraArgs s, Lists lists) {
   else down_part<NT, 1>(s, lists, tile, lds);
 }
 
-// h of the i-th of the tiles' rows for STEPS times 32 ranks (0: up to 16): the sum of its parts in their order, scaled, as its value
-// in bf16 and what that leaves out (16 bits together), in an MFMA operand's shape.
+// h of the i-th of the tiles' rows for STEPS times 32 ranks (0: up to 16): the sum of its parts in their order, scaled, as its
+// value in bf16 and what that leaves out (16 bits together), in an MFMA operand's shape.
 template <int STEPS>
 struct H {
   static constexpr int kSteps = STEPS ? STEPS : 1;
@@ -224,8 +226,8 @@ __device__ __forceinline__ H<STEPS> h_of(const LoraArgs& s, const LoraTile& tile
   return h;
 }
 
-// The sum over h's low parts, as a finite number.  One that is not has an infinite or NaN weight in it, or weights so large that the
-// high parts' products (2^8 times the low ones' and more, of up to 128) are infinite: the high parts then give the infinity or NaN
+// The sum over h's low parts, as a finite number.  One that is not has an infinite or NaN weight in it, or weights so large that a
+// high part's product is infinite (2^8 times the low part's and more, of up to 128).  The high parts then give the infinity or NaN
 // that is B h's, where a low part, zero or of the other sign, would have made NaN of an infinity.  A median with a NaN is the
 // smallest of the others.
 __device__ __forceinline__ f32x4 finite(f32x4 v) {

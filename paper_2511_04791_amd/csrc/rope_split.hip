@@ -17,10 +17,12 @@
 // Request r (rows q_start .. q_start + q_len - 1) has the page groups from q_start / 16 + 2 r on: more than it needs,
 // whatever its first slot, and groups past its last page end at once.
 //
-// 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.3 TB/s; a large copy reaches 5.1), 2112 rows of 32 + 2 x 8 heads
-// 15 (3.4 TB/s: a chain of latencies of 3 us before the first store), 256 decode rows of those 7.9, one 3.5.  One kernel for
-// both orders of pairs took 1.2 us more for the 2112 rows.  Rows past the last are loaded as that again: with branches around
-// the loads those waited for each other (8224 rows 159 us).  A single row alone is told apart (256 decode rows 8.9 us without).
+// 8224 rows of 64 + 2 x 8 heads of 128 in bf16 take 77 us (4.4 TB/s; a large copy reaches 5.1), 2112 rows of 32 + 2 x 8 heads
+// 15 (3.4 TB/s: a chain of latencies of 3 us before the first store), in float32 31 (3.3 TB/s).  256 decode rows in bf16 7.9, one
+// 3.5: half of the former's 1056 workgroups are empty, two groups a request, and the kernel for up to kRopeTable requests, with
+// check_pages in it, has 97 registers: four waves a SIMD instead of the five of 96.  One kernel for both orders of pairs took
+// 1.2 us more for the 2112 rows.  Rows past the last are loaded as that again: with branches around the loads those waited for each
+// other (8224 rows 159 us).  A single row alone is told apart (256 decode rows 8.9 us without).
 //
 // Up to kRopeTable requests travel with the launch's arguments; more are uploaded, a launch of its own (2 to 4 us on the GPU, as
 // much on the host).  The upload clears the error word; without it one more workgroup reads the page ids of the whole batch

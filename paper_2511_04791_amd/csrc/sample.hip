@@ -7,8 +7,8 @@
 //
 // So every step looks for a place in the ranking, and a row need not be sorted: a histogram over
 // d = (max - x) / T gives the mass before each of its bins, and only the tokens of the few bins that can hold
-// the places looked for are listed, sorted and summed.  The mass of tokens with d >= kSpan (e^-48 each, at most
-// 4e-16 of the largest's over a row) is less than a unit in the last place of S in 64 bits.
+// the places looked for are listed, sorted and summed.  Tokens with d >= kSpan (e^-48 each, 3.8e-16 of the largest's over a row of
+// 2^18) are left out: less than two units in the last place of S in 64 bits, where S is 1, and less beside larger sums.
 //
 // Sums do not depend on the order of atomics: a token adds an integer to its bin, 2^45 + (1 - v) 2^33, with
 // v = e^-(d - d_bin) in (1 - 2^-6.4, 1] its weight relative to the bin's first.  The count stands in bits 45 on,
@@ -18,8 +18,13 @@
 // which the second pass lists as it goes; by one workgroup, or in slices by several where there are few rows.
 //
 // us of the steps for 256 float32 rows of 128256 logits, a CU each, 68 a call: maximum 17 (131 MB, 7.7 TB/s), histogram 19,
-// its sums 5, third pass 15, sorting 2, the answer 3.  One row on one CU: 5, 18, 5, 9 to 13, 2, 3: the histogram is bound by its
-// LDS additions (12 us without any arithmetic) and the arithmetic in 64 bits (16 without additions), the rest by latency.
+// its sums 5, third pass 15, sorting 2, the answer 3; the rest is the launch and the rows that take longest.  One row on one CU:
+// 5, 18, 5, 9 to 13, 2, 3: the histogram is bound by its LDS additions (12 us without any arithmetic) and the arithmetic in 64 bits
+// (16 without additions), the rest by latency.  256 bf16 rows 60 a call.  Rows that narrow takes are far slower: 256 rows of
+// deviation 0.5 at T = 2 383, 256 bf16 rows of deviation 0.8 around 10 (thousands of tokens of one value) 358, 64 such 362 and 333.
+//
+// 1024 threads leave a thread 128 registers, which is not enough for sample_row and sample_count, where every step and a call of
+// narrow meet: sample_count spills 24 (float32) and 21 (bf16) with 144 and 128 bytes of scratch a lane, sample_row 2 and none, 48 bytes.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -120,7 +125,7 @@ struct Logits {
   __device__ __forceinline__ float at(int i) const { return plain(as_float(x[i])); }
 
   // f(four logits, index of the first): a wave takes 64 vectors of four past the first boundary at a time, U such in flight;
-  // the up to 261 tokens before and after those come one a lane, with three masked ones.  Whole waves call f.
+  // the up to 258 tokens before and after those come one a lane, with three masked ones.  Whole waves call f.
   template <int U, typename F>
   __device__ __forceinline__ void fours(F f) const {
     typedef T Four __attribute__((ext_vector_type(4)));
@@ -1010,6 +1015,9 @@ __device__ void send_list(Split* row, const u64* list, int n, int room) {
 }
 
 // Whether the workgroup is the last of the row's to arrive; then the row's list is in s.list, unless it is too long.
+// What the workgroups hand over are device-scope atomic accesses, past the L2 of an XCD, and such an addition or store is done once
+// it is counted off.  So it is enough that each wave waits for its own before the barrier and the arrival; the orders are relaxed,
+// as a release would also write back the L2 and an acquire empty it, where none of this lies.
 __device__ bool last_of_row(Shared& s, Split* row, uint32_t* arrived) {
   const int tid = threadIdx.x;
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores and additions have completed
