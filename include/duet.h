@@ -351,6 +351,67 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
                 const duet_sampling* params, const float* u, int32_t* ids, float* probs, void* workspace,
                 size_t workspace_bytes, void* stream);
 
+/* A layer's paged cache.  scales NULL: k [P, h_kv, 16, d] and v [P, h_kv, d, 16] of shape.dtype.  Otherwise an 8-bit cache: the
+ * same layouts of bytes, e4m3 values (4 exponent bits, largest 448), and a byte e for each token, kv head and side: its d values
+ * are e4m3 times 2^(e - 127).  scales [P, h_kv, 2, 16]: the keys' bytes, then the values'.  All lie on 16 bytes. */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* scales;
+  int64_t num_phys_pages;
+} duet_kv_cache;
+
+/* The norm of each head of queries and keys: x / sqrt(mean(x^2) + eps) * weight over its d dimensions. */
+typedef struct {
+  const void* q_weight; /* [d] of shape.dtype (device, on 16 bytes), or NULL: ones */
+  const void* k_weight;
+  float eps;            /* above 0 */
+} duet_head_norm;
+
+/* duet_qkv_rope_split with the norm of each head before the rotation; rope NULL: nothing turns.  Sums, norm and rotation in fp32
+ * with one rounding.  Arguments, workspace and error word as there. */
+int duet_qkv_norm_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope,
+                             const void* qkv, const int32_t* positions, void* q, void* k_cache, void* v_cache,
+                             int64_t num_phys_pages, const int32_t* page_table, int32_t max_pages_per_req,
+                             const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream);
+/* The same into an 8-bit cache, norm and rope both optional (bf16 only): the keys as turned, in fp32, and the values, are stored
+ * over the smallest power of two, at least 2^-126, that brings the largest finite one of a token's head to at most 448, rounded
+ * once (to even); what is not finite is stored as NaN. */
+int duet_qkv_split8(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope,
+                    const void* qkv, const int32_t* positions, void* q, const duet_kv_cache* cache,
+                    const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch, void* workspace,
+                    size_t workspace_bytes, void* stream);
+/* Reads the requests' whole contexts (cached_len + q_len tokens) back from an 8-bit cache into bf16 pages k_out [N, h_kv, 16, d] and
+ * v_out [N, h_kv, d, 16]: logical page j of request r goes to page out_table[r * max_out_pages_per_req + j].  So prefill attention
+ * over an 8-bit cache is this call and duet_attn_mixed_batch on its pages.  Exact, but values past bf16's largest become infinities and
+ * those under its smallest normal one, 2^-126, are rounded.
+ * Slots past a request's last token stay as they are.  No page may be written through two entries of out_table.  Workspace as
+ * duet_qkv_rope_split: NULL for up to DUET_ROPE_NO_WORKSPACE requests, else of duet_rope_workspace_bytes().  Page ids outside either pool
+ * are neither read nor written and set the error word. */
+int duet_cache8_read(duet_ctx* ctx, const duet_shape* shape, const duet_kv_cache* cache, const int32_t* page_table,
+                     int32_t max_pages_per_req, const duet_batch* batch, void* k_out, void* v_out, int64_t num_out_pages,
+                     const int32_t* out_table, int32_t max_out_pages_per_req, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Prefixes that requests share (host arrays): every request r with of[r] = i >= 0 has the same physical pages for its first len[i]
+ * tokens.  They are read through the row of the first of them, once for all. */
+typedef struct {
+  int32_t num;        /* at most 65536 */
+  const int32_t* len; /* [num], multiples of 16, at most the context of each of its requests */
+  const int32_t* of;  /* [num_reqs], -1: none */
+} duet_prefixes;
+
+/* Workspace of duet_attn_decode_shared.  Host only. */
+int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes,
+                                size_t* bytes);
+/* Decode attention of one layer, as duet_attn_mixed_batch gives it for a batch of decode requests: bf16 q and out [R, h_q, d], over a
+ * bf16 or an 8-bit cache.  prefixes NULL: nothing is shared.  The result does not depend on the pages' placement nor on the stream;
+ * the order of its sums follows the batch's lengths and prefixes.  Probabilities are rounded to bf16.  q, out and the workspace lie on
+ * 16 bytes; out is none of the others.  Page ids outside the pool are not read, their tokens do not count, and they set the error word. */
+int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* q, const duet_kv_cache* cache,
+                            const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch,
+                            const duet_prefixes* prefixes, void* workspace, size_t workspace_bytes, void* out, void* stream);
+
 /* ---- GPU context ----------------------------------------------------------------------------- */
 
 /* Infrastructure (no passage of its own): the device state every call below uses.

@@ -21,7 +21,8 @@ from ._native import (AGG, BF16, CONCURRENT, CU_STEP, F32, KIND_DECODE, KIND_PRE
 from .workloads import AttnShape
 
 __all__ = ["AGG", "SPLIT", "CONCURRENT", "CuSplit", "Context", "Model", "DuetError", "attn_mixed_batch", "predict_iter_latency",
-           "choose_cu_split", "default_context", "AttnShape", "Rope", "Lora", "STATUS_SLO_INFEASIBLE", "STATUS_UNCALIBRATED"]
+           "choose_cu_split", "default_context", "AttnShape", "Rope", "Lora", "HeadNorm", "Cache8",
+           "STATUS_SLO_INFEASIBLE", "STATUS_UNCALIBRATED"]
 
 
 @dataclass(frozen=True)
@@ -411,6 +412,48 @@ class Lora:
                         int(a.shape[1]), int(a.shape[2]), int(b.shape[1]))
 
 
+class HeadNorm:
+    """The norm of each head of queries and keys (duet_head_norm): contiguous device tensors q_weight and k_weight [d] of the
+    projection's type, or None (ones)."""
+
+    def __init__(self, q_weight=None, k_weight=None, eps: float = 1e-6):
+        for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None and (t.dim() != 1 or not t.is_cuda or not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous device tensor [d]")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
+        self.c = N.HeadNorm(*[t.data_ptr() if t is not None else None for t in (q_weight, k_weight)], self.eps)
+
+
+class Cache8:
+    """An 8-bit paged cache (duet_kv_cache): contiguous device tensors k [P, h_kv, 16, d] and v [P, h_kv, d, 16] of uint8 or
+    torch.float8_e4m3fn, and scales [P, h_kv, 2, 16] uint8."""
+
+    def __init__(self, k, v, scales):
+        import torch
+        if k.dim() != 4 or k.shape[2] != 16 or tuple(v.shape) != (k.shape[0], k.shape[1], k.shape[3], 16):
+            raise ValueError("k must be [P, h_kv, 16, d] and v [P, h_kv, d, 16]")
+        if scales.dtype != torch.uint8 or tuple(scales.shape) != (k.shape[0], k.shape[1], 2, 16):
+            raise ValueError(f"scales must be uint8 [{k.shape[0]}, {k.shape[1]}, 2, 16]")
+        for t, name in ((k, "k"), (v, "v"), (scales, "scales")):
+            if t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+                raise ValueError(f"{name} must be uint8 or float8_e4m3fn")
+            if not t.is_cuda or not t.is_contiguous() or t.device != k.device:
+                raise ValueError("k, v and scales must be contiguous tensors of one device")
+        self.k, self.v, self.scales, self.device = k, v, scales, k.get_device()
+        self.pages, self.num_kv_heads, _, self.head_dim = (int(n) for n in k.shape)
+        self.c = N.KvCache(k.data_ptr(), v.data_ptr(), scales.data_ptr(), self.pages)
+
+    @staticmethod
+    def empty(pages: int, num_kv_heads: int, head_dim: int, device=0) -> "Cache8":
+        """A cache whose pages hold zeros."""
+        import torch
+        dev = torch.device("cuda", device) if isinstance(device, int) else device
+
+        def zeros(*shape):
+            return torch.zeros(pages, num_kv_heads, *shape, dtype=torch.uint8, device=dev)
+        return Cache8(zeros(16, head_dim), zeros(head_dim, 16), zeros(2, 16))
+
+
 def _stream_of(t, stream) -> ctypes.c_void_p:
     """The caller's stream, or torch's current one on the tensor's device."""
     if stream is None:
@@ -748,6 +791,162 @@ class Context:
                                 vocab, stride, ctypes.byref(params), u.data_ptr(), out.data_ptr(), probs.data_ptr(),
                                 workspace.data_ptr(), workspace.nbytes, self._current(stream)), "duet_sample")
         return out, probs
+
+    def _check_table(self, table, name, reqs):
+        if table.dim() != 2 or table.shape[0] < reqs:
+            raise ValueError(f"{name} must be [R, max_pages] with a row per request")
+        self._check_on(table, name, self._torch.int32, table.shape)
+
+    def _check_cache8(self, cache, shape: AttnShape):
+        if not isinstance(cache, Cache8):
+            raise TypeError("cache must be a Cache8")
+        if (cache.device, cache.num_kv_heads, cache.head_dim) != (self.device, shape.num_kv_heads, shape.head_dim):
+            raise ValueError(f"the cache must lie on cuda:{self.device} with {shape.num_kv_heads} heads of {shape.head_dim}")
+
+    def _request_space(self, b, workspace, stream, check_errors):
+        """Pointer and size of a workspace for the requests' table and the error word, and the tensor; none where nobody would
+        read the error word and the table travels with the launch."""
+        if workspace is None and not check_errors and len(b.rows) <= N.ROPE_NO_WORKSPACE:
+            return (None, 0), None
+        n = ctypes.c_size_t()
+        N.check(N.lib().duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+        workspace = self._space(workspace, n.value, stream)
+        return (workspace.data_ptr(), workspace.nbytes), workspace
+
+    def _split_args(self, qkv, page_table, b, shape: AttnShape, norm, rope, positions, q, stream):
+        """Checks and the query tensor of the splits with a norm."""
+        torch = self._torch
+        T, dt = b.end_row(), torch.bfloat16 if shape.dtype == "bf16" else torch.float32
+        hq, hkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+        self._check_on(qkv, "qkv", dt, (T, (hq + 2 * hkv) * d))
+        self._check_table(page_table, "page_table", len(b.rows))
+        if norm is not None:
+            for t, name in ((norm.q_weight, "q_weight"), (norm.k_weight, "k_weight")):
+                if t is not None:
+                    self._check_on(t, name, dt, (d,))
+        if positions is not None:
+            if rope is None:
+                raise ValueError("positions without a rope")
+            self._check_on(positions, "positions", torch.int32,
+                           (T,) if rope.axes == 1 and positions.dim() == 1 else (rope.axes, T))
+        if q is None:
+            return self._empty((T, hq, d), dt, stream)
+        self._check_on(q, "q", dt, (T, hq, d))
+        return q
+
+    def qkv_norm_rope_split(self, qkv, k_cache, v_cache, page_table, seq_meta, shape: AttnShape, norm: HeadNorm,
+                            rope: Rope | None = None, *, positions=None, q=None, workspace=None, stream=None,
+                            check_errors: bool = False):
+        """duet_qkv_norm_rope_split: qkv_rope_split with the norm of each head of queries and keys before the rotation (rope
+        None: no rotation)."""
+        b, lib = _BatchC(seq_meta), N.lib()
+        q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
+        pages = int(k_cache.shape[0])
+        self._check_on(k_cache, "k_cache", qkv.dtype, (pages, shape.num_kv_heads, shape.page_size, shape.head_dim))
+        self._check_on(v_cache, "v_cache", qkv.dtype, (pages, shape.num_kv_heads, shape.head_dim, shape.page_size))
+        ws, workspace = self._request_space(b, workspace, stream, check_errors)
+        if len(b.rows) == 0:
+            return q
+        st = self._current(stream)
+        N.check(lib.duet_qkv_norm_rope_split(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(norm.c),
+                                             ctypes.byref(rope.c) if rope is not None else None, qkv.data_ptr(),
+                                             positions.data_ptr() if positions is not None else None, q.data_ptr(),
+                                             k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(),
+                                             page_table.shape[1], ctypes.byref(b.c), *ws, st), "duet_qkv_norm_rope_split")
+        if check_errors:
+            N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
+        return q
+
+    def qkv_split8(self, qkv, cache: Cache8, page_table, seq_meta, shape: AttnShape, *, norm: HeadNorm | None = None,
+                   rope: Rope | None = None, positions=None, q=None, workspace=None, stream=None, check_errors: bool = False):
+        """duet_qkv_split8: the query rows out of qkv (bf16), keys and values into an 8-bit cache, after the norm of each head and
+        the rotation where they are given."""
+        b, lib = _BatchC(seq_meta), N.lib()
+        q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
+        self._check_cache8(cache, shape)
+        ws, workspace = self._request_space(b, workspace, stream, check_errors)
+        if len(b.rows) == 0:
+            return q
+        st = self._current(stream)
+        N.check(lib.duet_qkv_split8(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(norm.c) if norm is not None else None,
+                                    ctypes.byref(rope.c) if rope is not None else None, qkv.data_ptr(),
+                                    positions.data_ptr() if positions is not None else None, q.data_ptr(), ctypes.byref(cache.c),
+                                    page_table.data_ptr(), page_table.shape[1], ctypes.byref(b.c), *ws, st), "duet_qkv_split8")
+        if check_errors:
+            N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
+        return q
+
+    def cache8_read(self, cache: Cache8, page_table, seq_meta, k_out, v_out, out_table, *, workspace=None, stream=None,
+                    check_errors: bool = False):
+        """duet_cache8_read: the requests' contexts out of an 8-bit cache into bf16 pages k_out and v_out, whose ids out_table
+        [R, max_pages] gives."""
+        torch, b, lib = self._torch, _BatchC(seq_meta), N.lib()
+        shape = AttnShape(cache.num_kv_heads, cache.num_kv_heads, cache.head_dim, "bf16")
+        self._check_cache8(cache, shape)
+        self._check_table(page_table, "page_table", len(b.rows))
+        self._check_table(out_table, "out_table", len(b.rows))
+        pages = int(k_out.shape[0])
+        self._check_on(k_out, "k_out", torch.bfloat16, (pages, cache.num_kv_heads, 16, cache.head_dim))
+        self._check_on(v_out, "v_out", torch.bfloat16, (pages, cache.num_kv_heads, cache.head_dim, 16))
+        ws, workspace = self._request_space(b, workspace, stream, check_errors)
+        if len(b.rows) == 0:
+            return k_out, v_out
+        st = self._current(stream)
+        N.check(lib.duet_cache8_read(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(cache.c), page_table.data_ptr(),
+                                     page_table.shape[1], ctypes.byref(b.c), k_out.data_ptr(), v_out.data_ptr(), pages,
+                                     out_table.data_ptr(), out_table.shape[1], *ws, st), "duet_cache8_read")
+        if check_errors:
+            N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
+        return k_out, v_out
+
+    def attn_decode_shared(self, q, cache, page_table, seq_meta, *, prefix_of=None, prefix_len=None, out=None, workspace=None,
+                           stream=None, check_errors: bool = False):
+        """duet_attn_decode_shared: decode attention of bf16 q [R, h_q, d] over a Cache8, or a pair (k_cache, v_cache) of bf16
+        tensors.  prefix_of: for each request the index of the prefix it shares, or -1; prefix_len: the prefixes' tokens, whole
+        pages, whose pages the requests' rows of page_table have in common."""
+        torch, b, lib = self._torch, _BatchC(seq_meta), N.lib()
+        if q.dim() != 3:
+            raise ValueError("q must be [R, h_q, d]")
+        R, hq, d = b.end_row(), int(q.shape[1]), int(q.shape[2])
+        self._check_on(q, "q", torch.bfloat16, (R, hq, d))
+        if isinstance(cache, Cache8):
+            shape = AttnShape(hq, cache.num_kv_heads, d, "bf16")
+            self._check_cache8(cache, shape)
+            c = cache.c
+        else:
+            k, v = cache
+            pages, hkv = int(k.shape[0]), int(k.shape[1])
+            shape = AttnShape(hq, hkv, d, "bf16")
+            self._check_on(k, "k_cache", torch.bfloat16, (pages, hkv, 16, d))
+            self._check_on(v, "v_cache", torch.bfloat16, (pages, hkv, d, 16))
+            c = N.KvCache(k.data_ptr(), v.data_ptr(), None, pages)
+        self._check_table(page_table, "page_table", len(b.rows))
+        prefixes = None
+        if (prefix_of is None) != (prefix_len is None):
+            raise ValueError("prefix_of and prefix_len come together")
+        if prefix_of is not None:
+            of, length = (np.ascontiguousarray(x, dtype=np.int32) for x in (prefix_of, prefix_len))
+            if of.shape != (len(b.rows),) or length.ndim != 1:
+                raise ValueError(f"prefix_of must hold {len(b.rows)} values, one per request, and prefix_len one per prefix")
+            as_ints = ctypes.POINTER(ctypes.c_int32)
+            prefixes = ctypes.byref(N.Prefixes(len(length), length.ctypes.data_as(as_ints), of.ctypes.data_as(as_ints)))
+        if out is None:
+            out = self._empty((R, hq, d), torch.bfloat16, stream)
+        else:
+            self._check_on(out, "out", torch.bfloat16, (R, hq, d))
+        n, s = ctypes.c_size_t(), _shape_c(shape)
+        N.check(lib.duet_shared_workspace_bytes(ctypes.byref(s), ctypes.byref(b.c), prefixes, ctypes.byref(n)),
+                "duet_shared_workspace_bytes")
+        workspace = self._space(workspace, n.value, stream)
+        if len(b.rows) == 0:
+            return out
+        st = self._current(stream)
+        N.check(lib.duet_attn_decode_shared(self.handle, ctypes.byref(s), q.data_ptr(), ctypes.byref(c), page_table.data_ptr(),
+                                            page_table.shape[1], ctypes.byref(b.c), prefixes, workspace.data_ptr(),
+                                            workspace.nbytes, out.data_ptr(), st), "duet_attn_decode_shared")
+        if check_errors:
+            N.check(lib.duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")
+        return out
 
     def attn_iteration(self, qs, k_caches, v_caches, page_table, seq_meta, cu_split: CuSplit = CuSplit.agg(), *,
                        outs=None, workspace=None, stream=None, check_errors: bool = False):

@@ -60,6 +60,18 @@ class Sampling(ctypes.Structure):
     _fields_ = [("temperature", c_void_p), ("top_k", c_void_p), ("top_p", c_void_p), ("min_p", c_void_p)]
 
 
+class KvCache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("scales", c_void_p), ("num_phys_pages", c_int64)]
+
+
+class HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", ctypes.c_float)]
+
+
+class Prefixes(ctypes.Structure):
+    _fields_ = [("num", c_int32), ("len", ctypes.POINTER(c_int32)), ("of", ctypes.POINTER(c_int32))]
+
+
 class KernelTimes(ctypes.Structure):
     _fields_ = [("decode_partial_us", c_double), ("decode_reduce_us", c_double), ("prefill_us", c_double),
                 ("decode_total_us", c_double), ("iteration_us", c_double),
@@ -121,6 +133,15 @@ _SIGS = {
     "duet_sample_workspace_bytes": (c_int32, [c_int32, c_int32, P(c_size_t)]),
     "duet_sample": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int64, P(Sampling), c_void_p, c_void_p,
                               c_void_p, c_void_p, c_size_t, c_void_p]),
+    "duet_qkv_norm_rope_split": (c_int32, [c_void_p, P(Shape), P(HeadNorm), P(Rope), c_void_p, c_void_p, c_void_p, c_void_p,
+                                           c_void_p, c_int64, c_void_p, c_int32, P(Batch), c_void_p, c_size_t, c_void_p]),
+    "duet_qkv_split8": (c_int32, [c_void_p, P(Shape), P(HeadNorm), P(Rope), c_void_p, c_void_p, c_void_p, P(KvCache), c_void_p,
+                                  c_int32, P(Batch), c_void_p, c_size_t, c_void_p]),
+    "duet_cache8_read": (c_int32, [c_void_p, P(Shape), P(KvCache), c_void_p, c_int32, P(Batch), c_void_p, c_void_p, c_int64,
+                                   c_void_p, c_int32, c_void_p, c_size_t, c_void_p]),
+    "duet_shared_workspace_bytes": (c_int32, [P(Shape), P(Batch), P(Prefixes), P(c_size_t)]),
+    "duet_attn_decode_shared": (c_int32, [c_void_p, P(Shape), c_void_p, P(KvCache), c_void_p, c_int32, P(Batch), P(Prefixes),
+                                          c_void_p, c_size_t, c_void_p, c_void_p]),
     "duet_attn_mixed_batch": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32,
                                         P(Batch), CuSplit, c_void_p, c_size_t, c_void_p, c_void_p]),
     "duet_attn_mixed_batch_noalloc": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p,

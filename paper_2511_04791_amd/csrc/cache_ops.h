@@ -1,0 +1,65 @@
+// Launch interface of the operators around the 8-bit cache and shared prefixes (internal).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "serving_ops.h"
+
+namespace duet {
+
+// The rotating QKV split with a norm of each head before the rotation, into pages of the projection's type or 8-bit
+// ones (norm_split.hip).  rope.rot_dim 0: nothing turns.  For 8-bit pages k_cache and v_cache hold bytes.
+struct NormSplitArgs {
+  RopeSplitArgs rope;
+  const void *wq, *wk;  // [d] of rope.dtype, or null: ones
+  float eps;
+  int32_t norm;         // heads are normalised
+  uint8_t* scales;      // [P, h_kv, 2, 16] of 8-bit pages, else null
+};
+hipError_t launch_norm_split(const NormSplitArgs& a, const int4* requests, hipStream_t s);
+
+// Requests' pages out of the 8-bit cache into bf16 pages (cache8.hip).
+struct Cache8ReadArgs {
+  const uint8_t *k, *v, *scales;
+  const int32_t *table, *out_table;
+  __bf16 *k_out, *v_out;
+  const int2* reqs;  // [R + 1] (pages of the requests before it, tokens), uploaded; not used for up to kRopeTable requests
+  long long pages, out_pages;
+  int32_t* err;      // may be null for up to kRopeTable requests
+  int32_t num_reqs, max_pages, out_max_pages, h_kv, head_dim, groups;
+};
+hipError_t launch_cache8_read(const Cache8ReadArgs& a, const int2* reqs, hipStream_t s);
+
+// Decode attention over runs of pages that one or several requests share (attn_shared.hip).  An entry is a run and the
+// query rows that attend it: of `members` requests, listed from list[member0] on, the g heads of each kv head.
+struct SharedEntry {
+  int32_t first_item;  // items (split, kv head, row block) of the launch's entries before it
+  int32_t member0, members;
+  int32_t table_row, page0, tokens;  // the run: pages from page0 of a row of the page table
+  int32_t split_pages;
+  int32_t slot_off;    // split s of member r is slot first_slot[r] + slot_off + s
+};
+struct SharedArgs {
+  const __bf16* q;  // [R, h_q, d]
+  const void *k, *v;
+  const uint8_t* scales;  // null: bf16 pages
+  const int32_t* table;
+  long long pages;
+  __bf16* out;
+  const SharedEntry* entries;  // of both launches: n_wide entries for 64 rows a wave, then n_narrow for 16
+  const int32_t* list;         // requests
+  const int2* slots;           // [R] (first slot, slots)
+  float* acc;                  // [slots, h_q, d] unnormalised outputs
+  float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator)
+  int32_t* err;
+  int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
+  int32_t n_wide, n_narrow, wide_items, narrow_items;
+  float scale_log2;
+};
+constexpr int kWideRows = 64, kNarrowRows = 16;
+hipError_t launch_shared(const SharedArgs& a, hipStream_t s);
+
+}  // namespace duet

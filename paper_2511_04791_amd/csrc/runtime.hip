@@ -29,6 +29,7 @@
 #include "duet_internal.h"
 #include "gemm.h"
 #include "kernels.h"
+#include "cache_ops.h"
 #include "serving_ops.h"
 
 namespace {
@@ -1274,6 +1275,7 @@ struct DeviceGuard {
 // fits a grid.
 constexpr int kMaxOpTokens = 1 << 22;
 constexpr int kMaxSampleRows = 1 << 20;
+constexpr int kMaxReadPages = 1 << 24;  // of one read-back: a workgroup each
 
 int batch_tokens(const duet_batch* b, int32_t* tokens) {
   int64_t t = 0;
@@ -1313,6 +1315,33 @@ int check_rope(const duet_shape* s, const duet_rope* r) {
     if (!(std::fabs(r->inv_freq[i]) <= 64.0)) return fail(DUET_EINVAL, "frequency %d is not within [-64, 64]", i);
     if (r->pair_axis && r->pair_axis[i] >= r->axes)
       return fail(DUET_EINVAL, "pair %d: axis %d not in [0, %d)", i, r->pair_axis[i], r->axes);
+  }
+  return DUET_OK;
+}
+
+// What the splits with a rotation are called with (rope may be NULL: nothing turns); num_phys_pages, err and meta are left out.
+int rope_args(const duet_shape* shape, const duet_rope* rope, const void* qkv, const int32_t* positions, void* q,
+              void* k_cache, void* v_cache, const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch,
+              RopeSplitArgs* a) {
+  const int rc = batch_tokens(batch, &a->tokens);
+  if (rc) return rc;
+  a->qkv = qkv;
+  a->q = q;
+  a->k_cache = k_cache;
+  a->v_cache = v_cache;
+  a->page_table = page_table;
+  a->positions = positions;
+  a->num_reqs = batch->num_reqs;
+  a->max_pages = max_pages_per_req;
+  a->h_q = shape->num_q_heads;
+  a->h_kv = shape->num_kv_heads;
+  a->head_dim = shape->head_dim;
+  a->dtype = shape->dtype;
+  a->rot_dim = rope ? rope->rot_dim : 0;
+  a->adjacent = rope ? rope->adjacent : 0;
+  for (int i = 0; i < a->rot_dim / 2; ++i) {
+    a->turns[i] = rope->inv_freq[i] / 6.283185307179586476925;
+    a->pair_axis[i] = rope->pair_axis ? rope->pair_axis[i] : 0;
   }
   return DUET_OK;
 }
@@ -1899,26 +1928,8 @@ int duet_qkv_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_rope*
   if (workspace && workspace_bytes < request_table_bytes(batch))
     return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, request_table_bytes(batch));
   RopeSplitArgs a{};
-  if ((rc = batch_tokens(batch, &a.tokens))) return rc;
-  a.qkv = qkv;
-  a.q = q;
-  a.k_cache = k_cache;
-  a.v_cache = v_cache;
-  a.page_table = page_table;
-  a.positions = positions;
+  if ((rc = rope_args(shape, rope, qkv, positions, q, k_cache, v_cache, page_table, max_pages_per_req, batch, &a))) return rc;
   a.num_phys_pages = num_phys_pages;
-  a.num_reqs = batch->num_reqs;
-  a.max_pages = max_pages_per_req;
-  a.h_q = shape->num_q_heads;
-  a.h_kv = shape->num_kv_heads;
-  a.head_dim = shape->head_dim;
-  a.dtype = shape->dtype;
-  a.rot_dim = rope->rot_dim;
-  a.adjacent = rope->adjacent;
-  for (int i = 0; i < rope->rot_dim / 2; ++i) {
-    a.turns[i] = rope->inv_freq[i] / 6.283185307179586476925;
-    a.pair_axis[i] = rope->pair_axis ? rope->pair_axis[i] : 0;
-  }
   std::lock_guard<std::mutex> lock(ctx->mu);
   DeviceGuard device(ctx->device);
   HIP_TRY(device.status);
@@ -2067,6 +2078,329 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
   DeviceGuard device(ctx->device);
   HIP_TRY(device.status);
   HIP_TRY(launch_sample(a, workspace, static_cast<hipStream_t>(stream)));
+  return DUET_OK;
+}
+
+namespace {
+
+int check_cache8(const duet_kv_cache* c) {
+  if (!c) return fail(DUET_EINVAL, "cache is NULL");
+  int rc;
+  if ((rc = check_device_ptr(c->k, "cache.k")) || (rc = check_device_ptr(c->v, "cache.v"))) return rc;
+  for (const void* p : {static_cast<const void*>(c->k), static_cast<const void*>(c->v), static_cast<const void*>(c->scales)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "the cache must lie on 16 bytes");
+  if (c->k == c->v || c->k == c->scales || c->v == c->scales) return fail(DUET_EINVAL, "the cache's parts alias");
+  return DUET_OK;
+}
+
+// The splits with a norm: into pages of the projection's type (scales NULL) or 8-bit ones.
+int norm_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope, const void* qkv,
+               const int32_t* positions, void* q, const duet_kv_cache& cache, const int32_t* page_table,
+               int32_t max_pages_per_req, const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_shape(shape);
+  if (rc || (rope && (rc = check_rope(shape, rope)))) return rc;
+  if (norm && !(norm->eps > 0.f && std::isfinite(norm->eps))) return fail(DUET_EINVAL, "eps must be above 0");
+  if (cache.scales && shape->dtype != DUET_BF16) return fail(DUET_EUNSUPPORTED, "an 8-bit cache is written from bf16");
+  const void* q_l[1] = {qkv};
+  const void* k_l[1] = {cache.k};
+  const void* v_l[1] = {cache.v};
+  const void* o_l[1] = {q};
+  rc = check_call(ctx, shape, 1, q_l, k_l, v_l, cache.num_phys_pages, page_table, max_pages_per_req, batch,
+                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace ? workspace : ctx, o_l, 0);
+  if (rc) return rc;
+  const void* wq = norm ? norm->q_weight : nullptr;
+  const void* wk = norm ? norm->k_weight : nullptr;
+  for (const void* p : {qkv, static_cast<const void*>(q), static_cast<const void*>(cache.k), static_cast<const void*>(cache.v),
+                        wq, wk})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "qkv, q, the weights and the caches must lie on 16 bytes");
+  for (const void* o : {static_cast<const void*>(q), static_cast<const void*>(cache.k), static_cast<const void*>(cache.v),
+                        static_cast<const void*>(cache.scales)})
+    if (o && (o == qkv || o == wq || o == wk || o == page_table || o == positions))
+      return fail(DUET_EINVAL, "an output aliases an input");
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
+  if (!workspace && batch->num_reqs > kRopeTable)
+    return fail(DUET_EINVAL, "workspace is NULL with more than %d requests", kRopeTable);
+  if (workspace && workspace_bytes < request_table_bytes(batch))
+    return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, request_table_bytes(batch));
+  NormSplitArgs a{};
+  if ((rc = rope_args(shape, rope, qkv, positions, q, cache.k, cache.v, page_table, max_pages_per_req, batch, &a.rope))) return rc;
+  a.rope.num_phys_pages = cache.num_phys_pages;
+  a.wq = wq;
+  a.wk = wk;
+  a.eps = norm ? norm->eps : 1.f;
+  a.norm = norm != nullptr;
+  a.scales = cache.scales;
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  const UploadPart table{batch->reqs, batch->num_reqs * sizeof(int4), kAlign};
+  if (batch->num_reqs > kRopeTable && (rc = upload_parts(ctx, &table, 1, ws, st))) return rc;
+  if (ws) a.rope.meta = reinterpret_cast<const int4*>(ws + kAlign);
+  a.rope.err = reinterpret_cast<int32_t*>(ws);
+  HIP_TRY(launch_norm_split(a, reinterpret_cast<const int4*>(batch->reqs), st));
+  return DUET_OK;
+}
+
+// How decode attention over shared prefixes is cut.  The rule goes by the batch only.
+struct SharedPlan {
+  std::vector<SharedEntry> wide, narrow;
+  std::vector<int32_t> list;  // the requests themselves, then the groups' members
+  std::vector<int2> slots;
+  int64_t wide_items = 0, narrow_items = 0, n_slots = 0;
+  size_t off_entries = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
+};
+
+int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
+  if (!p) return DUET_OK;
+  if (p->num < 0 || p->num > 65536) return fail(DUET_EINVAL, "%d prefixes: 0 to 65536", p->num);
+  if ((p->num > 0 && !p->len) || (b->num_reqs > 0 && !p->of)) return fail(DUET_EINVAL, "the prefixes' lists are NULL");
+  for (int i = 0; i < p->num; ++i)
+    if (p->len[i] < 0 || p->len[i] % 16) return fail(DUET_EINVAL, "prefix %d: %d tokens are no whole pages", i, p->len[i]);
+  for (int r = 0; r < b->num_reqs; ++r) {
+    const int i = p->of[r];
+    if (i < -1 || i >= p->num) return fail(DUET_EINVAL, "request %d: prefix %d not in [-1, %d)", r, i, p->num);
+    if (i >= 0 && p->len[i] > b->reqs[r].cached_len + 1)
+      return fail(DUET_EINVAL, "request %d: its prefix of %d tokens is longer than its context", r, p->len[i]);
+  }
+  return DUET_OK;
+}
+
+int pages_per_split(int64_t pages, int64_t waves) {
+  const int64_t even = (pages + waves - 1) / waves;
+  return (int)std::min<int64_t>(64, std::max<int64_t>(8, (even + 3) / 4 * 4));
+}
+
+int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, SharedPlan* plan) {
+  const int R = b->num_reqs, g = s->num_q_heads / s->num_kv_heads, hkv = s->num_kv_heads;
+  for (int r = 0; r < R; ++r)
+    if (b->reqs[r].kind != DUET_KIND_DECODE) return fail(DUET_EUNSUPPORTED, "request %d is no decode request", r);
+  try {
+    std::vector<int32_t> count(p ? p->num : 0), first(p ? p->num : 0);
+    for (int r = 0; p && r < R; ++r)
+      if (p->of[r] >= 0) ++count[p->of[r]];
+    // A prefix of one request, or of no token, is nothing shared.
+    auto shared = [&](int r) { return p && p->of[r] >= 0 && count[p->of[r]] > 1 && p->len[p->of[r]] > 0; };
+    int64_t wide_pages = 0, narrow_pages = 0;
+    for (int r = 0; r < R; ++r)
+      narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
+    for (size_t i = 0; i < count.size(); ++i)
+      if (count[i] > 1) wide_pages += (int64_t)((count[i] * g + kWideRows - 1) / kWideRows) * (p->len[i] / 16);
+    const int wide_split = pages_per_split(wide_pages * hkv, 1024), narrow_split = pages_per_split(narrow_pages * hkv, 2048);
+    plan->list.resize(R);
+    for (int r = 0; r < R; ++r) plan->list[r] = r;
+    plan->slots.assign(R, make_int2(0, 0));
+    for (size_t i = 0; i < count.size(); ++i) {
+      if (count[i] < 2 || p->len[i] == 0) continue;
+      const int member0 = (int)plan->list.size(), pages = p->len[i] / 16, n = (pages + wide_split - 1) / wide_split;
+      for (int r = 0; r < R; ++r)
+        if (p->of[r] == (int)i) plan->list.push_back(r), plan->slots[r].y = n;
+      plan->wide.push_back(SharedEntry{(int32_t)plan->wide_items, member0, count[i], plan->list[member0], 0, p->len[i],
+                                       wide_split, 0});
+      plan->wide_items += (int64_t)n * hkv * ((count[i] * g + kWideRows - 1) / kWideRows);
+    }
+    for (int r = 0; r < R; ++r) {
+      const int before = shared(r) ? p->len[p->of[r]] : 0, tokens = b->reqs[r].cached_len + 1 - before;
+      if (tokens > 0) {
+        const int n = ((tokens + 15) / 16 + narrow_split - 1) / narrow_split;
+        plan->narrow.push_back(SharedEntry{(int32_t)plan->narrow_items, r, 1, r, before / 16, tokens, narrow_split,
+                                           plan->slots[r].y});
+        plan->slots[r].y += n;
+        plan->narrow_items += (int64_t)n * hkv;
+      }
+      plan->slots[r].x = (int)std::min<int64_t>(plan->n_slots, INT32_MAX);
+      plan->n_slots += plan->slots[r].y;
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(DUET_ENOMEM, "host allocation failed");
+  }
+  if (plan->wide_items > INT32_MAX / 2 || plan->narrow_items > INT32_MAX / 2 || plan->n_slots > INT32_MAX / 2)
+    return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
+  plan->off_entries = kAlign;
+  plan->off_list = plan->off_entries + align_up((plan->wide.size() + plan->narrow.size()) * sizeof(SharedEntry));
+  plan->off_slots = plan->off_list + align_up(plan->list.size() * sizeof(int32_t));
+  plan->off_ml = plan->off_slots + align_up(plan->slots.size() * sizeof(int2));
+  plan->off_acc = plan->off_ml + align_up((size_t)plan->n_slots * s->num_q_heads * sizeof(float2));
+  plan->total = plan->off_acc + align_up((size_t)plan->n_slots * s->num_q_heads * s->head_dim * sizeof(float));
+  return DUET_OK;
+}
+
+int check_shared(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes) {
+  int rc = check_shape(shape);
+  if (rc || (rc = check_batch(shape, batch, true)) || (rc = check_prefixes(batch, prefixes))) return rc;
+  if (shape->dtype != DUET_BF16) return fail(DUET_EUNSUPPORTED, "decode attention with shared prefixes runs bf16 only");
+  return DUET_OK;
+}
+
+}  // namespace
+
+int duet_qkv_norm_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope,
+                             const void* qkv, const int32_t* positions, void* q, void* k_cache, void* v_cache,
+                             int64_t num_phys_pages, const int32_t* page_table, int32_t max_pages_per_req,
+                             const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  if (!norm) return fail(DUET_EINVAL, "norm is NULL");
+  return norm_split(ctx, shape, norm, rope, qkv, positions, q, duet_kv_cache{k_cache, v_cache, nullptr, num_phys_pages},
+                    page_table, max_pages_per_req, batch, workspace, workspace_bytes, stream);
+}
+
+int duet_qkv_split8(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope,
+                    const void* qkv, const int32_t* positions, void* q, const duet_kv_cache* cache,
+                    const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  clear_error();
+  const int rc = check_cache8(cache);
+  if (rc) return rc;
+  if (!cache->scales) return fail(DUET_EINVAL, "cache.scales is NULL");
+  return norm_split(ctx, shape, norm, rope, qkv, positions, q, *cache, page_table, max_pages_per_req, batch, workspace,
+                    workspace_bytes, stream);
+}
+
+int duet_cache8_read(duet_ctx* ctx, const duet_shape* shape, const duet_kv_cache* cache, const int32_t* page_table,
+                     int32_t max_pages_per_req, const duet_batch* batch, void* k_out, void* v_out, int64_t num_out_pages,
+                     const int32_t* out_table, int32_t max_out_pages_per_req, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  clear_error();
+  int rc = check_cache8(cache);
+  if (rc) return rc;
+  if (!cache->scales) return fail(DUET_EINVAL, "cache.scales is NULL");
+  if ((rc = check_shape(shape))) return rc;
+  if (shape->dtype != DUET_BF16) return fail(DUET_EUNSUPPORTED, "an 8-bit cache is read back into bf16");
+  const void* k_l[1] = {cache->k};
+  const void* v_l[1] = {cache->v};
+  const void* o_l[1] = {k_out};
+  rc = check_call(ctx, shape, 1, k_l, k_l, v_l, cache->num_phys_pages, page_table, max_pages_per_req, batch,
+                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace ? workspace : ctx, o_l, 0);
+  if (rc || (rc = check_device_ptr(v_out, "v_out")) || (rc = check_device_ptr(out_table, "out_table"))) return rc;
+  if (num_out_pages < 1 || num_out_pages > (int64_t)INT32_MAX)
+    return fail(DUET_EINVAL, "num_out_pages %lld out of range", (long long)num_out_pages);
+  for (const void* o : {static_cast<const void*>(k_out), static_cast<const void*>(v_out)}) {
+    if (reinterpret_cast<uintptr_t>(o) % 16) return fail(DUET_EINVAL, "k_out and v_out must lie on 16 bytes");
+    if (o == cache->k || o == cache->v || o == cache->scales || o == page_table || o == out_table)
+      return fail(DUET_EINVAL, "an output aliases an input");
+  }
+  if (k_out == v_out) return fail(DUET_EINVAL, "k_out and v_out are one");
+  if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
+  if (!workspace && batch->num_reqs > kRopeTable)
+    return fail(DUET_EINVAL, "workspace is NULL with more than %d requests", kRopeTable);
+  if (workspace && workspace_bytes < request_table_bytes(batch))
+    return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, request_table_bytes(batch));
+  std::vector<int2> reqs;
+  int64_t groups = 0;
+  try {
+    for (int r = 0; r <= batch->num_reqs; ++r) {
+      const int n = r < batch->num_reqs ? batch->reqs[r].cached_len + batch->reqs[r].q_len : 0;
+      if (r < batch->num_reqs && (n + 15) / 16 > max_out_pages_per_req)
+        return fail(DUET_EINVAL, "request %d needs %d pages, out_table rows hold %d", r, (n + 15) / 16, max_out_pages_per_req);
+      reqs.push_back(make_int2((int)std::min<int64_t>(groups, INT32_MAX), n));
+      groups += (n + 15) / 16;
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(DUET_ENOMEM, "host allocation failed");
+  }
+  if (groups > kMaxReadPages) return fail(DUET_EUNSUPPORTED, "%lld pages, at most %d", (long long)groups, kMaxReadPages);
+  Cache8ReadArgs a{};
+  a.k = static_cast<const uint8_t*>(cache->k);
+  a.v = static_cast<const uint8_t*>(cache->v);
+  a.scales = cache->scales;
+  a.table = page_table;
+  a.out_table = out_table;
+  a.k_out = static_cast<__bf16*>(k_out);
+  a.v_out = static_cast<__bf16*>(v_out);
+  a.pages = cache->num_phys_pages;
+  a.out_pages = num_out_pages;
+  a.num_reqs = batch->num_reqs;
+  a.max_pages = max_pages_per_req;
+  a.out_max_pages = max_out_pages_per_req;
+  a.h_kv = shape->num_kv_heads;
+  a.head_dim = shape->head_dim;
+  a.groups = (int)groups;
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  const bool passed = !ws;
+  if (ws) {  // the upload clears the error word
+    const UploadPart table{reqs.data(), batch->num_reqs * sizeof(int2), kAlign};
+    if ((rc = upload_parts(ctx, &table, 1, ws, st))) return rc;
+    a.reqs = reinterpret_cast<const int2*>(ws + kAlign);
+    a.err = reinterpret_cast<int32_t*>(ws);
+  }
+  HIP_TRY(launch_cache8_read(a, passed ? reqs.data() : nullptr, st));
+  return DUET_OK;
+}
+
+int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes,
+                                size_t* bytes) {
+  clear_error();
+  int rc = check_shared(shape, batch, prefixes);
+  if (rc) return rc;
+  if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
+  SharedPlan plan;
+  if ((rc = plan_shared(shape, batch, prefixes, &plan))) return rc;
+  *bytes = plan.total;
+  return DUET_OK;
+}
+
+int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* q, const duet_kv_cache* cache,
+                            const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch,
+                            const duet_prefixes* prefixes, void* workspace, size_t workspace_bytes, void* out, void* stream) {
+  clear_error();
+  int rc = check_cache8(cache);
+  if (rc || (rc = check_shared(shape, batch, prefixes))) return rc;
+  const void* q_l[1] = {q};
+  const void* k_l[1] = {cache->k};
+  const void* v_l[1] = {cache->v};
+  const void* o_l[1] = {out};
+  rc = check_call(ctx, shape, 1, q_l, k_l, v_l, cache->num_phys_pages, page_table, max_pages_per_req, batch,
+                  duet_cu_split{DUET_AGG, DUET_TOTAL_CUS, 0, 1}, workspace, o_l, 0);
+  if (rc) return rc;
+  if (out == cache->scales || out == page_table) return fail(DUET_EINVAL, "out aliases an input");
+  for (const void* p : {q, static_cast<const void*>(out), static_cast<const void*>(workspace)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "q, out and the workspace must lie on 16 bytes");
+  SharedPlan plan;
+  if ((rc = plan_shared(shape, batch, prefixes, &plan))) return rc;
+  if (workspace_bytes < plan.total) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, plan.total);
+  if (batch->num_reqs == 0) return DUET_OK;
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  DeviceGuard device(ctx->device);
+  HIP_TRY(device.status);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  const size_t wide_bytes = plan.wide.size() * sizeof(SharedEntry);
+  const UploadPart parts[4] = {{plan.wide.data(), wide_bytes, plan.off_entries},
+                               {plan.narrow.data(), plan.narrow.size() * sizeof(SharedEntry), plan.off_entries + wide_bytes},
+                               {plan.list.data(), plan.list.size() * sizeof(int32_t), plan.off_list},
+                               {plan.slots.data(), plan.slots.size() * sizeof(int2), plan.off_slots}};
+  if ((rc = upload_parts(ctx, parts, 4, ws, st))) return rc;
+  SharedArgs a{};
+  a.q = static_cast<const __bf16*>(q);
+  a.k = cache->k;
+  a.v = cache->v;
+  a.scales = cache->scales;
+  a.table = page_table;
+  a.pages = cache->num_phys_pages;
+  a.out = static_cast<__bf16*>(out);
+  a.entries = reinterpret_cast<const SharedEntry*>(ws + plan.off_entries);
+  a.list = reinterpret_cast<const int32_t*>(ws + plan.off_list);
+  a.slots = reinterpret_cast<const int2*>(ws + plan.off_slots);
+  a.acc = reinterpret_cast<float*>(ws + plan.off_acc);
+  a.ml = reinterpret_cast<float2*>(ws + plan.off_ml);
+  a.err = reinterpret_cast<int32_t*>(ws);
+  a.num_reqs = batch->num_reqs;
+  a.max_pages = max_pages_per_req;
+  a.h_q = shape->num_q_heads;
+  a.h_kv = shape->num_kv_heads;
+  a.group = a.h_q / a.h_kv;
+  a.head_dim = shape->head_dim;
+  a.n_wide = (int)plan.wide.size();
+  a.n_narrow = (int)plan.narrow.size();
+  a.wide_items = (int)plan.wide_items;
+  a.narrow_items = (int)plan.narrow_items;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
+  HIP_TRY(launch_shared(a, st));
   return DUET_OK;
 }
 
