@@ -13,17 +13,14 @@
 // 8-bit values become bf16 exactly; a key's power of two multiplies its scores, a value's its probability.
 #include <hip/hip_runtime.h>
 
+#include "attn_shared_wide.h"
 #include "cache_ops.h"
 #include "wave_ops.h"
 
 namespace duet {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kSlack = 8.f;  // the reference maximum moves when a score passes it by 2^8
+using namespace shared;
 
 __device__ __forceinline__ bf16x8 widened(uint2 x) {
   union {
@@ -35,9 +32,6 @@ __device__ __forceinline__ bf16x8 widened(uint2 x) {
   u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.y, 1.f, false);
   u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.y, 1.f, true);
   return u.v;
-}
-__device__ __forceinline__ float power(unsigned word, int byte) {
-  return __uint_as_float((word >> (8 * byte) & 255u) << 23);
 }
 // The first n of 16 values of 8 or 16 bits, the others zero.
 __device__ __forceinline__ unsigned first_bytes(unsigned x, int n) {  // of 4
@@ -204,27 +198,75 @@ __global__ __launch_bounds__(256) void shared_partial(SharedArgs a, const Shared
   if (__any(bad) && lane == 0) atomicOr(a.err, 1);
 }
 
-// Joins the runs of one (request, query head): a wave.
-template <int D>
+template <int D, bool EIGHT>
+__global__ __launch_bounds__(kWideThreads, 1) void shared_wide(SharedArgs a) {
+  extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
+  const int item = blockIdx.x;
+  const SharedEntry e = a.entries[uniform(find_request(a.n_wide, [&](int i) { return a.entries[i].first_item <= item; }))];
+  wide_item<D, EIGHT>(a, e, item - e.first_item, lds);
+}
+
+// Joins the runs of one (request, query head): W waves, each every W-th run, eight loads in flight.
+template <int D, int W>
 __global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
   constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63, pair = uniform(4 * blockIdx.x + (threadIdx.x >> 6));
-  if (pair >= a.num_reqs * a.h_q) return;
+  __shared__ float part[W > 1 ? W : 1][D + 2];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), w = wave % W;
+  const int pair = (blockIdx.x * 4 + wave) / W;
+  if (pair >= a.num_reqs * a.h_q) return;  // the whole workgroup where W is 4
   const int r = pair / a.h_q;
   const int2 at = a.slots[r];
   const size_t first = (size_t)at.x * a.h_q + pair - r * a.h_q;
-  float top = -INFINITY;
-  for (int s = lane; s < at.y; s += 64) top = fmaxf(top, a.ml[first + (size_t)s * a.h_q].x);
+  float top = -INFINITY, den = 0.f, num[E] = {};
+  for (int s0 = w; s0 < at.y; s0 += 8 * W) {
+    float2 ml[8];
+    float x[8][E];
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  float den = 0.f, num[E] = {};
-  for (int s = 0; s < at.y; ++s) {
-    const size_t row = first + (size_t)s * a.h_q;
-    const float2 ml = a.ml[row];
-    const float w = fast_exp2(ml.x - top);
-    den += w * ml.y;
+    for (int u = 0; u < 8; ++u) {
+      const int s = min(s0 + u * W, at.y - 1);
+      const size_t row = first + (size_t)s * a.h_q;
+      ml[u] = a.ml[row];
+      if (s0 + u * W >= at.y) ml[u] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-    for (int i = 0; i < E; ++i) num[i] += w * a.acc[row * D + 64 * i + lane];
+      for (int i = 0; i < E; ++i) x[u][i] = a.acc[row * D + 64 * i + lane];
+    }
+    float to = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) to = fmaxf(to, ml[u].x);
+    if (to == -INFINITY) continue;  // runs without a key that counts
+    const float f = fast_exp2(top - to);
+    top = to;
+    den *= f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) num[i] *= f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float wgt = fast_exp2(ml[u].x - to);
+      if (s0 + u * W >= at.y) break;
+      den += wgt * ml[u].y;
+#pragma unroll
+      for (int i = 0; i < E; ++i) num[i] += wgt * x[u][i];
+    }
+  }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) part[w][64 * i + lane] = num[i];
+    if (lane == 0) part[w][D] = top, part[w][D + 1] = den;
+    __syncthreads();
+    if (w) return;
+    float to = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < W; ++u) to = fmaxf(to, part[u][D]);
+    den = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) num[i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      const float wgt = to == -INFINITY ? 0.f : fast_exp2(part[u][D] - to);
+      den += wgt * part[u][D + 1];
+#pragma unroll
+      for (int i = 0; i < E; ++i) num[i] += wgt * part[u][64 * i + lane];
+    }
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) a.out[(size_t)pair * D + 64 * i + lane] = static_cast<__bf16>(num[i] / den);
@@ -232,13 +274,19 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
 
 template <int D, bool EIGHT>
 hipError_t launch(const SharedArgs& a, hipStream_t s) {
-  if (a.wide_items)
-    hipLaunchKernelGGL((shared_partial<D, EIGHT, kWideRows / 16>), dim3((a.wide_items + 3) / 4), dim3(256), 0, s, a, a.entries,
-                       a.n_wide, a.wide_items);
+  if (a.wide_items) {
+    constexpr size_t kBytes = WideLds<D, EIGHT>::kBytes;
+    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_wide<D, EIGHT>),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+    if (set != hipSuccess) return set;
+    hipLaunchKernelGGL((shared_wide<D, EIGHT>), dim3(a.wide_items), dim3(kWideThreads), kBytes, s, a);
+  }
   if (a.narrow_items)
     hipLaunchKernelGGL((shared_partial<D, EIGHT, kNarrowRows / 16>), dim3((a.narrow_items + 3) / 4), dim3(256), 0, s, a,
                        a.entries + a.n_wide, a.n_narrow, a.narrow_items);
-  hipLaunchKernelGGL((shared_merge<D>), dim3((a.num_reqs * a.h_q + 3) / 4), dim3(256), 0, s, a);
+  const int pairs = a.num_reqs * a.h_q;
+  if (a.max_slots > 16) hipLaunchKernelGGL((shared_merge<D, 4>), dim3(pairs), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((shared_merge<D, 1>), dim3((pairs + 3) / 4), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -36,7 +36,7 @@ hipError_t launch_cache8_read(const Cache8ReadArgs& a, const int2* reqs, hipStre
 // Decode attention over runs of pages that one or several requests share (attn_shared.hip).  An entry is a run and the
 // query rows that attend it: of `members` requests, listed from list[member0] on, the g heads of each kv head.
 struct SharedEntry {
-  int32_t first_item;  // items (split, kv head, row block) of the launch's entries before it
+  int32_t first_item;  // items (split, kv head, row block) of its kind's entries before it
   int32_t member0, members;
   int32_t table_row, page0, tokens;  // the run: pages from page0 of a row of the page table
   int32_t split_pages;
@@ -49,17 +49,18 @@ struct SharedArgs {
   const int32_t* table;
   long long pages;
   __bf16* out;
-  const SharedEntry* entries;  // of both launches: n_wide entries for 64 rows a wave, then n_narrow for 16
+  const SharedEntry* entries;  // n_wide of many rows, then n_narrow of at most kNarrowRows
   const int32_t* list;         // requests
   const int2* slots;           // [R] (first slot, slots)
   float* acc;                  // [slots, h_q, d] unnormalised outputs
   float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator)
   int32_t* err;
   int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
-  int32_t n_wide, n_narrow, wide_items, narrow_items;
+  int32_t n_wide, n_narrow, wide_items, narrow_items, max_slots;
   float scale_log2;
 };
-constexpr int kWideRows = 64, kNarrowRows = 16;
+constexpr int kWideRows = 256, kNarrowRows = 16;
+constexpr int kWidePages = 1024;  // most pages of a wide split
 hipError_t launch_shared(const SharedArgs& a, hipStream_t s);
 
 }  // namespace duet

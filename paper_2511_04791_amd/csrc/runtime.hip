@@ -2149,6 +2149,7 @@ struct SharedPlan {
   std::vector<int32_t> list;  // the requests themselves, then the groups' members
   std::vector<int2> slots;
   int64_t wide_items = 0, narrow_items = 0, n_slots = 0;
+  int max_slots = 0;
   size_t off_entries = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
 };
 
@@ -2167,9 +2168,24 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
   return DUET_OK;
 }
 
-int pages_per_split(int64_t pages, int64_t waves) {
-  const int64_t even = (pages + waves - 1) / waves;
-  return (int)std::min<int64_t>(64, std::max<int64_t>(8, (even + 3) / 4 * 4));
+int blocks_of(int64_t rows) { return (int)((rows + kWideRows - 1) / kWideRows); }
+
+// Pages of a wide split, the fewest (at least four tiles) with which the runs fill the CUs once, or 1024 workgroups where they fill
+// them more often.
+int wide_split_pages(const std::vector<std::pair<int, int>>& runs, int hkv) {  // (pages, row blocks)
+  auto items = [&](int split) {
+    int64_t n = 0;
+    for (const auto& r : runs) n += (int64_t)((r.first + split - 1) / split) * r.second * hkv;
+    return n;
+  };
+  const int64_t most = items(kWidePages) <= DUET_TOTAL_CUS ? DUET_TOTAL_CUS : 4 * DUET_TOTAL_CUS;
+  int lo = 4, hi = kWidePages / 4;  // in tiles
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (items(4 * mid) <= most) hi = mid;
+    else lo = mid + 1;
+  }
+  return 4 * lo;
 }
 
 int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, SharedPlan* plan) {
@@ -2177,28 +2193,44 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
   for (int r = 0; r < R; ++r)
     if (b->reqs[r].kind != DUET_KIND_DECODE) return fail(DUET_EUNSUPPORTED, "request %d is no decode request", r);
   try {
-    std::vector<int32_t> count(p ? p->num : 0), first(p ? p->num : 0);
+    std::vector<int32_t> count(p ? p->num : 0), member0(p ? p->num : 0);
     for (int r = 0; p && r < R; ++r)
       if (p->of[r] >= 0) ++count[p->of[r]];
     // A prefix of one request, or of no token, is nothing shared.
     auto shared = [&](int r) { return p && p->of[r] >= 0 && count[p->of[r]] > 1 && p->len[p->of[r]] > 0; };
-    int64_t wide_pages = 0, narrow_pages = 0;
-    for (int r = 0; r < R; ++r)
-      narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
-    for (size_t i = 0; i < count.size(); ++i)
-      if (count[i] > 1) wide_pages += (int64_t)((count[i] * g + kWideRows - 1) / kWideRows) * (p->len[i] / 16);
-    const int wide_split = pages_per_split(wide_pages * hkv, 1024), narrow_split = pages_per_split(narrow_pages * hkv, 2048);
     plan->list.resize(R);
     for (int r = 0; r < R; ++r) plan->list[r] = r;
+    std::vector<std::pair<int, int>> runs;
+    int64_t narrow_pages = 0;
+    int at = R;
+    for (size_t i = 0; i < count.size(); ++i) {
+      if (count[i] < 2 || p->len[i] == 0) continue;
+      const int64_t rows = (int64_t)count[i] * g;
+      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, blocks_of(rows)});
+      else narrow_pages += p->len[i] / 16;
+      member0[i] = at;
+      at += count[i];
+    }
+    plan->list.resize(at);
+    std::vector<int32_t> next(member0);
+    for (int r = 0; r < R; ++r) {
+      if (shared(r)) plan->list[next[p->of[r]]++] = r;
+      narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
+    }
+    const int wide_split = wide_split_pages(runs, hkv);
+    const int64_t even = (narrow_pages * hkv + 2047) / 2048;
+    const int narrow_split = (int)std::min<int64_t>(64, std::max<int64_t>(8, (even + 3) / 4 * 4));
     plan->slots.assign(R, make_int2(0, 0));
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
-      const int member0 = (int)plan->list.size(), pages = p->len[i] / 16, n = (pages + wide_split - 1) / wide_split;
-      for (int r = 0; r < R; ++r)
-        if (p->of[r] == (int)i) plan->list.push_back(r), plan->slots[r].y = n;
-      plan->wide.push_back(SharedEntry{(int32_t)plan->wide_items, member0, count[i], plan->list[member0], 0, p->len[i],
-                                       wide_split, 0});
-      plan->wide_items += (int64_t)n * hkv * ((count[i] * g + kWideRows - 1) / kWideRows);
+      const int64_t rows = (int64_t)count[i] * g;
+      const bool wide = rows > kNarrowRows;
+      const int split = wide ? wide_split : narrow_split, n = (p->len[i] / 16 + split - 1) / split;
+      int64_t& items = wide ? plan->wide_items : plan->narrow_items;
+      (wide ? plan->wide : plan->narrow)
+          .push_back(SharedEntry{(int32_t)items, member0[i], count[i], plan->list[member0[i]], 0, p->len[i], split, 0});
+      items += (int64_t)n * hkv * (wide ? blocks_of(rows) : 1);
+      for (int m = 0; m < count[i]; ++m) plan->slots[plan->list[member0[i] + m]].y = n;
     }
     for (int r = 0; r < R; ++r) {
       const int before = shared(r) ? p->len[p->of[r]] : 0, tokens = b->reqs[r].cached_len + 1 - before;
@@ -2211,6 +2243,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       }
       plan->slots[r].x = (int)std::min<int64_t>(plan->n_slots, INT32_MAX);
       plan->n_slots += plan->slots[r].y;
+      plan->max_slots = std::max(plan->max_slots, plan->slots[r].y);
     }
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
@@ -2399,6 +2432,7 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.n_narrow = (int)plan.narrow.size();
   a.wide_items = (int)plan.wide_items;
   a.narrow_items = (int)plan.narrow_items;
+  a.max_slots = plan.max_slots;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
   HIP_TRY(launch_shared(a, st));
   return DUET_OK;
