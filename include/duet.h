@@ -365,7 +365,7 @@ typedef struct {
 typedef struct {
   const void* q_weight; /* [d] of shape.dtype (device, on 16 bytes), or NULL: ones */
   const void* k_weight;
-  float eps;            /* above 0 */
+  float eps;            /* above 0, not subnormal */
 } duet_head_norm;
 
 /* duet_qkv_rope_split with the norm of each head before the rotation; rope NULL: nothing turns.  Sums, norm and rotation in fp32

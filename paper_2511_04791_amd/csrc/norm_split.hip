@@ -11,6 +11,7 @@
 // 16 of them, and its sum or maximum is taken by that many lanes' moves inside a row of 16.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "cache_ops.h"
@@ -19,6 +20,8 @@
 
 namespace duet {
 namespace {
+
+constexpr int kRows = 4;  // of queries and keys a thread
 
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) {
@@ -36,19 +39,56 @@ __device__ __forceinline__ float over_lanes(float x, int lanes, F f) {
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ float most(float a, float b) { return fmaxf(a, b); }
 
-// The exponent's byte of a row whose largest finite magnitude is m: 448 is 1.75 2^8, so the power is 2^(exponent - 8), or
-// the next where the fraction is above 0.75.  At least 2^-126.
+// The exponent's byte of a row whose largest finite magnitude has these upper bits (fp32's, or bf16's alone): 448 is 1.75 2^8, so the
+// power is 2^(exponent - 8), or the next where the fraction is above 0.75.  At least 2^-126.
 __device__ __forceinline__ int scale_byte(float m) { return max((int)((__float_as_uint(m) + 0x1fffffu) >> 23) - 8, 1); }
-__device__ __forceinline__ float inverse_scale(int e) { return __uint_as_float((unsigned)(254 - e) << 23); }
+__device__ __forceinline__ int scale_byte_bf16(unsigned m) { return max((int)((m + 0x1fu) >> 7) - 8, 1); }
+__device__ __forceinline__ float power(int e) { return __uint_as_float((unsigned)e << 23); }
 __device__ __forceinline__ float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
-// Two values over the scale, as e4m3 in the low or high half; infinities become NaN (x times 0 is).
-template <bool HIGH>
-__device__ __forceinline__ int packed8(float a, float b, float inv, int old) {
-  return __builtin_amdgcn_cvt_pk_fp8_f32(fmaf(a, 0.f, a * inv), fmaf(b, 0.f, b * inv), old, HIGH);
+
+// Values over a power of two as e4m3, two in the low or high half of `old`: rounded to even, what is not finite as NaN.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned four8(float a, float b, float c, float d, float scale) {
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true));
+}
+__device__ __forceinline__ unsigned four8(unsigned ab, unsigned cd, float scale) {  // of bf16
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, ab), scale, false);
+  return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, cd), scale, true));
+}
+
+// bf16 magnitudes are ordered as their bits.
+__device__ __forceinline__ unsigned pk_max(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ unsigned largest(const uint4& x) {  // of eight, in the low half
+  const unsigned m = pk_max(pk_max(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), pk_max(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+  return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ unsigned finite16(unsigned x) {  // two magnitudes, what is not finite as 0
+  const unsigned lo = x & 0x7fffu, hi = x >> 16 & 0x7fffu;
+  return (lo < 0x7f80u ? lo : 0) | (hi < 0x7f80u ? hi : 0) << 16;
+}
+__device__ __forceinline__ unsigned largest_finite(const uint4& x) {
+  return largest(make_uint4(finite16(x.x), finite16(x.y), finite16(x.z), finite16(x.w)));
+}
+template <int CTRL>
+__device__ __forceinline__ unsigned moved_bits(unsigned x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ unsigned pk_max_over_lanes(unsigned x, int lanes) {  // 8 or 16 of them, as over_lanes
+  x = pk_max(x, moved_bits<0xB1>(x));
+  x = pk_max(x, moved_bits<0x4E>(x));
+  x = pk_max(x, moved_bits<0x141>(x));
+  return lanes >= 16 ? pk_max(x, moved_bits<0x140>(x)) : x;
 }
 
 template <typename T, bool ADJACENT, bool EIGHT, typename Table>
-__global__ __launch_bounds__(256) void norm_split(NormSplitArgs x, Table requests) {
+__global__ __launch_bounds__(256, 4) void norm_split(NormSplitArgs x, Table requests) {
   constexpr int N = Chunk<T>::N;
   constexpr bool kPassed = std::is_same<Table, Passed>::value;
   __shared__ float2 turn[16][kMaxPairs];
@@ -63,41 +103,57 @@ __global__ __launch_bounds__(256) void norm_split(NormSplitArgs x, Table request
     }
     --group;
   }
-  const int r = uniform(find_request(s.num_reqs, [&](int i) { return first_group(requests.row(i), i) <= group; }));
-  const Group at = group_of(requests[r], r, group);
+  int r = group;  // one row a request: one group each
+  Group at;
+  if (x.single) {
+    const Request q = requests[r];
+    at = Group{q.row, q.cached, 1, q.cached >> 4};
+  } else {
+    r = uniform(find_request(s.num_reqs, [&](int i) { return first_group(requests.row(i), i) <= group; }));
+    at = group_of(requests[r], r, group);
+  }
   const int n = at.rows, pos = at.pos, row = at.row, slot = pos & 15;
   if (n <= 0) return;
   const int id = s.page_table[(size_t)r * s.max_pages + at.page];
   const bool ok = page_ok(id, s.num_phys_pages);
   if (!kPassed && !ok && blockIdx.y == 0 && tid == 0) atomicOr(s.err, 1);
-  // Units as in rope_split.hip; those of values start on a multiple of 16, so that a head's lie in one row of lanes.
+  // A thread's unit: of queries and keys two chunks of kRows rows, neighbours in the row first; after those of all the page's
+  // rows, and from a multiple of 16 on, so that a head's lie in one row of lanes, eight columns of values, all rows.
   const int units = d / (2 * N), nqk = s.h_q + s.h_kv, width = (nqk + s.h_kv) * d;
-  const int qk_units = nqk * units, v_units = (qk_units + 15) & ~15, u = blockIdx.y * 256 + tid;
+  const int qk_units = nqk * units, v_units = (qk_units * x.parts + 15) & ~15, u = blockIdx.y * 256 + tid;
   const T* src = static_cast<const T*>(s.qkv) + (size_t)row * width;
-  const bool qk = u < qk_units;
-  const int head = u / units, k = u - head * units;
+  const bool qk = u < qk_units * x.parts;
+  const int part = u / qk_units, unit = u - part * qk_units, t0 = kRows * part;
+  const int head = unit / units, k = unit - head * units;
   const bool together = !ADJACENT && k < pairs / N;
   const int from = ADJACENT || together ? 0 : s.rot_dim - pairs, half = ADJACENT ? d / 2 : together ? pairs : (d - s.rot_dim) / 2;
   const int c0 = from + k * N, c1 = c0 + half;
   const int col = (u - v_units) * N;
   const bool value = !qk && col >= 0 && col < s.h_kv * d;
+  const bool there = qk && t0 < n;
   uint4 a[16];
-  auto load = [&](int t0) {
+  if (there && n == 1) {
+    a[0] = *reinterpret_cast<const uint4*>(src + head * d + c0);
+    a[kRows] = *reinterpret_cast<const uint4*>(src + head * d + c1);
+  } else if (there) {
+    const T* y = src + (size_t)t0 * width + head * d;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const T* y = src + (size_t)min(t0 + t, n - 1) * width + head * d;
-      a[t] = *reinterpret_cast<const uint4*>(y + c0);
-      a[8 + t] = *reinterpret_cast<const uint4*>(y + c1);
+    for (int t = 0; t < kRows; ++t) {
+      const T* z = y + (size_t)min(t, n - 1 - t0) * width;
+      a[t] = *reinterpret_cast<const uint4*>(z + c0);
+      a[kRows + t] = *reinterpret_cast<const uint4*>(z + c1);
     }
-  };
-  if (qk) {
-    load(0);
+  } else if (value && n == 1) {
+    a[0] = *reinterpret_cast<const uint4*>(src + nqk * d + col);
   } else if (value) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
-      a[t] = *reinterpret_cast<const uint4*>(src + (size_t)min(t, n - 1) * width + nqk * d + col);
+    for (int t = 0; t < 16; ++t)  // by the page's slots
+      a[t] = *reinterpret_cast<const uint4*>(src + (size_t)max(0, min(t - slot, n - 1)) * width + nqk * d + col);
   }
-  for (int i = tid; i < n * pairs; i += 256) {
+  // The sines of the rows that the workgroup's units of queries and keys have.
+  const int first_row = kRows * (int)(blockIdx.y * 256 / qk_units);
+  const int last_row = min(n, kRows * (min((int)blockIdx.y * 256 + 255, qk_units * x.parts - 1) / qk_units + 1));
+  for (int i = tid + first_row * pairs; i < last_row * pairs; i += 256) {
     const int t = i / pairs, pair = i - t * pairs;
     const int p = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
     turn[t][pair] = cos_sin_of(p * s.turns[pair]);
@@ -105,17 +161,23 @@ __global__ __launch_bounds__(256) void norm_split(NormSplitArgs x, Table request
   __syncthreads();
   if (qk) {
     const bool is_q = head < s.h_q;
-    if (!is_q && !ok) return;
+    if (!there || (!is_q && !ok)) return;
     const T* w = static_cast<const T*>(is_q ? x.wq : x.wk);
-    float w0[N], w1[N];
+    Chunk<T> w0, w1;
+    if (w) {
+      w0 = *reinterpret_cast<const Chunk<T>*>(w + c0);
+      w1 = *reinterpret_cast<const Chunk<T>*>(w + c1);
+    } else {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      w0[e] = w ? static_cast<float>(w[c0 + e]) : 1.f;
-      w1[e] = w ? static_cast<float>(w[c1 + e]) : 1.f;
+      for (int e = 0; e < N; ++e) w0.v[e] = w1.v[e] = static_cast<T>(1.f);
     }
     const size_t slab = (size_t)id * s.h_kv + head - s.h_q;
-    auto one = [&](int t, int t0) {
-      const Chunk<T> v0 = __builtin_bit_cast(Chunk<T>, a[t]), v1 = __builtin_bit_cast(Chunk<T>, a[8 + t]);
+    const float mean = 1.f / d;  // d is 64 or 128: exact
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+      if (t0 + t >= n) break;
+      __builtin_amdgcn_sched_barrier(0);  // a row at a time: the registers of all four together leave room for fewer waves
+      const Chunk<T> v0 = __builtin_bit_cast(Chunk<T>, a[t]), v1 = __builtin_bit_cast(Chunk<T>, a[kRows + t]);
       float y0[N], y1[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) y0[e] = static_cast<float>(v0.v[e]), y1[e] = static_cast<float>(v1.v[e]);
@@ -124,9 +186,9 @@ __global__ __launch_bounds__(256) void norm_split(NormSplitArgs x, Table request
 #pragma unroll
         for (int e = 0; e < N; ++e) sum = fmaf(y0[e], y0[e], fmaf(y1[e], y1[e], sum));
         sum = over_lanes(sum, units, add);
-        const float inv = 1.f / sqrtf(sum / d + x.eps);
+        const float inv = __builtin_amdgcn_rsqf(fmaf(sum, mean, x.eps));
 #pragma unroll
-        for (int e = 0; e < N; ++e) y0[e] *= inv * w0[e], y1[e] *= inv * w1[e];
+        for (int e = 0; e < N; ++e) y0[e] *= inv * static_cast<float>(w0.v[e]), y1[e] *= inv * static_cast<float>(w1.v[e]);
       }
       const float2* turns = turn[t0 + t];
       if constexpr (ADJACENT) {
@@ -151,105 +213,162 @@ __global__ __launch_bounds__(256) void norm_split(NormSplitArgs x, Table request
           y0[e] = p * z.x - q * z.y, y1[e] = p * z.y + q * z.x;
         }
       }
-      if constexpr (EIGHT) {
-        if (!is_q) {
+      const int token = slot + t0 + t;
+      if (EIGHT && !is_q) {
+        if constexpr (EIGHT) {
           float m = 0.f;
 #pragma unroll
-          for (int e = 0; e < N; ++e) m = fmaxf(m, fmaxf(finite_size(y0[e]), finite_size(y1[e])));
+          for (int e = 0; e < N; ++e) m = fmaxf(m, fmaxf(fabsf(y0[e]), fabsf(y1[e])));
+          if (__any(m == INFINITY)) {
+            m = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) m = fmaxf(m, fmaxf(finite_size(y0[e]), finite_size(y1[e])));
+          }
           m = over_lanes(m, units, most);
           const int byte = scale_byte(m);
-          const float inv = inverse_scale(byte);
-          int2 b0, b1;
-          b0.x = packed8<true>(y0[2], y0[3], inv, packed8<false>(y0[0], y0[1], inv, 0));
-          b0.y = packed8<true>(y0[6], y0[7], inv, packed8<false>(y0[4], y0[5], inv, 0));
-          b1.x = packed8<true>(y1[2], y1[3], inv, packed8<false>(y1[0], y1[1], inv, 0));
-          b1.y = packed8<true>(y1[6], y1[7], inv, packed8<false>(y1[4], y1[5], inv, 0));
-          uint8_t* y = static_cast<uint8_t*>(s.k_cache) + (slab * 16 + slot + t0 + t) * d;
-          *reinterpret_cast<int2*>(y + c0) = b0;
-          *reinterpret_cast<int2*>(y + c1) = b1;
-          if (k == 0) x.scales[slab * 32 + slot + t0 + t] = (uint8_t)byte;
-          return;
+          const float scale = power(byte);
+          const uint2 b0 = make_uint2(four8(y0[0], y0[1], y0[2], y0[3], scale), four8(y0[4], y0[5], y0[6], y0[7], scale));
+          const uint2 b1 = make_uint2(four8(y1[0], y1[1], y1[2], y1[3], scale), four8(y1[4], y1[5], y1[6], y1[7], scale));
+          uint8_t* y = static_cast<uint8_t*>(s.k_cache) + (slab * 16 + token) * d;
+          *reinterpret_cast<uint2*>(y + c0) = b0;
+          *reinterpret_cast<uint2*>(y + c1) = b1;
+          if (k == 0) x.scales[slab * 32 + token] = (uint8_t)byte;
         }
+      } else {
+        Chunk<T> o0, o1;
+#pragma unroll
+        for (int e = 0; e < N; ++e) o0.v[e] = static_cast<T>(y0[e]), o1.v[e] = static_cast<T>(y1[e]);
+        T* y = is_q ? static_cast<T*>(s.q) + ((size_t)(row + t0 + t) * s.h_q + head) * d
+                    : static_cast<T*>(s.k_cache) + (slab * 16 + token) * d;
+        *reinterpret_cast<uint4*>(y + c0) = __builtin_bit_cast(uint4, o0);
+        *reinterpret_cast<uint4*>(y + c1) = __builtin_bit_cast(uint4, o1);
       }
-      Chunk<T> o0, o1;
-#pragma unroll
-      for (int e = 0; e < N; ++e) o0.v[e] = static_cast<T>(y0[e]), o1.v[e] = static_cast<T>(y1[e]);
-      T* y = is_q ? static_cast<T*>(s.q) + ((size_t)(row + t0 + t) * s.h_q + head) * d
-                  : static_cast<T*>(s.k_cache) + (slab * 16 + slot + t0 + t) * d;
-      *reinterpret_cast<uint4*>(y + c0) = __builtin_bit_cast(uint4, o0);
-      *reinterpret_cast<uint4*>(y + c1) = __builtin_bit_cast(uint4, o1);
-    };
-    for (int t0 = 0; t0 < n; t0 += 8) {
-      if (t0) load(t0);
-#pragma unroll
-      for (int t = 0; t < 8; ++t)
-        if (t0 + t < n) one(t, t0);
     }
     return;
   }
   if (!value || !ok) return;
   const size_t slab = (size_t)id * s.h_kv + col / d;
-  Chunk<T> v[16];
-#pragma unroll
-  for (int t = 0; t < 16; ++t) v[t] = __builtin_bit_cast(Chunk<T>, a[t]);
   if constexpr (EIGHT) {
-    uint8_t* y = static_cast<uint8_t*>(s.v_cache) + (slab * d + col % d) * 16 + slot;
-    float inv[16];
+    uint8_t* y = static_cast<uint8_t*>(s.v_cache) + (slab * d + col % d) * 16;
+    uint8_t* bytes = x.scales + slab * 32 + 16;
+    const bool first = col % d == 0;
+    if (n == 1) {
+      y += slot;
+      bytes += slot;
+      unsigned m = largest(a[0]);
+      if (__any(m >= 0x7f80u)) m = largest_finite(a[0]);
+      const int byte = scale_byte_bf16(pk_max_over_lanes(m, d / N));
+      const unsigned w[2] = {four8(a[0].x, a[0].y, power(byte)), four8(a[0].z, a[0].w, power(byte))};
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      float m = 0.f;
-#pragma unroll
-      for (int e = 0; e < N; ++e) m = fmaxf(m, finite_size(static_cast<float>(v[t].v[e])));
-      m = over_lanes(m, d / N, most);
-      const int byte = scale_byte(m);
-      inv[t] = inverse_scale(byte);
-      if (col % d == 0 && t < n) x.scales[slab * 32 + 16 + slot + t] = (uint8_t)byte;
+      for (int e = 0; e < N; ++e) y[e * 16] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+      if (first) *bytes = (uint8_t)byte;
+      return;
     }
+    // The rows' exponents, two rows a register.
+    unsigned m[8], any = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      int p[4];
+    for (int t = 0; t < 8; ++t) {
+      m[t] = largest(a[2 * t]) | largest(a[2 * t + 1]) << 16;
+      any = pk_max(any, m[t]);
+    }
+    if (__any((any & 0xffffu) >= 0x7f80u || any >> 16 >= 0x7f80u)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        auto at8 = [&](int t) { const float f = static_cast<float>(v[t].v[e]); return fmaf(f, 0.f, f * inv[t]); };
-        p[i] = __builtin_amdgcn_cvt_pk_fp8_f32(at8(4 * i), at8(4 * i + 1), 0, false);
-        p[i] = __builtin_amdgcn_cvt_pk_fp8_f32(at8(4 * i + 2), at8(4 * i + 3), p[i], true);
+      for (int t = 0; t < 8; ++t) m[t] = largest_finite(a[2 * t]) | largest_finite(a[2 * t + 1]) << 16;
+    }
+    unsigned e4[4];  // the bytes of four rows
+    unsigned out[N][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int byte[4];
+#pragma unroll
+      for (int t = 0; t < 4; t += 2) {
+        const unsigned both = pk_max_over_lanes(m[2 * i + t / 2], d / N);
+        byte[t] = scale_byte_bf16(both & 0xffffu);
+        byte[t + 1] = scale_byte_bf16(both >> 16);
       }
-      if (n == 16) {
-        *reinterpret_cast<int4*>(y + e * 16) = make_int4(p[0], p[1], p[2], p[3]);
-      } else {
+      e4[i] = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+      // Four rows of four columns in a register each, turned into a column's four rows each.
 #pragma unroll
-        for (int t = 0; t < 16; ++t)
-          if (t < n) y[e * 16 + t] = (uint8_t)(p[t / 4] >> (8 * (t % 4)));
+      for (int h = 0; h < 2; ++h) {
+        unsigned w[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint4 v = a[4 * i + t];
+          w[t] = four8(h ? v.z : v.x, h ? v.w : v.y, power(byte[t]));
+        }
+        const unsigned lo01 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), hi01 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+        const unsigned lo23 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), hi23 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+        out[4 * h][i] = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u);
+        out[4 * h + 1][i] = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
+        out[4 * h + 2][i] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100u);
+        out[4 * h + 3][i] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302u);
       }
     }
-  } else {
-    T* y = static_cast<T*>(s.v_cache) + (slab * d + col % d) * 16 + slot;
-    if (n < 16) {
+    if (n == 16) {
 #pragma unroll
-      for (int t = 0; t < 16; ++t)
-        if (t < n)
-#pragma unroll
-          for (int e = 0; e < N; ++e) y[e * 16 + t] = v[t].v[e];
+      for (int e = 0; e < N; ++e) *reinterpret_cast<uint4*>(y + e * 16) = make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]);
+      if (first) *reinterpret_cast<uint4*>(bytes) = make_uint4(e4[0], e4[1], e4[2], e4[3]);
       return;
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e)
+    for (int i = 0; i < 4; ++i) {
+      if (4 * i >= slot && 4 * i + 4 <= slot + n) {
 #pragma unroll
-      for (int t = 0; t < 16; t += N) {
-        Chunk<T> o;
-#pragma unroll
-        for (int i = 0; i < N; ++i) o.v[i] = v[t + i].v[e];
-        *reinterpret_cast<uint4*>(y + e * 16 + t) = __builtin_bit_cast(uint4, o);
+        for (int e = 0; e < N; ++e) *reinterpret_cast<unsigned*>(y + e * 16 + 4 * i) = out[e][i];
+        if (first) *reinterpret_cast<unsigned*>(bytes + 4 * i) = e4[i];
+        continue;
       }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (4 * i + t < slot || 4 * i + t >= slot + n) continue;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e * 16 + 4 * i + t] = (uint8_t)(out[e][i] >> (8 * t));
+        if (first) bytes[4 * i + t] = (uint8_t)(e4[i] >> (8 * t));
+      }
+    }
+  } else {
+    T* y = static_cast<T*>(s.v_cache) + (slab * d + col % d) * 16;
+    if (n == 1) {
+      const Chunk<T> v = __builtin_bit_cast(Chunk<T>, a[0]);
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e * 16 + slot] = v.v[e];
+      return;
+    }
+    Chunk<T> v[16];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) v[t] = __builtin_bit_cast(Chunk<T>, a[t]);
+#pragma unroll
+    for (int t = 0; t < 16; t += N) {  // N slots of a column are 16 bytes
+      if (t >= slot && t + N <= slot + n) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          Chunk<T> o;
+#pragma unroll
+          for (int i = 0; i < N; ++i) o.v[i] = v[t + i].v[e];
+          *reinterpret_cast<uint4*>(y + e * 16 + t) = __builtin_bit_cast(uint4, o);
+        }
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (t + i < slot || t + i >= slot + n) continue;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e * 16 + t + i] = v[t + i].v[e];
+      }
+    }
   }
 }
 
 template <typename T, bool ADJACENT, bool EIGHT>
-hipError_t launch(const NormSplitArgs& x, const int4* requests, hipStream_t s) {
+hipError_t launch(NormSplitArgs x, const int4* requests, hipStream_t s) {
   const RopeSplitArgs& a = x.rope;
   const int n = 16 / sizeof(T), d = a.head_dim;
-  const int units = (((a.h_q + a.h_kv) * d / (2 * n) + 15) & ~15) + a.h_kv * d / n;
-  const int groups = a.tokens / 16 + 2 * a.num_reqs, columns = (units + 255) / 256;
+  int longest = 0;
+  for (int r = 0; r < a.num_reqs; ++r) longest = std::max(longest, requests[r].z);
+  x.single = longest == 1;
+  x.parts = (std::min(longest, 16) + kRows - 1) / kRows;
+  const int units = (((a.h_q + a.h_kv) * d / (2 * n) * x.parts + 15) & ~15) + a.h_kv * d / n;
+  const int groups = x.single ? a.num_reqs : a.tokens / 16 + 2 * a.num_reqs, columns = (units + 255) / 256;
   if (a.num_reqs <= kRopeTable) {
     Passed p;
     for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);

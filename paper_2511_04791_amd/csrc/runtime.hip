@@ -2099,7 +2099,8 @@ int norm_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* nor
                int32_t max_pages_per_req, const duet_batch* batch, void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_shape(shape);
   if (rc || (rope && (rc = check_rope(shape, rope)))) return rc;
-  if (norm && !(norm->eps > 0.f && std::isfinite(norm->eps))) return fail(DUET_EINVAL, "eps must be above 0");
+  if (norm && !(norm->eps >= 1.1754944e-38f && std::isfinite(norm->eps)))
+    return fail(DUET_EINVAL, "eps must be a finite normal number above 0");
   if (cache.scales && shape->dtype != DUET_BF16) return fail(DUET_EUNSUPPORTED, "an 8-bit cache is written from bf16");
   const void* q_l[1] = {qkv};
   const void* k_l[1] = {cache.k};
