@@ -1,8 +1,9 @@
 // Pages of the 8-bit cache read back into bf16 pages: a value is e4m3 times its token's power of two, which bf16 holds exactly
 // (four significant bits), past its largest as infinity, under its smallest normal one rounded.
 //
-// Bound by memory: 2 d + 2 bytes of a token and head read, 4 d written.  A workgroup takes a logical page of a request, all
-// heads; a thread 16 bytes at a time: 16 values of a key's row, or the 16 tokens of a dimension of values.
+// Bound by memory: 2 d + 2 bytes of a token and head read, 4 d written.  A workgroup takes a part of a logical page of a request; a
+// thread's piece is 8 bytes in and 16 out, so that neighbours write neighbouring chunks: 8 values of a key's row, or 8 tokens of a
+// dimension of values.  Its four pieces' loads go out together.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -22,6 +23,8 @@ struct UploadedPages {
   __device__ __forceinline__ int2 operator[](int r) const { return at[r]; }
 };
 
+constexpr int kPieces = 4;
+
 __device__ __forceinline__ float power(int byte) { return __uint_as_float((unsigned)byte << 23); }
 
 template <typename Table>
@@ -33,53 +36,52 @@ __global__ __launch_bounds__(256) void cache8_read(Cache8ReadArgs a, Table reqs)
   if (n <= 0) return;
   const int id = a.table[(size_t)r * a.max_pages + page], to = a.out_table[(size_t)r * a.out_max_pages + page];
   if (!page_ok(id, a.pages) || !page_ok(to, a.out_pages)) {
-    if (a.err && threadIdx.x == 0) atomicOr(a.err, 1);
+    if (a.err && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.err, 1);
     return;
   }
-  const int d = a.head_dim, all = a.h_kv * 2 * d;  // 16-byte pieces
-  for (int u = threadIdx.x; u < all; u += 256) {
-    const int head = u / (2 * d), i = u - head * 2 * d;
-    const bool key = i < d;
-    const int piece = key ? i : i - d;
-    const size_t from = (size_t)id * a.h_kv + head, slab = (size_t)to * a.h_kv + head;
-    const uint4 x = *reinterpret_cast<const uint4*>((key ? a.k : a.v) + from * 16 * d + piece * 16);
-    const uint8_t* scales = a.scales + from * 32;
-    const unsigned w[4] = {x.x, x.y, x.z, x.w};
-    float f[16];
+  const int d = a.head_dim, all = a.h_kv * 4 * d;
+  uint2 x[kPieces], e[kPieces];
+  auto piece = [&](int i) { return (int)(blockIdx.y * kPieces + i) * 256 + (int)threadIdx.x; };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
+  for (int i = 0; i < kPieces; ++i) {
+    const int u = min(piece(i), all - 1), head = u / (4 * d), w = u - head * 4 * d;  // 2 d pieces of keys, then of values
+    const bool key = w < 2 * d;
+    const int at8 = (key ? w : w - 2 * d) * 8;
+    const size_t from = (size_t)id * a.h_kv + head;
+    x[i] = *reinterpret_cast<const uint2*>((key ? a.k : a.v) + from * 16 * d + at8);
+    const uint8_t* scales = a.scales + from * 32;
+    if (key) e[i].x = scales[at8 / d];
+    else e[i] = *reinterpret_cast<const uint2*>(scales + 16 + (at8 & 8));
+  }
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    if (piece(i) >= all) break;
+    const int u = piece(i), head = u / (4 * d), w = u - head * 4 * d;
+    const bool key = w < 2 * d;
+    const int at8 = (key ? w : w - 2 * d) * 8;
+    const int token = key ? at8 / d : at8 & 8;
+    if (token >= n) continue;
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(j ? x[i].y : x[i].x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(j ? x[i].y : x[i].x, true);
       f[4 * j] = lo[0], f[4 * j + 1] = lo[1], f[4 * j + 2] = hi[0], f[4 * j + 3] = hi[1];
     }
-    const int token = piece / (d / 16);
-    if (key) {
-      if (token >= n) continue;
-      const float scale = power(scales[token]);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) f[j] *= scale;
-    } else {
-      const uint4 b = *reinterpret_cast<const uint4*>(scales + 16);
-      const unsigned e[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int j = 0; j < 16; ++j) f[j] *= power(e[j / 4] >> (8 * (j % 4)) & 255);
-    }
     struct Row {
-      __bf16 v[16];
+      __bf16 v[8];
     } o;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) o.v[j] = static_cast<__bf16>(f[j]);
-    __bf16* y = (key ? a.k_out : a.v_out) + slab * 16 * d + piece * 16;
-    if (key || n == 16) {
-      struct Two {
-        uint4 v[2];
-      };
-      const Two t = __builtin_bit_cast(Two, o);
-      reinterpret_cast<uint4*>(y)[0] = t.v[0];
-      reinterpret_cast<uint4*>(y)[1] = t.v[1];
+    for (int j = 0; j < 8; ++j) {
+      const unsigned byte = key ? e[i].x : (j < 4 ? e[i].x : e[i].y) >> (8 * (j % 4)) & 255;
+      o.v[j] = static_cast<__bf16>(f[j] * power(byte));
+    }
+    __bf16* y = (key ? a.k_out : a.v_out) + ((size_t)to * a.h_kv + head) * 16 * d + at8;
+    if (key || token + 8 <= n) {
+      *reinterpret_cast<uint4*>(y) = __builtin_bit_cast(uint4, o);
     } else {
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (j < n) y[j] = o.v[j];
+      for (int j = 0; j < 8; ++j)
+        if (token + j < n) y[j] = o.v[j];
     }
   }
 }
@@ -88,12 +90,13 @@ __global__ __launch_bounds__(256) void cache8_read(Cache8ReadArgs a, Table reqs)
 
 hipError_t launch_cache8_read(const Cache8ReadArgs& a, const int2* reqs, hipStream_t s) {
   if (a.groups <= 0) return hipSuccess;
+  const dim3 grid(a.groups, (a.h_kv * 4 * a.head_dim + 256 * kPieces - 1) / (256 * kPieces));
   if (reqs) {
     PassedPages p;
     for (int r = 0; r <= a.num_reqs; ++r) p.at[r] = reqs[r];
-    hipLaunchKernelGGL((cache8_read<PassedPages>), dim3(a.groups), dim3(256), 0, s, a, p);
+    hipLaunchKernelGGL((cache8_read<PassedPages>), grid, dim3(256), 0, s, a, p);
   } else {
-    hipLaunchKernelGGL((cache8_read<UploadedPages>), dim3(a.groups), dim3(256), 0, s, a, UploadedPages{a.reqs});
+    hipLaunchKernelGGL((cache8_read<UploadedPages>), grid, dim3(256), 0, s, a, UploadedPages{a.reqs});
   }
   return hipGetLastError();
 }

@@ -88,7 +88,7 @@ __device__ __forceinline__ unsigned pk_max_over_lanes(unsigned x, int lanes) {  
 }
 
 template <typename T, bool ADJACENT, bool EIGHT, typename Table>
-__global__ __launch_bounds__(256, 4) void norm_split(NormSplitArgs x, Table requests) {
+__global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x, Table requests) {
   constexpr int N = Chunk<T>::N;
   constexpr bool kPassed = std::is_same<Table, Passed>::value;
   __shared__ float2 turn[16][kMaxPairs];
