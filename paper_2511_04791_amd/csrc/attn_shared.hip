@@ -5,7 +5,7 @@
 // prefix is cut once and attended by the rows of every member, so its pages are read once for all of them, and a page
 // that one request holds alone is attended by the g heads of its group.
 //
-// A wave takes an item: a run (split), a kv head and up to 16 or 64 query rows, and walks the run 64 keys at a time.
+// Up to 16 rows: a wave, or a team of four that shares a run, walks it 64 keys at a time.
 //   S^T [tokens x rows] = K Q^T and O^T [dims x rows] += V^T P^T on 16x16x32 matrix instructions.
 // The tokens of S^T's rows are chosen so that a lane of quad y (16 lanes) gets all 16 tokens of the step's page y: instruction
 // p takes tokens 4 p .. 4 p + 3 of each of the four pages.  P^T is then already the operand of the second product, and a
@@ -41,49 +41,33 @@ __device__ __forceinline__ uint4 first_bytes(uint4 x, int n) {  // of 16
   return make_uint4(first_bytes(x.x, n), first_bytes(x.y, n - 4), first_bytes(x.z, n - 8), first_bytes(x.w, n - 12));
 }
 
-template <int D, bool EIGHT, int MT>
-__global__ __launch_bounds__(256) void shared_partial(SharedArgs a, const SharedEntry* entries, int n_entries, int n_items) {
+// What a wave has of its rows: lane (quad, col) holds row `col`, dims 16 n + 4 quad .. + 3 of the output.
+template <int D>
+struct Rows {
+  f32x4 acc[D / 16];
+  float l, m;
+};
+
+// The wave's steps of a run: pages first, first + 1 .. + 3, then `stride` pages on.
+template <int D, bool EIGHT>
+__device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n_tok, int j, int first, int stride,
+                                     const bf16x8 (&qf)[D / 32], Rows<D>& o) {
   constexpr int kB = EIGHT ? 1 : 2;           // bytes of a value
   constexpr int kLoads = D * kB / 64;         // 16-byte loads of a key's row by four lanes
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-  const int item = uniform(4 * blockIdx.x + (threadIdx.x >> 6));
-  if (item >= n_items) return;
-  const SharedEntry e = entries[uniform(find_request(n_entries, [&](int i) { return entries[i].first_item <= item; }))];
-  const int g = a.group, rows = e.members * g, blocks = (rows + 16 * MT - 1) / (16 * MT);
-  // Row blocks of one run and head next to each other, then heads, then runs.
-  const int i = item - e.first_item, block = i % blocks, j = i / blocks % a.h_kv, split = i / blocks / a.h_kv;
-  const int page0 = e.page0 + split * e.split_pages;
-  const int n_tok = min(e.tokens - 16 * split * e.split_pages, 16 * e.split_pages);
   const int n_pages = (n_tok + 15) >> 4;
-  const int* prow = a.table + (size_t)e.table_row * a.max_pages + page0;
-
-  int head_row[MT];  // request * h_q + head of the tile's row `col`, or -1
-  bf16x8 qf[MT][D / 32];
+  o.l = 0.f, o.m = -INFINITY;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int row = (block * MT + m) * 16 + col;
-    head_row[m] = row < rows ? a.list[e.member0 + row / g] * a.h_q + j * g + row % g : -1;
-    const __bf16* q = a.q + (size_t)max(head_row[m], 0) * D;
-#pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) {
-      // The dimensions of contraction step ks that this quad holds, as the keys' loads give them.
-      const int dim = EIGHT ? 64 * (ks / 2) + 16 * quad + 8 * (ks % 2) : 32 * ks + 8 * quad;
-      const uint4 u = head_row[m] >= 0 ? *reinterpret_cast<const uint4*>(q + dim) : make_uint4(0, 0, 0, 0);
-      qf[m][ks] = __builtin_bit_cast(bf16x8, u);
-    }
-  }
-  f32x4 acc[MT][D / 16];
-  float l[MT], m_ref[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    l[m] = 0.f, m_ref[m] = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int n = 0; n < D / 16; ++n) o.acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
   bool bad = false;
-  for (int p0 = 0; p0 < n_pages; p0 += 4) {
-    const int kpage = p0 + (col >> 2), vpage = p0 + quad;
-    const int kid = prow[min(kpage, n_pages - 1)], vid = prow[min(vpage, n_pages - 1)];
+  int kid = 0, vid = 0;
+  auto ids = [&](int p0) {
+    kid = prow[min(p0 + (col >> 2), n_pages - 1)];
+    vid = prow[min(p0 + quad, n_pages - 1)];
+  };
+  if (first < n_pages) ids(first);
+  for (int p0 = first; p0 < n_pages; p0 += stride) {
+    const int vpage = p0 + quad;
     const bool kok = page_ok(kid, a.pages), vok = page_ok(vid, a.pages);
     bad |= !vok;
     const size_t kslab = (size_t)(kok ? kid : 0) * a.h_kv + j, vslab = (size_t)(vok ? vid : 0) * a.h_kv + j;
@@ -96,17 +80,38 @@ __global__ __launch_bounds__(256) void shared_partial(SharedArgs a, const Shared
     for (int p = 0; p < 4; ++p)
 #pragma unroll
       for (int s = 0; s < kLoads; ++s) kr[p][s] = *reinterpret_cast<const uint4*>(kp + 4 * p * D * kB + 64 * s);
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n)
-#pragma unroll
-      for (int h = 0; h < kB; ++h) vr[n][h] = *reinterpret_cast<const uint4*>(vp + n * 256 * kB + 16 * h);
     uint4 ke = make_uint4(0, 0, 0, 0), ve = ke;
     if constexpr (EIGHT) {
       ke = *reinterpret_cast<const uint4*>(a.scales + vslab * 32);
       ve = *reinterpret_cast<const uint4*>(a.scales + vslab * 32 + 16);
     }
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+      for (int h = 0; h < kB; ++h) vr[n][h] = *reinterpret_cast<const uint4*>(vp + n * 256 * kB + 16 * h);
+    ids(p0 + stride);
     const bool part = __any(nv < 16);
+    // Scores S^T: the lane's are the 16 tokens of page `vpage` for row `col`.
+    float sc[16];
+    const unsigned kw[4] = {ke.x, ke.y, ke.z, ke.w};
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if constexpr (EIGHT) {
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(make_uint2(kr[p][i].x, kr[p][i].y)), qf[2 * i], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(make_uint2(kr[p][i].z, kr[p][i].w)), qf[2 * i + 1], s, 0, 0, 0);
+        } else {
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[p][i]), qf[i], s, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[4 * p + i] = s[i] * (EIGHT ? power(kw[p], i) * a.scale_log2 : a.scale_log2);
+    }
     if (part) {
+#pragma unroll
+      for (int t = 0; t < 16; ++t) sc[t] = t < nv ? sc[t] : -INFINITY;
       ve = first_bytes(ve, nv);
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) {
@@ -118,60 +123,36 @@ __global__ __launch_bounds__(256) void shared_partial(SharedArgs a, const Shared
         }
       }
     }
-    bf16x8 kf[4][D / 32];
+    float mx = sc[0];
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+    for (int t = 1; t < 16; ++t) mx = fmaxf(mx, sc[t]);
+    mx = max_rows(mx);
+    if (__any(mx > o.m + kSlack)) {
+      const float to = fmaxf(o.m, mx);
+      const float alpha = to == -INFINITY ? 1.f : fast_exp2(o.m - to);
+      o.m = to;
+      o.l *= alpha;
 #pragma unroll
-      for (int s = 0; s < kLoads; ++s) {
-        if constexpr (EIGHT) {
-          kf[p][2 * s] = widened(make_uint2(kr[p][s].x, kr[p][s].y));
-          kf[p][2 * s + 1] = widened(make_uint2(kr[p][s].z, kr[p][s].w));
-        } else {
-          kf[p][s] = __builtin_bit_cast(bf16x8, kr[p][s]);
-        }
-      }
-    float kscale[16], vscale[16];
-    const unsigned kw[4] = {ke.x, ke.y, ke.z, ke.w}, vw[4] = {ve.x, ve.y, ve.z, ve.w};
-#pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      kscale[t] = EIGHT ? power(kw[t / 4], t % 4) * a.scale_log2 : a.scale_log2;
-      vscale[t] = EIGHT ? power(vw[t / 4], t % 4) : 1.f;
+      for (int n = 0; n < D / 16; ++n) o.acc[n] *= alpha;
     }
-    bf16x8 pf[MT][2];
+    const float sub = o.m == -INFINITY ? 0.f : o.m;  // no key yet that counts: every weight is 0
+    // The denominator sums the probabilities as the second product takes them.
+    const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+    const unsigned vw[4] = {ve.x, ve.y, ve.z, ve.w};
+    bf16x8 pf[2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      float sc[16];
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[p][ks], qf[m][ks], s, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[4 * p + i] = s[i] * kscale[4 * p + i];
-      }
-      if (part) {
-#pragma unroll
-        for (int t = 0; t < 16; ++t) sc[t] = t < nv ? sc[t] : -INFINITY;
-      }
-      float mx = sc[0];
-#pragma unroll
-      for (int t = 1; t < 16; ++t) mx = fmaxf(mx, sc[t]);
-      mx = max_rows(mx);
-      if (__any(mx > m_ref[m] + kSlack)) {
-        const float to = fmaxf(m_ref[m], mx);
-        const float alpha = to == -INFINITY ? 1.f : fast_exp2(m_ref[m] - to);
-        m_ref[m] = to;
-        l[m] *= alpha;
-#pragma unroll
-        for (int n = 0; n < D / 16; ++n) acc[m][n] *= alpha;
-      }
-      const float sub = m_ref[m] == -INFINITY ? 0.f : m_ref[m];  // no key yet that counts: every weight is 0
-#pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        // The denominator sums the probabilities as the second product takes them.
-        const __bf16 w = static_cast<__bf16>(fast_exp2(sc[t] - sub));
-        l[m] += static_cast<float>(w);
-        pf[m][t / 8][t % 8] = EIGHT ? static_cast<__bf16>(static_cast<float>(w) * vscale[t]) : w;
+    for (int t = 0; t < 16; t += 2) {
+      const bf16x2 w = {static_cast<__bf16>(fast_exp2(sc[t] - sub)), static_cast<__bf16>(fast_exp2(sc[t + 1] - sub))};
+      o.l = __builtin_amdgcn_fdot2_f32_bf16(w, ones, o.l, false);
+      if constexpr (EIGHT) {
+        // Times a power of two: the upper halves of the products are exact.
+        const unsigned b = __builtin_bit_cast(unsigned, w);
+        const unsigned x = __float_as_uint(__uint_as_float(b << 16) * power(vw[t / 4], t % 4));
+        const unsigned y = __float_as_uint(__uint_as_float(b & 0xffff0000u) * power(vw[t / 4], t % 4 + 1));
+        const bf16x2 z = __builtin_bit_cast(bf16x2, highs(x, y));
+        pf[t / 8][t % 8] = z[0], pf[t / 8][t % 8 + 1] = z[1];
+      } else {
+        pf[t / 8][t % 8] = w[0], pf[t / 8][t % 8 + 1] = w[1];
       }
     }
 #pragma unroll
@@ -181,43 +162,140 @@ __global__ __launch_bounds__(256) void shared_partial(SharedArgs a, const Shared
         bf16x8 vf;
         if constexpr (EIGHT) vf = widened(h ? make_uint2(vr[n][0].z, vr[n][0].w) : make_uint2(vr[n][0].x, vr[n][0].y));
         else vf = __builtin_bit_cast(bf16x8, vr[n][h % kB]);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[m][h], acc[m][n], 0, 0, 0);
+        o.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h], o.acc[n], 0, 0, 0);
       }
   }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const float total = sum_rows(l[m]);
-    if (head_row[m] < 0) continue;
-    const int r = head_row[m] / a.h_q;
-    const size_t at = (size_t)(a.slots[r].x + e.slot_off + split) * a.h_q + (head_row[m] - r * a.h_q);
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(a.acc + at * D + 16 * n + 4 * quad) = acc[m][n];
-    if (quad == 0) a.ml[at] = make_float2(m_ref[m], total);
-  }
-  if (__any(bad) && lane == 0) atomicOr(a.err, 1);
+  o.l = sum_rows(o.l);
+  return __any(bad);
 }
 
+// An item of an entry of up to 16 rows: split, kv head, the run's pages, and the lane's row.
 template <int D, bool EIGHT>
-__global__ __launch_bounds__(kWideThreads, 1) void shared_wide(SharedArgs a) {
+struct Item {
+  int split, j, n_tok, rows;
+  const int* prow;
+  int head_row;  // request * h_q + head of row `col`, or -1
+  bf16x8 qf[D / 32];
+
+  template <typename Table>
+  __device__ __forceinline__ Item(const SharedArgs& a, const Table& tab, const SharedEntry& e, int i) {
+    const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, g = a.group;
+    j = i % a.h_kv;
+    split = i / a.h_kv;
+    rows = e.members * g;
+    const int skip = split * e.split_pages;
+    n_tok = min(e.tokens - 16 * skip, 16 * e.split_pages);
+    prow = a.table + (size_t)e.table_row * a.max_pages + e.page0 + skip;
+    head_row = col < rows ? tab.list[e.member0 + col / g] * a.h_q + j * g + col % g : -1;
+    const __bf16* q = a.q + (size_t)max(head_row, 0) * D;
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      // The dimensions of contraction step ks that this quad holds, as the keys' loads give them.
+      const int dim = EIGHT ? 64 * (ks / 2) + 16 * quad + 8 * (ks % 2) : 32 * ks + 8 * quad;
+      const uint4 u = head_row >= 0 ? *reinterpret_cast<const uint4*>(q + dim) : make_uint4(0, 0, 0, 0);
+      qf[ks] = __builtin_bit_cast(bf16x8, u);
+    }
+  }
+};
+
+template <int D>
+constexpr int team_floats(int rows) { return kTeamWaves * rows * (D + 4); }  // LDS; rows start on different banks
+
+// Teams first, a workgroup each, then lone waves.
+template <int D, bool EIGHT, typename Table>
+__global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, Table tab) {
+  extern __shared__ __attribute__((aligned(16))) float part[];
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, wave = uniform(threadIdx.x >> 6);
+  const bool direct = a.direct;
+  if (!direct && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
+  const bool team = (int)blockIdx.x < a.team_items;
+  const int item = team ? blockIdx.x : ((int)blockIdx.x - a.team_items) * kTeamWaves + wave;
+  if (!team && item >= a.lone_items) return;
+  const int e0 = a.n_wide + (team ? 0 : a.n_team), n = team ? a.n_team : a.n_lone;
+  const SharedEntry e = tab.entries[e0 + uniform(find_request(n, [&](int i) { return tab.entries[e0 + i].first_item <= item; }))];
+  const Item<D, EIGHT> it(a, tab, e, item - e.first_item);
+  Rows<D> o;
+  bool bad = walk<D, EIGHT>(a, it.prow, it.n_tok, it.j, team ? 4 * wave : 0, team ? 4 * kTeamWaves : 4, it.qf, o);
+  if (!team) {
+    if (direct && bad && lane == 0) atomicOr(a.err, 1);
+    if (it.head_row < 0) return;
+    if (direct) {
+      __bf16* y = a.out + (size_t)it.head_row * D + 4 * quad;
+      const float inv = 1.f / o.l;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[16 * n + i] = static_cast<__bf16>(o.acc[n][i] * inv);
+      return;
+    }
+    const int r = it.head_row / a.h_q;
+    const size_t at = (size_t)(tab.slots[r].x + e.slot_off + it.split) * a.h_q + (it.head_row - r * a.h_q);
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(a.acc + at * D + 16 * n + 4 * quad) = o.acc[n];
+    if (quad == 0) a.ml[at] = make_float2(o.m, marked(o.l, bad));
+    return;
+  }
+  // The team's four states are joined through LDS.
+  const int rows = it.rows;
+  float* mine = part + wave * rows * (D + 4) + col * (D + 4);
+  if (col < rows) {
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(mine + 16 * n + 4 * quad) = o.acc[n];
+    if (quad == 0) mine[D] = o.m, mine[D + 1] = o.l;
+  }
+  bad = __syncthreads_or(bad);
+  if (direct && bad && threadIdx.x == 0) atomicOr(a.err, 1);
+  const int g = a.group;
+  for (int x = 4 * threadIdx.x; x < rows * D; x += 4 * 64 * kTeamWaves) {
+    const int row = x / D, dim = x % D;
+    const float* p = part + row * (D + 4);
+    float m[kTeamWaves], to = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kTeamWaves; ++w) m[w] = p[w * rows * (D + 4) + D], to = fmaxf(to, m[w]);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kTeamWaves; ++w) {
+      const float f = m[w] == -INFINITY ? 0.f : fast_exp2(m[w] - to);
+      l += f * p[w * rows * (D + 4) + D + 1];
+      sum += f * *reinterpret_cast<const f32x4*>(p + w * rows * (D + 4) + dim);
+    }
+    const int r = tab.list[e.member0 + row / g], head = it.j * g + row % g;
+    if (direct) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      const float inv = 1.f / l;
+      *reinterpret_cast<bf16x4*>(a.out + ((size_t)r * a.h_q + head) * D + dim) =
+          bf16x4{static_cast<__bf16>(sum[0] * inv), static_cast<__bf16>(sum[1] * inv), static_cast<__bf16>(sum[2] * inv),
+                 static_cast<__bf16>(sum[3] * inv)};
+    } else {
+      const size_t at = (size_t)(tab.slots[r].x + e.slot_off + it.split) * a.h_q + head;
+      *reinterpret_cast<f32x4*>(a.acc + at * D + dim) = sum;
+      if (dim == 0) a.ml[at] = make_float2(to, marked(l, bad));
+    }
+  }
+}
+
+template <int D, bool EIGHT, typename Table>
+__global__ __launch_bounds__(kWideThreads, 1) void shared_wide(SharedArgs a, Table tab) {
   extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
   const int item = blockIdx.x;
-  const SharedEntry e = a.entries[uniform(find_request(a.n_wide, [&](int i) { return a.entries[i].first_item <= item; }))];
-  wide_item<D, EIGHT>(a, e, item - e.first_item, lds);
+  if (item == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
+  const SharedEntry e = tab.entries[uniform(find_request(a.n_wide, [&](int i) { return tab.entries[i].first_item <= item; }))];
+  wide_item<D, EIGHT>(a, tab, e, item - e.first_item, lds);
 }
 
 // Joins the runs of one (request, query head): W waves, each every W-th run, eight loads in flight.
-template <int D, int W>
-__global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
+template <int D, int W, typename Table>
+__global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs a, Table tab) {
   constexpr int E = D / 64;
   __shared__ float part[W > 1 ? W : 1][D + 2];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), w = wave % W;
-  const int pair = (blockIdx.x * 4 + wave) / W;
-  if (pair >= a.num_reqs * a.h_q) return;  // the whole workgroup where W is 4
+  const int pair = W >= 4 ? (int)blockIdx.x : (int)(blockIdx.x * 4 + wave) / W;
+  if (pair >= a.num_reqs * a.h_q) return;  // the whole workgroup where W is not 1
   const int r = pair / a.h_q;
-  const int2 at = a.slots[r];
+  const int2 at = tab.slots[r];
   const size_t first = (size_t)at.x * a.h_q + pair - r * a.h_q;
   float top = -INFINITY, den = 0.f, num[E] = {};
+  bool bad = false;
   for (int s0 = w; s0 < at.y; s0 += 8 * W) {
     float2 ml[8];
     float x[8][E];
@@ -226,13 +304,16 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
       const int s = min(s0 + u * W, at.y - 1);
       const size_t row = first + (size_t)s * a.h_q;
       ml[u] = a.ml[row];
-      if (s0 + u * W >= at.y) ml[u] = make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int i = 0; i < E; ++i) x[u][i] = a.acc[row * D + 64 * i + lane];
     }
     float to = top;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) to = fmaxf(to, ml[u].x);
+    for (int u = 0; u < 8; ++u) {
+      bad |= __float_as_uint(ml[u].y) >> 31;
+      ml[u].y = fabsf(ml[u].y);
+      to = fmaxf(to, ml[u].x);
+    }
     if (to == -INFINITY) continue;  // runs without a key that counts
     const float f = fast_exp2(top - to);
     top = to;
@@ -241,13 +322,14 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
     for (int i = 0; i < E; ++i) num[i] *= f;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
+      const bool there = s0 + u * W < at.y;  // selected, not branched on: the loads stay together
       const float wgt = fast_exp2(ml[u].x - to);
-      if (s0 + u * W >= at.y) break;
-      den += wgt * ml[u].y;
+      den += there ? wgt * ml[u].y : 0.f;
 #pragma unroll
-      for (int i = 0; i < E; ++i) num[i] += wgt * x[u][i];
+      for (int i = 0; i < E; ++i) num[i] += there ? wgt * x[u][i] : 0.f;
     }
   }
+  if (bad && lane == 0) atomicOr(a.err, 1);
   if constexpr (W > 1) {
 #pragma unroll
     for (int i = 0; i < E; ++i) part[w][64 * i + lane] = num[i];
@@ -272,30 +354,37 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a) {
   for (int i = 0; i < E; ++i) a.out[(size_t)pair * D + 64 * i + lane] = static_cast<__bf16>(num[i] / den);
 }
 
-template <int D, bool EIGHT>
-hipError_t launch(const SharedArgs& a, hipStream_t s) {
+template <int D, bool EIGHT, typename Table>
+hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
   if (a.wide_items) {
     constexpr size_t kBytes = WideLds<D, EIGHT>::kBytes;
-    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_wide<D, EIGHT>),
+    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_wide<D, EIGHT, Table>),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     if (set != hipSuccess) return set;
-    hipLaunchKernelGGL((shared_wide<D, EIGHT>), dim3(a.wide_items), dim3(kWideThreads), kBytes, s, a);
+    hipLaunchKernelGGL((shared_wide<D, EIGHT, Table>), dim3(a.wide_items), dim3(kWideThreads), kBytes, s, a, tab);
   }
-  if (a.narrow_items)
-    hipLaunchKernelGGL((shared_partial<D, EIGHT, kNarrowRows / 16>), dim3((a.narrow_items + 3) / 4), dim3(256), 0, s, a,
-                       a.entries + a.n_wide, a.n_narrow, a.narrow_items);
+  const int narrow = a.team_items + (a.lone_items + kTeamWaves - 1) / kTeamWaves;
+  if (narrow)
+    hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(narrow), dim3(64 * kTeamWaves),
+                       team_floats<D>(kNarrowRows) * sizeof(float), s, a, tab);
+  if (a.direct) return hipGetLastError();
   const int pairs = a.num_reqs * a.h_q;
-  if (a.max_slots > 16) hipLaunchKernelGGL((shared_merge<D, 4>), dim3(pairs), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((shared_merge<D, 1>), dim3((pairs + 3) / 4), dim3(256), 0, s, a);
+  if (a.max_slots > 64) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);
+  else if (a.max_slots > 16) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
+  else hipLaunchKernelGGL((shared_merge<D, 1, Table>), dim3((pairs + 3) / 4), dim3(256), 0, s, a, tab);
   return hipGetLastError();
+}
+template <typename Table>
+hipError_t launch(const SharedArgs& a, const Table& t, hipStream_t s) {
+  if (a.scales) return a.head_dim == 128 ? launch<128, true>(a, t, s) : launch<64, true>(a, t, s);
+  return a.head_dim == 128 ? launch<128, false>(a, t, s) : launch<64, false>(a, t, s);
 }
 
 }  // namespace
 
-hipError_t launch_shared(const SharedArgs& a, hipStream_t s) {
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, hipStream_t s) {
   if (a.num_reqs == 0) return hipSuccess;
-  if (a.scales) return a.head_dim == 128 ? launch<128, true>(a, s) : launch<64, true>(a, s);
-  return a.head_dim == 128 ? launch<128, false>(a, s) : launch<64, false>(a, s);
+  return passed ? launch(a, *passed, s) : launch(a, tables, s);
 }
 
 }  // namespace duet

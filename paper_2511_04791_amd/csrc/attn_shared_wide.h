@@ -21,6 +21,11 @@ __device__ __forceinline__ float power(unsigned word, int byte) {
   return __uint_as_float((word >> (8 * byte) & 255u) << 23);
 }
 
+// A denominator with the mark of a bad page.
+__device__ __forceinline__ float marked(float l, bool bad) {
+  return __uint_as_float((__float_as_uint(l) & 0x7fffffffu) | (bad ? 0x80000000u : 0u));
+}
+
 constexpr int kWideThreads = 512, kWideWaves = 8;
 constexpr int kTile = 64;  // keys of a tile: four pages
 
@@ -34,8 +39,8 @@ struct WideLds {
 };
 
 // One item of a wide entry: up to 256 rows, 32 a wave, over the pages page0 .. of a run of n_pages whole pages.
-template <int D, bool EIGHT>
-__device__ __forceinline__ void wide_item(const SharedArgs& a, const SharedEntry& e, int i, __bf16* const lds) {
+template <int D, bool EIGHT, typename Table>
+__device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab, const SharedEntry& e, int i, __bf16* const lds) {
   using L = WideLds<D, EIGHT>;
   using namespace prefill;
   constexpr int NK = D / 16, NO = D / 32, KCH = D / 8, VCH = kTile / 8, S = L::kStages;
@@ -49,7 +54,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const SharedEntry
   const int row = (block * per + wave) * 32 + (lane & 31);
   const bool active = wave < per && (block * per + wave) * 32 < rows;  // the wave has rows
   const bool row_ok = active && row < rows;
-  const int member = row_ok ? a.list[e.member0 + row / g] : 0, head = j * g + (row_ok ? row % g : 0);
+  const int member = row_ok ? tab.list[e.member0 + row / g] : 0, head = j * g + (row_ok ? row % g : 0);
 
   bf16x8 qf[NK];
   {
@@ -70,8 +75,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const SharedEntry
     bad |= p < n_pages && !ok;
     ids[p] = ok ? id : -1;
   }
-  if (bad) atomicOr(a.err, 1);
-  __syncthreads();
+  bad = __syncthreads_or(bad);
   auto page_mask = [&](int t) {  // which of a tile's pages count
     const int4 v = *reinterpret_cast<const int4*>(ids + 4 * t);
     return uniform((v.x >= 0 ? 1 : 0) | (v.y >= 0 ? 2 : 0) | (v.z >= 0 ? 4 : 0) | (v.w >= 0 ? 8 : 0));
@@ -281,7 +285,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const SharedEntry
     }
   }
   if (!row_ok) return;
-  const size_t at = (size_t)(a.slots[member].x + e.slot_off + split) * a.h_q + head;
+  const size_t at = (size_t)(tab.slots[member].x + e.slot_off + split) * a.h_q + head;
   float* o = a.acc + at * D + 4 * hh;
 #pragma unroll
   for (int n = 0; n < NO; ++n)
@@ -289,7 +293,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const SharedEntry
     for (int v = 0; v < 16; v += 4)
       *reinterpret_cast<f32x4*>(o + 32 * n + 2 * v) = f32x4{oacc[n][v], oacc[n][v + 1], oacc[n][v + 2], oacc[n][v + 3]};
   const float total = pair_sum(l_run);
-  if (hh == 0) a.ml[at] = make_float2(m_ref, total);
+  if (hh == 0) a.ml[at] = make_float2(m_ref, marked(total, bad));
 }
 
 }  // namespace shared

@@ -43,6 +43,19 @@ struct SharedEntry {
   int32_t split_pages;
   int32_t slot_off;    // split s of member r is slot first_slot[r] + slot_off + s
 };
+// What of the batch the kernels read: entries of many rows (wide), of at most kNarrowRows rows in runs that a team of waves
+// takes, and of so few pages that a wave takes them alone; the members' requests; (first slot, slots) of each request.
+constexpr int kSharedPassed = 64;  // up to this many entries and requests travel with the launches
+struct SharedTables {
+  const SharedEntry* entries;
+  const int32_t* list;
+  const int2* slots;
+};
+struct SharedPassed {
+  SharedEntry entries[kSharedPassed];
+  int32_t list[2 * kSharedPassed];
+  int2 slots[kSharedPassed];
+};
 struct SharedArgs {
   const __bf16* q;  // [R, h_q, d]
   const void *k, *v;
@@ -50,18 +63,19 @@ struct SharedArgs {
   const int32_t* table;
   long long pages;
   __bf16* out;
-  const SharedEntry* entries;  // n_wide of many rows, then n_narrow of at most kNarrowRows
-  const int32_t* list;         // requests
-  const int2* slots;           // [R] (first slot, slots)
   float* acc;                  // [slots, h_q, d] unnormalised outputs
-  float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator)
+  float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator; the latter's sign bit: a bad page)
   int32_t* err;
   int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
-  int32_t n_wide, n_narrow, wide_items, narrow_items, max_slots;
+  int32_t n_wide, n_team, n_lone, wide_items, team_items, lone_items;
+  int32_t max_slots;  // of a request
+  int32_t direct;     // one slot each and no wide entry: the results go straight to out, and err is clear beforehand
   float scale_log2;
 };
 constexpr int kWideRows = 256, kNarrowRows = 16;
 constexpr int kWidePages = 1024;  // most pages of a wide split
-hipError_t launch_shared(const SharedArgs& a, hipStream_t s);
+constexpr int kTeamWaves = 4;
+// passed: on the host, or null (then `tables` is in device memory).
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, hipStream_t s);
 
 }  // namespace duet

@@ -2146,11 +2146,13 @@ int norm_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* nor
 
 // How decode attention over shared prefixes is cut.  The rule goes by the batch only.
 struct SharedPlan {
-  std::vector<SharedEntry> wide, narrow;
+  std::vector<SharedEntry> wide, team, lone;
   std::vector<int32_t> list;  // the requests themselves, then the groups' members
   std::vector<int2> slots;
-  int64_t wide_items = 0, narrow_items = 0, n_slots = 0;
+  int64_t wide_items = 0, team_items = 0, lone_items = 0, n_slots = 0;
   int max_slots = 0;
+  bool direct = false;  // results go straight to out
+  bool passed = false;  // the lists travel with the launches
   size_t off_entries = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
 };
 
@@ -2168,6 +2170,9 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
   }
   return DUET_OK;
 }
+
+// Teams of waves that the runs of few rows are cut for, and the most pages of one's.
+constexpr int kTeamsWanted = 512, kTeamPages = 128;
 
 int blocks_of(int64_t rows) { return (int)((rows + kWideRows - 1) / kWideRows); }
 
@@ -2219,28 +2224,38 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
     }
     const int wide_split = wide_split_pages(runs, hkv);
-    const int64_t even = (narrow_pages * hkv + 2047) / 2048;
-    const int narrow_split = (int)std::min<int64_t>(64, std::max<int64_t>(8, (even + 3) / 4 * 4));
+    const int64_t even = (narrow_pages * hkv + kTeamsWanted - 1) / kTeamsWanted;
+    const int narrow_split = (int)std::min<int64_t>(kTeamPages, std::max<int64_t>(16, (even + 15) / 16 * 16));
+    // Runs of up to 16 rows: a team of waves takes one of more than four pages.
+    auto add_narrow = [&](SharedEntry e, int n) {
+      const bool team = e.tokens > 64;
+      int64_t& items = team ? plan->team_items : plan->lone_items;
+      e.first_item = (int32_t)std::min<int64_t>(items, INT32_MAX);
+      items += (int64_t)n * hkv;
+      (team ? plan->team : plan->lone).push_back(e);
+    };
     plan->slots.assign(R, make_int2(0, 0));
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
       const int64_t rows = (int64_t)count[i] * g;
       const bool wide = rows > kNarrowRows;
       const int split = wide ? wide_split : narrow_split, n = (p->len[i] / 16 + split - 1) / split;
-      int64_t& items = wide ? plan->wide_items : plan->narrow_items;
-      (wide ? plan->wide : plan->narrow)
-          .push_back(SharedEntry{(int32_t)items, member0[i], count[i], plan->list[member0[i]], 0, p->len[i], split, 0});
-      items += (int64_t)n * hkv * (wide ? blocks_of(rows) : 1);
+      SharedEntry e{0, member0[i], count[i], plan->list[member0[i]], 0, p->len[i], split, 0};
+      if (wide) {
+        e.first_item = (int32_t)std::min<int64_t>(plan->wide_items, INT32_MAX);
+        plan->wide_items += (int64_t)n * hkv * blocks_of(rows);
+        plan->wide.push_back(e);
+      } else {
+        add_narrow(e, n);
+      }
       for (int m = 0; m < count[i]; ++m) plan->slots[plan->list[member0[i] + m]].y = n;
     }
     for (int r = 0; r < R; ++r) {
       const int before = shared(r) ? p->len[p->of[r]] : 0, tokens = b->reqs[r].cached_len + 1 - before;
       if (tokens > 0) {
         const int n = ((tokens + 15) / 16 + narrow_split - 1) / narrow_split;
-        plan->narrow.push_back(SharedEntry{(int32_t)plan->narrow_items, r, 1, r, before / 16, tokens, narrow_split,
-                                           plan->slots[r].y});
+        add_narrow(SharedEntry{0, r, 1, r, before / 16, tokens, narrow_split, plan->slots[r].y}, n);
         plan->slots[r].y += n;
-        plan->narrow_items += (int64_t)n * hkv;
       }
       plan->slots[r].x = (int)std::min<int64_t>(plan->n_slots, INT32_MAX);
       plan->n_slots += plan->slots[r].y;
@@ -2249,10 +2264,14 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
   }
-  if (plan->wide_items > INT32_MAX / 2 || plan->narrow_items > INT32_MAX / 2 || plan->n_slots > INT32_MAX / 2)
+  if (plan->wide_items > INT32_MAX / 2 || plan->team_items > INT32_MAX / 2 || plan->lone_items > INT32_MAX / 2 ||
+      plan->n_slots > INT32_MAX / 2)
     return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
+  const size_t n_entries = plan->wide.size() + plan->team.size() + plan->lone.size();
+  plan->direct = plan->max_slots <= 1 && plan->wide.empty();
+  plan->passed = !plan->direct && n_entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed && R <= kSharedPassed;
   plan->off_entries = kAlign;
-  plan->off_list = plan->off_entries + align_up((plan->wide.size() + plan->narrow.size()) * sizeof(SharedEntry));
+  plan->off_list = plan->off_entries + align_up(n_entries * sizeof(SharedEntry));
   plan->off_slots = plan->off_list + align_up(plan->list.size() * sizeof(int32_t));
   plan->off_ml = plan->off_slots + align_up(plan->slots.size() * sizeof(int2));
   plan->off_acc = plan->off_ml + align_up((size_t)plan->n_slots * s->num_q_heads * sizeof(float2));
@@ -2403,12 +2422,6 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   HIP_TRY(device.status);
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  const size_t wide_bytes = plan.wide.size() * sizeof(SharedEntry);
-  const UploadPart parts[4] = {{plan.wide.data(), wide_bytes, plan.off_entries},
-                               {plan.narrow.data(), plan.narrow.size() * sizeof(SharedEntry), plan.off_entries + wide_bytes},
-                               {plan.list.data(), plan.list.size() * sizeof(int32_t), plan.off_list},
-                               {plan.slots.data(), plan.slots.size() * sizeof(int2), plan.off_slots}};
-  if ((rc = upload_parts(ctx, parts, 4, ws, st))) return rc;
   SharedArgs a{};
   a.q = static_cast<const __bf16*>(q);
   a.k = cache->k;
@@ -2417,9 +2430,6 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.table = page_table;
   a.pages = cache->num_phys_pages;
   a.out = static_cast<__bf16*>(out);
-  a.entries = reinterpret_cast<const SharedEntry*>(ws + plan.off_entries);
-  a.list = reinterpret_cast<const int32_t*>(ws + plan.off_list);
-  a.slots = reinterpret_cast<const int2*>(ws + plan.off_slots);
   a.acc = reinterpret_cast<float*>(ws + plan.off_acc);
   a.ml = reinterpret_cast<float2*>(ws + plan.off_ml);
   a.err = reinterpret_cast<int32_t*>(ws);
@@ -2430,12 +2440,32 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.group = a.h_q / a.h_kv;
   a.head_dim = shape->head_dim;
   a.n_wide = (int)plan.wide.size();
-  a.n_narrow = (int)plan.narrow.size();
+  a.n_team = (int)plan.team.size();
+  a.n_lone = (int)plan.lone.size();
   a.wide_items = (int)plan.wide_items;
-  a.narrow_items = (int)plan.narrow_items;
+  a.team_items = (int)plan.team_items;
+  a.lone_items = (int)plan.lone_items;
   a.max_slots = plan.max_slots;
+  a.direct = plan.direct;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
-  HIP_TRY(launch_shared(a, st));
+  const SharedTables tables{reinterpret_cast<const SharedEntry*>(ws + plan.off_entries),
+                            reinterpret_cast<const int32_t*>(ws + plan.off_list), reinterpret_cast<const int2*>(ws + plan.off_slots)};
+  SharedPassed passed;
+  if (plan.passed) {
+    SharedEntry* e = std::copy(plan.wide.begin(), plan.wide.end(), passed.entries);
+    std::copy(plan.lone.begin(), plan.lone.end(), std::copy(plan.team.begin(), plan.team.end(), e));
+    std::copy(plan.list.begin(), plan.list.end(), passed.list);
+    std::copy(plan.slots.begin(), plan.slots.end(), passed.slots);
+  } else {
+    const size_t wide_bytes = plan.wide.size() * sizeof(SharedEntry), team_bytes = plan.team.size() * sizeof(SharedEntry);
+    const UploadPart parts[5] = {{plan.wide.data(), wide_bytes, plan.off_entries},
+                                 {plan.team.data(), team_bytes, plan.off_entries + wide_bytes},
+                                 {plan.lone.data(), plan.lone.size() * sizeof(SharedEntry), plan.off_entries + wide_bytes + team_bytes},
+                                 {plan.list.data(), plan.list.size() * sizeof(int32_t), plan.off_list},
+                                 {plan.slots.data(), plan.slots.size() * sizeof(int2), plan.off_slots}};
+    if ((rc = upload_parts(ctx, parts, 5, ws, st))) return rc;
+  }
+  HIP_TRY(launch_shared(a, tables, plan.passed ? &passed : nullptr, st));
   return DUET_OK;
 }
 
