@@ -13,6 +13,8 @@
 // 8-bit values become bf16 exactly; a key's power of two multiplies its scores, a value's its probability.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "attn_shared_wide.h"
 #include "cache_ops.h"
 #include "wave_ops.h"
@@ -201,21 +203,23 @@ struct Item {
 template <int D>
 constexpr int team_floats(int rows) { return kTeamWaves * rows * (D + 4); }  // LDS; rows start on different banks
 
-// Teams first, a workgroup each, then lone waves.
-template <int D, bool EIGHT, typename Table>
-__global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, Table tab) {
-  extern __shared__ __attribute__((aligned(16))) float part[];
+// Runs of up to 16 rows, by a workgroup of W waves: `block` counts the workgroups of such runs, teams first, then lone waves.
+template <int D, bool EIGHT, int W, typename Table>
+__device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& tab, int block, float* lds) {
+  constexpr int kTeams = W / kTeamWaves;
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, wave = uniform(threadIdx.x >> 6);
   const bool direct = a.direct;
-  if (!direct && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
-  const bool team = (int)blockIdx.x < a.team_items;
-  const int item = team ? blockIdx.x : ((int)blockIdx.x - a.team_items) * kTeamWaves + wave;
-  if (!team && item >= a.lone_items) return;
+  const int team_blocks = (a.team_items + kTeams - 1) / kTeams;
+  const bool team = block < team_blocks;
+  const int item = team ? block * kTeams + wave / kTeamWaves : (block - team_blocks) * W + wave;
+  const bool has = item < (team ? a.team_items : a.lone_items);
+  if (!team && !has) return;
   const int e0 = a.n_wide + (team ? 0 : a.n_team), n = team ? a.n_team : a.n_lone;
   const SharedEntry e = tab.entries[e0 + uniform(find_request(n, [&](int i) { return tab.entries[e0 + i].first_item <= item; }))];
-  const Item<D, EIGHT> it(a, tab, e, item - e.first_item);
+  const Item<D, EIGHT> it(a, tab, e, has ? item - e.first_item : 0);
   Rows<D> o;
-  bool bad = walk<D, EIGHT>(a, it.prow, it.n_tok, it.j, team ? 4 * wave : 0, team ? 4 * kTeamWaves : 4, it.qf, o);
+  const int member = wave % kTeamWaves;  // of its team
+  bool bad = walk<D, EIGHT>(a, it.prow, has ? it.n_tok : 0, it.j, team ? 4 * member : 0, team ? 4 * kTeamWaves : 4, it.qf, o);
   if (!team) {
     if (direct && bad && lane == 0) atomicOr(a.err, 1);
     if (it.head_row < 0) return;
@@ -237,7 +241,8 @@ __global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, T
   }
   // The team's four states are joined through LDS.
   const int rows = it.rows;
-  float* mine = part + wave * rows * (D + 4) + col * (D + 4);
+  float* const part = lds + wave / kTeamWaves * team_floats<D>(kNarrowRows);
+  float* mine = part + (member * rows + col) * (D + 4);
   if (col < rows) {
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(mine + 16 * n + 4 * quad) = o.acc[n];
@@ -245,8 +250,9 @@ __global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, T
   }
   bad = __syncthreads_or(bad);
   if (direct && bad && threadIdx.x == 0) atomicOr(a.err, 1);
+  if (!has) return;
   const int g = a.group;
-  for (int x = 4 * threadIdx.x; x < rows * D; x += 4 * 64 * kTeamWaves) {
+  for (int x = 4 * (64 * member + lane); x < rows * D; x += 4 * 64 * kTeamWaves) {
     const int row = x / D, dim = x % D;
     const float* p = part + row * (D + 4);
     float m[kTeamWaves], to = -INFINITY, l = 0.f;
@@ -275,10 +281,22 @@ __global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, T
 }
 
 template <int D, bool EIGHT, typename Table>
-__global__ __launch_bounds__(kWideThreads, 1) void shared_wide(SharedArgs a, Table tab) {
+__global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, Table tab) {
+  extern __shared__ __attribute__((aligned(16))) float part[];
+  if (!a.direct && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
+  narrow_items<D, EIGHT, kTeamWaves>(a, tab, blockIdx.x, part);
+}
+
+// Runs of many rows first, then those of few: the one is bound by the matrix cores, the other by memory.
+template <int D, bool EIGHT, typename Table>
+__global__ __launch_bounds__(kWideThreads, 1) void shared_mixed(SharedArgs a, Table tab) {
   extern __shared__ __attribute__((aligned(16))) __bf16 lds[];
   const int item = blockIdx.x;
   if (item == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
+  if (item >= a.wide_items) {
+    narrow_items<D, EIGHT, kWideWaves>(a, tab, item - a.wide_items, reinterpret_cast<float*>(lds));
+    return;
+  }
   const SharedEntry e = tab.entries[uniform(find_request(a.n_wide, [&](int i) { return tab.entries[i].first_item <= item; }))];
   wide_item<D, EIGHT>(a, tab, e, item - e.first_item, lds);
 }
@@ -356,17 +374,19 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
 
 template <int D, bool EIGHT, typename Table>
 hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
+  auto blocks = [&](int waves) {
+    return (a.team_items + waves / kTeamWaves - 1) / (waves / kTeamWaves) + (a.lone_items + waves - 1) / waves;
+  };
   if (a.wide_items) {
-    constexpr size_t kBytes = WideLds<D, EIGHT>::kBytes;
-    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_wide<D, EIGHT, Table>),
+    constexpr size_t kBytes = std::max(WideLds<D, EIGHT>::kBytes, 2 * team_floats<D>(kNarrowRows) * sizeof(float));
+    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_mixed<D, EIGHT, Table>),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     if (set != hipSuccess) return set;
-    hipLaunchKernelGGL((shared_wide<D, EIGHT, Table>), dim3(a.wide_items), dim3(kWideThreads), kBytes, s, a, tab);
-  }
-  const int narrow = a.team_items + (a.lone_items + kTeamWaves - 1) / kTeamWaves;
-  if (narrow)
-    hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(narrow), dim3(64 * kTeamWaves),
+    hipLaunchKernelGGL((shared_mixed<D, EIGHT, Table>), dim3(a.wide_items + blocks(kWideWaves)), dim3(kWideThreads), kBytes, s, a, tab);
+  } else {
+    hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(blocks(kTeamWaves)), dim3(64 * kTeamWaves),
                        team_floats<D>(kNarrowRows) * sizeof(float), s, a, tab);
+  }
   if (a.direct) return hipGetLastError();
   const int pairs = a.num_reqs * a.h_q;
   if (a.max_slots > 64) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);

@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <chrono>
 #include <cmath>
 #include <cstring>
@@ -2176,16 +2177,22 @@ constexpr int kTeamsWanted = 512, kTeamPages = 128;
 
 int blocks_of(int64_t rows) { return (int)((rows + kWideRows - 1) / kWideRows); }
 
-// Pages of a wide split, the fewest (at least four tiles) with which the runs fill the CUs once, or 1024 workgroups where they fill
-// them more often.
-int wide_split_pages(const std::vector<std::pair<int, int>>& runs, int hkv) {  // (pages, row blocks)
+// Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
+// workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
+// 1 us and 0.18 for each of its waves with rows, and a CU reads some 25 KB of the other runs in a us.
+int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes) {  // (pages, row blocks, rows)
+  if (runs.empty()) return 4;
+  double wide_us = 0;
+  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * (1.0 + 0.18 * std::min(8, (r[2] / r[1] + 31) / 32));
+  const double share = wide_us / (wide_us + narrow_bytes / 25000.0);
   auto items = [&](int split) {
     int64_t n = 0;
-    for (const auto& r : runs) n += (int64_t)((r.first + split - 1) / split) * r.second * hkv;
+    for (const auto& r : runs) n += (int64_t)((r[0] + split - 1) / split) * r[1] * hkv;
     return n;
   };
-  const int64_t most = items(kWidePages) <= DUET_TOTAL_CUS ? DUET_TOTAL_CUS : 4 * DUET_TOTAL_CUS;
-  int lo = 4, hi = kWidePages / 4;  // in tiles
+  const int64_t cus = std::max<int64_t>(16, (int64_t)(DUET_TOTAL_CUS * share));
+  const int64_t most = items(kWidePages) <= cus ? cus : 4 * DUET_TOTAL_CUS;
+  int lo = 1, hi = kWidePages / 4;  // in tiles
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
     if (items(4 * mid) <= most) hi = mid;
@@ -2194,7 +2201,7 @@ int wide_split_pages(const std::vector<std::pair<int, int>>& runs, int hkv) {  /
   return 4 * lo;
 }
 
-int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, SharedPlan* plan) {
+int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, bool eight, SharedPlan* plan) {
   const int R = b->num_reqs, g = s->num_q_heads / s->num_kv_heads, hkv = s->num_kv_heads;
   for (int r = 0; r < R; ++r)
     if (b->reqs[r].kind != DUET_KIND_DECODE) return fail(DUET_EUNSUPPORTED, "request %d is no decode request", r);
@@ -2206,13 +2213,13 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     auto shared = [&](int r) { return p && p->of[r] >= 0 && count[p->of[r]] > 1 && p->len[p->of[r]] > 0; };
     plan->list.resize(R);
     for (int r = 0; r < R; ++r) plan->list[r] = r;
-    std::vector<std::pair<int, int>> runs;
+    std::vector<std::array<int, 3>> runs;
     int64_t narrow_pages = 0;
     int at = R;
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
       const int64_t rows = (int64_t)count[i] * g;
-      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, blocks_of(rows)});
+      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, blocks_of(rows), (int)rows});
       else narrow_pages += p->len[i] / 16;
       member0[i] = at;
       at += count[i];
@@ -2223,7 +2230,8 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       if (shared(r)) plan->list[next[p->of[r]]++] = r;
       narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
     }
-    const int wide_split = wide_split_pages(runs, hkv);
+    const int64_t page_bytes = 32 * s->head_dim * (eight ? 1 : 2);  // of a head
+    const int wide_split = wide_split_pages(runs, hkv, narrow_pages * hkv * page_bytes);
     const int64_t even = (narrow_pages * hkv + kTeamsWanted - 1) / kTeamsWanted;
     const int narrow_split = (int)std::min<int64_t>(kTeamPages, std::max<int64_t>(16, (even + 15) / 16 * 16));
     // Runs of up to 16 rows: a team of waves takes one of more than four pages.
@@ -2391,9 +2399,13 @@ int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch
   int rc = check_shared(shape, batch, prefixes);
   if (rc) return rc;
   if (!bytes) return fail(DUET_EINVAL, "bytes is NULL");
-  SharedPlan plan;
-  if ((rc = plan_shared(shape, batch, prefixes, &plan))) return rc;
-  *bytes = plan.total;
+  size_t most = 0;
+  for (bool eight : {false, true}) {  // cut differently
+    SharedPlan plan;
+    if ((rc = plan_shared(shape, batch, prefixes, eight, &plan))) return rc;
+    most = std::max(most, plan.total);
+  }
+  *bytes = most;
   return DUET_OK;
 }
 
@@ -2414,7 +2426,7 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   for (const void* p : {q, static_cast<const void*>(out), static_cast<const void*>(workspace)})
     if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DUET_EINVAL, "q, out and the workspace must lie on 16 bytes");
   SharedPlan plan;
-  if ((rc = plan_shared(shape, batch, prefixes, &plan))) return rc;
+  if ((rc = plan_shared(shape, batch, prefixes, cache->scales != nullptr, &plan))) return rc;
   if (workspace_bytes < plan.total) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, plan.total);
   if (batch->num_reqs == 0) return DUET_OK;
   std::lock_guard<std::mutex> lock(ctx->mu);
