@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_shared_wide.h"
 #include "cache_ops.h"
@@ -67,31 +68,40 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
     kid = prow[min(p0 + (col >> 2), n_pages - 1)];
     vid = prow[min(p0 + quad, n_pages - 1)];
   };
-  if (first < n_pages) ids(first);
-  for (int p0 = first; p0 < n_pages; p0 += stride) {
-    const int vpage = p0 + quad;
-    const bool kok = page_ok(kid, a.pages), vok = page_ok(vid, a.pages);
-    bad |= !vok;
-    const size_t kslab = (size_t)(kok ? kid : 0) * a.h_kv + j, vslab = (size_t)(vok ? vid : 0) * a.h_kv + j;
+  uint4 kr[4][kLoads], vr[D / 16][kB], ke = make_uint4(0, 0, 0, 0), ve = ke;
+  size_t vslab = 0;
+  bool vok = false;
+  auto load_k = [&] {
+    const bool kok = page_ok(kid, a.pages);
+    const size_t kslab = (size_t)(kok ? kid : 0) * a.h_kv + j;
     const char* kp = static_cast<const char*>(a.k) + kslab * 16 * D * kB + (col & 3) * D * kB + quad * 16;
-    const char* vp = static_cast<const char*>(a.v) + vslab * 16 * D * kB + col * 16 * kB;
-    // Tokens of page `vpage` that count.
-    const int nv = vok ? max(0, min(16, n_tok - 16 * vpage)) : 0;
-    uint4 kr[4][kLoads], vr[D / 16][kB];
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
       for (int s = 0; s < kLoads; ++s) kr[p][s] = *reinterpret_cast<const uint4*>(kp + 4 * p * D * kB + 64 * s);
-    uint4 ke = make_uint4(0, 0, 0, 0), ve = ke;
-    if constexpr (EIGHT) {
-      ke = *reinterpret_cast<const uint4*>(a.scales + vslab * 32);
-      ve = *reinterpret_cast<const uint4*>(a.scales + vslab * 32 + 16);
-    }
+    vok = page_ok(vid, a.pages);
+    bad |= !vok;
+    vslab = (size_t)(vok ? vid : 0) * a.h_kv + j;
+    if constexpr (EIGHT) ke = *reinterpret_cast<const uint4*>(a.scales + vslab * 32);
+  };
+  auto load_v = [&] {
+    const char* vp = static_cast<const char*>(a.v) + vslab * 16 * D * kB + col * 16 * kB;
 #pragma unroll
     for (int n = 0; n < D / 16; ++n)
 #pragma unroll
       for (int h = 0; h < kB; ++h) vr[n][h] = *reinterpret_cast<const uint4*>(vp + n * 256 * kB + 16 * h);
-    ids(p0 + stride);
+    if constexpr (EIGHT) ve = *reinterpret_cast<const uint4*>(a.scales + vslab * 32 + 16);
+  };
+  // A step's keys are loaded once the step before has its scores, its values once that has its product; page ids a step earlier.
+  if (first >= n_pages) return false;
+  ids(first);
+  load_k();
+  load_v();
+  ids(first + stride);
+  for (int p0 = first;; p0 += stride) {
+    const int vpage = p0 + quad;
+    // Tokens of page `vpage` that count.
+    const int nv = vok ? max(0, min(16, n_tok - 16 * vpage)) : 0;
     const bool part = __any(nv < 16);
     // Scores S^T: the lane's are the 16 tokens of page `vpage` for row `col`.
     float sc[16];
@@ -111,19 +121,14 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
 #pragma unroll
       for (int i = 0; i < 4; ++i) sc[4 * p + i] = s[i] * (EIGHT ? power(kw[p], i) * a.scale_log2 : a.scale_log2);
     }
+    const bool more = p0 + stride < n_pages;
+    if (more) {
+      load_k();
+      ids(p0 + 2 * stride);
+    }
     if (part) {
 #pragma unroll
       for (int t = 0; t < 16; ++t) sc[t] = t < nv ? sc[t] : -INFINITY;
-      ve = first_bytes(ve, nv);
-#pragma unroll
-      for (int n = 0; n < D / 16; ++n) {
-        if constexpr (EIGHT) {
-          vr[n][0] = first_bytes(vr[n][0], nv);
-        } else {
-          vr[n][0] = first_bytes(vr[n][0], 2 * nv);
-          vr[n][kB - 1] = first_bytes(vr[n][kB - 1], 2 * nv - 16);
-        }
-      }
     }
     float mx = sc[0];
 #pragma unroll
@@ -140,7 +145,8 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
     const float sub = o.m == -INFINITY ? 0.f : o.m;  // no key yet that counts: every weight is 0
     // The denominator sums the probabilities as the second product takes them.
     const bf16x2 ones = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-    const unsigned vw[4] = {ve.x, ve.y, ve.z, ve.w};
+    const uint4 vx = part ? first_bytes(ve, nv) : ve;
+    const unsigned vw[4] = {vx.x, vx.y, vx.z, vx.w};
     bf16x8 pf[2];
 #pragma unroll
     for (int t = 0; t < 16; t += 2) {
@@ -157,15 +163,24 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
         pf[t / 8][t % 8] = w[0], pf[t / 8][t % 8 + 1] = w[1];
       }
     }
+    // Values that do not count are zeroed: their weights are 0, and 0 times NaN is NaN.
+    auto product = [&](auto masked) {
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n)
+      for (int n = 0; n < D / 16; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 vf;
-        if constexpr (EIGHT) vf = widened(h ? make_uint2(vr[n][0].z, vr[n][0].w) : make_uint2(vr[n][0].x, vr[n][0].y));
-        else vf = __builtin_bit_cast(bf16x8, vr[n][h % kB]);
-        o.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h], o.acc[n], 0, 0, 0);
-      }
+        for (int h = 0; h < 2; ++h) {
+          uint4 v = vr[n][h % kB];
+          if constexpr (decltype(masked)::value) v = first_bytes(v, EIGHT ? nv : 2 * nv - 16 * h);
+          bf16x8 vf;
+          if constexpr (EIGHT) vf = widened(h ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y));
+          else vf = __builtin_bit_cast(bf16x8, v);
+          o.acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h], o.acc[n], 0, 0, 0);
+        }
+    };
+    if (part) product(std::true_type{});
+    else product(std::false_type{});
+    if (!more) break;
+    load_v();
   }
   o.l = sum_rows(o.l);
   return __any(bad);
