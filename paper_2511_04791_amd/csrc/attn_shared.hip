@@ -186,34 +186,28 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
   return __any(bad);
 }
 
-// An item of an entry of up to 16 rows: split, kv head, the run's pages, and the lane's row.
-template <int D, bool EIGHT>
-struct Item {
-  int split, j, n_tok, rows;
-  const int* prow;
-  int head_row;  // request * h_q + head of row `col`, or -1
-  bf16x8 qf[D / 32];
-
-  template <typename Table>
-  __device__ __forceinline__ Item(const SharedArgs& a, const Table& tab, const SharedEntry& e, int i) {
-    const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, g = a.group;
-    j = i % a.h_kv;
-    split = i / a.h_kv;
-    rows = e.members * g;
-    const int skip = split * e.split_pages;
-    n_tok = min(e.tokens - 16 * skip, 16 * e.split_pages);
-    prow = a.table + (size_t)e.table_row * a.max_pages + e.page0 + skip;
-    head_row = col < rows ? tab.list[e.member0 + col / g] * a.h_q + j * g + col % g : -1;
-    const __bf16* q = a.q + (size_t)max(head_row, 0) * D;
-#pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) {
-      // The dimensions of contraction step ks that this quad holds, as the keys' loads give them.
-      const int dim = EIGHT ? 64 * (ks / 2) + 16 * quad + 8 * (ks % 2) : 32 * ks + 8 * quad;
-      const uint4 u = head_row >= 0 ? *reinterpret_cast<const uint4*>(q + dim) : make_uint4(0, 0, 0, 0);
-      qf[ks] = __builtin_bit_cast(bf16x8, u);
-    }
+// Item `item` of the runs of one kind, n of them from `first` on: its part of a run.
+template <bool WIDE>
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedTables& tab, int first, int n, int item) {
+  return tab.runs[first + min(item / a.h_kv, n - 1)];
+}
+template <bool WIDE>
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPassed& tab, int first, int n, int item) {
+  const SharedEntry e =
+      tab.entries[first + uniform(find_request(n, [&](int i) { return tab.entries[first + i].first_item <= item; }))];
+  SharedRun r = e.run;
+  int part = (item - e.first_item) / a.h_kv;
+  if (WIDE) {
+    const int rows = r.members * a.group, blocks = wide_blocks(rows);
+    r.waves = wide_waves(rows);
+    r.row0 = part % blocks * r.waves * 32;
+    part /= blocks;
   }
-};
+  r.page0 += part * e.split_pages;
+  r.tokens = min(r.tokens - 16 * part * e.split_pages, 16 * e.split_pages);
+  r.slot += part;
+  return r;
+}
 
 template <int D>
 constexpr int team_floats(int rows) { return kTeamWaves * rows * (D + 4); }  // LDS; rows start on different banks
@@ -230,16 +224,32 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
   const bool has = item < (team ? a.team_items : a.lone_items);
   if (!team && !has) return;
   const int e0 = a.n_wide + (team ? 0 : a.n_team), n = team ? a.n_team : a.n_lone;
-  const SharedEntry e = tab.entries[e0 + uniform(find_request(n, [&](int i) { return tab.entries[e0 + i].first_item <= item; }))];
-  const Item<D, EIGHT> it(a, tab, e, has ? item - e.first_item : 0);
+  const SharedRun e = run_of<false>(a, tab, e0, n, has ? item : 0);
+  const int g = a.group, rows = e.members * g, j = (has ? item : 0) % a.h_kv;
+  // The lane's row, as request * h_q + head, or -1.  A request alone is its row of the page table.
+  auto request = [&](int row) { return e.members == 1 ? e.table_row : tab.list[e.member0 + row / g]; };
+  const int head_row = col < rows ? request(col) * a.h_q + j * g + col % g : -1;
+  bf16x8 qf[D / 32];
+  {
+    const __bf16* q = a.q + (size_t)max(head_row, 0) * D;
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      // The dimensions of contraction step ks that this quad holds, as the keys' loads give them.
+      const int dim = EIGHT ? 64 * (ks / 2) + 16 * quad + 8 * (ks % 2) : 32 * ks + 8 * quad;
+      const uint4 u = head_row >= 0 ? *reinterpret_cast<const uint4*>(q + dim) : make_uint4(0, 0, 0, 0);
+      qf[ks] = __builtin_bit_cast(bf16x8, u);
+    }
+  }
+  auto slot = [&](int r) { return (size_t)(e.members == 1 ? e.slot : tab.slots[r].x + e.slot); };
   Rows<D> o;
   const int member = wave % kTeamWaves;  // of its team
-  bool bad = walk<D, EIGHT>(a, it.prow, has ? it.n_tok : 0, it.j, team ? 4 * member : 0, team ? 4 * kTeamWaves : 4, it.qf, o);
+  const int* prow = a.table + (size_t)e.table_row * a.max_pages + e.page0;
+  bool bad = walk<D, EIGHT>(a, prow, has ? e.tokens : 0, j, team ? 4 * member : 0, team ? 4 * kTeamWaves : 4, qf, o);
   if (!team) {
     if (direct && bad && lane == 0) atomicOr(a.err, 1);
-    if (it.head_row < 0) return;
+    if (head_row < 0) return;
     if (direct) {
-      __bf16* y = a.out + (size_t)it.head_row * D + 4 * quad;
+      __bf16* y = a.out + (size_t)head_row * D + 4 * quad;
       const float inv = 1.f / o.l;
 #pragma unroll
       for (int n = 0; n < D / 16; ++n)
@@ -247,15 +257,14 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
         for (int i = 0; i < 4; ++i) y[16 * n + i] = static_cast<__bf16>(o.acc[n][i] * inv);
       return;
     }
-    const int r = it.head_row / a.h_q;
-    const size_t at = (size_t)(tab.slots[r].x + e.slot_off + it.split) * a.h_q + (it.head_row - r * a.h_q);
+    const int r = head_row / a.h_q;
+    const size_t at = slot(r) * a.h_q + (head_row - r * a.h_q);
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(a.acc + at * D + 16 * n + 4 * quad) = o.acc[n];
     if (quad == 0) a.ml[at] = make_float2(o.m, marked(o.l, bad));
     return;
   }
   // The team's four states are joined through LDS.
-  const int rows = it.rows;
   float* const part = lds + wave / kTeamWaves * team_floats<D>(kNarrowRows);
   float* mine = part + (member * rows + col) * (D + 4);
   if (col < rows) {
@@ -266,7 +275,6 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
   bad = __syncthreads_or(bad);
   if (direct && bad && threadIdx.x == 0) atomicOr(a.err, 1);
   if (!has) return;
-  const int g = a.group;
   for (int x = 4 * (64 * member + lane); x < rows * D; x += 4 * 64 * kTeamWaves) {
     const int row = x / D, dim = x % D;
     const float* p = part + row * (D + 4);
@@ -280,7 +288,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
       l += f * p[w * rows * (D + 4) + D + 1];
       sum += f * *reinterpret_cast<const f32x4*>(p + w * rows * (D + 4) + dim);
     }
-    const int r = tab.list[e.member0 + row / g], head = it.j * g + row % g;
+    const int r = request(row), head = j * g + row % g;
     if (direct) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       const float inv = 1.f / l;
@@ -288,7 +296,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
           bf16x4{static_cast<__bf16>(sum[0] * inv), static_cast<__bf16>(sum[1] * inv), static_cast<__bf16>(sum[2] * inv),
                  static_cast<__bf16>(sum[3] * inv)};
     } else {
-      const size_t at = (size_t)(tab.slots[r].x + e.slot_off + it.split) * a.h_q + head;
+      const size_t at = slot(r) * a.h_q + head;
       *reinterpret_cast<f32x4*>(a.acc + at * D + dim) = sum;
       if (dim == 0) a.ml[at] = make_float2(to, marked(l, bad));
     }
@@ -312,8 +320,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void shared_mixed(SharedArgs a, Ta
     narrow_items<D, EIGHT, kWideWaves>(a, tab, item - a.wide_items, reinterpret_cast<float*>(lds));
     return;
   }
-  const SharedEntry e = tab.entries[uniform(find_request(a.n_wide, [&](int i) { return tab.entries[i].first_item <= item; }))];
-  wide_item<D, EIGHT>(a, tab, e, item - e.first_item, lds);
+  wide_item<D, EIGHT>(a, tab, run_of<true>(a, tab, 0, a.n_wide, item), item % a.h_kv, lds);
 }
 
 // Joins the runs of one (request, query head): W waves, each every W-th run, eight loads in flight.

@@ -38,21 +38,17 @@ struct WideLds {
   static constexpr size_t kBytes = kTileBytes + kWidePages * sizeof(int);
 };
 
-// One item of a wide entry: up to 256 rows, 32 a wave, over the pages page0 .. of a run of n_pages whole pages.
+// Up to 256 rows of a run, 32 a wave, with kv head j.  The run is of whole pages.
 template <int D, bool EIGHT, typename Table>
-__device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab, const SharedEntry& e, int i, __bf16* const lds) {
+__device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab, const SharedRun& e, int j, __bf16* const lds) {
   using L = WideLds<D, EIGHT>;
   using namespace prefill;
   constexpr int NK = D / 16, NO = D / 32, KCH = D / 8, VCH = kTile / 8, S = L::kStages;
   constexpr int kB = EIGHT ? 1 : 2;
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, hh = lane >> 5;
-  const int g = a.group, rows = e.members * g, tiles32 = (rows + 31) / 32;
-  const int blocks = (tiles32 + kWideWaves - 1) / kWideWaves, per = (tiles32 + blocks - 1) / blocks;  // waves with rows
-  const int block = i % blocks, j = i / blocks % a.h_kv, split = i / blocks / a.h_kv;
-  const int page0 = e.page0 + split * e.split_pages;
-  const int n_pages = min(e.tokens / 16 - split * e.split_pages, e.split_pages), n_tiles = (n_pages + 3) >> 2;
-  const int row = (block * per + wave) * 32 + (lane & 31);
-  const bool active = wave < per && (block * per + wave) * 32 < rows;  // the wave has rows
+  const int g = a.group, rows = e.members * g, n_pages = e.tokens / 16, n_tiles = (n_pages + 3) >> 2;
+  const int row = e.row0 + 32 * wave + (lane & 31);
+  const bool active = wave < e.waves && e.row0 + 32 * wave < rows;  // the wave has rows
   const bool row_ok = active && row < rows;
   const int member = row_ok ? tab.list[e.member0 + row / g] : 0, head = j * g + (row_ok ? row % g : 0);
 
@@ -67,7 +63,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
   }
   // The run's page ids, -1 for those outside the pool and past the end (up to a whole tile).
   int* const ids = reinterpret_cast<int*>(reinterpret_cast<char*>(lds) + L::kTileBytes);
-  const int* prow = a.table + (size_t)e.table_row * a.max_pages + page0;
+  const int* prow = a.table + (size_t)e.table_row * a.max_pages + e.page0;
   bool bad = false;
   for (int p = tid; p < 4 * n_tiles; p += kWideThreads) {
     const int id = p < n_pages ? prow[p] : -1;
@@ -285,7 +281,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
     }
   }
   if (!row_ok) return;
-  const size_t at = (size_t)(tab.slots[member].x + e.slot_off + split) * a.h_q + head;
+  const size_t at = (size_t)(tab.slots[member].x + e.slot) * a.h_q + head;
   float* o = a.acc + at * D + 4 * hh;
 #pragma unroll
   for (int n = 0; n < NO; ++n)

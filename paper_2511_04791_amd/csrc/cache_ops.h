@@ -34,22 +34,36 @@ struct Cache8ReadArgs {
 };
 hipError_t launch_cache8_read(const Cache8ReadArgs& a, const int2* reqs, hipStream_t s);
 
-// Decode attention over runs of pages that one or several requests share (attn_shared.hip).  An entry is a run and the
-// query rows that attend it: of `members` requests, listed from list[member0] on, the g heads of each kv head.
-struct SharedEntry {
-  int32_t first_item;  // items (split, kv head, row block) of its kind's entries before it
+// Decode attention over runs of pages that one or several requests share (attn_shared.hip).  A run is attended by the query
+// rows of its members, requests listed from list[member0] on: of each the g heads of a kv head.  A workgroup, a team of its waves or
+// a wave takes a run (or a part of it and of its rows) and a kv head, heads next to each other.
+struct SharedRun {
+  int32_t table_row, page0, tokens;  // pages from page0 of a row of the page table
+  int32_t slot;      // where the rows' states go: of one member, else counted from each member's first slot
   int32_t member0, members;
-  int32_t table_row, page0, tokens;  // the run: pages from page0 of a row of the page table
-  int32_t split_pages;
-  int32_t slot_off;    // split s of member r is slot first_slot[r] + slot_off + s
+  int32_t row0, waves;  // of many rows: a workgroup's first, and its waves with rows
 };
-// What of the batch the kernels read: entries of many rows (wide), of at most kNarrowRows rows in runs that a team of waves
-// takes, and of so few pages that a wave takes them alone; the members' requests; (first slot, slots) of each request.
-constexpr int kSharedPassed = 64;  // up to this many entries and requests travel with the launches
+// A run before it is cut, as it travels with a launch: part s is of split_pages pages and goes to slot + s.
+struct SharedEntry {
+  SharedRun run;
+  int32_t first_item, split_pages;  // items (part, block of rows, head) of its kind's entries before it
+};
+constexpr int kWideRows = 256, kNarrowRows = 16;
+constexpr int kWidePages = 1024;  // most pages of a part of a run of many rows
+constexpr int kTeamWaves = 4;
+inline __host__ __device__ int wide_blocks(int rows) { return (rows + kWideRows - 1) / kWideRows; }
+inline __host__ __device__ int wide_waves(int rows) {  // of a workgroup, where the blocks share the rows evenly
+  return ((rows + 31) / 32 + wide_blocks(rows) - 1) / wide_blocks(rows);
+}
+
+// What of the batch the kernels read.  Up to kSharedPassed entries and requests travel with the launches; otherwise all runs as
+// they are cut are in device memory.  Runs of many rows (wide) come first, then those of at most kNarrowRows rows that a team of
+// waves takes, and those of so few pages that a wave takes them alone.
+constexpr int kSharedPassed = 64;
 struct SharedTables {
-  const SharedEntry* entries;
+  const SharedRun* runs;
   const int32_t* list;
-  const int2* slots;
+  const int2* slots;  // [R] (first slot, slots)
 };
 struct SharedPassed {
   SharedEntry entries[kSharedPassed];
@@ -67,15 +81,13 @@ struct SharedArgs {
   float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator; the latter's sign bit: a bad page)
   int32_t* err;
   int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
-  int32_t n_wide, n_team, n_lone, wide_items, team_items, lone_items;
+  int32_t n_wide, n_team, n_lone;  // entries (of SharedPassed) or runs (of SharedTables)
+  int32_t wide_items, team_items, lone_items;
   int32_t max_slots;  // of a request
   int32_t direct;     // one slot each and no wide entry: the results go straight to out, and err is clear beforehand
   float scale_log2;
 };
-constexpr int kWideRows = 256, kNarrowRows = 16;
-constexpr int kWidePages = 1024;  // most pages of a wide split
-constexpr int kTeamWaves = 4;
-// passed: on the host, or null (then `tables` is in device memory).
+// passed: on the host, or null (then what `tables` names is in device memory).
 hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, hipStream_t s);
 
 }  // namespace duet

@@ -2148,13 +2148,14 @@ int norm_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* nor
 // How decode attention over shared prefixes is cut.  The rule goes by the batch only.
 struct SharedPlan {
   std::vector<SharedEntry> wide, team, lone;
+  std::vector<SharedRun> runs;  // where they are not passed
   std::vector<int32_t> list;  // the requests themselves, then the groups' members
   std::vector<int2> slots;
   int64_t wide_items = 0, team_items = 0, lone_items = 0, n_slots = 0;
   int max_slots = 0;
   bool direct = false;  // results go straight to out
   bool passed = false;  // the lists travel with the launches
-  size_t off_entries = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
+  size_t off_runs = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
 };
 
 int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
@@ -2174,8 +2175,6 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
 
 // Teams of waves that the runs of few rows are cut for, and the most pages of one's.
 constexpr int kTeamsWanted = 512, kTeamPages = 128;
-
-int blocks_of(int64_t rows) { return (int)((rows + kWideRows - 1) / kWideRows); }
 
 // Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
 // workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
@@ -2219,7 +2218,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
       const int64_t rows = (int64_t)count[i] * g;
-      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, blocks_of(rows), (int)rows});
+      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, wide_blocks((int)rows), (int)rows});
       else narrow_pages += p->len[i] / 16;
       member0[i] = at;
       at += count[i];
@@ -2235,12 +2234,14 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     const int64_t even = (narrow_pages * hkv + kTeamsWanted - 1) / kTeamsWanted;
     const int narrow_split = (int)std::min<int64_t>(kTeamPages, std::max<int64_t>(16, (even + 15) / 16 * 16));
     // Runs of up to 16 rows: a team of waves takes one of more than four pages.
-    auto add_narrow = [&](SharedEntry e, int n) {
-      const bool team = e.tokens > 64;
-      int64_t& items = team ? plan->team_items : plan->lone_items;
+    auto add = [&](std::vector<SharedEntry>& to, int64_t& items, SharedEntry e, int64_t parts) {
       e.first_item = (int32_t)std::min<int64_t>(items, INT32_MAX);
-      items += (int64_t)n * hkv;
-      (team ? plan->team : plan->lone).push_back(e);
+      items += parts * hkv;
+      to.push_back(e);
+    };
+    auto add_narrow = [&](const SharedEntry& e, int n) {
+      if (e.run.tokens > 64) add(plan->team, plan->team_items, e, n);
+      else add(plan->lone, plan->lone_items, e, n);
     };
     plan->slots.assign(R, make_int2(0, 0));
     for (size_t i = 0; i < count.size(); ++i) {
@@ -2248,26 +2249,42 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       const int64_t rows = (int64_t)count[i] * g;
       const bool wide = rows > kNarrowRows;
       const int split = wide ? wide_split : narrow_split, n = (p->len[i] / 16 + split - 1) / split;
-      SharedEntry e{0, member0[i], count[i], plan->list[member0[i]], 0, p->len[i], split, 0};
-      if (wide) {
-        e.first_item = (int32_t)std::min<int64_t>(plan->wide_items, INT32_MAX);
-        plan->wide_items += (int64_t)n * hkv * blocks_of(rows);
-        plan->wide.push_back(e);
-      } else {
-        add_narrow(e, n);
-      }
+      const SharedEntry e{{plan->list[member0[i]], 0, p->len[i], 0, member0[i], count[i], 0, 0}, 0, split};
+      if (wide) add(plan->wide, plan->wide_items, e, (int64_t)n * wide_blocks((int)rows));
+      else add_narrow(e, n);
       for (int m = 0; m < count[i]; ++m) plan->slots[plan->list[member0[i] + m]].y = n;
     }
     for (int r = 0; r < R; ++r) {
       const int before = shared(r) ? p->len[p->of[r]] : 0, tokens = b->reqs[r].cached_len + 1 - before;
+      plan->slots[r].x = (int)std::min<int64_t>(plan->n_slots, INT32_MAX);
       if (tokens > 0) {
         const int n = ((tokens + 15) / 16 + narrow_split - 1) / narrow_split;
-        add_narrow(SharedEntry{0, r, 1, r, before / 16, tokens, narrow_split, plan->slots[r].y}, n);
+        add_narrow(SharedEntry{{r, before / 16, tokens, plan->slots[r].x + plan->slots[r].y, r, 1, 0, 0}, 0, narrow_split}, n);
         plan->slots[r].y += n;
       }
-      plan->slots[r].x = (int)std::min<int64_t>(plan->n_slots, INT32_MAX);
       plan->n_slots += plan->slots[r].y;
       plan->max_slots = std::max(plan->max_slots, plan->slots[r].y);
+      if (plan->n_slots > INT32_MAX / 2) return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
+    }
+    const size_t entries = plan->wide.size() + plan->team.size() + plan->lone.size();
+    plan->direct = plan->max_slots <= 1 && plan->wide.empty();
+    plan->passed = !plan->direct && entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed && R <= kSharedPassed;
+    if (!plan->passed) {
+      // The entries cut, each part by blocks of rows.
+      for (const auto* kind : {&plan->wide, &plan->team, &plan->lone})
+        for (const SharedEntry& e : *kind) {
+          const int rows = e.run.members * g, blocks = kind == &plan->wide ? wide_blocks(rows) : 1;
+          for (int64_t at = 0; at < e.run.tokens; at += 16 * e.split_pages)
+            for (int k = 0; k < blocks; ++k) {
+              SharedRun r = e.run;
+              r.page0 += (int)(at / 16);
+              r.tokens = (int)std::min<int64_t>(r.tokens - at, 16 * e.split_pages);
+              r.slot += (int)(at / 16 / e.split_pages);
+              r.waves = kind == &plan->wide ? wide_waves(rows) : 0;
+              r.row0 = 32 * r.waves * k;
+              plan->runs.push_back(r);
+            }
+        }
     }
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
@@ -2275,11 +2292,8 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
   if (plan->wide_items > INT32_MAX / 2 || plan->team_items > INT32_MAX / 2 || plan->lone_items > INT32_MAX / 2 ||
       plan->n_slots > INT32_MAX / 2)
     return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
-  const size_t n_entries = plan->wide.size() + plan->team.size() + plan->lone.size();
-  plan->direct = plan->max_slots <= 1 && plan->wide.empty();
-  plan->passed = !plan->direct && n_entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed && R <= kSharedPassed;
-  plan->off_entries = kAlign;
-  plan->off_list = plan->off_entries + align_up(n_entries * sizeof(SharedEntry));
+  plan->off_runs = kAlign;
+  plan->off_list = plan->off_runs + align_up(plan->runs.size() * sizeof(SharedRun));
   plan->off_slots = plan->off_list + align_up(plan->list.size() * sizeof(int32_t));
   plan->off_ml = plan->off_slots + align_up(plan->slots.size() * sizeof(int2));
   plan->off_acc = plan->off_ml + align_up((size_t)plan->n_slots * s->num_q_heads * sizeof(float2));
@@ -2451,16 +2465,16 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.h_kv = shape->num_kv_heads;
   a.group = a.h_q / a.h_kv;
   a.head_dim = shape->head_dim;
-  a.n_wide = (int)plan.wide.size();
-  a.n_team = (int)plan.team.size();
-  a.n_lone = (int)plan.lone.size();
+  a.n_wide = plan.passed ? (int)plan.wide.size() : (int)(plan.wide_items / a.h_kv);
+  a.n_team = plan.passed ? (int)plan.team.size() : (int)(plan.team_items / a.h_kv);
+  a.n_lone = plan.passed ? (int)plan.lone.size() : (int)(plan.lone_items / a.h_kv);
   a.wide_items = (int)plan.wide_items;
   a.team_items = (int)plan.team_items;
   a.lone_items = (int)plan.lone_items;
   a.max_slots = plan.max_slots;
   a.direct = plan.direct;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
-  const SharedTables tables{reinterpret_cast<const SharedEntry*>(ws + plan.off_entries),
+  const SharedTables tables{reinterpret_cast<const SharedRun*>(ws + plan.off_runs),
                             reinterpret_cast<const int32_t*>(ws + plan.off_list), reinterpret_cast<const int2*>(ws + plan.off_slots)};
   SharedPassed passed;
   if (plan.passed) {
@@ -2469,13 +2483,10 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
     std::copy(plan.list.begin(), plan.list.end(), passed.list);
     std::copy(plan.slots.begin(), plan.slots.end(), passed.slots);
   } else {
-    const size_t wide_bytes = plan.wide.size() * sizeof(SharedEntry), team_bytes = plan.team.size() * sizeof(SharedEntry);
-    const UploadPart parts[5] = {{plan.wide.data(), wide_bytes, plan.off_entries},
-                                 {plan.team.data(), team_bytes, plan.off_entries + wide_bytes},
-                                 {plan.lone.data(), plan.lone.size() * sizeof(SharedEntry), plan.off_entries + wide_bytes + team_bytes},
+    const UploadPart parts[3] = {{plan.runs.data(), plan.runs.size() * sizeof(SharedRun), plan.off_runs},
                                  {plan.list.data(), plan.list.size() * sizeof(int32_t), plan.off_list},
                                  {plan.slots.data(), plan.slots.size() * sizeof(int2), plan.off_slots}};
-    if ((rc = upload_parts(ctx, parts, 5, ws, st))) return rc;
+    if ((rc = upload_parts(ctx, parts, 3, ws, st))) return rc;
   }
   HIP_TRY(launch_shared(a, tables, plan.passed ? &passed : nullptr, st));
   return DUET_OK;
