@@ -209,6 +209,31 @@ __device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPas
   return r;
 }
 
+template <bool WIDE>
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPlain& tab, int first, int n, int item) {
+  const int slot = item / a.h_kv, r = uniform(find_request(a.num_reqs, [&](int i) { return tab.first[i] <= slot; }));
+  const int part = slot - tab.first[r];
+  return SharedRun{r, part * tab.split_pages, min(tab.tokens[r] - 16 * part * tab.split_pages, 16 * tab.split_pages), slot, r, 1, 0, 0};
+}
+__device__ __forceinline__ int2 slots_of(const SharedTables& tab, int r) { return tab.slots[r]; }
+__device__ __forceinline__ int2 slots_of(const SharedPassed& tab, int r) { return tab.slots[r]; }
+__device__ __forceinline__ int2 slots_of(const SharedSlots& tab, int r) { return tab.slots[r]; }
+__device__ __forceinline__ int2 slots_of(const SharedPlain& tab, int r) { return make_int2(tab.first[r], tab.first[r + 1] - tab.first[r]); }
+__device__ __forceinline__ int listed(const SharedTables& tab, int i) { return tab.list[i]; }
+__device__ __forceinline__ int listed(const SharedPassed& tab, int i) { return tab.list[i]; }
+__device__ __forceinline__ int listed(const SharedPlain&, int i) { return i; }
+
+// The error word of a launch that nothing cleared it for: a workgroup checks every page id that the others read.
+__device__ void check_pages(const SharedArgs& a, const SharedPlain& tab) {
+  bool bad = false;
+  for (int r = 0; r < a.num_reqs; ++r) {
+    const int* row = a.table + (size_t)r * a.max_pages;
+    for (int p = threadIdx.x; p < (tab.tokens[r] + 15) >> 4; p += blockDim.x) bad |= !page_ok(row[p], a.pages);
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *a.err = bad;
+}
+
 template <int D>
 constexpr int team_floats(int rows) { return kTeamWaves * rows * (D + 4); }  // LDS; rows start on different banks
 
@@ -217,6 +242,7 @@ template <int D, bool EIGHT, int W, typename Table>
 __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& tab, int block, float* lds) {
   constexpr int kTeams = W / kTeamWaves;
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, wave = uniform(threadIdx.x >> 6);
+  constexpr bool kChecked = std::is_same<Table, SharedPlain>::value;  // direct: the error word is another workgroup's
   const bool direct = a.direct;
   const int team_blocks = (a.team_items + kTeams - 1) / kTeams;
   const bool team = block < team_blocks;
@@ -227,7 +253,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
   const SharedRun e = run_of<false>(a, tab, e0, n, has ? item : 0);
   const int g = a.group, rows = e.members * g, j = (has ? item : 0) % a.h_kv;
   // The lane's row, as request * h_q + head, or -1.  A request alone is its row of the page table.
-  auto request = [&](int row) { return e.members == 1 ? e.table_row : tab.list[e.member0 + row / g]; };
+  auto request = [&](int row) { return e.members == 1 ? e.table_row : listed(tab, e.member0 + row / g); };
   const int head_row = col < rows ? request(col) * a.h_q + j * g + col % g : -1;
   bf16x8 qf[D / 32];
   {
@@ -240,13 +266,13 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
       qf[ks] = __builtin_bit_cast(bf16x8, u);
     }
   }
-  auto slot = [&](int r) { return (size_t)(e.members == 1 ? e.slot : tab.slots[r].x + e.slot); };
+  auto slot = [&](int r) { return (size_t)(e.members == 1 ? e.slot : slots_of(tab, r).x + e.slot); };
   Rows<D> o;
   const int member = wave % kTeamWaves;  // of its team
   const int* prow = a.table + (size_t)e.table_row * a.max_pages + e.page0;
   bool bad = walk<D, EIGHT>(a, prow, has ? e.tokens : 0, j, team ? 4 * member : 0, team ? 4 * kTeamWaves : 4, qf, o);
   if (!team) {
-    if (direct && bad && lane == 0) atomicOr(a.err, 1);
+    if (!kChecked && direct && bad && lane == 0) atomicOr(a.err, 1);
     if (head_row < 0) return;
     if (direct) {
       __bf16* y = a.out + (size_t)head_row * D + 4 * quad;
@@ -273,7 +299,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
     if (quad == 0) mine[D] = o.m, mine[D + 1] = o.l;
   }
   bad = __syncthreads_or(bad);
-  if (direct && bad && threadIdx.x == 0) atomicOr(a.err, 1);
+  if (!kChecked && direct && bad && threadIdx.x == 0) atomicOr(a.err, 1);
   if (!has) return;
   for (int x = 4 * (64 * member + lane); x < rows * D; x += 4 * 64 * kTeamWaves) {
     const int row = x / D, dim = x % D;
@@ -306,6 +332,13 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
 template <int D, bool EIGHT, typename Table>
 __global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, Table tab) {
   extern __shared__ __attribute__((aligned(16))) float part[];
+  if constexpr (std::is_same<Table, SharedPlain>::value) {
+    if (a.direct) {
+      if (blockIdx.x == 0) check_pages(a, tab);
+      else narrow_items<D, EIGHT, kTeamWaves>(a, tab, blockIdx.x - 1, part);
+      return;
+    }
+  }
   if (!a.direct && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;  // the join sets it
   narrow_items<D, EIGHT, kTeamWaves>(a, tab, blockIdx.x, part);
 }
@@ -332,7 +365,7 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
   const int pair = W >= 4 ? (int)blockIdx.x : (int)(blockIdx.x * 4 + wave) / W;
   if (pair >= a.num_reqs * a.h_q) return;  // the whole workgroup where W is not 1
   const int r = pair / a.h_q;
-  const int2 at = tab.slots[r];
+  const int2 at = slots_of(tab, r);
   const size_t first = (size_t)at.x * a.h_q + pair - r * a.h_q;
   float top = -INFINITY, den = 0.f, num[E] = {};
   bool bad = false;
@@ -394,26 +427,42 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
   for (int i = 0; i < E; ++i) a.out[(size_t)pair * D + 64 * i + lane] = static_cast<__bf16>(num[i] / den);
 }
 
-template <int D, bool EIGHT, typename Table>
-hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
-  auto blocks = [&](int waves) {
-    return (a.team_items + waves / kTeamWaves - 1) / (waves / kTeamWaves) + (a.lone_items + waves - 1) / waves;
-  };
-  if (a.wide_items) {
-    constexpr size_t kBytes = std::max(WideLds<D, EIGHT>::kBytes, 2 * team_floats<D>(kNarrowRows) * sizeof(float));
-    static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_mixed<D, EIGHT, Table>),
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
-    if (set != hipSuccess) return set;
-    hipLaunchKernelGGL((shared_mixed<D, EIGHT, Table>), dim3(a.wide_items + blocks(kWideWaves)), dim3(kWideThreads), kBytes, s, a, tab);
-  } else {
-    hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(blocks(kTeamWaves)), dim3(64 * kTeamWaves),
-                       team_floats<D>(kNarrowRows) * sizeof(float), s, a, tab);
-  }
-  if (a.direct) return hipGetLastError();
+template <int D, typename Table>
+void launch_merge(const SharedArgs& a, const Table& tab, hipStream_t s) {
   const int pairs = a.num_reqs * a.h_q;
   if (a.max_slots > 64) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);
   else if (a.max_slots > 16) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
   else hipLaunchKernelGGL((shared_merge<D, 1, Table>), dim3((pairs + 3) / 4), dim3(256), 0, s, a, tab);
+}
+
+template <int D, bool EIGHT, typename Table>
+hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
+  constexpr bool kPlain = std::is_same<Table, SharedPlain>::value;
+  auto blocks = [&](int waves) {
+    return (a.team_items + waves / kTeamWaves - 1) / (waves / kTeamWaves) + (a.lone_items + waves - 1) / waves;
+  };
+  bool wide = false;
+  if constexpr (!kPlain) {
+    if (a.wide_items) {
+      wide = true;
+      constexpr size_t kBytes = std::max(WideLds<D, EIGHT>::kBytes, 2 * team_floats<D>(kNarrowRows) * sizeof(float));
+      static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&shared_mixed<D, EIGHT, Table>),
+                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+      if (set != hipSuccess) return set;
+      hipLaunchKernelGGL((shared_mixed<D, EIGHT, Table>), dim3(a.wide_items + blocks(kWideWaves)), dim3(kWideThreads), kBytes, s, a, tab);
+    }
+  }
+  if (!wide)
+    hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(blocks(kTeamWaves) + (kPlain && a.direct ? 1 : 0)),
+                       dim3(64 * kTeamWaves), team_floats<D>(std::is_same<Table, SharedPlain>::value ? a.group : kNarrowRows) * sizeof(float), s, a, tab);
+  if (a.direct) return hipGetLastError();
+  if constexpr (std::is_same<Table, SharedPassed>::value) {
+    SharedSlots slots;
+    std::copy(tab.slots, tab.slots + a.num_reqs, slots.slots);
+    launch_merge<D>(a, slots, s);
+  } else {
+    launch_merge<D>(a, tab, s);
+  }
   return hipGetLastError();
 }
 template <typename Table>
@@ -424,9 +473,10 @@ hipError_t launch(const SharedArgs& a, const Table& t, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, hipStream_t s) {
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, const SharedPlain* plain,
+                         hipStream_t s) {
   if (a.num_reqs == 0) return hipSuccess;
-  return passed ? launch(a, *passed, s) : launch(a, tables, s);
+  return plain ? launch(a, *plain, s) : passed ? launch(a, *passed, s) : launch(a, tables, s);
 }
 
 }  // namespace duet

@@ -56,20 +56,30 @@ inline __host__ __device__ int wide_waves(int rows) {  // of a workgroup, where 
   return ((rows + 31) / 32 + wide_blocks(rows) - 1) / wide_blocks(rows);
 }
 
-// What of the batch the kernels read.  Up to kSharedPassed entries and requests travel with the launches; otherwise all runs as
-// they are cut are in device memory.  Runs of many rows (wide) come first, then those of at most kNarrowRows rows that a team of
-// waves takes, and those of so few pages that a wave takes them alone.
-constexpr int kSharedPassed = 64;
-struct SharedTables {
+// What of the batch the kernels read, in one of three ways: runs of many rows (wide) come first, then those of at most kNarrowRows
+// rows that a team of waves takes, and those of so few pages that a wave takes them alone.
+struct SharedTables {  // in device memory, every part of a run listed
   const SharedRun* runs;
   const int32_t* list;
   const int2* slots;  // [R] (first slot, slots)
 };
-struct SharedPassed {
+constexpr int kSharedPassed = 64;
+struct SharedPassed {  // with the launches: up to kSharedPassed entries and requests
   SharedEntry entries[kSharedPassed];
   int32_t list[2 * kSharedPassed];
   int2 slots[kSharedPassed];
 };
+struct SharedSlots {
+  int2 slots[kSharedPassed];
+};
+constexpr int kSharedPlain = 256;
+struct SharedPlain {  // with the launches: up to kSharedPlain requests that share nothing, all of them taken by teams or all by lone waves
+  int32_t first[kSharedPlain + 1];  // the requests' first slots, the slots' end after the last
+  int32_t tokens[kSharedPlain];
+  int32_t split_pages;
+};
+constexpr int kSharedCheckedPages = 8192;  // page ids that a workgroup beside the others checks
+
 struct SharedArgs {
   const __bf16* q;  // [R, h_q, d]
   const void *k, *v;
@@ -84,10 +94,11 @@ struct SharedArgs {
   int32_t n_wide, n_team, n_lone;  // entries (of SharedPassed) or runs (of SharedTables)
   int32_t wide_items, team_items, lone_items;
   int32_t max_slots;  // of a request
-  int32_t direct;     // one slot each and no wide entry: the results go straight to out, and err is clear beforehand
+  int32_t direct;     // one slot each and no run of many rows: the results go straight to out
   float scale_log2;
 };
-// passed: on the host, or null (then what `tables` names is in device memory).
-hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, hipStream_t s);
+// On the host one of plain and passed, or neither (then what `tables` names is in device memory).
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, const SharedPlain* plain,
+                         hipStream_t s);
 
 }  // namespace duet

@@ -2152,9 +2152,9 @@ struct SharedPlan {
   std::vector<int32_t> list;  // the requests themselves, then the groups' members
   std::vector<int2> slots;
   int64_t wide_items = 0, team_items = 0, lone_items = 0, n_slots = 0;
-  int max_slots = 0;
+  int max_slots = 0, split = 0;
   bool direct = false;  // results go straight to out
-  bool passed = false;  // the lists travel with the launches
+  bool passed = false, plain = false;  // the lists travel with the launches
   size_t off_runs = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
 };
 
@@ -2174,7 +2174,7 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
 }
 
 // Teams of waves that the runs of few rows are cut for, and the most pages of one's.
-constexpr int kTeamsWanted = 512, kTeamPages = 128;
+constexpr int kTeamsWanted = 256, kTeamPages = 128;
 
 // Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
 // workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
@@ -2225,8 +2225,10 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     }
     plan->list.resize(at);
     std::vector<int32_t> next(member0);
+    int longest = 0;
     for (int r = 0; r < R; ++r) {
       if (shared(r)) plan->list[next[p->of[r]]++] = r;
+      longest = std::max(longest, b->reqs[r].cached_len + 1);
       narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
     }
     const int64_t page_bytes = 32 * s->head_dim * (eight ? 1 : 2);  // of a head
@@ -2239,8 +2241,9 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       items += parts * hkv;
       to.push_back(e);
     };
+    const bool all_teams = at == R && R <= kSharedPlain && longest > 64;  // so that the requests travel with the launch
     auto add_narrow = [&](const SharedEntry& e, int n) {
-      if (e.run.tokens > 64) add(plan->team, plan->team_items, e, n);
+      if (all_teams || e.run.tokens > 64) add(plan->team, plan->team_items, e, n);
       else add(plan->lone, plan->lone_items, e, n);
     };
     plan->slots.assign(R, make_int2(0, 0));
@@ -2268,8 +2271,12 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     }
     const size_t entries = plan->wide.size() + plan->team.size() + plan->lone.size();
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
-    plan->passed = !plan->direct && entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed && R <= kSharedPassed;
-    if (!plan->passed) {
+    plan->plain = at == R && R <= kSharedPlain && (plan->team.empty() || plan->lone.empty()) &&
+                  (!plan->direct || narrow_pages <= kSharedCheckedPages);
+    plan->passed = !plan->plain && !plan->direct && entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed &&
+                   R <= kSharedPassed;
+    plan->split = narrow_split;
+    if (!plan->passed && !plan->plain) {
       // The entries cut, each part by blocks of rows.
       for (const auto* kind : {&plan->wide, &plan->team, &plan->lone})
         for (const SharedEntry& e : *kind) {
@@ -2477,7 +2484,12 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   const SharedTables tables{reinterpret_cast<const SharedRun*>(ws + plan.off_runs),
                             reinterpret_cast<const int32_t*>(ws + plan.off_list), reinterpret_cast<const int2*>(ws + plan.off_slots)};
   SharedPassed passed;
-  if (plan.passed) {
+  SharedPlain plain;
+  if (plan.plain) {
+    for (int r = 0; r < a.num_reqs; ++r) plain.first[r] = plan.slots[r].x, plain.tokens[r] = batch->reqs[r].cached_len + 1;
+    plain.first[a.num_reqs] = (int)plan.n_slots;
+    plain.split_pages = plan.split;
+  } else if (plan.passed) {
     SharedEntry* e = std::copy(plan.wide.begin(), plan.wide.end(), passed.entries);
     std::copy(plan.lone.begin(), plan.lone.end(), std::copy(plan.team.begin(), plan.team.end(), e));
     std::copy(plan.list.begin(), plan.list.end(), passed.list);
@@ -2488,7 +2500,7 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
                                  {plan.slots.data(), plan.slots.size() * sizeof(int2), plan.off_slots}};
     if ((rc = upload_parts(ctx, parts, 3, ws, st))) return rc;
   }
-  HIP_TRY(launch_shared(a, tables, plan.passed ? &passed : nullptr, st));
+  HIP_TRY(launch_shared(a, tables, plan.passed ? &passed : nullptr, plan.plain ? &plain : nullptr, st));
   return DUET_OK;
 }
 
