@@ -63,11 +63,11 @@ struct SharedTables {  // in device memory, every part of a run listed
   const int32_t* list;
   const int2* slots;  // [R] (first slot, slots)
 };
-constexpr int kSharedPassed = 64;
-struct SharedPassed {  // with the launches: up to kSharedPassed entries and requests
-  SharedEntry entries[kSharedPassed];
-  int32_t list[2 * kSharedPassed];
+constexpr int kSharedPassed = 64, kSharedEntries = 72;
+struct SharedPassed {  // with the launches: up to kSharedPassed requests and kSharedEntries entries
+  SharedEntry entries[kSharedEntries];
   int2 slots[kSharedPassed];
+  uint16_t list[2 * kSharedPassed];
 };
 struct SharedSlots {
   int2 slots[kSharedPassed];

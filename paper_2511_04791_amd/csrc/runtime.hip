@@ -2273,7 +2273,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
     plan->plain = at == R && R <= kSharedPlain && (plan->team.empty() || plan->lone.empty()) &&
                   (!plan->direct || narrow_pages <= kSharedCheckedPages);
-    plan->passed = !plan->plain && !plan->direct && entries <= kSharedPassed && plan->list.size() <= 2 * kSharedPassed &&
+    plan->passed = !plan->plain && !plan->direct && entries <= kSharedEntries && plan->list.size() <= 2 * kSharedPassed &&
                    R <= kSharedPassed;
     plan->split = narrow_split;
     if (!plan->passed && !plan->plain) {
