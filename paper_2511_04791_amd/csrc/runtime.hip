@@ -2178,11 +2178,13 @@ constexpr int kTeamsWanted = 256, kTeamPages = 128;
 
 // Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
 // workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
-// 1 us and 0.18 for each of its waves with rows, and a CU reads some 25 KB of the other runs in a us.
-int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes) {  // (pages, row blocks, rows)
+// 1 us and 0.18 for each of its waves with rows, 1.6 times that where it widens 8-bit values, and a CU reads some 25 KB of the
+// other runs in a us.  us by the CUs that the runs of many rows are cut for, 88 / 112 / 144 / 180 / 256 / 512: 256 requests in five
+// groups, 8-bit, 73 / 66 / 68 / 69 / 75 / 89; 64 requests after 32768 tokens, bf16, 216 / 163 / 131 / 114 / 124 / 141.
+int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes, bool eight) {  // (pages, row blocks, rows)
   if (runs.empty()) return 4;
   double wide_us = 0;
-  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * (1.0 + 0.18 * std::min(8, (r[2] / r[1] + 31) / 32));
+  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * (1.0 + 0.18 * std::min(8, (r[2] / r[1] + 31) / 32)) * (eight ? 1.6 : 1.0);
   const double share = wide_us / (wide_us + narrow_bytes / 25000.0);
   auto items = [&](int split) {
     int64_t n = 0;
@@ -2232,7 +2234,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
     }
     const int64_t page_bytes = 32 * s->head_dim * (eight ? 1 : 2);  // of a head
-    const int wide_split = wide_split_pages(runs, hkv, narrow_pages * hkv * page_bytes);
+    const int wide_split = wide_split_pages(runs, hkv, narrow_pages * hkv * page_bytes, eight);
     const int64_t even = (narrow_pages * hkv + kTeamsWanted - 1) / kTeamsWanted;
     const int narrow_split = (int)std::min<int64_t>(kTeamPages, std::max<int64_t>(16, (even + 15) / 16 * 16));
     // Runs of up to 16 rows: a team of waves takes one of more than four pages.
