@@ -93,7 +93,10 @@ class _BatchC:
 
     def end_row(self) -> int:
         """One past the last request's rows: the tokens of a batch whose rows are packed, as the library checks."""
-        return int(self.rows[-1][1]) + int(self.rows[-1][2]) if len(self.rows) else 0
+        if not len(self.rows):
+            return 0
+        last = self.arr[len(self.rows) - 1]
+        return last.q_start + last.q_len
 
     def num_decodes(self) -> int:
         return self.rows[:, 0].tolist().count(KIND_DECODE) if len(self.rows) else 0
@@ -480,7 +483,7 @@ class Context:
         else:
             N.check(N.lib().duet_init_with_model(device, model_path.encode(), ctypes.byref(h)), "duet_init_with_model")
         self.handle = h
-        self._torch, self._dev = torch, torch.device("cuda", device)
+        self._torch, self._dev, self._lib = torch, torch.device("cuda", device), N.lib()
         self.model = Model(N.lib().duet_ctx_model(h), owner=self)
         self._ws = None
 
@@ -792,16 +795,19 @@ class Context:
                                 workspace.data_ptr(), workspace.nbytes, self._current(stream)), "duet_sample")
         return out, probs
 
-    def _check_table(self, table, name, reqs):
-        if table.dim() != 2 or table.shape[0] < reqs:
+    def _check_table(self, table, name, reqs) -> int:
+        """A page table's columns."""
+        shape = table.shape
+        if len(shape) != 2 or shape[0] < reqs:
             raise ValueError(f"{name} must be [R, max_pages] with a row per request")
-        self._check_on(table, name, self._torch.int32, table.shape)
+        self._check_on(table, name, self._torch.int32, shape)
+        return shape[1]
 
-    def _check_cache8(self, cache, shape: AttnShape):
+    def _check_cache8(self, cache, hkv: int, d: int):
         if not isinstance(cache, Cache8):
             raise TypeError("cache must be a Cache8")
-        if (cache.device, cache.num_kv_heads, cache.head_dim) != (self.device, shape.num_kv_heads, shape.head_dim):
-            raise ValueError(f"the cache must lie on cuda:{self.device} with {shape.num_kv_heads} heads of {shape.head_dim}")
+        if cache.device != self.device or cache.num_kv_heads != hkv or cache.head_dim != d:
+            raise ValueError(f"the cache must lie on cuda:{self.device} with {hkv} heads of {d}")
 
     def _request_space(self, b, workspace, stream, check_errors):
         """Pointer and size of a workspace for the requests' table and the error word, and the tensor; none where nobody would
@@ -809,17 +815,17 @@ class Context:
         if workspace is None and not check_errors and len(b.rows) <= N.ROPE_NO_WORKSPACE:
             return (None, 0), None
         n = ctypes.c_size_t()
-        N.check(N.lib().duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
+        N.check(self._lib.duet_rope_workspace_bytes(ctypes.byref(b.c), ctypes.byref(n)), "duet_rope_workspace_bytes")
         workspace = self._space(workspace, n.value, stream)
         return (workspace.data_ptr(), workspace.nbytes), workspace
 
     def _split_args(self, qkv, page_table, b, shape: AttnShape, norm, rope, positions, q, stream):
-        """Checks and the query tensor of the splits with a norm."""
+        """Checks of the splits with a norm: the page table's columns and the query tensor."""
         torch = self._torch
         T, dt = b.end_row(), torch.bfloat16 if shape.dtype == "bf16" else torch.float32
         hq, hkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
         self._check_on(qkv, "qkv", dt, (T, (hq + 2 * hkv) * d))
-        self._check_table(page_table, "page_table", len(b.rows))
+        columns = self._check_table(page_table, "page_table", len(b.rows))
         if norm is not None:
             for t, name in ((norm.q_weight, "q_weight"), (norm.k_weight, "k_weight")):
                 if t is not None:
@@ -830,17 +836,17 @@ class Context:
             self._check_on(positions, "positions", torch.int32,
                            (T,) if rope.axes == 1 and positions.dim() == 1 else (rope.axes, T))
         if q is None:
-            return self._empty((T, hq, d), dt, stream)
+            return columns, self._empty((T, hq, d), dt, stream)
         self._check_on(q, "q", dt, (T, hq, d))
-        return q
+        return columns, q
 
     def qkv_norm_rope_split(self, qkv, k_cache, v_cache, page_table, seq_meta, shape: AttnShape, norm: HeadNorm,
                             rope: Rope | None = None, *, positions=None, q=None, workspace=None, stream=None,
                             check_errors: bool = False):
         """duet_qkv_norm_rope_split: qkv_rope_split with the norm of each head of queries and keys before the rotation (rope
         None: no rotation)."""
-        b, lib = _BatchC(seq_meta), N.lib()
-        q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
+        b, lib = _BatchC(seq_meta), self._lib
+        columns, q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
         pages = int(k_cache.shape[0])
         self._check_on(k_cache, "k_cache", qkv.dtype, (pages, shape.num_kv_heads, shape.page_size, shape.head_dim))
         self._check_on(v_cache, "v_cache", qkv.dtype, (pages, shape.num_kv_heads, shape.head_dim, shape.page_size))
@@ -852,7 +858,7 @@ class Context:
                                              ctypes.byref(rope.c) if rope is not None else None, qkv.data_ptr(),
                                              positions.data_ptr() if positions is not None else None, q.data_ptr(),
                                              k_cache.data_ptr(), v_cache.data_ptr(), pages, page_table.data_ptr(),
-                                             page_table.shape[1], ctypes.byref(b.c), *ws, st), "duet_qkv_norm_rope_split")
+                                             columns, ctypes.byref(b.c), *ws, st), "duet_qkv_norm_rope_split")
         if check_errors:
             N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
         return q
@@ -861,9 +867,9 @@ class Context:
                    rope: Rope | None = None, positions=None, q=None, workspace=None, stream=None, check_errors: bool = False):
         """duet_qkv_split8: the query rows out of qkv (bf16), keys and values into an 8-bit cache, after the norm of each head and
         the rotation where they are given."""
-        b, lib = _BatchC(seq_meta), N.lib()
-        q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
-        self._check_cache8(cache, shape)
+        b, lib = _BatchC(seq_meta), self._lib
+        columns, q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
+        self._check_cache8(cache, shape.num_kv_heads, shape.head_dim)
         ws, workspace = self._request_space(b, workspace, stream, check_errors)
         if len(b.rows) == 0:
             return q
@@ -871,7 +877,7 @@ class Context:
         N.check(lib.duet_qkv_split8(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(norm.c) if norm is not None else None,
                                     ctypes.byref(rope.c) if rope is not None else None, qkv.data_ptr(),
                                     positions.data_ptr() if positions is not None else None, q.data_ptr(), ctypes.byref(cache.c),
-                                    page_table.data_ptr(), page_table.shape[1], ctypes.byref(b.c), *ws, st), "duet_qkv_split8")
+                                    page_table.data_ptr(), columns, ctypes.byref(b.c), *ws, st), "duet_qkv_split8")
         if check_errors:
             N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
         return q
@@ -880,21 +886,21 @@ class Context:
                     check_errors: bool = False):
         """duet_cache8_read: the requests' contexts out of an 8-bit cache into bf16 pages k_out and v_out, whose ids out_table
         [R, max_pages] gives."""
-        torch, b, lib = self._torch, _BatchC(seq_meta), N.lib()
-        shape = AttnShape(cache.num_kv_heads, cache.num_kv_heads, cache.head_dim, "bf16")
-        self._check_cache8(cache, shape)
-        self._check_table(page_table, "page_table", len(b.rows))
-        self._check_table(out_table, "out_table", len(b.rows))
+        torch, b, lib = self._torch, _BatchC(seq_meta), self._lib
+        self._check_cache8(cache, cache.num_kv_heads, cache.head_dim)
+        hkv, d = cache.num_kv_heads, cache.head_dim
+        columns = self._check_table(page_table, "page_table", len(b.rows))
+        out_columns = self._check_table(out_table, "out_table", len(b.rows))
         pages = int(k_out.shape[0])
-        self._check_on(k_out, "k_out", torch.bfloat16, (pages, cache.num_kv_heads, 16, cache.head_dim))
-        self._check_on(v_out, "v_out", torch.bfloat16, (pages, cache.num_kv_heads, cache.head_dim, 16))
+        self._check_on(k_out, "k_out", torch.bfloat16, (pages, hkv, 16, d))
+        self._check_on(v_out, "v_out", torch.bfloat16, (pages, hkv, d, 16))
         ws, workspace = self._request_space(b, workspace, stream, check_errors)
         if len(b.rows) == 0:
             return k_out, v_out
         st = self._current(stream)
-        N.check(lib.duet_cache8_read(self.handle, ctypes.byref(_shape_c(shape)), ctypes.byref(cache.c), page_table.data_ptr(),
-                                     page_table.shape[1], ctypes.byref(b.c), k_out.data_ptr(), v_out.data_ptr(), pages,
-                                     out_table.data_ptr(), out_table.shape[1], *ws, st), "duet_cache8_read")
+        N.check(lib.duet_cache8_read(self.handle, ctypes.byref(N.Shape(hkv, hkv, d, 16, BF16, 1)), ctypes.byref(cache.c),
+                                     page_table.data_ptr(), columns, ctypes.byref(b.c), k_out.data_ptr(), v_out.data_ptr(), pages,
+                                     out_table.data_ptr(), out_columns, *ws, st), "duet_cache8_read")
         if check_errors:
             N.check(lib.duet_check_device_error(self.handle, ws[0], st), "duet_check_device_error")
         return k_out, v_out
@@ -904,23 +910,21 @@ class Context:
         """duet_attn_decode_shared: decode attention of bf16 q [R, h_q, d] over a Cache8, or a pair (k_cache, v_cache) of bf16
         tensors.  prefix_of: for each request the index of the prefix it shares, or -1; prefix_len: the prefixes' tokens, whole
         pages, whose pages the requests' rows of page_table have in common."""
-        torch, b, lib = self._torch, _BatchC(seq_meta), N.lib()
+        torch, b, lib = self._torch, _BatchC(seq_meta), self._lib
         if q.dim() != 3:
             raise ValueError("q must be [R, h_q, d]")
-        R, hq, d = b.end_row(), int(q.shape[1]), int(q.shape[2])
+        R, (_, hq, d) = b.end_row(), q.shape
         self._check_on(q, "q", torch.bfloat16, (R, hq, d))
         if isinstance(cache, Cache8):
-            shape = AttnShape(hq, cache.num_kv_heads, d, "bf16")
-            self._check_cache8(cache, shape)
-            c = cache.c
+            hkv, c = cache.num_kv_heads, cache.c
+            self._check_cache8(cache, hkv, d)
         else:
             k, v = cache
-            pages, hkv = int(k.shape[0]), int(k.shape[1])
-            shape = AttnShape(hq, hkv, d, "bf16")
+            pages, hkv = k.shape[:2]
             self._check_on(k, "k_cache", torch.bfloat16, (pages, hkv, 16, d))
             self._check_on(v, "v_cache", torch.bfloat16, (pages, hkv, d, 16))
             c = N.KvCache(k.data_ptr(), v.data_ptr(), None, pages)
-        self._check_table(page_table, "page_table", len(b.rows))
+        columns = self._check_table(page_table, "page_table", len(b.rows))
         prefixes = None
         if (prefix_of is None) != (prefix_len is None):
             raise ValueError("prefix_of and prefix_len come together")
@@ -928,13 +932,13 @@ class Context:
             of, length = (np.ascontiguousarray(x, dtype=np.int32) for x in (prefix_of, prefix_len))
             if of.shape != (len(b.rows),) or length.ndim != 1:
                 raise ValueError(f"prefix_of must hold {len(b.rows)} values, one per request, and prefix_len one per prefix")
-            as_ints = ctypes.POINTER(ctypes.c_int32)
-            prefixes = ctypes.byref(N.Prefixes(len(length), length.ctypes.data_as(as_ints), of.ctypes.data_as(as_ints)))
+            prefixes = ctypes.byref(N.Prefixes(len(length), *[(ctypes.c_int32 * len(x)).from_buffer_copy(x) if len(x) else None
+                                                              for x in (length, of)]))
         if out is None:
             out = self._empty((R, hq, d), torch.bfloat16, stream)
         else:
             self._check_on(out, "out", torch.bfloat16, (R, hq, d))
-        n, s = ctypes.c_size_t(), _shape_c(shape)
+        n, s = ctypes.c_size_t(), N.Shape(hq, hkv, d, 16, BF16, 1)
         N.check(lib.duet_shared_workspace_bytes(ctypes.byref(s), ctypes.byref(b.c), prefixes, ctypes.byref(n)),
                 "duet_shared_workspace_bytes")
         workspace = self._space(workspace, n.value, stream)
@@ -942,7 +946,7 @@ class Context:
             return out
         st = self._current(stream)
         N.check(lib.duet_attn_decode_shared(self.handle, ctypes.byref(s), q.data_ptr(), ctypes.byref(c), page_table.data_ptr(),
-                                            page_table.shape[1], ctypes.byref(b.c), prefixes, workspace.data_ptr(),
+                                            columns, ctypes.byref(b.c), prefixes, workspace.data_ptr(),
                                             workspace.nbytes, out.data_ptr(), st), "duet_attn_decode_shared")
         if check_errors:
             N.check(lib.duet_check_device_error(self.handle, workspace.data_ptr(), st), "duet_check_device_error")

@@ -2427,6 +2427,7 @@ int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch
     SharedPlan plan;
     if ((rc = plan_shared(shape, batch, prefixes, eight, &plan))) return rc;
     most = std::max(most, plan.total);
+    if (plan.wide.empty()) break;  // only runs of many rows are
   }
   *bytes = most;
   return DUET_OK;
