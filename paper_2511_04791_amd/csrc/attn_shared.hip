@@ -427,11 +427,12 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
   for (int i = 0; i < E; ++i) a.out[(size_t)pair * D + 64 * i + lane] = static_cast<__bf16>(num[i] / den);
 }
 
+// Waves for each (request, query head) so that a round or two of loads is enough, within the 2^32 threads that a grid may have.
 template <int D, typename Table>
 void launch_merge(const SharedArgs& a, const Table& tab, hipStream_t s) {
   const int pairs = a.num_reqs * a.h_q;
-  if (a.max_slots > 64) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);
-  else if (a.max_slots > 16) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
+  if (a.max_slots > 64 && pairs <= 1 << 21) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);
+  else if (a.max_slots > 8 && pairs <= 1 << 23) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
   else hipLaunchKernelGGL((shared_merge<D, 1, Table>), dim3((pairs + 3) / 4), dim3(256), 0, s, a, tab);
 }
 

@@ -1276,7 +1276,8 @@ struct DeviceGuard {
 // fits a grid.
 constexpr int kMaxOpTokens = 1 << 22;
 constexpr int kMaxSampleRows = 1 << 20;
-constexpr int kMaxReadPages = 1 << 24;  // of one read-back: a workgroup each
+constexpr int kMaxReadPages = (1 << 24) - 1;  // of one read-back, workgroups of 256: a grid has under 2^32 threads
+constexpr int kMaxSharedItems = 1 << 22;      // workgroups of up to 512
 
 int batch_tokens(const duet_batch* b, int32_t* tokens) {
   int64_t t = 0;
@@ -2298,8 +2299,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
   }
-  if (plan->wide_items > INT32_MAX / 2 || plan->team_items > INT32_MAX / 2 || plan->lone_items > INT32_MAX / 2 ||
-      plan->n_slots > INT32_MAX / 2)
+  if (plan->wide_items > kMaxSharedItems || plan->team_items > kMaxSharedItems || plan->lone_items > kMaxSharedItems)
     return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
   plan->off_runs = kAlign;
   plan->off_list = plan->off_runs + align_up(plan->runs.size() * sizeof(SharedRun));
