@@ -71,8 +71,11 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
     bad |= p < n_pages && !ok;
     ids[p] = ok ? id : -1;
   }
-  bad = __syncthreads_or(bad);
-  auto page_mask = [&](int t) {  // which of a tile's pages count
+  bad = uniform(__syncthreads_or(bad));
+  // Which of a tile's pages count.  All of most: the ids are read again only where some do not, since waiting for them would mean
+  // waiting for the operands read before.
+  auto page_mask = [&](int t) {
+    if (!bad && (t + 1 < n_tiles || n_pages % 4 == 0)) return 15;
     const int4 v = *reinterpret_cast<const int4*>(ids + 4 * t);
     return uniform((v.x >= 0 ? 1 : 0) | (v.y >= 0 ? 2 : 0) | (v.z >= 0 ? 4 : 0) | (v.w >= 0 ? 8 : 0));
   };
