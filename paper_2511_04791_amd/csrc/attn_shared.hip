@@ -251,10 +251,13 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
   if (!team && !has) return;
   const int e0 = a.n_wide + (team ? 0 : a.n_team), n = team ? a.n_team : a.n_lone;
   const SharedRun e = run_of<false>(a, tab, e0, n, has ? item : 0);
-  const int g = a.group, rows = e.members * g, j = (has ? item : 0) % a.h_kv;
-  // The lane's row, as request * h_q + head, or -1.  A request alone is its row of the page table.
-  auto request = [&](int row) { return e.members == 1 ? e.table_row : listed(tab, e.member0 + row / g); };
-  const int head_row = col < rows ? request(col) * a.h_q + j * g + col % g : -1;
+  const int g = a.group, rows = min(kNarrowRows, e.members * g - e.row0), j = (has ? item : 0) % a.h_kv;
+  // A row as request * h_q + head.  A request alone is its row of the page table.
+  auto head_of = [&](int row) {
+    row += e.row0;
+    return (e.members == 1 ? e.table_row : listed(tab, e.member0 + row / g)) * a.h_q + j * g + row % g;
+  };
+  const int head_row = col < rows ? head_of(col) : -1;
   bf16x8 qf[D / 32];
   {
     const __bf16* q = a.q + (size_t)max(head_row, 0) * D;
@@ -266,7 +269,10 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
       qf[ks] = __builtin_bit_cast(bf16x8, u);
     }
   }
-  auto slot = [&](int r) { return (size_t)(e.members == 1 ? e.slot : slots_of(tab, r).x + e.slot); };
+  auto state = [&](int head_row) {  // where the row's state goes
+    const int r = head_row / a.h_q;
+    return (size_t)(e.members == 1 ? e.slot : slots_of(tab, r).x + e.slot) * a.h_q + (head_row - r * a.h_q);
+  };
   Rows<D> o;
   const int member = wave % kTeamWaves;  // of its team
   const int* prow = a.table + (size_t)e.table_row * a.max_pages + e.page0;
@@ -283,8 +289,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
         for (int i = 0; i < 4; ++i) y[16 * n + i] = static_cast<__bf16>(o.acc[n][i] * inv);
       return;
     }
-    const int r = head_row / a.h_q;
-    const size_t at = slot(r) * a.h_q + (head_row - r * a.h_q);
+    const size_t at = state(head_row);
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(a.acc + at * D + 16 * n + 4 * quad) = o.acc[n];
     if (quad == 0) a.ml[at] = make_float2(o.m, marked(o.l, bad));
@@ -314,15 +319,15 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
       l += f * p[w * rows * (D + 4) + D + 1];
       sum += f * *reinterpret_cast<const f32x4*>(p + w * rows * (D + 4) + dim);
     }
-    const int r = request(row), head = j * g + row % g;
+    const int to_row = head_of(row);
     if (direct) {
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       const float inv = 1.f / l;
-      *reinterpret_cast<bf16x4*>(a.out + ((size_t)r * a.h_q + head) * D + dim) =
+      *reinterpret_cast<bf16x4*>(a.out + (size_t)to_row * D + dim) =
           bf16x4{static_cast<__bf16>(sum[0] * inv), static_cast<__bf16>(sum[1] * inv), static_cast<__bf16>(sum[2] * inv),
                  static_cast<__bf16>(sum[3] * inv)};
     } else {
-      const size_t at = slot(r) * a.h_q + head;
+      const size_t at = state(to_row);
       *reinterpret_cast<f32x4*>(a.acc + at * D + dim) = sum;
       if (dim == 0) a.ml[at] = make_float2(to, marked(l, bad));
     }

@@ -41,7 +41,7 @@ struct SharedRun {
   int32_t table_row, page0, tokens;  // pages from page0 of a row of the page table
   int32_t slot;      // where the rows' states go: of one member, else counted from each member's first slot
   int32_t member0, members;
-  int32_t row0, waves;  // of many rows: a workgroup's first, and its waves with rows
+  int32_t row0, waves;  // the first row; of many rows: a workgroup's waves with rows
 };
 // A run before it is cut, as it travels with a launch: part s is of split_pages pages and goes to slot + s.
 struct SharedEntry {

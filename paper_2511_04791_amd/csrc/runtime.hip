@@ -2176,16 +2176,22 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
 
 // Teams of waves that the runs of few rows are cut for, and the most pages of one's.
 constexpr int kTeamsWanted = 256, kTeamPages = 128;
+constexpr double kTeamUs = 4.0;
 
 // Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
 // workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
 // 1 us and 0.18 for each of its waves with rows, 1.6 times that where it widens 8-bit values, and a CU reads some 25 KB of the
 // other runs in a us.  us by the CUs that the runs of many rows are cut for, 88 / 112 / 144 / 180 / 256 / 512: 256 requests in five
 // groups, 8-bit, 73 / 66 / 68 / 69 / 75 / 89; 64 requests after 32768 tokens, bf16, 216 / 163 / 131 / 114 / 124 / 141.
+// us that a CU takes for a tile of 64 keys of a kv head: for up to 256 rows as a workgroup takes them, where a wave takes 32; for
+// each 16 as teams of waves do, which read the tile for each again.
+double wide_tile_us(int waves, bool eight) { return (1.0 + 0.18 * waves) * (eight ? 1.6 : 1.0); }
+double narrow_tile_us(int d, bool eight) { return 256.0 * d * (eight ? 1 : 2) / 2 / 25000.0; }
+
 int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes, bool eight) {  // (pages, row blocks, rows)
   if (runs.empty()) return 4;
   double wide_us = 0;
-  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * (1.0 + 0.18 * std::min(8, (r[2] / r[1] + 31) / 32)) * (eight ? 1.6 : 1.0);
+  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * wide_tile_us(std::min(8, (r[2] / r[1] + 31) / 32), eight);
   const double share = wide_us / (wide_us + narrow_bytes / 25000.0);
   auto items = [&](int split) {
     int64_t n = 0;
@@ -2215,14 +2221,24 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     auto shared = [&](int r) { return p && p->of[r] >= 0 && count[p->of[r]] > 1 && p->len[p->of[r]] > 0; };
     plan->list.resize(R);
     for (int r = 0; r < R; ++r) plan->list[r] = r;
+    // Rows of a prefix go to teams of waves, 16 each, where all prefixes together keep the CUs busy for kTeamUs at most, or where that
+    // takes less of their time than workgroups of 256 rows do; a team's short run ends sooner.
+    auto row_blocks = [&](int i) { return (count[i] * g + kNarrowRows - 1) / kNarrowRows; };
+    double team_us = 0;
+    for (size_t i = 0; i < count.size(); ++i)
+      if (count[i] > 1) team_us += (double)hkv * p->len[i] / 64 * row_blocks((int)i) * narrow_tile_us(s->head_dim, eight);
+    auto is_wide = [&](int i) {
+      const int rows = count[i] * g, blocks = wide_blocks(rows);
+      return rows > kNarrowRows && team_us > kTeamUs * DUET_TOTAL_CUS &&
+             row_blocks(i) * narrow_tile_us(s->head_dim, eight) > blocks * wide_tile_us(std::min(8, (rows / blocks + 31) / 32), eight);
+    };
     std::vector<std::array<int, 3>> runs;
     int64_t narrow_pages = 0;
     int at = R;
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
-      const int64_t rows = (int64_t)count[i] * g;
-      if (rows > kNarrowRows) runs.push_back({p->len[i] / 16, wide_blocks((int)rows), (int)rows});
-      else narrow_pages += p->len[i] / 16;
+      if (is_wide((int)i)) runs.push_back({p->len[i] / 16, wide_blocks(count[i] * g), count[i] * g});
+      else narrow_pages += (int64_t)(p->len[i] / 16) * row_blocks((int)i);
       member0[i] = at;
       at += count[i];
     }
@@ -2252,12 +2268,12 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     plan->slots.assign(R, make_int2(0, 0));
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
-      const int64_t rows = (int64_t)count[i] * g;
-      const bool wide = rows > kNarrowRows;
+      const bool wide = is_wide((int)i);
       const int split = wide ? wide_split : narrow_split, n = (p->len[i] / 16 + split - 1) / split;
-      const SharedEntry e{{plan->list[member0[i]], 0, p->len[i], 0, member0[i], count[i], 0, 0}, 0, split};
-      if (wide) add(plan->wide, plan->wide_items, e, (int64_t)n * wide_blocks((int)rows));
-      else add_narrow(e, n);
+      SharedEntry e{{plan->list[member0[i]], 0, p->len[i], 0, member0[i], count[i], 0, 0}, 0, split};
+      if (wide) add(plan->wide, plan->wide_items, e, (int64_t)n * wide_blocks(count[i] * g));
+      else
+        for (; e.run.row0 < count[i] * g; e.run.row0 += kNarrowRows) add_narrow(e, n);
       for (int m = 0; m < count[i]; ++m) plan->slots[plan->list[member0[i] + m]].y = n;
     }
     for (int r = 0; r < R; ++r) {
@@ -2290,8 +2306,10 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
               r.page0 += (int)(at / 16);
               r.tokens = (int)std::min<int64_t>(r.tokens - at, 16 * e.split_pages);
               r.slot += (int)(at / 16 / e.split_pages);
-              r.waves = kind == &plan->wide ? wide_waves(rows) : 0;
-              r.row0 = 32 * r.waves * k;
+              if (kind == &plan->wide) {
+                r.waves = wide_waves(rows);
+                r.row0 = 32 * r.waves * k;
+              }
               plan->runs.push_back(r);
             }
         }
