@@ -2176,34 +2176,36 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
 
 // Teams of waves that the runs of few rows are cut for, and the most pages of one's.
 constexpr int kTeamsWanted = 256, kTeamPages = 128;
-constexpr double kTeamUs = 4.0;
+constexpr double kTeamUs = 2.0;
 
-// Pages of a wide split: the fewest, at least a tile, with which the runs of many rows take their share of the CUs once, or 1024
-// workgroups where they fill those more often.  The share is that of the time: a tile of 64 keys takes a workgroup some
-// 1 us and 0.18 for each of its waves with rows, 1.6 times that where it widens 8-bit values, and a CU reads some 25 KB of the
-// other runs in a us.  us by the CUs that the runs of many rows are cut for, 88 / 112 / 144 / 180 / 256 / 512: 256 requests in five
-// groups, 8-bit, 73 / 66 / 68 / 69 / 75 / 89; 64 requests after 32768 tokens, bf16, 216 / 163 / 131 / 114 / 124 / 141.
 // us that a CU takes for a tile of 64 keys of a kv head: for up to 256 rows as a workgroup takes them, where a wave takes 32; for
-// each 16 as teams of waves do, which read the tile for each again.
+// each 16 as teams of waves do, which read the tile for each again (some 25 KB a us).
 double wide_tile_us(int waves, bool eight) { return (1.0 + 0.18 * waves) * (eight ? 1.6 : 1.0); }
 double narrow_tile_us(int d, bool eight) { return 256.0 * d * (eight ? 1 : 2) / 2 / 25000.0; }
 
+// Pages of a part of a run of many rows.  Its kind's share of the CUs is that of the time.  The parts are as few as take those CUs once;
+// where whole runs are more than that already, they last at most half as long as all (and four tiles at least).  us by the CUs that the
+// runs of many rows are cut for, 88 / 112 / 144 / 180 / 256 / 512: 256 requests in five groups, 8-bit, 73 / 66 / 68 / 69 / 75 / 89;
+// 64 requests after 32768 tokens, bf16, 216 / 163 / 131 / 114 / 124 / 141.
 int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes, bool eight) {  // (pages, row blocks, rows)
   if (runs.empty()) return 4;
   double wide_us = 0;
   for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * wide_tile_us(std::min(8, (r[2] / r[1] + 31) / 32), eight);
-  const double share = wide_us / (wide_us + narrow_bytes / 25000.0);
+  const double all_us = wide_us + narrow_bytes / 25000.0;
   auto items = [&](int split) {
     int64_t n = 0;
     for (const auto& r : runs) n += (int64_t)((r[0] + split - 1) / split) * r[1] * hkv;
     return n;
   };
-  const int64_t cus = std::max<int64_t>(16, (int64_t)(DUET_TOTAL_CUS * share));
-  const int64_t most = items(kWidePages) <= cus ? cus : 4 * DUET_TOTAL_CUS;
+  const int64_t cus = std::clamp<int64_t>((int64_t)(DUET_TOTAL_CUS * wide_us / all_us) + 4, 16, DUET_TOTAL_CUS);
+  if (items(kWidePages) > cus) {
+    const double tiles = all_us / DUET_TOTAL_CUS / 2 / wide_tile_us(8, eight);
+    return 4 * std::max(4, (int)std::min<double>(kWidePages / 4, tiles));
+  }
   int lo = 1, hi = kWidePages / 4;  // in tiles
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
-    if (items(4 * mid) <= most) hi = mid;
+    if (items(4 * mid) <= cus) hi = mid;
     else lo = mid + 1;
   }
   return 4 * lo;

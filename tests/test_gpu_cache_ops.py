@@ -457,6 +457,94 @@ def test_attn_decode_shared(ctx, name, heads, cache):
     assert torch.equal(out, ctx.attn_decode_shared(*args, **pre))  # a workspace of its own, nobody reads the error word
 
 
+# Prefixes long enough for workgroups of many rows: one, two and no whole tile of 64 keys at the end, one block of 256 rows and two, of
+# which the last is not full, tables in device memory and with the launches.
+WIDE = {
+    "one": ((32, 8, 128), [1008], [(0, 1 + i % 40) for i in range(60)]),
+    "two": ((32, 8, 128), [976, 1280], [(i % 3 - 1, 3 + 7 * i % 90) for i in range(80)]),
+    "blocks": ((64, 8, 64), [2000], [(0, i % 20) for i in range(37)]),
+    "group16": ((32, 2, 128), [4096, 3008], [(i % 2, 1 + i % 17) for i in range(43)]),
+    "group3": ((24, 8, 64), [2064], [(0, 5 + i) for i in range(31)]),
+    "long": ((8, 1, 128), [66000], [(0, 2), (0, 300), (0, 17), (0, 1), (0, 64), (-1, 5)]),
+}
+
+
+def _wide_case(name, seed, cache):
+    import paper_2511_04791_amd as duet
+    heads, prefixes, reqs = WIDE[name]
+    sh = duet.AttnShape(*heads, "bf16")
+    table, meta, pool, used = _shared_batch(sh, seed, prefixes, reqs)
+    q, c, values = _attn_inputs(sh, cache, seed + 1, pool, used, len(reqs))
+    return sh, table, meta, pool, q, c, values, dict(prefix_of=[i for i, _ in reqs], prefix_len=prefixes)
+
+
+@pytest.mark.parametrize("name", list(WIDE))
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_attn_of_many_rows(ctx, name, cache):
+    """Also with pages outside the pool in the prefix and behind it, then clean again."""
+    import paper_2511_04791_amd as duet
+    sh, table, meta, pool, q, c, values, pre = _wide_case(name, 9000, cache)
+    ws = torch.full((_space(sh, meta, pre),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    q_gpu = q.cuda()
+    for again in range(2):
+        ctx.attn_decode_shared(q_gpu, c, torch.as_tensor(table, device="cuda"), meta, out=out, workspace=ws, check_errors=True, **pre)
+        _check_attn(out, q, values, table, meta)
+        if again:
+            break
+        bad = table.copy()
+        members = [r for r, i in enumerate(pre["prefix_of"]) if i == 0]
+        for j, page in ((0, -1), (5, pool), (14, 2 ** 31 - 1), (15, -7), (pre["prefix_len"][0] // 16 - 1, pool + 3)):
+            bad[members, j] = page
+        bad[members[-1], meta[members[-1], 3] // 16] = -2
+        with pytest.raises(duet.DuetError) as e:
+            ctx.attn_decode_shared(q_gpu, c, torch.as_tensor(bad, device="cuda"), meta, out=out, workspace=ws, check_errors=True, **pre)
+        assert e.value.code == -6
+        _check_attn(out, q, values, bad, meta)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_attn_of_many_rows_in_a_graph(ctx, cache):
+    sh, table, meta, pool, q, c, values, pre = _wide_case("two", 9100, cache)
+    pt, x, g = torch.as_tensor(table, device="cuda"), q.cuda(), torch.cuda.CUDAGraph()
+    out = torch.empty_like(x)
+    ctx.attn_decode_shared(x, c, pt, meta, out=out, **pre)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        ctx.attn_decode_shared(x, c, pt, meta, out=out, **pre)
+    for i in range(3):
+        x.copy_(_randn(9110 + i, *q.shape))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ctx.attn_decode_shared(x, c, pt, meta, **pre))
+        ctx.attn_decode_shared(x[:1], c, pt[:1], meta[:1])
+    _check_attn(out, x.cpu(), values, table, meta)
+
+
+def test_attn_of_many_rows_of_infinite_scores(ctx):
+    """Runs of keys whose scores are all -inf, for some rows and for all; a NaN reaches the rows that see it alone."""
+    from oracle import cache8 as oc
+    sh, table, meta, pool, q, c, _, pre = _wide_case("two", 9200, "bf16")
+    q = q.abs() + 0.1
+    q[5, 3] = -q[5, 3]  # sees +inf where the others see -inf
+    k, v = c[0].cpu(), c[1].cpu()
+    first = [r for r, i in enumerate(pre["prefix_of"]) if i == 0]
+    for t in range(200, 800):
+        k[table[first[0], t // 16], :, t % 16] = float("-inf")
+    k[table[first[2], meta[first[2], 3] // 16], :, meta[first[2], 3] % 16] = float("nan")
+    out = ctx.attn_decode_shared(q.cuda(), (k.cuda(), c[1]), torch.as_tensor(table, device="cuda"), meta, **pre).cpu()
+    in_first = 5 in first
+    want, mag, most = oc.decode_attention(to64(q), np.where(np.isinf(to64(k)), -1e6, to64(k)), to64(v), table, meta)
+    bad = np.isnan(to64(out))
+    assert bad[first[2]].all() and (bad[5, 3].all() if in_first else not bad[5].any())
+    rows = [r for r in range(len(meta)) if r not in (5, first[2])]
+    assert not bad[rows].any()
+    finite = np.abs(np.where(np.isfinite(to64(k)), to64(k), 0)).max() * np.abs(to64(q)).sum(-1).max() / np.sqrt(128)
+    err = np.abs(to64(out) - want)[rows]
+    bound = (U * np.abs(want) + (1.1 * U + 2 * (132 * finite + 2000) * E) * (mag + np.abs(want)))[rows]
+    assert (err <= bound).all()
+
+
 def _space(sh, meta, pre):
     import ctypes
     import paper_2511_04791_amd as duet
