@@ -262,9 +262,10 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
   };
 
   if constexpr (EIGHT) {
-    Raw next = fetch(0);
-    put(0, next);
+    const Raw first = fetch(0);
+    Raw next = first;
     if (n_tiles > 1) next = fetch(1);
+    put(0, first);
     __syncthreads();
     for (int t = 0; t < n_tiles; ++t) {
       // Tile t + 1 was loaded during the step before, t + 2 is during this one.
