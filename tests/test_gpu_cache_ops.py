@@ -744,6 +744,37 @@ def test_attention_in_a_graph(ctx, name):
         ctx.attn_decode_shared(q[:1], c, pt[:1], meta[:1])
 
 
+def test_graphs_that_share_a_workspace(ctx):
+    """Calls after each other in one workspace, captured ones among them: none finds what another left."""
+    import paper_2511_04791_amd as duet
+    sh = duet.AttnShape(8, 2, 64, "bf16")
+    calls = []
+    for i, name in enumerate(("plain", "groups", "two", "short", "many")):
+        prefixes, reqs = BATCHES[name]
+        table, meta, pool, used = _shared_batch(sh, 8900 + i, prefixes, reqs)
+        q, c, _ = _attn_inputs(sh, "e4m3", 8910 + i, pool, used, len(reqs))
+        pre = dict(prefix_of=[i for i, _ in reqs], prefix_len=prefixes) if prefixes else {}
+        args = (q.cuda(), c, torch.as_tensor(table, device="cuda"), meta)
+        calls.append((args, pre, ctx.attn_decode_shared(*args, **pre), _space(sh, meta, pre)))
+    ws = torch.full((max(n for *_, n in calls),), 255, dtype=torch.uint8, device="cuda")
+    graphs = []
+    torch.cuda.synchronize()
+    for args, pre, _, _ in calls:
+        g = torch.cuda.CUDAGraph()
+        out = torch.empty_like(args[0])
+        with torch.cuda.graph(g):
+            ctx.attn_decode_shared(*args, out=out, workspace=ws, **pre)
+        graphs.append((g, out))
+    for order in ((0, 1, 2, 3, 4), (4, 2, 0, 3, 1), (1, 1, 3, 0, 4, 2)):
+        for i in order:
+            graphs[i][1].zero_()
+            graphs[i][0].replay()
+            args, pre, want, _ = calls[(i + 1) % 5]
+            assert torch.equal(ctx.attn_decode_shared(*args, workspace=ws, **pre), want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(graphs[i][1], calls[i][2]) for i in order)
+
+
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_a_step_in_a_graph(ctx, cache):
     """Split, attention and read-back captured with buffers and workspaces of their own, replayed with eager work between."""
