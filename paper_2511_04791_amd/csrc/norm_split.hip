@@ -21,8 +21,6 @@
 namespace duet {
 namespace {
 
-constexpr int kRows = 4;  // of queries and keys a thread
-
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) {
   return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xf, 0xf, true));
@@ -87,7 +85,7 @@ __device__ __forceinline__ unsigned pk_max_over_lanes(unsigned x, int lanes) {  
   return lanes >= 16 ? pk_max(x, moved_bits<0x140>(x)) : x;
 }
 
-template <typename T, bool ADJACENT, bool EIGHT, typename Table>
+template <typename T, bool ADJACENT, bool EIGHT, int kRows, typename Table>
 __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x, Table requests) {
   constexpr int N = Chunk<T>::N;
   constexpr bool kPassed = std::is_same<Table, Passed>::value;
@@ -359,25 +357,35 @@ __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x
   }
 }
 
-template <typename T, bool ADJACENT, bool EIGHT>
-hipError_t launch(NormSplitArgs x, const int4* requests, hipStream_t s) {
+// kRows rows of queries and keys a thread: four, or two where that leaves fewer than four workgroups a CU.  us with 1 / 2 / 4 / 8: 8224
+// rows of 64 + 2 x 8 heads, bf16, . / 85.5 / 77.8 / 82.5; 2588 rows of 8 + 2 x 1 into 8 bits 8.3 / 7.6 / 11.1 / 13.1.
+template <typename T, bool ADJACENT, bool EIGHT, int kRows>
+hipError_t launch_rows(NormSplitArgs x, int groups, int longest, const int4* requests, hipStream_t s) {
   const RopeSplitArgs& a = x.rope;
   const int n = 16 / sizeof(T), d = a.head_dim;
-  int longest = 0;
-  for (int r = 0; r < a.num_reqs; ++r) longest = std::max(longest, requests[r].z);
-  x.single = longest == 1;
   x.parts = (std::min(longest, 16) + kRows - 1) / kRows;
   const int units = (((a.h_q + a.h_kv) * d / (2 * n) * x.parts + 15) & ~15) + a.h_kv * d / n;
-  const int groups = x.single ? a.num_reqs : a.tokens / 16 + 2 * a.num_reqs, columns = (units + 255) / 256;
+  const int columns = (units + 255) / 256;
   if (a.num_reqs <= kRopeTable) {
     Passed p;
     for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);
     p.at[a.num_reqs] = make_int2(a.tokens, 0);
-    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, x, p);
+    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, x, p);
   } else {
-    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, Uploaded>), dim3(groups, columns), dim3(256), 0, s, x, Uploaded{a.meta});
+    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Uploaded>), dim3(groups, columns), dim3(256), 0, s, x, Uploaded{a.meta});
   }
   return hipGetLastError();
+}
+template <typename T, bool ADJACENT, bool EIGHT>
+hipError_t launch(NormSplitArgs x, const int4* requests, hipStream_t s) {
+  const RopeSplitArgs& a = x.rope;
+  int longest = 0;
+  for (int r = 0; r < a.num_reqs; ++r) longest = std::max(longest, requests[r].z);
+  x.single = longest == 1;
+  const int groups = x.single ? a.num_reqs : a.tokens / 16 + 2 * a.num_reqs;
+  const long long threads = (long long)groups * (a.h_q + a.h_kv) * a.head_dim * (int)sizeof(T) / 32 * ((std::min(longest, 16) + 3) / 4);
+  return threads < 4 * 256 * 256 ? launch_rows<T, ADJACENT, EIGHT, 2>(x, groups, longest, requests, s)
+                                 : launch_rows<T, ADJACENT, EIGHT, 4>(x, groups, longest, requests, s);
 }
 
 }  // namespace
