@@ -11,6 +11,16 @@
 // p takes tokens 4 p .. 4 p + 3 of each of the four pages.  P^T is then already the operand of the second product, and a
 // lane's values are whole rows of a dim-major page: 16 bytes a load for 8-bit pages as for bf16 ones.
 // 8-bit values become bf16 exactly; a key's power of two multiplies its scores, a value's its probability.
+// Bound by memory: 256 requests of 512 to 8192 tokens, 8 kv heads, 8-bit: 264 us, 5.5 TB/s.  A step's loads go out during the step
+// before; two teams fit a CU.  A wave's runs of more than 32 pages are slower than a team's (100 pages: 301 us).
+//
+// More rows (attn_shared_wide.h): a workgroup takes up to 256 of them and brings tiles of 64 keys through LDS, bound by the matrix
+// cores, the exponentials and the LDS reads alike: 512 rows a kv head after 131072 tokens 800 TFLOP/s over bf16, 838 over 8-bit pages.
+// Both kinds run in one launch.  64 requests of 64 / 8 heads after 32768 shared tokens with 200 to 1000 of their own: 86 and 41 us one
+// after the other, 110 together.
+//
+// The runs' states are joined by a second launch; where every request has one run, results go straight out.  What the kernels know
+// of the batch travels with their launches if it is small: an upload is a launch of 4.5 us of its own.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -51,7 +61,9 @@ struct Rows {
   float l, m;
 };
 
-// The wave's steps of a run: pages first, first + 1 .. + 3, then `stride` pages on.
+// The wave's steps of a run: pages first, first + 1 .. + 3, then `stride` pages on.  Whether a page lay outside the pool.
+// (Loaded values are masked as they enter the product, not in place: modified in a branch, they were given registers of other values
+// by the compiler.)
 template <int D, bool EIGHT>
 __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n_tok, int j, int first, int stride,
                                      const bf16x8 (&qf)[D / 32], Rows<D>& o) {
@@ -432,12 +444,13 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
   for (int i = 0; i < E; ++i) a.out[(size_t)pair * D + 64 * i + lane] = static_cast<__bf16>(num[i] / den);
 }
 
-// Waves for each (request, query head) so that a round or two of loads is enough, within the 2^32 threads that a grid may have.
+// Waves for each (request, query head) so that a round or two of loads is enough where there are few of them (us of 32 with 16 runs: one
+// wave 4.3, four 3.4; of 4096 with 13: 7.2 against 9.4), within the 2^32 threads that a grid may have.
 template <int D, typename Table>
 void launch_merge(const SharedArgs& a, const Table& tab, hipStream_t s) {
   const int pairs = a.num_reqs * a.h_q;
   if (a.max_slots > 64 && pairs <= 1 << 21) hipLaunchKernelGGL((shared_merge<D, 16, Table>), dim3(pairs), dim3(1024), 0, s, a, tab);
-  else if (a.max_slots > 8 && pairs <= 1 << 23) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
+  else if (a.max_slots > (pairs < 1024 ? 8 : 16) && pairs <= 1 << 23) hipLaunchKernelGGL((shared_merge<D, 4, Table>), dim3(pairs), dim3(256), 0, s, a, tab);
   else hipLaunchKernelGGL((shared_merge<D, 1, Table>), dim3((pairs + 3) / 4), dim3(256), 0, s, a, tab);
 }
 

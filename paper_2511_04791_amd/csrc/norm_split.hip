@@ -6,9 +6,16 @@
 // head share: the smallest that brings the largest of them to 448, e4m3's largest, so the exponent follows from the bits of
 // the largest value and the division is exact; one rounding in all, after the rotation.
 //
-// Bound by memory, and laid out as rope_split.hip: a workgroup takes the rows of one request on one page, a thread two
-// 16-byte chunks of a head's row (or eight columns of values) for all of them, so a head's row lies in neighbouring lanes, 4 to
-// 16 of them, and its sum or maximum is taken by that many lanes' moves inside a row of 16.
+// Bound by memory: the projection is read once, queries and pages are written.  The rows of one request on one page go to a group of
+// workgroups; a thread takes two 16-byte chunks of a head for two or four of the rows, or eight columns of values for all of them, which
+// whole pages need turned around.  A head's row lies in 4 to 16 neighbouring lanes, and its sum or maximum is taken by moves inside a
+// row of 16 lanes.  With all sixteen rows of queries and keys a thread, as rope_split.hip has it, a small batch waited for one chain of
+// norms (five chunks on a rank, 2588 rows, into 8 bits 25 us; now 7.7) and few waves fitted (8224 rows of 64 + 2 x 8 heads 90 us; now
+// 78, 4.3 TB/s; a large copy reaches 5.1).  8192 rows of 32 + 2 x 8 heads into 8 bits 46 us (4.0 TB/s); one decode row 4.5.
+//
+// Values are converted two of a row at a time, as the row shares the power, and turned as bytes; magnitudes of bf16 are compared
+// as their bits, two in a register.  Both took a third of the instructions of a value at a time.  A page that is covered in part gets
+// whole words where four slots are new, else bytes.  Requests of one row each need no search for their group.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
