@@ -404,8 +404,8 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
       ml[u].y = fabsf(ml[u].y);
       to = fmaxf(to, ml[u].x);
     }
-    if (to == -INFINITY) continue;  // runs without a key that counts
-    const float f = fast_exp2(top - to);
+    // Runs without a key that counts weigh 0, and a NaN among their denominators stays.
+    const float sub = to == -INFINITY ? 0.f : to, f = fast_exp2(top - sub);
     top = to;
     den *= f;
 #pragma unroll
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const bool there = s0 + u * W < at.y;  // selected, not branched on: the loads stay together
-      const float wgt = fast_exp2(ml[u].x - to);
+      const float wgt = fast_exp2(ml[u].x - sub);
       den += there ? wgt * ml[u].y : 0.f;
 #pragma unroll
       for (int i = 0; i < E; ++i) num[i] += there ? wgt * x[u][i] : 0.f;

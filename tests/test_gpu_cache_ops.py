@@ -655,6 +655,25 @@ def test_attn_of_infinite_scores(ctx):
     assert (err <= bound).all()
 
 
+@pytest.mark.parametrize("prefix", [0, 2048])
+def test_attn_of_nan_among_scores_of_minus_infinity(ctx, prefix):
+    """A NaN score in a run whose others are -inf reaches the result, over many runs of -inf before the finite ones."""
+    import paper_2511_04791_amd as duet
+    sh = duet.AttnShape(16, 1, 64, "bf16")
+    prefixes, reqs = ([prefix], [(0, 8192), (0, 40)]) if prefix else ([], [(-1, 10240)])
+    table, meta, pool, used = _shared_batch(sh, 8050, prefixes, reqs)
+    q, c, _ = _attn_inputs(sh, "bf16", 8051, pool, used, len(reqs))
+    q, k = q.abs() + 0.1, c[0].cpu()
+    for t in range(0, 8192):
+        k[table[0, t // 16], :, t % 16] = float("-inf")
+    pt, q = torch.as_tensor(table, device="cuda"), q.cuda()
+    pre = dict(prefix_of=[0, 0], prefix_len=prefixes) if prefix else {}
+    assert torch.isfinite(ctx.attn_decode_shared(q, (k.cuda(), c[1]), pt, meta, **pre)).all()
+    k[table[0, 3], :, 5] = float("nan")
+    out = ctx.attn_decode_shared(q, (k.cuda(), c[1]), pt, meta, **pre)
+    assert torch.isnan(out).all()
+
+
 def test_attn_far_powers(ctx):
     """Powers far from 1: tiny and huge values and keys; a value's power never leaves what fp32 and bf16 hold."""
     import paper_2511_04791_amd as duet
