@@ -235,12 +235,13 @@ __device__ __forceinline__ int listed(const SharedTables& tab, int i) { return t
 __device__ __forceinline__ int listed(const SharedPassed& tab, int i) { return tab.list[i]; }
 __device__ __forceinline__ int listed(const SharedPlain&, int i) { return i; }
 
-// The error word of a launch that nothing cleared it for: a workgroup checks every page id that the others read.
+// The error word of a launch that nothing cleared it for: a workgroup checks every page id that the others read, 16 lanes a request.
+// (All lanes on one request after another: 52 us for 256 requests of 16 to 100 tokens.)
 __device__ void check_pages(const SharedArgs& a, const SharedPlain& tab) {
   bool bad = false;
-  for (int r = 0; r < a.num_reqs; ++r) {
+  for (int r = threadIdx.x / 16; r < a.num_reqs; r += blockDim.x / 16) {
     const int* row = a.table + (size_t)r * a.max_pages;
-    for (int p = threadIdx.x; p < (tab.tokens[r] + 15) >> 4; p += blockDim.x) bad |= !page_ok(row[p], a.pages);
+    for (int p = threadIdx.x % 16; p < (tab.tokens[r] + 15) >> 4; p += 16) bad |= !page_ok(row[p], a.pages);
   }
   bad = __syncthreads_or(bad);
   if (threadIdx.x == 0) *a.err = bad;
