@@ -353,7 +353,8 @@ int duet_sample(duet_ctx* ctx, const void* logits, int32_t dtype, int32_t rows, 
 
 /* A layer's paged cache.  scales NULL: k [P, h_kv, 16, d] and v [P, h_kv, d, 16] of shape.dtype.  Otherwise an 8-bit cache: the
  * same layouts of bytes, e4m3 values (4 exponent bits, largest 448), and a byte e for each token, kv head and side: its d values
- * are e4m3 times 2^(e - 127).  scales [P, h_kv, 2, 16]: the keys' bytes, then the values'.  All lie on 16 bytes. */
+ * are e4m3 times 2^(e - 127), e of 1 to 254 (a token that nobody attends may hold anything).  scales [P, h_kv, 2, 16]: the keys'
+ * bytes, then the values'.  All lie on 16 bytes. */
 typedef struct {
   void* k;
   void* v;
@@ -369,7 +370,7 @@ typedef struct {
 } duet_head_norm;
 
 /* duet_qkv_rope_split with the norm of each head before the rotation; rope NULL: nothing turns.  Sums, norm and rotation in fp32
- * with one rounding.  Arguments, workspace and error word as there. */
+ * with one rounding: a head whose squares' sum passes fp32's largest becomes zeros.  Arguments, workspace and error word as there. */
 int duet_qkv_norm_rope_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* norm, const duet_rope* rope,
                              const void* qkv, const int32_t* positions, void* q, void* k_cache, void* v_cache,
                              int64_t num_phys_pages, const int32_t* page_table, int32_t max_pages_per_req,
@@ -407,7 +408,8 @@ int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch
 /* Decode attention of one layer, as duet_attn_mixed_batch gives it for a batch of decode requests: bf16 q and out [R, h_q, d], over a
  * bf16 or an 8-bit cache.  prefixes NULL: nothing is shared.  The result does not depend on the pages' placement nor on the stream;
  * the order of its sums follows the batch's lengths and prefixes.  Probabilities are rounded to bf16.  q, out and the workspace lie on
- * 16 bytes; out is none of the others.  Page ids outside the pool are not read, their tokens do not count, and they set the error word. */
+ * 16 bytes; out is none of the others.  Page ids outside the pool are not read, their tokens do not count, and they set the error word;
+ * a request none of whose tokens count gives NaN.  A batch of no requests clears the error word. */
 int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* q, const duet_kv_cache* cache,
                             const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch,
                             const duet_prefixes* prefixes, void* workspace, size_t workspace_bytes, void* out, void* stream);

@@ -846,6 +846,8 @@ class Context:
         """duet_qkv_norm_rope_split: qkv_rope_split with the norm of each head of queries and keys before the rotation (rope
         None: no rotation)."""
         b, lib = _BatchC(seq_meta), self._lib
+        if norm is None:
+            raise TypeError("norm must be a HeadNorm")
         columns, q = self._split_args(qkv, page_table, b, shape, norm, rope, positions, q, stream)
         pages = int(k_cache.shape[0])
         self._check_on(k_cache, "k_cache", qkv.dtype, (pages, shape.num_kv_heads, shape.page_size, shape.head_dim))
@@ -939,8 +941,9 @@ class Context:
         else:
             self._check_on(out, "out", torch.bfloat16, (R, hq, d))
         n, s = ctypes.c_size_t(), N.Shape(hq, hkv, d, 16, BF16, 1)
-        N.check(lib.duet_shared_workspace_bytes(ctypes.byref(s), ctypes.byref(b.c), prefixes, ctypes.byref(n)),
-                "duet_shared_workspace_bytes")
+        if workspace is None:  # the library checks the size of a given one
+            N.check(lib.duet_shared_workspace_bytes(ctypes.byref(s), ctypes.byref(b.c), prefixes, ctypes.byref(n)),
+                    "duet_shared_workspace_bytes")
         workspace = self._space(workspace, n.value, stream)
         if len(b.rows) == 0:
             return out

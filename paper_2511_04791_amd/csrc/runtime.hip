@@ -2120,6 +2120,7 @@ int norm_split(duet_ctx* ctx, const duet_shape* shape, const duet_head_norm* nor
                         static_cast<const void*>(cache.scales)})
     if (o && (o == qkv || o == wq || o == wk || o == page_table || o == positions))
       return fail(DUET_EINVAL, "an output aliases an input");
+  if (cache.scales && q == cache.scales) return fail(DUET_EINVAL, "q is the cache's scales");
   if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(DUET_EINVAL, "the workspace must lie on 16 bytes");
   if (!workspace && batch->num_reqs > kRopeTable)
     return fail(DUET_EINVAL, "workspace is NULL with more than %d requests", kRopeTable);
@@ -2268,6 +2269,8 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       else add(plan->lone, plan->lone_items, e, n);
     };
     plan->slots.assign(R, make_int2(0, 0));
+    plan->team.reserve(R);
+    if (!all_teams) plan->lone.reserve(R);
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
       const bool wide = is_wide((int)i);
@@ -2290,6 +2293,8 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       plan->max_slots = std::max(plan->max_slots, plan->slots[r].y);
       if (plan->n_slots > INT32_MAX / 2) return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
     }
+    if (plan->wide_items > kMaxSharedItems || plan->team_items > kMaxSharedItems || plan->lone_items > kMaxSharedItems)
+      return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
     const size_t entries = plan->wide.size() + plan->team.size() + plan->lone.size();
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
     plan->plain = at == R && R <= kSharedPlain && (plan->team.empty() || plan->lone.empty()) &&
@@ -2319,8 +2324,6 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
   } catch (const std::bad_alloc&) {
     return fail(DUET_ENOMEM, "host allocation failed");
   }
-  if (plan->wide_items > kMaxSharedItems || plan->team_items > kMaxSharedItems || plan->lone_items > kMaxSharedItems)
-    return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
   plan->off_runs = kAlign;
   plan->off_list = plan->off_runs + align_up(plan->runs.size() * sizeof(SharedRun));
   plan->off_slots = plan->off_list + align_up(plan->list.size() * sizeof(int32_t));
@@ -2472,12 +2475,15 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   SharedPlan plan;
   if ((rc = plan_shared(shape, batch, prefixes, cache->scales != nullptr, &plan))) return rc;
   if (workspace_bytes < plan.total) return fail(DUET_EWORKSPACE, "workspace %zu bytes, need %zu", workspace_bytes, plan.total);
-  if (batch->num_reqs == 0) return DUET_OK;
   std::lock_guard<std::mutex> lock(ctx->mu);
   DeviceGuard device(ctx->device);
   HIP_TRY(device.status);
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
+  if (batch->num_reqs == 0) {  // the upload clears the error word
+    const UploadPart none{nullptr, 0, kAlign};
+    return upload_parts(ctx, &none, 1, ws, st);
+  }
   SharedArgs a{};
   a.q = static_cast<const __bf16*>(q);
   a.k = cache->k;

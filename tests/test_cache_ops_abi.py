@@ -60,6 +60,14 @@ def test_shared_takes_decodes_of_bf16(native):
     assert native.duet_shared_workspace_bytes(B(N.Shape(34, 2, 64, 16, N.BF16, 1)), B(b), None, B(n)) == -2
 
 
+def test_shared_refuses_too_many_keys(native):
+    """Before their parts are listed: of 2000 requests of 2^30 - 16 tokens these would take 33 GB."""
+    n = ctypes.c_size_t()
+    for requests, code in ((1, 0), (5, -2), (2000, -2), (3000, -2)):
+        arr, b = _batch([(1, r, 1, (1 << 30) - 17) for r in range(requests)])
+        assert native.duet_shared_workspace_bytes(B(SHAPE), B(b), None, B(n)) == code
+
+
 def test_prefix_lists_are_needed(native):
     n = ctypes.c_size_t()
     arr, b = _batch(DECODES)

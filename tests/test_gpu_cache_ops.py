@@ -572,6 +572,24 @@ def test_attn_of_an_empty_batch(ctx):
     ctx.cache8_read(cache, table, meta, k, v, table)
 
 
+def test_attn_of_an_empty_batch_clears_the_error_word(ctx):
+    import ctypes
+    import paper_2511_04791_amd as duet
+    from paper_2511_04791_amd import _native as N
+    cache, b = duet.Cache8.empty(1, 2, 64), duet._BatchC(np.zeros((0, 4), np.int32))
+    ws, x = (torch.full((4096,), 255, dtype=torch.uint8, device="cuda") for _ in range(2))
+    st, shape = torch.cuda.current_stream().cuda_stream, N.Shape(4, 2, 64, 16, N.BF16, 1)
+    n = ctypes.c_size_t()
+    N.check(N.lib().duet_shared_workspace_bytes(ctypes.byref(shape), ctypes.byref(b.c), None, ctypes.byref(n)), "bytes")
+    assert n.value <= ws.nbytes
+    for _ in range(2):
+        ws.fill_(255)
+        N.check(N.lib().duet_attn_decode_shared(ctx.handle, ctypes.byref(shape), x.data_ptr(), ctypes.byref(cache.c), x.data_ptr(), 1,
+                                                ctypes.byref(b.c), None, ws.data_ptr(), ws.nbytes, x.data_ptr() + 2048, st), "attn")
+        N.check(N.lib().duet_check_device_error(ctx.handle, ws.data_ptr(), st), "error word")
+    assert (x == 255).all()
+
+
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_attn_placement_and_neighbours(ctx, cache):
     """The same bits wherever the pages lie."""
