@@ -209,12 +209,11 @@ __device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPas
       tab.entries[first + uniform(find_request(n, [&](int i) { return tab.entries[first + i].first_item <= item; }))];
   SharedRun r = e.run;
   int part = (item - e.first_item) / a.h_kv;
-  if (WIDE) {
-    const int rows = r.members * a.group, blocks = wide_blocks(rows);
-    r.waves = wide_waves(rows);
-    r.row0 = part % blocks * r.waves * 32;
-    part /= blocks;
-  }
+  // The blocks of rows of one part next to each other, so that its tiles are in their XCD's L2.
+  const int rows = r.members * a.group, blocks = WIDE ? wide_blocks(rows) : narrow_blocks(rows);
+  if (WIDE) r.waves = wide_waves(rows);
+  r.row0 = part % blocks * (WIDE ? 32 * r.waves : kNarrowRows);
+  part /= blocks;
   r.page0 += part * e.split_pages;
   r.tokens = min(r.tokens - 16 * part * e.split_pages, 16 * e.split_pages);
   r.slot += part;

@@ -51,6 +51,7 @@ struct SharedEntry {
 constexpr int kWideRows = 256, kNarrowRows = 16;
 constexpr int kWidePages = 1024;  // most pages of a part of a run of many rows
 constexpr int kTeamWaves = 4;
+inline __host__ __device__ int narrow_blocks(int rows) { return (rows + kNarrowRows - 1) / kNarrowRows; }
 inline __host__ __device__ int wide_blocks(int rows) { return (rows + kWideRows - 1) / kWideRows; }
 inline __host__ __device__ int wide_waves(int rows) {  // of a workgroup, where the blocks share the rows evenly
   return ((rows + 31) / 32 + wide_blocks(rows) - 1) / wide_blocks(rows);

@@ -2226,7 +2226,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     for (int r = 0; r < R; ++r) plan->list[r] = r;
     // Rows of a prefix go to teams of waves, 16 each, where all prefixes together keep the CUs busy for kTeamUs at most, or where that
     // takes less of their time than workgroups of 256 rows do; a team's short run ends sooner.
-    auto row_blocks = [&](int i) { return (count[i] * g + kNarrowRows - 1) / kNarrowRows; };
+    auto row_blocks = [&](int i) { return narrow_blocks(count[i] * g); };
     double team_us = 0;
     for (size_t i = 0; i < count.size(); ++i)
       if (count[i] > 1) team_us += (double)hkv * p->len[i] / 64 * row_blocks((int)i) * narrow_tile_us(s->head_dim, eight);
@@ -2264,7 +2264,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       to.push_back(e);
     };
     const bool all_teams = at == R && R <= kSharedPlain && longest > 64;  // so that the requests travel with the launch
-    auto add_narrow = [&](const SharedEntry& e, int n) {
+    auto add_narrow = [&](const SharedEntry& e, int64_t n) {
       if (all_teams || e.run.tokens > 64) add(plan->team, plan->team_items, e, n);
       else add(plan->lone, plan->lone_items, e, n);
     };
@@ -2277,8 +2277,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       const int split = wide ? wide_split : narrow_split, n = (p->len[i] / 16 + split - 1) / split;
       SharedEntry e{{plan->list[member0[i]], 0, p->len[i], 0, member0[i], count[i], 0, 0}, 0, split};
       if (wide) add(plan->wide, plan->wide_items, e, (int64_t)n * wide_blocks(count[i] * g));
-      else
-        for (; e.run.row0 < count[i] * g; e.run.row0 += kNarrowRows) add_narrow(e, n);
+      else add_narrow(e, (int64_t)n * narrow_blocks(count[i] * g));
       for (int m = 0; m < count[i]; ++m) plan->slots[plan->list[member0[i] + m]].y = n;
     }
     for (int r = 0; r < R; ++r) {
@@ -2306,17 +2305,15 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       // The entries cut, each part by blocks of rows.
       for (const auto* kind : {&plan->wide, &plan->team, &plan->lone})
         for (const SharedEntry& e : *kind) {
-          const int rows = e.run.members * g, blocks = kind == &plan->wide ? wide_blocks(rows) : 1;
+          const int rows = e.run.members * g, blocks = kind == &plan->wide ? wide_blocks(rows) : narrow_blocks(rows);
           for (int64_t at = 0; at < e.run.tokens; at += 16 * e.split_pages)
             for (int k = 0; k < blocks; ++k) {
               SharedRun r = e.run;
               r.page0 += (int)(at / 16);
               r.tokens = (int)std::min<int64_t>(r.tokens - at, 16 * e.split_pages);
               r.slot += (int)(at / 16 / e.split_pages);
-              if (kind == &plan->wide) {
-                r.waves = wide_waves(rows);
-                r.row0 = 32 * r.waves * k;
-              }
+              if (kind == &plan->wide) r.waves = wide_waves(rows);
+              r.row0 = (kind == &plan->wide ? 32 * r.waves : kNarrowRows) * k;
               plan->runs.push_back(r);
             }
         }
