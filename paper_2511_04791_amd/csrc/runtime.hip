@@ -16,7 +16,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <array>
 #include <chrono>
 #include <cmath>
 #include <cstring>
@@ -2177,39 +2176,63 @@ int check_prefixes(const duet_batch* b, const duet_prefixes* p) {
 
 // Teams of waves that the runs of few rows are cut for, and the most pages of one's.
 constexpr int kTeamsWanted = 256, kTeamPages = 128;
-constexpr double kTeamUs = 2.0;
 
-// us that a CU takes for a tile of 64 keys of a kv head: for up to 256 rows as a workgroup takes them, where a wave takes 32; for
-// each 16 as teams of waves do, which read the tile for each again (some 25 KB a us).
-double wide_tile_us(int waves, bool eight) { return (1.0 + 0.18 * waves) * (eight ? 1.6 : 1.0); }
-double narrow_tile_us(int d, bool eight) { return 256.0 * d * (eight ? 1 : 2) / 2 / 25000.0; }
+// us that a CU takes for a tile of 64 keys of a kv head, as measured over 32768 to 131072 tokens for 32 to 256 rows.  A workgroup of up
+// to 256 rows, 32 a wave: 1.4 with a wave a SIMD, 2.1 with two (64 dimensions: 0.8 and 1.4; 8-bit pages 0.1 more).  Teams of waves, 16
+// rows each next to each other, for every block of rows, and for reading the tile once: bf16 pages of 128 dimensions 1.8 for two
+// blocks, 5.3 for eight; 8-bit ones 1.0 and 3.1.
+double wide_tile_us(int rows, int d, bool eight) {  // of all blocks
+  const int waves = wide_waves(rows);
+  return wide_blocks(rows) * ((waves <= 4 ? 1.4 : 1.3 + 0.1 * waves) * (d == 64 ? 0.65 : 1.0) + (eight ? 0.1 : 0.0));
+}
+double narrow_tile_us(int blocks, int d, bool eight) { return d * (eight ? 1 : 2) / 8.0 * std::max(0.04, 0.015 + 0.02 * blocks); }
+// What a workgroup of many rows, a team and a wave alone (eight a workgroup) take besides, and what workgroups of many rows have to save
+// in all: their states are more, and the few that fit a CU start and end together.
+constexpr double kPartUs = 5.0, kTeamUs = 1.5, kLoneUs = 0.4, kWideUs = 6.0, kLateUs = 8.0;
 
-// Pages of a part of a run of many rows.  Its kind's share of the CUs is that of the time.  The parts are as few as take those CUs once;
-// where whole runs are more than that already, they last at most half as long as all (and four tiles at least).  us by the CUs that the
-// runs of many rows are cut for, 88 / 112 / 144 / 180 / 256 / 512: 256 requests in five groups, 8-bit, 73 / 66 / 68 / 69 / 75 / 89;
-// 64 requests after 32768 tokens, bf16, 216 / 163 / 131 / 114 / 124 / 141.
-int wide_split_pages(const std::vector<std::array<int, 3>>& runs, int hkv, int64_t narrow_bytes, bool eight) {  // (pages, row blocks, rows)
+struct WideRun {
+  int pages, rows;
+};
+
+// Pages of a part of a run of many rows: those that an estimate says end soonest.  Up to a part a CU all run at once, beside the runs of
+// few rows; more of them fill the CUs better and end less evenly.  Every part writes and the join reads a state a row.
+int wide_split_pages(const std::vector<WideRun>& runs, int hkv, int d, double narrow_us, bool eight) {
   if (runs.empty()) return 4;
-  double wide_us = 0;
-  for (const auto& r : runs) wide_us += hkv * r[1] * (r[0] / 4.0) * wide_tile_us(std::min(8, (r[2] / r[1] + 31) / 32), eight);
-  const double all_us = wide_us + narrow_bytes / 25000.0;
-  auto items = [&](int split) {
-    int64_t n = 0;
-    for (const auto& r : runs) n += (int64_t)((r[0] + split - 1) / split) * r[1] * hkv;
-    return n;
-  };
-  const int64_t cus = std::clamp<int64_t>((int64_t)(DUET_TOTAL_CUS * wide_us / all_us) + 4, 16, DUET_TOTAL_CUS);
-  if (items(kWidePages) > cus) {
-    const double tiles = all_us / DUET_TOTAL_CUS / 2 / wide_tile_us(8, eight);
-    return 4 * std::max(4, (int)std::min<double>(kWidePages / 4, tiles));
+  double tile = 0, wide_us = 0;
+  int longest = 0, waves = 0;
+  for (const WideRun& r : runs) {
+    waves = std::max(waves, wide_waves(r.rows));
+    const double us = wide_tile_us(r.rows, d, eight);
+    tile = std::max(tile, us / wide_blocks(r.rows));
+    wide_us += hkv * (r.pages / 4.0) * us;
+    longest = std::max(longest, (r.pages + 3) / 4);
   }
-  int lo = 1, hi = kWidePages / 4;  // in tiles
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (items(4 * mid) <= cus) hi = mid;
-    else lo = mid + 1;
+  const int tries = std::clamp<int>(2048 / (int)runs.size(), 8, 64);
+  int best = 0, last = 0;
+  double best_us = 0;
+  for (int k = 2; k <= 2 * tries; ++k) {
+    // The longest run in k / 2 parts, all alike or the last one shorter.
+    const int t = std::min(kWidePages / 4, ((longest - 1) / (k / 2) + (longest - 1) / ((k + 1) / 2)) / 2 + 1);
+    if (t == last) continue;
+    last = t;
+    int64_t items = 0, states = 0;
+    for (const WideRun& r : runs) {
+      const int64_t n = (r.pages + 4 * t - 1) / (4 * t);
+      items += n * wide_blocks(r.rows) * hkv;
+      states += n * r.rows * hkv;
+    }
+    // Fewer busy CUs run faster, where the matrix cores are what they wait for.
+    const double cus = std::min<int64_t>(items, DUET_TOTAL_CUS) / (double)DUET_TOTAL_CUS;
+    const double slow = 1.0 - (1.0 - cus) * (d == 128 && !eight && waves > 4 ? 0.05 * (waves - 2.5) : 0.1);
+    const double part = t * tile * slow + kPartUs;
+    const int64_t rounded = (items + 31) / 32 * 32;
+    const double busy = wide_us * slow + items * kPartUs, spare = (DUET_TOTAL_CUS + items - rounded) * part - busy;
+    const double left = 1.15 * narrow_us - (rounded < DUET_TOTAL_CUS ? std::max(0.0, spare) : 0.0);  // uneven runs, whole rounds of them
+    const double us = (rounded > DUET_TOTAL_CUS ? (busy + narrow_us) / DUET_TOTAL_CUS + 0.75 * part
+                                                : part + (left > 0 ? kLateUs + left / DUET_TOTAL_CUS : 0)) + states * d * 8 / 5.1e6;
+    if (!best || us < best_us) best = t, best_us = us;
   }
-  return 4 * lo;
+  return 4 * best;
 }
 
 int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, bool eight, SharedPlan* plan) {
@@ -2224,24 +2247,31 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     auto shared = [&](int r) { return p && p->of[r] >= 0 && count[p->of[r]] > 1 && p->len[p->of[r]] > 0; };
     plan->list.resize(R);
     for (int r = 0; r < R; ++r) plan->list[r] = r;
-    // Rows of a prefix go to teams of waves, 16 each, where all prefixes together keep the CUs busy for kTeamUs at most, or where that
-    // takes less of their time than workgroups of 256 rows do; a team's short run ends sooner.
-    auto row_blocks = [&](int i) { return narrow_blocks(count[i] * g); };
-    double team_us = 0;
-    for (size_t i = 0; i < count.size(); ++i)
-      if (count[i] > 1) team_us += (double)hkv * p->len[i] / 64 * row_blocks((int)i) * narrow_tile_us(s->head_dim, eight);
-    auto is_wide = [&](int i) {
-      const int rows = count[i] * g, blocks = wide_blocks(rows);
-      return rows > kNarrowRows && team_us > kTeamUs * DUET_TOTAL_CUS &&
-             row_blocks(i) * narrow_tile_us(s->head_dim, eight) > blocks * wide_tile_us(std::min(8, (rows / blocks + 31) / 32), eight);
+    // Rows of a prefix go to workgroups of 256 where that takes the CUs less time than teams of waves, 16 rows each, and all such prefixes
+    // together save enough.
+    auto saved_us = [&](int i) {
+      const int rows = count[i] * g;
+      if (rows <= kNarrowRows || p->len[i] == 0) return 0.0;
+      return hkv * (p->len[i] / 64.0 * (narrow_tile_us(narrow_blocks(rows), s->head_dim, eight) - wide_tile_us(rows, s->head_dim, eight)) +
+                    kTeamUs * narrow_blocks(rows) * (1 + p->len[i] / (16 * kTeamPages)) - kPartUs * wide_blocks(rows) * (1 + p->len[i] / 2048));
     };
-    std::vector<std::array<int, 3>> runs;
+    double all_saved = 0;
+    for (size_t i = 0; i < count.size(); ++i) all_saved += std::max(0.0, saved_us((int)i));
+    auto is_wide = [&](int i) { return all_saved > kWideUs * DUET_TOTAL_CUS && saved_us(i) > 0; };
+    std::vector<WideRun> runs;
     int64_t narrow_pages = 0;
+    double narrow_us = 0;
     int at = R;
     for (size_t i = 0; i < count.size(); ++i) {
       if (count[i] < 2 || p->len[i] == 0) continue;
-      if (is_wide((int)i)) runs.push_back({p->len[i] / 16, wide_blocks(count[i] * g), count[i] * g});
-      else narrow_pages += (int64_t)(p->len[i] / 16) * row_blocks((int)i);
+      const int rows = count[i] * g;
+      if (is_wide((int)i)) {
+        runs.push_back({p->len[i] / 16, rows});
+      } else {
+        narrow_pages += (int64_t)(p->len[i] / 16) * narrow_blocks(rows);
+        narrow_us += hkv * (p->len[i] / 64.0 * narrow_tile_us(narrow_blocks(rows), s->head_dim, eight) +
+                            kTeamUs * narrow_blocks(rows) * (1 + p->len[i] / (16 * kTeamPages)));
+      }
       member0[i] = at;
       at += count[i];
     }
@@ -2251,10 +2281,11 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     for (int r = 0; r < R; ++r) {
       if (shared(r)) plan->list[next[p->of[r]]++] = r;
       longest = std::max(longest, b->reqs[r].cached_len + 1);
-      narrow_pages += ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
+      const int64_t own = ((int64_t)b->reqs[r].cached_len + 16) / 16 - (shared(r) ? p->len[p->of[r]] / 16 : 0);
+      narrow_pages += own;
+      narrow_us += hkv * (own / 4.0 * narrow_tile_us(1, s->head_dim, eight) + (own > 4 ? kTeamUs * (1 + own / kTeamPages) : kLoneUs));
     }
-    const int64_t page_bytes = 32 * s->head_dim * (eight ? 1 : 2);  // of a head
-    const int wide_split = wide_split_pages(runs, hkv, narrow_pages * hkv * page_bytes, eight);
+    const int wide_split = wide_split_pages(runs, hkv, s->head_dim, narrow_us, eight);
     const int64_t even = (narrow_pages * hkv + kTeamsWanted - 1) / kTeamsWanted;
     const int narrow_split = (int)std::min<int64_t>(kTeamPages, std::max<int64_t>(16, (even + 15) / 16 * 16));
     // Runs of up to 16 rows: a team of waves takes one of more than four pages.
@@ -2447,7 +2478,7 @@ int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch
     SharedPlan plan;
     if ((rc = plan_shared(shape, batch, prefixes, eight, &plan))) return rc;
     most = std::max(most, plan.total);
-    if (plan.wide.empty()) break;  // only runs of many rows are
+    if (!prefixes || prefixes->num == 0) break;  // only prefixes are
   }
   *bytes = most;
   return DUET_OK;
