@@ -18,7 +18,7 @@ struct NormSplitArgs {
   float eps;
   int32_t norm;         // heads are normalised
   uint8_t* scales;      // [P, h_kv, 2, 16] of 8-bit pages, else null
-  int32_t parts, single;  // parts of a page's rows; every request has one row (the launch sets both)
+  int32_t parts, single, groups;  // parts of a page's rows; every request has one row; groups of workgroups (the launch sets them)
 };
 hipError_t launch_norm_split(const NormSplitArgs& a, const int4* requests, hipStream_t s);
 

@@ -11,7 +11,7 @@
 // whole pages need turned around.  A head's row lies in 4 to 16 neighbouring lanes, and its sum or maximum is taken by moves inside a
 // row of 16 lanes.  With all sixteen rows of queries and keys a thread, as rope_split.hip has it, a small batch waited for one chain of
 // norms (five chunks on a rank, 2588 rows, into 8 bits 25 us; now 7.7) and few waves fitted (8224 rows of 64 + 2 x 8 heads 90 us; now
-// 78, 4.3 TB/s; a large copy reaches 5.1).  8192 rows of 32 + 2 x 8 heads into 8 bits 46 us (4.0 TB/s); one decode row 4.5.
+// 71, 4.7 TB/s; a large copy reaches 5.1).  8192 rows of 32 + 2 x 8 heads into 8 bits 41 us (4.5 TB/s); one decode row 4.5.
 //
 // Values are converted two of a row at a time, as the row shares the power, and turned as bytes; magnitudes of bf16 are compared
 // as their bits, two in a register.  Both took a third of the instructions of a value at a time.  A page that is covered in part gets
@@ -92,6 +92,11 @@ __device__ __forceinline__ unsigned pk_max_over_lanes(unsigned x, int lanes) {  
   return lanes >= 16 ? pk_max(x, moved_bits<0x140>(x)) : x;
 }
 
+// The workgroups of a group next to each other, so that rows are read from one end to the other: 8224 rows of 64 + 2 x 8 heads 71 us, 78
+// with the groups next to each other; 8192 rows of 32 + 2 x 8 into 8 bits 41 against 46.
+constexpr int kGridY = 32768;
+dim3 grid_of(int columns, int groups) { return dim3(columns, std::min(groups, kGridY), (groups + kGridY - 1) / kGridY); }
+
 template <typename T, bool ADJACENT, bool EIGHT, int kRows, typename Table>
 __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x, Table requests) {
   constexpr int N = Chunk<T>::N;
@@ -99,11 +104,12 @@ __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x
   __shared__ float2 turn[16][kMaxPairs];
   const RopeSplitArgs& s = x.rope;
   const int d = s.head_dim, pairs = s.rot_dim / 2, tid = threadIdx.x;
-  int group = blockIdx.x;
+  int group = blockIdx.z * kGridY + blockIdx.y;
+  if (group >= x.groups) return;
   if (kPassed && s.err) {
     if (group == 0) {
       if constexpr (kPassed)
-        if (blockIdx.y == 0) check_pages(s, requests, reinterpret_cast<int2*>(turn));
+        if (blockIdx.x == 0) check_pages(s, requests, reinterpret_cast<int2*>(turn));
       return;
     }
     --group;
@@ -121,11 +127,11 @@ __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x
   if (n <= 0) return;
   const int id = s.page_table[(size_t)r * s.max_pages + at.page];
   const bool ok = page_ok(id, s.num_phys_pages);
-  if (!kPassed && !ok && blockIdx.y == 0 && tid == 0) atomicOr(s.err, 1);
+  if (!kPassed && !ok && blockIdx.x == 0 && tid == 0) atomicOr(s.err, 1);
   // A thread's unit: of queries and keys two chunks of kRows rows, neighbours in the row first; after those of all the page's
   // rows, and from a multiple of 16 on, so that a head's lie in one row of lanes, eight columns of values, all rows.
   const int units = d / (2 * N), nqk = s.h_q + s.h_kv, width = (nqk + s.h_kv) * d;
-  const int qk_units = nqk * units, v_units = (qk_units * x.parts + 15) & ~15, u = blockIdx.y * 256 + tid;
+  const int qk_units = nqk * units, v_units = (qk_units * x.parts + 15) & ~15, u = blockIdx.x * 256 + tid;
   const T* src = static_cast<const T*>(s.qkv) + (size_t)row * width;
   const bool qk = u < qk_units * x.parts;
   const int part = u / qk_units, unit = u - part * qk_units, t0 = kRows * part;
@@ -156,8 +162,8 @@ __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x
       a[t] = *reinterpret_cast<const uint4*>(src + (size_t)max(0, min(t - slot, n - 1)) * width + nqk * d + col);
   }
   // The sines of the rows that the workgroup's units of queries and keys have.
-  const int first_row = kRows * (int)(blockIdx.y * 256 / qk_units);
-  const int last_row = min(n, kRows * (min((int)blockIdx.y * 256 + 255, qk_units * x.parts - 1) / qk_units + 1));
+  const int first_row = kRows * (int)(blockIdx.x * 256 / qk_units);
+  const int last_row = min(n, kRows * (min((int)blockIdx.x * 256 + 255, qk_units * x.parts - 1) / qk_units + 1));
   for (int i = tid + first_row * pairs; i < last_row * pairs; i += 256) {
     const int t = i / pairs, pair = i - t * pairs;
     const int p = s.positions ? s.positions[(size_t)s.pair_axis[pair] * s.tokens + row + t] : pos + t;
@@ -373,13 +379,15 @@ hipError_t launch_rows(NormSplitArgs x, int groups, int longest, const int4* req
   x.parts = (std::min(longest, 16) + kRows - 1) / kRows;
   const int units = (((a.h_q + a.h_kv) * d / (2 * n) * x.parts + 15) & ~15) + a.h_kv * d / n;
   const int columns = (units + 255) / 256;
-  if (a.num_reqs <= kRopeTable) {
+  const bool passed = a.num_reqs <= kRopeTable;
+  x.groups = groups + (passed && a.err ? 1 : 0);  // the first clears the error word
+  if (passed) {
     Passed p;
     for (int r = 0; r < a.num_reqs; ++r) p.at[r] = make_int2(requests[r].y, requests[r].w);
     p.at[a.num_reqs] = make_int2(a.tokens, 0);
-    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Passed>), dim3(groups + (a.err ? 1 : 0), columns), dim3(256), 0, s, x, p);
+    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Passed>), grid_of(columns, x.groups), dim3(256), 0, s, x, p);
   } else {
-    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Uploaded>), dim3(groups, columns), dim3(256), 0, s, x, Uploaded{a.meta});
+    hipLaunchKernelGGL((norm_split<T, ADJACENT, EIGHT, kRows, Uploaded>), grid_of(columns, x.groups), dim3(256), 0, s, x, Uploaded{a.meta});
   }
   return hipGetLastError();
 }

@@ -228,6 +228,26 @@ def test_split8(ctx, name, heads, dtype, rot, adjacent, with_norm):
     _check_split8(sh, b, qkv, n64, (_freq(rot), adjacent) if rot else None, before, (cache.k, cache.v, cache.scales), q)
 
 
+def test_split_of_many_requests(ctx):
+    """More groups of workgroups than one dimension of the grid takes, of one row each and of more."""
+    import paper_2511_04791_amd as duet
+    from oracle import cache8 as oc
+    sh = duet.AttnShape(1, 1, 64, "bf16")
+    for rows, R in ((1, 33000), (2, 16500)):
+        meta = duet._meta_rows([(1 if rows == 1 else 0, rows, 3)] * R)
+        pt = torch.arange(R, dtype=torch.int32, device="cuda").view(R, 1)
+        qkv = _randn(7260, R * rows, 3 * 64)
+        cache = duet.Cache8.empty(R, 1, 64)
+        q = ctx.qkv_split8(qkv.cuda(), cache, pt, meta, sh, check_errors=True)
+        assert torch.equal(q.cpu()[:, 0], qkv[:, :64])
+        val = oc.e4m3_values()
+        want, e = oc.encode(to64(qkv)[:, 64:].reshape(-1, 2, 64))
+        k, v, s = cache.k.cpu().numpy()[:, 0, 3:3 + rows], cache.v.cpu().numpy()[:, 0, :, 3:3 + rows], cache.scales.cpu().numpy()[:, 0, :, 3:3 + rows]
+        assert np.array_equal(val[k].reshape(-1, 64), want[:, 0]) and np.array_equal(val[v.transpose(0, 2, 1)].reshape(-1, 64), want[:, 1])
+        assert np.array_equal(s.transpose(0, 2, 1).reshape(-1, 2), e)
+        assert int((cache.k != 0).sum()) <= R * rows * 64
+
+
 def test_split8_of_special_values(ctx):
     """Zeros, what is not finite, the smallest and largest magnitudes, the largest value on and next to a power's border."""
     import paper_2511_04791_amd as duet
