@@ -198,41 +198,44 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
   return __any(bad);
 }
 
-// Item `item` of the runs of one kind, n of them from `first` on: its part of a run.
-template <bool WIDE>
-__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedTables& tab, int first, int n, int item) {
+// Item `item` of the runs of one kind (0: many rows, 1: teams, 2: lone waves): its part of a run.
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedTables& tab, int kind, int item) {
+  const int first = kind == 0 ? 0 : kind == 1 ? a.n_wide : a.n_wide + a.n_team, n = kind == 0 ? a.n_wide : kind == 1 ? a.n_team : a.n_lone;
   return tab.runs[first + min(item / a.h_kv, n - 1)];
 }
-template <bool WIDE>
-__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPassed& tab, int first, int n, int item) {
-  const SharedEntry e =
-      tab.entries[first + uniform(find_request(n, [&](int i) { return tab.entries[first + i].first_item <= item; }))];
-  SharedRun r = e.run;
-  int part = (item - e.first_item) / a.h_kv;
-  // The blocks of rows of one part next to each other, so that its tiles are in their XCD's L2.
-  const int rows = r.members * a.group, blocks = WIDE ? wide_blocks(rows) : narrow_blocks(rows);
-  if (WIDE) r.waves = wide_waves(rows);
-  r.row0 = part % blocks * (WIDE ? 32 * r.waves : kNarrowRows);
-  part /= blocks;
-  r.page0 += part * e.split_pages;
-  r.tokens = min(r.tokens - 16 * part * e.split_pages, 16 * e.split_pages);
-  r.slot += part;
-  return r;
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPassed& tab, int kind, int item) {
+  int part = item / a.h_kv;
+  if (kind == 0 || part < tab.parts[kind - 1]) {
+    const int first = tab.kind[kind];
+    const SharedPassed::Prefix x =
+        tab.prefixes[first + uniform(find_request(tab.kind[kind + 1] - first, [&](int i) { return tab.prefixes[first + i].first <= part; }))];
+    // The blocks of rows of one part next to each other, so that its tiles are in their XCD's L2.
+    const int members = x.members >> 16, member0 = x.members & 65535, split = x.split_pages, rows = members * a.group;
+    const int blocks = kind ? narrow_blocks(rows) : wide_blocks(rows), waves = kind ? 0 : wide_waves(rows);
+    part -= x.first;
+    const int row0 = part % blocks * (kind ? kNarrowRows : 32 * waves);
+    part /= blocks;
+    return SharedRun{listed(tab, member0), part * split, min(x.tokens - 16 * part * split, 16 * split), part, member0, members, row0, waves};
+  }
+  part -= tab.parts[kind - 1];
+  const int first = tab.owners[kind - 1];
+  const SharedPassed::Own x =
+      tab.own[first + uniform(find_request(tab.owners[kind] - first, [&](int i) { return (int)(tab.own[first + i].at & 65535) <= part; }))];
+  const int r = x.at >> 16 & 255, of = x.at >> 24;
+  part -= x.at & 65535;
+  int page0 = 0, slot = tab.slots[r] + part;
+  if (of < kSharedPrefixes) {
+    const int split = tab.prefixes[of].split_pages;
+    page0 = tab.prefixes[of].tokens >> 4;
+    slot += (page0 + split - 1) / split;
+  }
+  return SharedRun{r, page0 + part * tab.split_pages, min(x.tokens - 16 * part * tab.split_pages, 16 * tab.split_pages), slot, r, 1, 0, 0};
 }
-
-template <bool WIDE>
-__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPlain& tab, int first, int n, int item) {
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPlain& tab, int, int item) {
   const int slot = item / a.h_kv, r = uniform(find_request(a.num_reqs, [&](int i) { return tab.first[i] <= slot; }));
   const int part = slot - tab.first[r];
   return SharedRun{r, part * tab.split_pages, min(tab.tokens[r] - 16 * part * tab.split_pages, 16 * tab.split_pages), slot, r, 1, 0, 0};
 }
-__device__ __forceinline__ int2 slots_of(const SharedTables& tab, int r) { return tab.slots[r]; }
-__device__ __forceinline__ int2 slots_of(const SharedPassed& tab, int r) { return tab.slots[r]; }
-__device__ __forceinline__ int2 slots_of(const SharedSlots& tab, int r) { return tab.slots[r]; }
-__device__ __forceinline__ int2 slots_of(const SharedPlain& tab, int r) { return make_int2(tab.first[r], tab.first[r + 1] - tab.first[r]); }
-__device__ __forceinline__ int listed(const SharedTables& tab, int i) { return tab.list[i]; }
-__device__ __forceinline__ int listed(const SharedPassed& tab, int i) { return tab.list[i]; }
-__device__ __forceinline__ int listed(const SharedPlain&, int i) { return i; }
 
 // The error word of a launch that nothing cleared it for: a workgroup checks every page id that the others read, 16 lanes a request.
 // (All lanes on one request after another: 52 us for 256 requests of 16 to 100 tokens.)
@@ -261,8 +264,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
   const int item = team ? block * kTeams + wave / kTeamWaves : (block - team_blocks) * W + wave;
   const bool has = item < (team ? a.team_items : a.lone_items);
   if (!team && !has) return;
-  const int e0 = a.n_wide + (team ? 0 : a.n_team), n = team ? a.n_team : a.n_lone;
-  const SharedRun e = run_of<false>(a, tab, e0, n, has ? item : 0);
+  const SharedRun e = run_of(a, tab, team ? 1 : 2, has ? item : 0);
   const int g = a.group, rows = min(kNarrowRows, e.members * g - e.row0), j = (has ? item : 0) % a.h_kv;
   // A row as request * h_q + head.  A request alone is its row of the page table.
   auto head_of = [&](int row) {
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void shared_mixed(SharedArgs a, Ta
     narrow_items<D, EIGHT, kWideWaves>(a, tab, item - a.wide_items, reinterpret_cast<float*>(lds));
     return;
   }
-  wide_item<D, EIGHT>(a, tab, run_of<true>(a, tab, 0, a.n_wide, item), item % a.h_kv, lds);
+  wide_item<D, EIGHT>(a, tab, run_of(a, tab, 0, item), item % a.h_kv, lds);
 }
 
 // Joins the runs of one (request, query head): W waves, each every W-th run, eight loads in flight.
@@ -477,7 +479,7 @@ hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
   if (a.direct) return hipGetLastError();
   if constexpr (std::is_same<Table, SharedPassed>::value) {
     SharedSlots slots;
-    std::copy(tab.slots, tab.slots + a.num_reqs, slots.slots);
+    std::copy(tab.slots, tab.slots + a.num_reqs + 1, slots.slots);
     launch_merge<D>(a, slots, s);
   } else {
     launch_merge<D>(a, tab, s);

@@ -32,6 +32,15 @@ __device__ __forceinline__ float marked(float l, bool bad) {
   return __uint_as_float((__float_as_uint(l) & 0x7fffffffu) | (bad ? 0x80000000u : 0u));
 }
 
+// A request's first slot and slots; the prefixes' members.
+__device__ __forceinline__ int2 slots_of(const SharedTables& tab, int r) { return tab.slots[r]; }
+__device__ __forceinline__ int2 slots_of(const SharedPassed& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
+__device__ __forceinline__ int2 slots_of(const SharedSlots& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
+__device__ __forceinline__ int2 slots_of(const SharedPlain& tab, int r) { return make_int2(tab.first[r], tab.first[r + 1] - tab.first[r]); }
+__device__ __forceinline__ int listed(const SharedTables& tab, int i) { return tab.list[i]; }
+__device__ __forceinline__ int listed(const SharedPassed& tab, int i) { return tab.list[i / 4] >> (i % 4 * 8) & 255; }
+__device__ __forceinline__ int listed(const SharedPlain&, int i) { return i; }
+
 constexpr int kWideThreads = 512, kWideWaves = 8;
 constexpr int kTile = 64;  // keys of a tile: four pages
 
@@ -56,7 +65,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
   const int row = e.row0 + 32 * wave + (lane & 31);
   const bool active = wave < e.waves && e.row0 + 32 * wave < rows;  // the wave has rows
   const bool row_ok = active && row < rows;
-  const int member = row_ok ? tab.list[e.member0 + row / g] : 0, head = j * g + (row_ok ? row % g : 0);
+  const int member = row_ok ? listed(tab, e.member0 + row / g) : 0, head = j * g + (row_ok ? row % g : 0);
 
   bf16x8 qf[NK];
   {
@@ -291,7 +300,7 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
     }
   }
   if (!row_ok) return;
-  const size_t at = (size_t)(tab.slots[member].x + e.slot) * a.h_q + head;
+  const size_t at = (size_t)(slots_of(tab, member).x + e.slot) * a.h_q + head;
   float* o = a.acc + at * D + 4 * hh;
 #pragma unroll
   for (int n = 0; n < NO; ++n)

@@ -43,7 +43,7 @@ struct SharedRun {
   int32_t member0, members;
   int32_t row0, waves;  // the first row; of many rows: a workgroup's waves with rows
 };
-// A run before it is cut, as it travels with a launch: part s is of split_pages pages and goes to slot + s.
+// A run before it is cut: part s is of split_pages pages and goes to slot + s.
 struct SharedEntry {
   SharedRun run;
   int32_t first_item, split_pages;  // items (part, block of rows, head) of its kind's entries before it
@@ -64,14 +64,27 @@ struct SharedTables {  // in device memory, every part of a run listed
   const int32_t* list;
   const int2* slots;  // [R] (first slot, slots)
 };
-constexpr int kSharedPassed = 64, kSharedEntries = 72;
-struct SharedPassed {  // with the launches: up to kSharedPassed requests and kSharedEntries entries
-  SharedEntry entries[kSharedEntries];
-  int2 slots[kSharedPassed];
-  uint16_t list[2 * kSharedPassed];
+constexpr int kSharedPassed = 256, kSharedPrefixes = 32;
+// Words throughout: of arrays of bytes and of words with one index the compiler made scalar loads whose base was odd, which drop its
+// low bits.
+struct SharedPassed {  // with the launches: up to kSharedPassed requests, kSharedPrefixes prefixes and 65535 slots
+  struct Prefix {
+    int32_t tokens, first;      // first: items before its, of one kv head and its kind
+    uint32_t split_pages;
+    uint32_t members;           // the first of its members in the list, and from bit 16 on how many they are
+  } prefixes[kSharedPrefixes];  // by their kind
+  struct Own {                  // a request's tokens behind its prefix
+    int32_t tokens;
+    uint32_t at;                // parts before its, of its kind; from bit 16 on the request, from bit 24 its prefix or 255
+  } own[kSharedPassed];         // those that teams take, then lone waves
+  int32_t slots[kSharedPassed + 1];  // the requests' first ones, their end after the last
+  uint32_t list[kSharedPassed / 4];  // the prefixes' members, a byte each
+  int32_t kind[4], owners[3];   // where the kinds' prefixes and requests start
+  int32_t split_pages;          // of the requests' own runs
+  int32_t parts[2];             // of the prefixes that teams and lone waves take, with their blocks of rows
 };
 struct SharedSlots {
-  int2 slots[kSharedPassed];
+  int32_t slots[kSharedPassed + 1];
 };
 constexpr int kSharedPlain = 256;
 struct SharedPlain {  // with the launches: up to kSharedPlain requests that share nothing, all of them taken by teams or all by lone waves
@@ -92,12 +105,13 @@ struct SharedArgs {
   float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator; the latter's sign bit: a bad page)
   int32_t* err;
   int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
-  int32_t n_wide, n_team, n_lone;  // entries (of SharedPassed) or runs (of SharedTables)
+  int32_t n_wide, n_team, n_lone;  // runs (of SharedTables)
   int32_t wide_items, team_items, lone_items;
   int32_t max_slots;  // of a request
   int32_t direct;     // one slot each and no run of many rows: the results go straight to out
   float scale_log2;
 };
+static_assert(sizeof(SharedArgs) + sizeof(SharedPassed) <= 4096 && sizeof(SharedArgs) + sizeof(SharedPlain) <= 4096, "arguments of a launch");
 // On the host one of plain and passed, or neither (then what `tables` names is in device memory).
 hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, const SharedPlain* plain,
                          hipStream_t s);

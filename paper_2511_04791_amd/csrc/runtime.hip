@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <chrono>
 #include <cmath>
 #include <cstring>
@@ -2259,6 +2260,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     for (size_t i = 0; i < count.size(); ++i) all_saved += std::max(0.0, saved_us((int)i));
     auto is_wide = [&](int i) { return all_saved > kWideUs * DUET_TOTAL_CUS && saved_us(i) > 0; };
     std::vector<WideRun> runs;
+    int shared_prefixes = 0;
     int64_t narrow_pages = 0;
     double narrow_us = 0;
     int at = R;
@@ -2272,6 +2274,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
         narrow_us += hkv * (p->len[i] / 64.0 * narrow_tile_us(narrow_blocks(rows), s->head_dim, eight) +
                             kTeamUs * narrow_blocks(rows) * (1 + p->len[i] / (16 * kTeamPages)));
       }
+      ++shared_prefixes;
       member0[i] = at;
       at += count[i];
     }
@@ -2325,12 +2328,10 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     }
     if (plan->wide_items > kMaxSharedItems || plan->team_items > kMaxSharedItems || plan->lone_items > kMaxSharedItems)
       return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
-    const size_t entries = plan->wide.size() + plan->team.size() + plan->lone.size();
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
     plan->plain = at == R && R <= kSharedPlain && (plan->team.empty() || plan->lone.empty()) &&
                   (!plan->direct || narrow_pages <= kSharedCheckedPages);
-    plan->passed = !plan->plain && !plan->direct && entries <= kSharedEntries && plan->list.size() <= 2 * kSharedPassed &&
-                   R <= kSharedPassed;
+    plan->passed = !plan->plain && !plan->direct && R <= kSharedPassed && shared_prefixes <= kSharedPrefixes && plan->n_slots <= 65535;
     plan->split = narrow_split;
     if (!plan->passed && !plan->plain) {
       // The entries cut, each part by blocks of rows.
@@ -2529,9 +2530,9 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.h_kv = shape->num_kv_heads;
   a.group = a.h_q / a.h_kv;
   a.head_dim = shape->head_dim;
-  a.n_wide = plan.passed ? (int)plan.wide.size() : (int)(plan.wide_items / a.h_kv);
-  a.n_team = plan.passed ? (int)plan.team.size() : (int)(plan.team_items / a.h_kv);
-  a.n_lone = plan.passed ? (int)plan.lone.size() : (int)(plan.lone_items / a.h_kv);
+  a.n_wide = (int)(plan.wide_items / a.h_kv);
+  a.n_team = (int)(plan.team_items / a.h_kv);
+  a.n_lone = (int)(plan.lone_items / a.h_kv);
   a.wide_items = (int)plan.wide_items;
   a.team_items = (int)plan.team_items;
   a.lone_items = (int)plan.lone_items;
@@ -2547,10 +2548,42 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
     plain.first[a.num_reqs] = (int)plan.n_slots;
     plain.split_pages = plan.split;
   } else if (plan.passed) {
-    SharedEntry* e = std::copy(plan.wide.begin(), plan.wide.end(), passed.entries);
-    std::copy(plan.lone.begin(), plan.lone.end(), std::copy(plan.team.begin(), plan.team.end(), e));
-    std::copy(plan.list.begin(), plan.list.end(), passed.list);
-    std::copy(plan.slots.begin(), plan.slots.end(), passed.slots);
+    std::array<uint8_t, kSharedPassed> of;
+    of.fill(255);
+    std::memset(passed.list, 0, sizeof(passed.list));
+    int n = 0, owners = 0, kind = 0;
+    for (const auto* entries : {&plan.wide, &plan.team, &plan.lone})
+      for (const SharedEntry& e : *entries)
+        if (e.run.members > 1) {
+          for (int m = 0; m < e.run.members; ++m) of[plan.list[e.run.member0 + m]] = (uint8_t)n;
+          ++n;
+        }
+    for (size_t m = a.num_reqs; m < plan.list.size(); ++m)
+      passed.list[(m - a.num_reqs) / 4] |= (uint32_t)plan.list[m] << ((m - a.num_reqs) % 4 * 8);
+    n = 0;
+    for (const auto* entries : {&plan.wide, &plan.team, &plan.lone}) {
+      passed.kind[kind] = n;
+      if (kind) passed.owners[kind - 1] = owners;
+      int prefix_parts = 0;
+      for (const SharedEntry& e : *entries) {
+        const SharedRun& run = e.run;
+        if (run.members > 1) {
+          const int rows = run.members * a.group, blocks = kind ? narrow_blocks(rows) : wide_blocks(rows);
+          passed.prefixes[n++] = {run.tokens, prefix_parts, (uint32_t)e.split_pages, (uint32_t)(run.member0 - a.num_reqs | run.members << 16)};
+          prefix_parts += (run.tokens / 16 + e.split_pages - 1) / e.split_pages * blocks;
+        } else {
+          const uint32_t before = e.first_item / a.h_kv - prefix_parts, r = run.table_row;
+          passed.own[owners++] = {run.tokens, before | r << 16 | (uint32_t)of[r] << 24};
+        }
+      }
+      if (kind) passed.parts[kind - 1] = prefix_parts;
+      ++kind;
+    }
+    passed.kind[3] = n;
+    passed.owners[2] = owners;
+    passed.split_pages = plan.split;
+    for (int r = 0; r < a.num_reqs; ++r) passed.slots[r] = plan.slots[r].x;
+    passed.slots[a.num_reqs] = (int)plan.n_slots;
   } else {
     const UploadPart parts[3] = {{plan.runs.data(), plan.runs.size() * sizeof(SharedRun), plan.off_runs},
                                  {plan.list.data(), plan.list.size() * sizeof(int32_t), plan.off_list},

@@ -453,8 +453,11 @@ BATCHES = {
     "whole": ([64, 16], [(0, 0), (1, 0), (0, 0), (1, 0)]),
     # up to 256 requests that share nothing, of several runs
     "plain": ([], [(-1, 1 + 97 * i % 900) for i in range(120)] + [(-1, 9000)]),
-    # more runs than travel with a launch, many and few rows, entries past one round of the search
+    # many prefixes, requests past one round of the search
     "groups": ([32 * (i + 1) for i in range(30)], [(i % 31 - 1, 1 + 41 * i % 300) for i in range(150)]),
+    # more prefixes than travel with a launch, and as many requests and prefixes as do
+    "prefixes": ([16 * (1 + 7 * i % 25) for i in range(40)], [(i % 41 - 1, 1 + 29 * i % 400) for i in range(130)]),
+    "full": ([16 * (1 + 5 * i % 30) for i in range(32)], [(i % 33 - 1, (1 + 31 * i % 180) * (i % 5 > 0 or i % 33 == 0)) for i in range(256)]),
 }
 
 
@@ -485,6 +488,8 @@ WIDE = {
     "blocks": ((64, 8, 64), [2000], [(0, i % 20) for i in range(37)]),
     "group16": ((32, 2, 128), [4096, 3008], [(i % 2, 1 + i % 17) for i in range(43)]),
     "group3": ((24, 8, 64), [2064], [(0, 5 + i) for i in range(31)]),
+    "uploaded": ((16, 4, 64), [3008, 2000, 1600], [(i % 4 - 1, (1 + 11 * i % 60) * (i % 3 > 0 or i % 4 == 0)) for i in range(290)]),
+    "full": ((8, 2, 128), [2400 + 16 * i for i in range(5)], [(i % 6 - 1, (1 + 11 * i % 130) * (i % 3 > 0 or i % 6 == 0)) for i in range(256)]),
     "long": ((8, 1, 128), [66000], [(0, 2), (0, 300), (0, 17), (0, 1), (0, 64), (-1, 5)]),
 }
 
@@ -628,7 +633,7 @@ def test_attn_placement_and_neighbours(ctx, cache):
     assert torch.equal(one, two)
 
 
-@pytest.mark.parametrize("name", ["prefix", "one", "short", "lone", "many_alone", "plain", "many", "groups", "whole", "long"])
+@pytest.mark.parametrize("name", ["prefix", "one", "short", "lone", "many_alone", "plain", "many", "groups", "whole", "long", "prefixes", "full"])
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_attn_pages_outside_the_pool(ctx, cache, name):
     """Their tokens do not count, in a prefix and in a request's own pages; reported; the next call starts clean."""
