@@ -198,16 +198,22 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
   return __any(bad);
 }
 
+template <typename Table>
+constexpr bool kIsPlain = false;
+template <int R>
+constexpr bool kIsPlain<SharedPlain<R>> = true;
+
 // Item `item` of the runs of one kind (0: many rows, 1: teams, 2: lone waves): its part of a run.
 __device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedTables& tab, int kind, int item) {
   const int first = kind == 0 ? 0 : kind == 1 ? a.n_wide : a.n_wide + a.n_team, n = kind == 0 ? a.n_wide : kind == 1 ? a.n_team : a.n_lone;
   return tab.runs[first + min(item / a.h_kv, n - 1)];
 }
-__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPassed& tab, int kind, int item) {
+template <int R, int P>
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPassed<R, P>& tab, int kind, int item) {
   int part = item / a.h_kv;
   if (kind == 0 || part < tab.parts[kind - 1]) {
     const int first = tab.kind[kind];
-    const SharedPassed::Prefix x =
+    const typename SharedPassed<R, P>::Prefix x =
         tab.prefixes[first + uniform(find_request(tab.kind[kind + 1] - first, [&](int i) { return tab.prefixes[first + i].first <= part; }))];
     // The blocks of rows of one part next to each other, so that its tiles are in their XCD's L2.
     const int members = x.members >> 16, member0 = x.members & 65535, split = x.split_pages, rows = members * a.group;
@@ -219,19 +225,20 @@ __device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPas
   }
   part -= tab.parts[kind - 1];
   const int first = tab.owners[kind - 1];
-  const SharedPassed::Own x =
+  const typename SharedPassed<R, P>::Own x =
       tab.own[first + uniform(find_request(tab.owners[kind] - first, [&](int i) { return (int)(tab.own[first + i].at & 65535) <= part; }))];
   const int r = x.at >> 16 & 255, of = x.at >> 24;
   part -= x.at & 65535;
   int page0 = 0, slot = tab.slots[r] + part;
-  if (of < kSharedPrefixes) {
+  if (of < P) {
     const int split = tab.prefixes[of].split_pages;
     page0 = tab.prefixes[of].tokens >> 4;
     slot += (page0 + split - 1) / split;
   }
   return SharedRun{r, page0 + part * tab.split_pages, min(x.tokens - 16 * part * tab.split_pages, 16 * tab.split_pages), slot, r, 1, 0, 0};
 }
-__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPlain& tab, int, int item) {
+template <int R>
+__device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPlain<R>& tab, int, int item) {
   const int slot = item / a.h_kv, r = uniform(find_request(a.num_reqs, [&](int i) { return tab.first[i] <= slot; }));
   const int part = slot - tab.first[r];
   return SharedRun{r, part * tab.split_pages, min(tab.tokens[r] - 16 * part * tab.split_pages, 16 * tab.split_pages), slot, r, 1, 0, 0};
@@ -239,7 +246,8 @@ __device__ __forceinline__ SharedRun run_of(const SharedArgs& a, const SharedPla
 
 // The error word of a launch that nothing cleared it for: a workgroup checks every page id that the others read, 16 lanes a request.
 // (All lanes on one request after another: 52 us for 256 requests of 16 to 100 tokens.)
-__device__ void check_pages(const SharedArgs& a, const SharedPlain& tab) {
+template <int R>
+__device__ void check_pages(const SharedArgs& a, const SharedPlain<R>& tab) {
   bool bad = false;
   for (int r = threadIdx.x / 16; r < a.num_reqs; r += blockDim.x / 16) {
     const int* row = a.table + (size_t)r * a.max_pages;
@@ -257,7 +265,7 @@ template <int D, bool EIGHT, int W, typename Table>
 __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& tab, int block, float* lds) {
   constexpr int kTeams = W / kTeamWaves;
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, wave = uniform(threadIdx.x >> 6);
-  constexpr bool kChecked = std::is_same<Table, SharedPlain>::value;  // direct: the error word is another workgroup's
+  constexpr bool kChecked = kIsPlain<Table>;  // direct: the error word is another workgroup's
   const bool direct = a.direct;
   const int team_blocks = (a.team_items + kTeams - 1) / kTeams;
   const bool team = block < team_blocks;
@@ -351,7 +359,7 @@ __device__ __forceinline__ void narrow_items(const SharedArgs& a, const Table& t
 template <int D, bool EIGHT, typename Table>
 __global__ __launch_bounds__(64 * kTeamWaves) void shared_narrow(SharedArgs a, Table tab) {
   extern __shared__ __attribute__((aligned(16))) float part[];
-  if constexpr (std::is_same<Table, SharedPlain>::value) {
+  if constexpr (kIsPlain<Table>) {
     if (a.direct) {
       if (blockIdx.x == 0) check_pages(a, tab);
       else narrow_items<D, EIGHT, kTeamWaves>(a, tab, blockIdx.x - 1, part);
@@ -456,9 +464,20 @@ void launch_merge(const SharedArgs& a, const Table& tab, hipStream_t s) {
   else hipLaunchKernelGGL((shared_merge<D, 1, Table>), dim3((pairs + 3) / 4), dim3(256), 0, s, a, tab);
 }
 
+template <int D, typename Table>
+void join(const SharedArgs& a, const Table& tab, hipStream_t s) {
+  launch_merge<D>(a, tab, s);
+}
+template <int D, int R, int P>
+void join(const SharedArgs& a, const SharedPassed<R, P>& tab, hipStream_t s) {  // the slots are all that it reads
+  SharedSlots<R> slots;
+  std::copy(tab.slots, tab.slots + a.num_reqs + 1, slots.slots);
+  launch_merge<D>(a, slots, s);
+}
+
 template <int D, bool EIGHT, typename Table>
 hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
-  constexpr bool kPlain = std::is_same<Table, SharedPlain>::value;
+  constexpr bool kPlain = kIsPlain<Table>;
   auto blocks = [&](int waves) {
     return (a.team_items + waves / kTeamWaves - 1) / (waves / kTeamWaves) + (a.lone_items + waves - 1) / waves;
   };
@@ -475,15 +494,9 @@ hipError_t launch(const SharedArgs& a, const Table& tab, hipStream_t s) {
   }
   if (!wide)
     hipLaunchKernelGGL((shared_narrow<D, EIGHT, Table>), dim3(blocks(kTeamWaves) + (kPlain && a.direct ? 1 : 0)),
-                       dim3(64 * kTeamWaves), team_floats<D>(std::is_same<Table, SharedPlain>::value ? a.group : kNarrowRows) * sizeof(float), s, a, tab);
+                       dim3(64 * kTeamWaves), team_floats<D>(kIsPlain<Table> ? a.group : kNarrowRows) * sizeof(float), s, a, tab);
   if (a.direct) return hipGetLastError();
-  if constexpr (std::is_same<Table, SharedPassed>::value) {
-    SharedSlots slots;
-    std::copy(tab.slots, tab.slots + a.num_reqs + 1, slots.slots);
-    launch_merge<D>(a, slots, s);
-  } else {
-    launch_merge<D>(a, tab, s);
-  }
+  join<D>(a, tab, s);
   return hipGetLastError();
 }
 template <typename Table>
@@ -492,12 +505,35 @@ hipError_t launch(const SharedArgs& a, const Table& t, hipStream_t s) {
   return a.head_dim == 128 ? launch<128, false>(a, t, s) : launch<64, false>(a, t, s);
 }
 
+SharedPassed<kSharedFew, kSharedFewPrefixes> few(const SharedArgs& a, const SharedPassedAll& t) {
+  SharedPassed<kSharedFew, kSharedFewPrefixes> f;
+  for (int i = 0; i < t.kind[3]; ++i) f.prefixes[i] = {t.prefixes[i].tokens, t.prefixes[i].first, t.prefixes[i].split_pages, t.prefixes[i].members};
+  for (int i = 0; i < t.owners[2]; ++i) f.own[i] = {t.own[i].tokens, t.own[i].at};
+  std::copy(t.slots, t.slots + a.num_reqs + 1, f.slots);
+  std::copy(t.list, t.list + kSharedFew / 4, f.list);
+  std::copy(t.kind, t.kind + 4, f.kind);
+  std::copy(t.owners, t.owners + 3, f.owners);
+  f.split_pages = t.split_pages;
+  std::copy(t.parts, t.parts + 2, f.parts);
+  return f;
+}
+SharedPlain<kSharedFew> few(const SharedArgs& a, const SharedPlainAll& t) {
+  SharedPlain<kSharedFew> f;
+  std::copy(t.first, t.first + a.num_reqs + 1, f.first);
+  std::copy(t.tokens, t.tokens + a.num_reqs, f.tokens);
+  f.split_pages = t.split_pages;
+  return f;
+}
+
 }  // namespace
 
-hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, const SharedPlain* plain,
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassedAll* passed, const SharedPlainAll* plain,
                          hipStream_t s) {
   if (a.num_reqs == 0) return hipSuccess;
-  return plain ? launch(a, *plain, s) : passed ? launch(a, *passed, s) : launch(a, tables, s);
+  const bool is_few = a.num_reqs <= kSharedFew;
+  if (plain) return is_few ? launch(a, few(a, *plain), s) : launch(a, *plain, s);
+  if (passed) return is_few && passed->kind[3] <= kSharedFewPrefixes ? launch(a, few(a, *passed), s) : launch(a, *passed, s);
+  return launch(a, tables, s);
 }
 
 }  // namespace duet

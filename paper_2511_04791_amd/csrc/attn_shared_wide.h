@@ -34,12 +34,17 @@ __device__ __forceinline__ float marked(float l, bool bad) {
 
 // A request's first slot and slots; the prefixes' members.
 __device__ __forceinline__ int2 slots_of(const SharedTables& tab, int r) { return tab.slots[r]; }
-__device__ __forceinline__ int2 slots_of(const SharedPassed& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
-__device__ __forceinline__ int2 slots_of(const SharedSlots& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
-__device__ __forceinline__ int2 slots_of(const SharedPlain& tab, int r) { return make_int2(tab.first[r], tab.first[r + 1] - tab.first[r]); }
+template <int R, int P>
+__device__ __forceinline__ int2 slots_of(const SharedPassed<R, P>& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
+template <int R>
+__device__ __forceinline__ int2 slots_of(const SharedSlots<R>& tab, int r) { return make_int2(tab.slots[r], tab.slots[r + 1] - tab.slots[r]); }
+template <int R>
+__device__ __forceinline__ int2 slots_of(const SharedPlain<R>& tab, int r) { return make_int2(tab.first[r], tab.first[r + 1] - tab.first[r]); }
 __device__ __forceinline__ int listed(const SharedTables& tab, int i) { return tab.list[i]; }
-__device__ __forceinline__ int listed(const SharedPassed& tab, int i) { return tab.list[i / 4] >> (i % 4 * 8) & 255; }
-__device__ __forceinline__ int listed(const SharedPlain&, int i) { return i; }
+template <int R, int P>
+__device__ __forceinline__ int listed(const SharedPassed<R, P>& tab, int i) { return tab.list[i / 4] >> (i % 4 * 8) & 255; }
+template <int R>
+__device__ __forceinline__ int listed(const SharedPlain<R>&, int i) { return i; }
 
 constexpr int kWideThreads = 512, kWideWaves = 8;
 constexpr int kTile = 64;  // keys of a tile: four pages

@@ -64,32 +64,36 @@ struct SharedTables {  // in device memory, every part of a run listed
   const int32_t* list;
   const int2* slots;  // [R] (first slot, slots)
 };
-constexpr int kSharedPassed = 256, kSharedPrefixes = 32;
+// Tables that travel with the launches: for up to 256 requests, and for up to 32, since 4 KB of arguments cost the host 1 us a launch
+// more (a call of one request 12.5 us against 12.0).
+constexpr int kSharedPassed = 256, kSharedPrefixes = 32, kSharedFew = 32, kSharedFewPrefixes = 8;
 // Words throughout: of arrays of bytes and of words with one index the compiler made scalar loads whose base was odd, which drop its
 // low bits.
-struct SharedPassed {  // with the launches: up to kSharedPassed requests, kSharedPrefixes prefixes and 65535 slots
+template <int R, int P>
+struct SharedPassed {  // up to R requests, P prefixes and 65535 slots
   struct Prefix {
     int32_t tokens, first;      // first: items before its, of one kv head and its kind
     uint32_t split_pages;
     uint32_t members;           // the first of its members in the list, and from bit 16 on how many they are
-  } prefixes[kSharedPrefixes];  // by their kind
+  } prefixes[P];  // by their kind
   struct Own {                  // a request's tokens behind its prefix
     int32_t tokens;
     uint32_t at;                // parts before its, of its kind; from bit 16 on the request, from bit 24 its prefix or 255
-  } own[kSharedPassed];         // those that teams take, then lone waves
-  int32_t slots[kSharedPassed + 1];  // the requests' first ones, their end after the last
-  uint32_t list[kSharedPassed / 4];  // the prefixes' members, a byte each
+  } own[R];         // those that teams take, then lone waves
+  int32_t slots[R + 1];         // the requests' first ones, their end after the last
+  uint32_t list[R / 4];         // the prefixes' members, a byte each
   int32_t kind[4], owners[3];   // where the kinds' prefixes and requests start
   int32_t split_pages;          // of the requests' own runs
   int32_t parts[2];             // of the prefixes that teams and lone waves take, with their blocks of rows
 };
+template <int R>
 struct SharedSlots {
-  int32_t slots[kSharedPassed + 1];
+  int32_t slots[R + 1];
 };
-constexpr int kSharedPlain = 256;
-struct SharedPlain {  // with the launches: up to kSharedPlain requests that share nothing, all of them taken by teams or all by lone waves
-  int32_t first[kSharedPlain + 1];  // the requests' first slots, the slots' end after the last
-  int32_t tokens[kSharedPlain];
+template <int R>
+struct SharedPlain {  // up to R requests that share nothing, all of them taken by teams or all by lone waves
+  int32_t first[R + 1];  // the requests' first slots, the slots' end after the last
+  int32_t tokens[R];
   int32_t split_pages;
 };
 constexpr int kSharedCheckedPages = 8192;  // page ids that a workgroup beside the others checks
@@ -111,9 +115,11 @@ struct SharedArgs {
   int32_t direct;     // one slot each and no run of many rows: the results go straight to out
   float scale_log2;
 };
-static_assert(sizeof(SharedArgs) + sizeof(SharedPassed) <= 4096 && sizeof(SharedArgs) + sizeof(SharedPlain) <= 4096, "arguments of a launch");
+using SharedPassedAll = SharedPassed<kSharedPassed, kSharedPrefixes>;
+using SharedPlainAll = SharedPlain<kSharedPassed>;
+static_assert(sizeof(SharedArgs) + sizeof(SharedPassedAll) <= 4096, "arguments of a launch");
 // On the host one of plain and passed, or neither (then what `tables` names is in device memory).
-hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassed* passed, const SharedPlain* plain,
+hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassedAll* passed, const SharedPlainAll* plain,
                          hipStream_t s);
 
 }  // namespace duet

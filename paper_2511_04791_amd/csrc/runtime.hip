@@ -2297,7 +2297,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
       items += parts * hkv;
       to.push_back(e);
     };
-    const bool all_teams = at == R && R <= kSharedPlain && longest > 64;  // so that the requests travel with the launch
+    const bool all_teams = at == R && R <= kSharedPassed && longest > 64;  // so that the requests travel with the launch
     auto add_narrow = [&](const SharedEntry& e, int64_t n) {
       if (all_teams || e.run.tokens > 64) add(plan->team, plan->team_items, e, n);
       else add(plan->lone, plan->lone_items, e, n);
@@ -2329,7 +2329,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     if (plan->wide_items > kMaxSharedItems || plan->team_items > kMaxSharedItems || plan->lone_items > kMaxSharedItems)
       return fail(DUET_EUNSUPPORTED, "the batch has too many keys");
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
-    plan->plain = at == R && R <= kSharedPlain && (plan->team.empty() || plan->lone.empty()) &&
+    plan->plain = at == R && R <= kSharedPassed && (plan->team.empty() || plan->lone.empty()) &&
                   (!plan->direct || narrow_pages <= kSharedCheckedPages);
     plan->passed = !plan->plain && !plan->direct && R <= kSharedPassed && shared_prefixes <= kSharedPrefixes && plan->n_slots <= 65535;
     plan->split = narrow_split;
@@ -2541,8 +2541,8 @@ int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* 
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)shape->head_dim));
   const SharedTables tables{reinterpret_cast<const SharedRun*>(ws + plan.off_runs),
                             reinterpret_cast<const int32_t*>(ws + plan.off_list), reinterpret_cast<const int2*>(ws + plan.off_slots)};
-  SharedPassed passed;
-  SharedPlain plain;
+  SharedPassedAll passed;
+  SharedPlainAll plain;
   if (plan.plain) {
     for (int r = 0; r < a.num_reqs; ++r) plain.first[r] = plan.slots[r].x, plain.tokens[r] = batch->reqs[r].cached_len + 1;
     plain.first[a.num_reqs] = (int)plan.n_slots;
