@@ -15,12 +15,12 @@
 // before; two teams fit a CU.  A wave's runs of more than 32 pages are slower than a team's (100 pages: 301 us).
 //
 // More rows (attn_shared_wide.h): a workgroup takes up to 256 of them and brings tiles of 64 keys through LDS, bound by the matrix
-// cores, the exponentials and the LDS reads alike: 512 rows a kv head after 131072 tokens 800 TFLOP/s over bf16, 838 over 8-bit pages.
-// Both kinds run in one launch.  64 requests of 64 / 8 heads after 32768 shared tokens with 200 to 1000 of their own: 86 and 41 us one
-// after the other, 110 together.
+// cores, the exponentials and the LDS reads alike: 512 rows a kv head after 131072 tokens 947 TFLOP/s over bf16, 919 over 8-bit pages.
+// Both kinds run in one launch, those of many rows on fewer CUs than there are: 64 requests of 64 / 8 heads after 32768 shared tokens with
+// 200 to 1000 of their own take 86 and 41 us one after the other, 103 together.
 //
 // The runs' states are joined by a second launch; where every request has one run, results go straight out.  What the kernels know
-// of the batch travels with their launches if it is small: an upload is a launch of 4.5 us of its own.
+// of the batch travels with their launches up to 256 requests and 32 prefixes: an upload is a launch of 4.5 us of its own.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

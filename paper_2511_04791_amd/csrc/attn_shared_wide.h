@@ -1,8 +1,8 @@
 // Device code for prefixes that many query rows share (attn_shared.hip says what it computes).
 //
 // Eight waves of 32 rows on 32x32x16 matrix instructions, S^T = K Q^T and O^T += V^T P^T, with the operand orders of the prefill kernel
-// (attn_prefill.hip): its tile loads, swizzles and softmax without the causal mask, over a run of whole pages.  Time a tile of 64 keys
-// some 1 us and 0.18 for each wave with rows.  Measured slower: 64 rows a wave on four waves, also with the matrix instructions of one
+// (attn_prefill.hip): its tile loads, swizzles and softmax without the causal mask, over a run of whole pages.  A tile of 64 keys
+// takes 1.4 us with one wave of rows a SIMD, 1.8 to 2.1 with two.  Measured slower: 64 rows a wave on four waves, also with the matrix instructions of one
 // half of the rows between the exponentials of the other (100 and 103 against 84 us for 512 rows after 32768 tokens), and one wave of a
 // SIMD half a step behind the other (93).
 #pragma once
