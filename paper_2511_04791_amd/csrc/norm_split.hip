@@ -11,7 +11,7 @@
 // whole pages need turned around.  A head's row lies in 4 to 16 neighbouring lanes, and its sum or maximum is taken by moves inside a
 // row of 16 lanes.  With all sixteen rows of queries and keys a thread, as rope_split.hip has it, a small batch waited for one chain of
 // norms (five chunks on a rank, 2588 rows, into 8 bits 25 us; now 7.7) and few waves fitted (8224 rows of 64 + 2 x 8 heads 90 us; now
-// 71, 4.7 TB/s; a large copy reaches 5.1).  8192 rows of 32 + 2 x 8 heads into 8 bits 41 us (4.5 TB/s); one decode row 4.5.
+// 71, 4.7 TB/s; a large copy reaches 5.1).  8192 rows of 32 + 2 x 8 heads into 8 bits 39 us (4.7 TB/s); one decode row 4.5.
 //
 // Values are converted two of a row at a time, as the row shares the power, and turned as bytes; magnitudes of bf16 are compared
 // as their bits, two in a register.  Both took a third of the instructions of a value at a time.  A page that is covered in part gets
@@ -370,8 +370,9 @@ __global__ __launch_bounds__(256, EIGHT ? 4 : 3) void norm_split(NormSplitArgs x
   }
 }
 
-// kRows rows of queries and keys a thread: four, or two where that leaves fewer than four workgroups a CU.  us with 1 / 2 / 4 / 8: 8224
-// rows of 64 + 2 x 8 heads, bf16, . / 85.5 / 77.8 / 82.5; 2588 rows of 8 + 2 x 1 into 8 bits 8.3 / 7.6 / 11.1 / 13.1.
+// kRows rows of queries and keys a thread: into 8 bits two, else four, or two where that leaves fewer than four workgroups a CU.  us with
+// 2 / 4: 8224 rows of 64 + 2 x 8 heads, bf16, 72.9 / 70.7; 8192 rows of 32 + 2 x 8 into 8 bits 39.0 / 41.5; 2588 rows of 8 + 2 x 1 into 8
+// bits 7.6 / 11.1 (one row 8.3, eight 13.1).
 template <typename T, bool ADJACENT, bool EIGHT, int kRows>
 hipError_t launch_rows(NormSplitArgs x, int groups, int longest, const int4* requests, hipStream_t s) {
   const RopeSplitArgs& a = x.rope;
@@ -399,8 +400,9 @@ hipError_t launch(NormSplitArgs x, const int4* requests, hipStream_t s) {
   x.single = longest == 1;
   const int groups = x.single ? a.num_reqs : a.tokens / 16 + 2 * a.num_reqs;
   const long long threads = (long long)groups * (a.h_q + a.h_kv) * a.head_dim * (int)sizeof(T) / 32 * ((std::min(longest, 16) + 3) / 4);
-  return threads < 4 * 256 * 256 ? launch_rows<T, ADJACENT, EIGHT, 2>(x, groups, longest, requests, s)
-                                 : launch_rows<T, ADJACENT, EIGHT, 4>(x, groups, longest, requests, s);
+  if constexpr (!EIGHT)
+    if (threads >= 4 * 256 * 256) return launch_rows<T, ADJACENT, EIGHT, 4>(x, groups, longest, requests, s);
+  return launch_rows<T, ADJACENT, EIGHT, 2>(x, groups, longest, requests, s);
 }
 
 }  // namespace
