@@ -85,7 +85,8 @@ __global__ __launch_bounds__(256) void cache8_read(Cache8ReadArgs a, Table reqs)
 }
 
 // Two pieces a thread where four would leave fewer than four workgroups a CU: one prompt of 100 tokens, 8 heads, 3.9 us against 5.2;
-// 32768 tokens 53.8 against 48.3 (202 MB, 4.2 TB/s; a large copy reaches 5.1), with eight 48.2.
+// 32768 tokens 53.8 against 48.3 (202 MB, 4.2 TB/s; a large copy reaches 5.1), with eight 48.2.  Pieces of 16 bytes in and 32 out, whose
+// stores leave every other chunk to the next, took 66; a page's workgroups next to each other the same 48.
 template <int P, typename Table>
 void launch_pieces(const Cache8ReadArgs& a, const Table& t, hipStream_t s) {
   const dim3 grid(a.groups, (a.h_kv * 4 * a.head_dim + 256 * P - 1) / (256 * P));
