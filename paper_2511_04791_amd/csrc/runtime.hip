@@ -2187,8 +2187,9 @@ double wide_tile_us(int rows, int d, bool eight) {  // of all blocks
   return wide_blocks(rows) * ((waves <= 4 ? 1.4 : 1.3 + 0.1 * waves) * (d == 64 ? 0.65 : 1.0) + (eight ? 0.1 : 0.0));
 }
 double narrow_tile_us(int blocks, int d, bool eight) { return d * (eight ? 1 : 2) / 8.0 * std::max(0.04, 0.015 + 0.02 * blocks); }
-// What a workgroup of many rows, a team and a wave alone (eight a workgroup) take besides, and what workgroups of many rows have to save
-// in all: their states are more, and the few that fit a CU start and end together.
+// What a workgroup of many rows, a team and a wave alone (eight a workgroup) take besides; what workgroups of many rows have to save in
+// all, as their states are more and they start and end together (us of the two ways: 8-bit, 64 rows after 32768 tokens 39.6 and 34.9, 96
+// rows 42.2 and 45.8, 16 prefixes of 2200 tokens with 72 rows each 50 and 60); runs of few rows that find a CU after them only.
 constexpr double kPartUs = 5.0, kTeamUs = 1.5, kLoneUs = 0.4, kWideUs = 6.0, kLateUs = 8.0;
 
 struct WideRun {
@@ -2196,7 +2197,10 @@ struct WideRun {
 };
 
 // Pages of a part of a run of many rows: those that an estimate says end soonest.  Up to a part a CU all run at once, beside the runs of
-// few rows; more of them fill the CUs better and end less evenly.  Every part writes and the join reads a state a row.
+// few rows; more of them fill the CUs better and end less evenly.  Workgroups go to the 32 shader engines in turn, so a round of 32 parts
+// that has begun takes a CU of each: the few rows of 60 requests after 24832 tokens wait for 240 parts (52 us) and not for 224 (44).
+// Every part writes and the join reads a state a row.  us by tiles of a part, 24 / 32 / 40 / 48 / 64: 64 requests after 32768 tokens of
+// bf16 124 / 121 / 117 / 99 / 121 (taken: 52, 102); 6 / 10 / 16 / 24: 40 requests after 4000 tokens 38 / 32 / 38 / 50 (14, 35).
 int wide_split_pages(const std::vector<WideRun>& runs, int hkv, int d, double narrow_us, bool eight) {
   if (runs.empty()) return 4;
   double tile = 0, wide_us = 0;
