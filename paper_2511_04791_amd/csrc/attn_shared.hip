@@ -1,7 +1,7 @@
 // Decode attention over a paged cache, bf16 or 8-bit, for requests that may share the pages of a prefix.
 //
 // A request's output is softmax(q K^T / sqrt(d)) V over its keys.  The keys are cut into runs; a run gives each query row an
-// unnormalised output, a reference maximum m and a denominator l, and a row's runs are joined by their exp(m).  A shared
+// unnormalised output, a reference m (kLift above its largest score) and a denominator l, and a row's runs are joined by their exp(m).  A shared
 // prefix is cut once and attended by the rows of every member, so its pages are read once for all of them, and a page
 // that one request holds alone is attended by the g heads of its group.
 //
@@ -146,8 +146,8 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
 #pragma unroll
     for (int t = 1; t < 16; ++t) mx = fmaxf(mx, sc[t]);
     mx = max_rows(mx);
-    if (__any(mx > o.m + kSlack)) {
-      const float to = fmaxf(o.m, mx);
+    if (__any(mx > o.m + (kSlack - kLift))) {
+      const float to = fmaxf(o.m, mx + kLift);
       const float alpha = to == -INFINITY ? 1.f : fast_exp2(o.m - to);
       o.m = to;
       o.l *= alpha;
@@ -165,7 +165,7 @@ __device__ __forceinline__ bool walk(const SharedArgs& a, const int* prow, int n
       const bf16x2 w = {static_cast<__bf16>(fast_exp2(sc[t] - sub)), static_cast<__bf16>(fast_exp2(sc[t + 1] - sub))};
       o.l = __builtin_amdgcn_fdot2_f32_bf16(w, ones, o.l, false);
       if constexpr (EIGHT) {
-        // Times a power of two: the upper halves of the products are exact.
+        // Times a power of two: the upper halves of the products are exact down to 2^-126, a value's 2^-93 at a weight of 1.
         const unsigned b = __builtin_bit_cast(unsigned, w);
         const unsigned x = __float_as_uint(__uint_as_float(b << 16) * power(vw[t / 4], t % 4));
         const unsigned y = __float_as_uint(__uint_as_float(b & 0xffff0000u) * power(vw[t / 4], t % 4 + 1));
@@ -395,6 +395,7 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
   const int2 at = slots_of(tab, r);
   const size_t first = (size_t)at.x * a.h_q + pair - r * a.h_q;
   float top = -INFINITY, den = 0.f, num[E] = {};
+  const float lift = at.y > 1 ? 32 - __builtin_clz(at.y - 1) : 0;  // weights of at most 1 / slots: the sum is no larger than a run's
   bool bad = false;
   for (int s0 = w; s0 < at.y; s0 += 8 * W) {
     float2 ml[8];
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(64 * (W > 4 ? W : 4)) void shared_merge(SharedArgs 
       to = fmaxf(to, ml[u].x);
     }
     // Runs without a key that counts weigh 0, and a NaN among their denominators stays.
-    const float sub = to == -INFINITY ? 0.f : to, f = fast_exp2(top - sub);
+    const float ref = to == -INFINITY ? 0.f : to, f = fast_exp2(top - ref), sub = ref + lift;
     top = to;
     den *= f;
 #pragma unroll

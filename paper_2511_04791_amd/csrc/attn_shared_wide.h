@@ -21,7 +21,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kSlack = 8.f;  // the reference maximum moves when a score passes it by 2^8
+// A row's reference is its largest score and kLift, and moves when a score passes that largest by kSlack, all in powers of two.  So weights
+// are at most 2^(kSlack - kLift), and the sums of a run, of up to 2^14 tokens, stay finite over bf16's largest values.  Weights under
+// 2^-102 of the largest become 0.
+constexpr float kLift = 24.f, kSlack = 8.f;
 
 __device__ __forceinline__ float power(unsigned word, int byte) {
   return __uint_as_float((word >> (8 * byte) & 255u) << 23);
@@ -256,8 +259,8 @@ __device__ __forceinline__ void wide_item(const SharedArgs& a, const Table& tab,
 #pragma unroll
       for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sacc[nb][v]);
     mx = pair_max(mx) * a.scale_log2;
-    if (__any(mx > m_ref + kSlack)) {
-      const float to = fmaxf(m_ref, mx), alpha = to == -INFINITY ? 1.f : fast_exp2(m_ref - to);
+    if (__any(mx > m_ref + (kSlack - kLift))) {
+      const float to = fmaxf(m_ref, mx + kLift), alpha = to == -INFINITY ? 1.f : fast_exp2(m_ref - to);
       m_ref = to;
       m_sub = to == -INFINITY ? 0.f : to;
       l_run *= alpha;

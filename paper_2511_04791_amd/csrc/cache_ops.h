@@ -106,7 +106,7 @@ struct SharedArgs {
   long long pages;
   __bf16* out;
   float* acc;                  // [slots, h_q, d] unnormalised outputs
-  float2* ml;                  // [slots, h_q] (reference maximum in base-2 units, denominator; the latter's sign bit: a bad page)
+  float2* ml;                  // [slots, h_q] (reference in base-2 units, denominator; the latter's sign bit: a bad page)
   int32_t* err;
   int32_t num_reqs, max_pages, h_q, h_kv, group, head_dim;
   int32_t n_wide, n_team, n_lone;  // runs (of SharedTables)
