@@ -405,6 +405,18 @@ typedef struct {
 /* Workspace of duet_attn_decode_shared.  Host only. */
 int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes,
                                 size_t* bytes);
+/* How duet_attn_decode_shared takes a batch. */
+typedef struct {
+  int32_t many_rows; /* workgroups that take up to 256 query rows of a kv head through a part of a prefix */
+  int32_t teams;     /* teams of four waves that take up to 16 rows through a part of a prefix or of a request's own tokens */
+  int32_t lone;      /* waves that do so alone */
+  int32_t direct;    /* 1: the results go straight to out, nothing is joined */
+  int32_t tables;    /* requests that the tables in the launches' arguments hold, 0: they are uploaded */
+} duet_shared_cut;
+/* Over a bf16 cache, or an 8-bit one.  block_rows [prefixes.num] (may be NULL): rows of prefix i that are taken at once, 16, or up to
+ * 256 by workgroups of many rows; 0 where no two requests share it.  Host only. */
+int duet_shared_plan(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes, int32_t eight_bits,
+                     duet_shared_cut* cut, int32_t* block_rows);
 /* Decode attention of one layer, as duet_attn_mixed_batch gives it for a batch of decode requests: bf16 q and out [R, h_q, d], over a
  * bf16 or an 8-bit cache.  prefixes NULL: nothing is shared.  The result does not depend on the pages' placement nor on the stream;
  * the order of its sums follows the batch's lengths and prefixes.  Probabilities are rounded to bf16.  Nothing overflows on the way

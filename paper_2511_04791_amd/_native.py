@@ -72,6 +72,10 @@ class Prefixes(ctypes.Structure):
     _fields_ = [("num", c_int32), ("len", ctypes.POINTER(c_int32)), ("of", ctypes.POINTER(c_int32))]
 
 
+class SharedCut(ctypes.Structure):
+    _fields_ = [("many_rows", c_int32), ("teams", c_int32), ("lone", c_int32), ("direct", c_int32), ("tables", c_int32)]
+
+
 class KernelTimes(ctypes.Structure):
     _fields_ = [("decode_partial_us", c_double), ("decode_reduce_us", c_double), ("prefill_us", c_double),
                 ("decode_total_us", c_double), ("iteration_us", c_double),
@@ -140,6 +144,7 @@ _SIGS = {
     "duet_cache8_read": (c_int32, [c_void_p, P(Shape), P(KvCache), c_void_p, c_int32, P(Batch), c_void_p, c_void_p, c_int64,
                                    c_void_p, c_int32, c_void_p, c_size_t, c_void_p]),
     "duet_shared_workspace_bytes": (c_int32, [P(Shape), P(Batch), P(Prefixes), P(c_size_t)]),
+    "duet_shared_plan": (c_int32, [P(Shape), P(Batch), P(Prefixes), c_int32, P(SharedCut), P(c_int32)]),
     "duet_attn_decode_shared": (c_int32, [c_void_p, P(Shape), c_void_p, P(KvCache), c_void_p, c_int32, P(Batch), P(Prefixes),
                                           c_void_p, c_size_t, c_void_p, c_void_p]),
     "duet_attn_mixed_batch": (c_int32, [c_void_p, P(Shape), c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32,

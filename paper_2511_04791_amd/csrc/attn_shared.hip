@@ -531,9 +531,8 @@ SharedPlain<kSharedFew> few(const SharedArgs& a, const SharedPlainAll& t) {
 hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassedAll* passed, const SharedPlainAll* plain,
                          hipStream_t s) {
   if (a.num_reqs == 0) return hipSuccess;
-  const bool is_few = a.num_reqs <= kSharedFew;
-  if (plain) return is_few ? launch(a, few(a, *plain), s) : launch(a, *plain, s);
-  if (passed) return is_few && passed->kind[3] <= kSharedFewPrefixes ? launch(a, few(a, *passed), s) : launch(a, *passed, s);
+  if (plain) return passed_tables(a.num_reqs, 0) == kSharedFew ? launch(a, few(a, *plain), s) : launch(a, *plain, s);
+  if (passed) return passed_tables(a.num_reqs, passed->kind[3]) == kSharedFew ? launch(a, few(a, *passed), s) : launch(a, *passed, s);
   return launch(a, tables, s);
 }
 

@@ -119,6 +119,9 @@ using SharedPassedAll = SharedPassed<kSharedPassed, kSharedPrefixes>;
 using SharedPlainAll = SharedPlain<kSharedPassed>;
 static_assert(sizeof(SharedArgs) + sizeof(SharedPassedAll) <= 4096, "arguments of a launch");
 // On the host one of plain and passed, or neither (then what `tables` names is in device memory).
+inline int passed_tables(int num_reqs, int prefixes) {  // requests of the smallest tables that hold so many
+  return num_reqs <= kSharedFew && prefixes <= kSharedFewPrefixes ? kSharedFew : kSharedPassed;
+}
 hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassedAll* passed, const SharedPlainAll* plain,
                          hipStream_t s);
 

@@ -2154,7 +2154,7 @@ struct SharedPlan {
   std::vector<int32_t> list;  // the requests themselves, then the groups' members
   std::vector<int2> slots;
   int64_t wide_items = 0, team_items = 0, lone_items = 0, n_slots = 0;
-  int max_slots = 0, split = 0;
+  int max_slots = 0, split = 0, prefixes = 0;  // prefixes that requests share
   bool direct = false;  // results go straight to out
   bool passed = false, plain = false;  // the lists travel with the launches
   size_t off_runs = 0, off_list = 0, off_slots = 0, off_ml = 0, off_acc = 0, total = 0;
@@ -2240,7 +2240,7 @@ int wide_split_pages(const std::vector<WideRun>& runs, int hkv, int d, double na
   return 4 * best;
 }
 
-int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, bool eight, SharedPlan* plan) {
+int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p, bool eight, SharedPlan* plan, int32_t* block_rows = nullptr) {
   const int R = b->num_reqs, g = s->num_q_heads / s->num_kv_heads, hkv = s->num_kv_heads;
   for (int r = 0; r < R; ++r)
     if (b->reqs[r].kind != DUET_KIND_DECODE) return fail(DUET_EUNSUPPORTED, "request %d is no decode request", r);
@@ -2264,13 +2264,14 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     for (size_t i = 0; i < count.size(); ++i) all_saved += std::max(0.0, saved_us((int)i));
     auto is_wide = [&](int i) { return all_saved > kWideUs * DUET_TOTAL_CUS && saved_us(i) > 0; };
     std::vector<WideRun> runs;
-    int shared_prefixes = 0;
     int64_t narrow_pages = 0;
     double narrow_us = 0;
     int at = R;
     for (size_t i = 0; i < count.size(); ++i) {
+      if (block_rows) block_rows[i] = 0;
       if (count[i] < 2 || p->len[i] == 0) continue;
       const int rows = count[i] * g;
+      if (block_rows) block_rows[i] = is_wide((int)i) ? 32 * wide_waves(rows) : kNarrowRows;
       if (is_wide((int)i)) {
         runs.push_back({p->len[i] / 16, rows});
       } else {
@@ -2278,7 +2279,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
         narrow_us += hkv * (p->len[i] / 64.0 * narrow_tile_us(narrow_blocks(rows), s->head_dim, eight) +
                             kTeamUs * narrow_blocks(rows) * (1 + p->len[i] / (16 * kTeamPages)));
       }
-      ++shared_prefixes;
+      ++plan->prefixes;
       member0[i] = at;
       at += count[i];
     }
@@ -2335,7 +2336,7 @@ int plan_shared(const duet_shape* s, const duet_batch* b, const duet_prefixes* p
     plan->direct = plan->max_slots <= 1 && plan->wide.empty();
     plan->plain = at == R && R <= kSharedPassed && (plan->team.empty() || plan->lone.empty()) &&
                   (!plan->direct || narrow_pages <= kSharedCheckedPages);
-    plan->passed = !plan->plain && !plan->direct && R <= kSharedPassed && shared_prefixes <= kSharedPrefixes && plan->n_slots <= 65535;
+    plan->passed = !plan->plain && !plan->direct && R <= kSharedPassed && plan->prefixes <= kSharedPrefixes && plan->n_slots <= 65535;
     plan->split = narrow_split;
     if (!plan->passed && !plan->plain) {
       // The entries cut, each part by blocks of rows.
@@ -2486,6 +2487,23 @@ int duet_shared_workspace_bytes(const duet_shape* shape, const duet_batch* batch
     if (!prefixes || prefixes->num == 0) break;  // only prefixes are
   }
   *bytes = most;
+  return DUET_OK;
+}
+
+int duet_shared_plan(const duet_shape* shape, const duet_batch* batch, const duet_prefixes* prefixes, int32_t eight_bits,
+                     duet_shared_cut* cut, int32_t* block_rows) {
+  clear_error();
+  int rc = check_shared(shape, batch, prefixes);
+  if (rc) return rc;
+  if (!cut) return fail(DUET_EINVAL, "cut is NULL");
+  if (eight_bits != 0 && eight_bits != 1) return fail(DUET_EINVAL, "eight_bits must be 0 or 1");
+  SharedPlan plan;
+  if ((rc = plan_shared(shape, batch, prefixes, eight_bits == 1, &plan, block_rows))) return rc;
+  cut->many_rows = (int32_t)plan.wide_items;
+  cut->teams = (int32_t)plan.team_items;
+  cut->lone = (int32_t)plan.lone_items;
+  cut->direct = plan.direct;
+  cut->tables = plan.plain || plan.passed ? passed_tables(batch->num_reqs, plan.prefixes) : 0;
   return DUET_OK;
 }
 
