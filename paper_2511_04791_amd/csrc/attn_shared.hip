@@ -10,7 +10,9 @@
 // The tokens of S^T's rows are chosen so that a lane of quad y (16 lanes) gets all 16 tokens of the step's page y: instruction
 // p takes tokens 4 p .. 4 p + 3 of each of the four pages.  P^T is then already the operand of the second product, and a
 // lane's values are whole rows of a dim-major page: 16 bytes a load for 8-bit pages as for bf16 ones.
-// 8-bit values become bf16 exactly; a key's power of two multiplies its scores, a value's its probability.
+// 8-bit values become bf16 exactly; a key's power of two multiplies its scores, a value's its probability.  Probabilities are rounded to
+// bf16, the second product's operands, and the denominator sums them as rounded: 256 requests of 512 to 8192 tokens are off by 0.0020 of
+// the results' size, 0.0017 of it their own rounding.
 // Bound by memory: 256 requests of 512 to 8192 tokens, 8 kv heads, 8-bit: 264 us, 5.5 TB/s.  A step's loads go out during the step
 // before; two teams fit a CU.  A wave's runs of more than 32 pages are slower than a team's (100 pages: 301 us).
 //

@@ -27,11 +27,12 @@ struct Cache8ReadArgs {
   const uint8_t *k, *v, *scales;
   const int32_t *table, *out_table;
   __bf16 *k_out, *v_out;
-  const int2* reqs;  // [R + 1] (pages of the requests before it, tokens), uploaded; not used for up to kRopeTable requests
+  const int2* reqs;  // [R] (pages of the requests before it, tokens), uploaded with the workspace; not used without one
   long long pages, out_pages;
-  int32_t* err;      // may be null for up to kRopeTable requests
+  int32_t* err;      // the workspace's, else null
   int32_t num_reqs, max_pages, out_max_pages, h_kv, head_dim, groups;
 };
+// reqs: where there is no workspace, [R + 1] on the host, for up to kRopeTable requests.
 hipError_t launch_cache8_read(const Cache8ReadArgs& a, const int2* reqs, hipStream_t s);
 
 // Decode attention over runs of pages that one or several requests share (attn_shared.hip).  A run is attended by the query
@@ -65,7 +66,8 @@ struct SharedTables {  // in device memory, every part of a run listed
   const int2* slots;  // [R] (first slot, slots)
 };
 // Tables that travel with the launches: for up to 256 requests, and for up to 32, since 4 KB of arguments cost the host 1 us a launch
-// more (a call of one request 12.5 us against 12.0).
+// more (a call of one request 12.5 us against 12.0).  Uploaded ones cost a call some 4 us (256 / 257 requests of 100 tokens 22.2 / 25.9, behind
+// five prefixes of 4000 tokens 77.2 / 81.6), and the host 0.03 us a request (1024 requests 50 to 80 us a call, under their kernels' 80 to 1480).
 constexpr int kSharedPassed = 256, kSharedPrefixes = 32, kSharedFew = 32, kSharedFewPrefixes = 8;
 // Words throughout: of arrays of bytes and of words with one index the compiler made scalar loads whose base was odd, which drop its
 // low bits.
