@@ -74,6 +74,17 @@ def _meta_rows(seq_meta):
     return np.ascontiguousarray(arr.astype(np.int32))
 
 
+def _int32s(x, name):
+    """x as a contiguous int32 array; what that would change is refused."""
+    if type(x) is np.ndarray and x.dtype == np.int32:
+        return np.ascontiguousarray(x)
+    x = np.asarray(x)
+    y = np.ascontiguousarray(x, dtype=np.int32)
+    if not np.array_equal(x, y):
+        raise ValueError(f"{name} must hold whole numbers of 32 bits")
+    return y
+
+
 class _BatchC:
     """The batch as the C ABI takes it.  Its ctypes array holds a copy of the rows."""
     __slots__ = ("rows", "arr", "c")
@@ -931,7 +942,7 @@ class Context:
         if (prefix_of is None) != (prefix_len is None):
             raise ValueError("prefix_of and prefix_len come together")
         if prefix_of is not None:
-            of, length = (np.ascontiguousarray(x, dtype=np.int32) for x in (prefix_of, prefix_len))
+            of, length = _int32s(prefix_of, "prefix_of"), _int32s(prefix_len, "prefix_len")
             if of.shape != (len(b.rows),) or length.ndim != 1:
                 raise ValueError(f"prefix_of must hold {len(b.rows)} values, one per request, and prefix_len one per prefix")
             prefixes = ctypes.byref(N.Prefixes(len(length), *[(ctypes.c_int32 * len(x)).from_buffer_copy(x) if len(x) else None

@@ -1,5 +1,9 @@
-"""What the library says of how it would cut a batch of decode requests with shared prefixes; refusals of that query."""
+"""What the library says of how it would cut a batch of decode requests with shared prefixes; refusals of that query
+and of the prefixes' lists."""
 import ctypes
+
+import numpy as np
+import pytest
 
 from paper_2511_04791_amd import _native as N
 from test_cache_ops_abi import DECODES, SHAPE, B, _batch, _prefixes
@@ -44,3 +48,18 @@ def test_plan_refusals(native):
     assert native.duet_shared_plan(B(SHAPE), B(b), B(p), 0, None, None) == -1
     assert native.duet_shared_plan(B(SHAPE), None, B(p), 0, B(cut), None) == -1
     assert native.duet_shared_plan(B(SHAPE), B(b), B(_prefixes([20], [0, 0, -1])), 0, B(cut), None) == -1
+
+
+@pytest.mark.parametrize("x", [np.array([2 ** 32]), np.array([-2 ** 31 - 1]), [0.5], np.array([np.nan]), [2 ** 31], np.array([2 ** 32 - 1], np.uint32)])
+def test_lists_of_prefixes_are_not_cut_to_32_bits(x):
+    """2^32 would be taken as prefix 0, whose pages the request does not have."""
+    import paper_2511_04791_amd as duet
+    with pytest.raises(ValueError), np.errstate(invalid="ignore"):
+        duet._int32s(x, "prefix_of")
+
+
+@pytest.mark.parametrize("x", [[], [3, -1], np.array([5, 7], np.int64), np.array([1.0, 2.0]), np.arange(6, dtype=np.int32)[::2], range(4), np.array([], np.int32)])
+def test_lists_of_prefixes(x):
+    import paper_2511_04791_amd as duet
+    y = duet._int32s(x, "prefix_of")
+    assert y.dtype == np.int32 and y.flags.c_contiguous and y.tolist() == [int(i) for i in x]
