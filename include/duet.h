@@ -422,8 +422,8 @@ int duet_shared_plan(const duet_shape* shape, const duet_batch* batch, const due
  * the order of its sums follows the batch's lengths and prefixes.  Probabilities are rounded to bf16.  Nothing overflows on the way
  * while the scores (over an 8-bit cache q times 448 d too) lie within fp32's range; a token whose weight is under 2^-80 of its row's
  * largest, or whose weight times value is under 2^-80, may count as nothing, and an 8-bit key or value past bf16's largest as
- * infinite.  q, out and the workspace lie on 16 bytes; out is none of the others.  Page ids outside the pool are not read, their tokens do not count, and they set the error word;
- * a request none of whose tokens count gives NaN.  A batch of no requests clears the error word. */
+ * infinite.  q, out and the workspace lie on 16 bytes; out is none of the others.  Page ids outside the pool are not read, their tokens
+ * do not count, and they set the error word; a request none of whose tokens count gives NaN.  A batch of no requests clears the error word. */
 int duet_attn_decode_shared(duet_ctx* ctx, const duet_shape* shape, const void* q, const duet_kv_cache* cache,
                             const int32_t* page_table, int32_t max_pages_per_req, const duet_batch* batch,
                             const duet_prefixes* prefixes, void* workspace, size_t workspace_bytes, void* out, void* stream);

@@ -1,9 +1,9 @@
 // Decode attention over a paged cache, bf16 or 8-bit, for requests that may share the pages of a prefix.
 //
 // A request's output is softmax(q K^T / sqrt(d)) V over its keys.  The keys are cut into runs; a run gives each query row an
-// unnormalised output, a reference m (kLift above its largest score) and a denominator l, and a row's runs are joined by their exp(m).  A shared
-// prefix is cut once and attended by the rows of every member, so its pages are read once for all of them, and a page
-// that one request holds alone is attended by the g heads of its group.
+// unnormalised output, a reference m (kLift above its largest score) and a denominator l, and a row's runs are joined by their
+// exp(m).  A shared prefix is cut once and attended by the rows of every member, so its pages are read once for all of them, and
+// a page that one request holds alone is attended by the g heads of its group.
 //
 // Up to 16 rows: a wave, or a team of four that shares a run, walks it 64 keys at a time.
 //   S^T [tokens x rows] = K Q^T and O^T [dims x rows] += V^T P^T on 16x16x32 matrix instructions.

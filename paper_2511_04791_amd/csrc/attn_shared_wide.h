@@ -21,9 +21,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// A row's reference is its largest score and kLift, and moves when a score passes that largest by kSlack, all in powers of two.  So weights
-// are at most 2^(kSlack - kLift), and the sums of a run, of up to 2^14 tokens, stay finite over bf16's largest values.  Weights under
-// 2^-102 of the largest become 0.
+// A row's reference lies kLift above its largest score, and moves when a score passes that one by kSlack, all in powers of two.  So
+// weights are at most 2^(kSlack - kLift), and the sums of a run, of up to 2^14 tokens, stay finite over bf16's largest values.  Weights
+// under 2^-102 of the largest become 0.
 constexpr float kLift = 24.f, kSlack = 8.f;
 
 __device__ __forceinline__ float power(unsigned word, int byte) {

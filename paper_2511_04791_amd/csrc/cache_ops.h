@@ -66,8 +66,9 @@ struct SharedTables {  // in device memory, every part of a run listed
   const int2* slots;  // [R] (first slot, slots)
 };
 // Tables that travel with the launches: for up to 256 requests, and for up to 32, since 4 KB of arguments cost the host 1 us a launch
-// more (a call of one request 12.5 us against 12.0).  Uploaded ones cost a call some 4 us (256 / 257 requests of 100 tokens 22.2 / 25.9, behind
-// five prefixes of 4000 tokens 77.2 / 81.6), and the host 0.03 us a request (1024 requests 50 to 80 us a call, under their kernels' 80 to 1480).
+// more (a call of one request 12.5 us against 12.0).  Uploaded ones cost a call some 4 us (256 / 257 requests of 100 tokens 22.2 / 25.9,
+// behind five prefixes of 4000 tokens 77.2 / 81.6), and the host 0.03 us a request (1024 requests 50 to 80 us a call, under their kernels'
+// 80 to 1480).
 constexpr int kSharedPassed = 256, kSharedPrefixes = 32, kSharedFew = 32, kSharedFewPrefixes = 8;
 // Words throughout: of arrays of bytes and of words with one index the compiler made scalar loads whose base was odd, which drop its
 // low bits.
@@ -120,10 +121,10 @@ struct SharedArgs {
 using SharedPassedAll = SharedPassed<kSharedPassed, kSharedPrefixes>;
 using SharedPlainAll = SharedPlain<kSharedPassed>;
 static_assert(sizeof(SharedArgs) + sizeof(SharedPassedAll) <= 4096, "arguments of a launch");
-// On the host one of plain and passed, or neither (then what `tables` names is in device memory).
 inline int passed_tables(int num_reqs, int prefixes) {  // requests of the smallest tables that hold so many
   return num_reqs <= kSharedFew && prefixes <= kSharedFewPrefixes ? kSharedFew : kSharedPassed;
 }
+// On the host one of plain and passed, or neither (then what `tables` names is in device memory).
 hipError_t launch_shared(const SharedArgs& a, const SharedTables& tables, const SharedPassedAll* passed, const SharedPlainAll* plain,
                          hipStream_t s);
 
